@@ -1,0 +1,489 @@
+"""GPU parity of the 8-bit key/value cache against the oracle.
+
+Stored codes and scales are defined in float32 and compared bit for bit. Attention
+is compared with float64, within bounds worked out from the arithmetic:
+
+* a score is a sum of at most R products in float32 of a query held to 2^-22 of its
+  value (float32 queries; others exactly) and whole codes, scaled three times: it is
+  off by at most (R + 8) 2^-24 reach, reach = scale sum |q_d k_jd|;
+* a probability is then off by twice that (itself and its sum) plus 2^-21 for the
+  exponential and the running maximum's products, and, where the type is not
+  float32, by 2^-11 for its rounding to float16 ahead of the second product;
+* the second sum adds at most len 2^-24 of sum p |v|;
+* the result is rounded once: half a unit in the last place is at most 2^-24, 2^-8 or 2^-11 of
+  it for the 24, 8 and 11 significant bits of float32, bfloat16, float16 (or 2^-25, half of the
+  smallest float16).
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv as ref
+from paper_2608_09291_amd import binding, kv
+from test_gpu_spmm import announce, torch_cuda  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ("f32", "bf16", "f16")
+
+
+def _torch_dtype(torch, name):
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+class Pool:
+    """A pool of random codes on both sides, with block tables of shuffled blocks."""
+
+    def __init__(self, torch, rng, lens, heads, head_dim, spare=0, spread=40.0):
+        self.torch, self.rng, self.D, self.H = torch, rng, head_dim, heads
+        R = ref.row_of(head_dim)
+        counts = [-(-n // 64) for n in lens]
+        self.n = sum(counts) + spare + 2
+        self.width = max(max(counts), 1)
+        # blocks that nobody may read: garbage and NaN scales
+        self.codes = [rng.integers(0, 256, size=(self.n, heads, 64 * R), dtype=np.uint8) for _ in range(2)]
+        self.scales = [np.full((self.n, heads), np.nan, np.float32) for _ in range(2)]
+        self.free = [int(i) for i in rng.permutation(self.n)]
+        self.blocks = self.table(counts, self.width)
+        self.lens = list(lens)
+        for i in range(2):
+            at = ref.places(head_dim, i == 0)
+            for row in self.blocks:
+                for blk in row:
+                    if blk >= 0:
+                        c = np.clip(np.rint(rng.normal(0, spread, size=(heads, 64, head_dim))), -127, 127) + 128
+                        for h in range(heads):
+                            self.codes[i][blk, h][at] = c[h].astype(np.uint8)
+                        self.scales[i][blk] = rng.uniform(0.01, 0.05, size=heads).astype(np.float32)
+
+    def table(self, counts, width):
+        return [[self.free.pop() for _ in range(c)] + [-1] * (width - c) for c in counts]
+
+    def cache(self):
+        t = self.torch
+        return kv.Cache(*[t.from_numpy(c).cuda() for c in self.codes], *[t.from_numpy(s).cuda() for s in self.scales], self.D)
+
+    def dev(self, x):
+        return self.torch.tensor(x, dtype=self.torch.int32, device="cuda")
+
+    def same(self, cache):
+        for name, want in zip(("k", "v", "k_scale", "v_scale"), self.codes + self.scales):
+            got = getattr(cache, name).cpu().numpy()
+            bits = np.uint8 if got.dtype == np.uint8 else np.uint32
+            assert np.array_equal(got.view(bits), want.view(bits)), name
+
+
+def _starts(counts):
+    return [0] + [int(c) for c in np.cumsum(counts)]
+
+
+# --- append and read -------------------------------------------------------------
+
+APPEND = [  # lens (with the new tokens), new tokens, heads, head_dim
+    ([1], [1], 1, 64), ([64], [1], 2, 128), ([65, 1, 64, 130], [1, 1, 1, 1], 3, 128),
+    ([63, 130, 64, 5], [63, 70, 64, 0], 2, 80), ([200, 129], [150, 129], 1, 96), ([70, 3], [5, 3], 2, 192),
+    ([100], [37], 1, 256), ([90, 257], [90, 193], 2, 1), ([66], [3], 1, 100), ([77, 64], [4, 62], 1, 13),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,heads,D", APPEND)
+def test_append_and_read(torch_cuda, lens, new, heads, D, dtype):
+    torch = torch_cuda
+    announce(f"kv append lens={lens} new={new} heads={heads} D={D} {dtype}")
+    rng = np.random.default_rng(sum(lens) + D)
+    p = Pool(torch, rng, lens, heads, D)
+    T = sum(new)
+    # keys small (scales stay), values large (scales grow); odd strides
+    dt = _torch_dtype(torch, dtype)
+    k = torch.from_numpy(rng.normal(0, 0.4, size=(T, heads, D)).astype(np.float32)).to(dt)
+    v = torch.from_numpy(rng.normal(0, 9.0, size=(T, heads, D)).astype(np.float32)).to(dt)
+    both = torch.zeros((T, heads, 2 * D + 3), dtype=dt, device="cuda")
+    both[:, :, 1:D + 1], both[:, :, D + 2:2 * D + 2] = k.cuda(), v.cuda()
+    cache = p.cache()
+    st = _starts(new)
+    one = new == [1] * len(new)
+    args = (p.dev(p.blocks), p.dev(lens))
+    kv.append(cache, *args, both[:, :, 1:D + 1], both[:, :, D + 2:2 * D + 2], starts=None if one else p.dev(st),
+              max_new=max(new))
+    before = p.blocks
+    for i, x in enumerate((k, v)):
+        ref.append(p.codes[i], p.scales[i], D, i == 0, before, lens, None if one else st, x.float().numpy())
+    torch.cuda.synchronize()
+    at = [ref.places(D, keys) for keys in (True, False)]
+    for i, (codes, scales) in enumerate(((cache.k, cache.k_scale), (cache.v, cache.v_scale))):
+        codes, scales = codes.cpu().numpy(), scales.cpu().numpy()
+        assert np.array_equal(scales.view(np.uint32), p.scales[i].view(np.uint32))
+        for row, n in zip(p.blocks, lens):
+            for j in range(n):
+                got, want = codes[row[j // 64]][:, at[i][j % 64]], p.codes[i][row[j // 64]][:, at[i][j % 64]]
+                assert np.array_equal(got, want), (i, j)
+    # a stored value is within half a step of its source (and the float32 roundings of x / s)
+    back = [torch.full((T, heads, D), math.nan, dtype=dt, device="cuda") for _ in range(2)]
+    kv.read(cache, *args, *back, starts=None if one else p.dev(st), max_new=max(new))
+    torch.cuda.synchronize()
+    for i, x in enumerate((k, v)):
+        for b, n in enumerate(lens):
+            for t in range(new[b]):
+                j = n - new[b] + t
+                blk = p.blocks[b][j // 64]
+                want = torch.from_numpy((p.codes[i][blk][:, at[i][j % 64]].astype(np.float32) - 128) * p.scales[i][blk][:, None])
+                assert torch.equal(back[i][st[b] + t].cpu(), want.to(dt)), (i, b, t)
+                step = p.scales[i][blk].astype(np.float64)[:, None]
+                off = np.abs(want.double().numpy() - x[st[b] + t].double().numpy())
+                assert (off <= step * (0.5 + 127 * 2.0 ** -22)).all()
+
+
+@pytest.mark.parametrize("case", ["zeros", "nan", "inf", "tiny", "huge"])
+def test_append_of_extremes(torch_cuda, case):
+    torch = torch_cuda
+    announce(f"kv append {case}")
+    rng = np.random.default_rng(4)
+    lens, new, D = [40], [30], 64
+    p = Pool(torch, rng, lens, 1, D)
+    x = rng.normal(0, 1.0, size=(30, 1, D)).astype(np.float32)
+    if case == "zeros":
+        x[:] = 0
+        p.scales[0][p.blocks[0][0]] = p.scales[1][p.blocks[0][0]] = 0
+    elif case == "nan":
+        x[3, 0, 5], x[7] = np.nan, np.nan
+    elif case == "inf":
+        x[3, 0, 5], x[4, 0, 6] = np.inf, -np.inf
+    elif case == "tiny":
+        x *= np.float32(1e-42)
+        p.scales[0][p.blocks[0][0]] = p.scales[1][p.blocks[0][0]] = 0
+    else:
+        x *= np.float32(1e37)
+    cache = p.cache()
+    xd = torch.from_numpy(x).cuda()
+    kv.append(cache, p.dev(p.blocks), p.dev(lens), xd, xd, starts=p.dev([0, 30]), max_new=30)
+    torch.cuda.synchronize()
+    blk = p.blocks[0][0]
+    for i, (codes, scales) in enumerate(((cache.k, cache.k_scale), (cache.v, cache.v_scale))):
+        ref.append(p.codes[i], p.scales[i], D, i == 0, p.blocks, lens, [0, 30], x)
+        assert scales[blk, 0].item() == p.scales[i][blk, 0]
+        at = ref.places(D, i == 0)[:40]
+        assert np.array_equal(codes[blk, 0].cpu().numpy()[at], p.codes[i][blk, 0][at])
+
+
+def test_tables_out_of_range_are_left_alone(torch_cuda):
+    """Blocks that are not in the pool, lengths past the table, rows past the arrays: nothing outside is touched."""
+    torch = torch_cuda
+    announce("kv tables out of range")
+    rng = np.random.default_rng(8)
+    p = Pool(torch, rng, [128, 64, 64], 2, 64)
+    tables = [[p.n, p.blocks[0][1]], [-5, -1], [p.blocks[2][0], 1 << 30]]
+    lens, st = [128, 64, 500], [0, 100, 130, 4000]
+    cache = p.cache()
+    x = torch.ones((140, 2, 64), device="cuda")
+    args = (p.dev(tables), p.dev(lens))
+    kv.append(cache, *args, x, x, starts=p.dev(st), max_new=100)
+    out = [torch.full((140, 2, 64), math.nan, device="cuda") for _ in range(2)]
+    kv.read(cache, *args, *out, starts=p.dev(st), max_new=100)
+    q = torch.ones((140, 4, 64), device="cuda")
+    o = torch.full_like(q, math.nan)
+    w = torch.zeros((3, 2, 128), device="cuda")
+    ws = kv.attend_workspace(cache, q, args[0], starts=p.dev(st), max_q=100, weights=w)
+    kv.attend(cache, *args, q, o, starts=p.dev(st), max_q=100, weights=w, ws=ws)
+    torch.cuda.synchronize()
+    assert not torch.isnan(out[0]).any() and not torch.isnan(o).any()
+    assert (out[0][:36] == 0).all()                        # tokens 28 .. 63 of a block that is not there
+    assert (out[0][36:100] - 1).abs().max() < 2.0 ** -20   # the block after it
+    assert (out[0][100:130] == 0).all() and (o[100:130] == 0).all()
+    unused = [i for i in range(p.n) if i not in (p.blocks[0][1], p.blocks[2][0])]
+    for i, (name, s) in enumerate((("k", "k_scale"), ("v", "v_scale"))):
+        assert np.array_equal(getattr(cache, name).cpu().numpy()[unused], p.codes[i][unused])
+        assert np.array_equal(getattr(cache, s).cpu().numpy()[unused].view(np.uint32), p.scales[i][unused].view(np.uint32))
+
+
+def test_read_more_rows_than_tokens(torch_cuda):
+    torch = torch_cuda
+    announce("kv read more rows than tokens")
+    p = Pool(torch, np.random.default_rng(3), [3, 0], 1, 64)
+    cache = p.cache()
+    out = [torch.full((14, 1, 64), math.nan, device="cuda") for _ in range(2)]
+    kv.read(cache, p.dev(p.blocks), p.dev([3, 0]), *out, starts=p.dev([0, 9, 14]), max_new=9)
+    torch.cuda.synchronize()
+    for i in range(2):
+        got = out[i][:, 0].cpu().numpy()
+        assert (got[:6] == 0).all() and (got[9:] == 0).all()
+        c, s = ref.tokens(p.codes[i], p.scales[i], 64, i == 0, p.blocks[0], 3, 0)
+        assert np.array_equal(got[6:9], (c.astype(np.float32) * s.astype(np.float32)[:, None]))
+
+
+# --- attention --------------------------------------------------------------------
+
+OUT = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def _check(torch, p, lens, new, q, out, dtype, w0=None, w1=None, **how):
+    st = _starts(new)
+    want, size, weights, reach = ref.attend(p.codes[0], p.scales[0], p.codes[1], p.scales[1], p.D, p.blocks, lens, st,
+                                            q.double().cpu().numpy(), **how)
+    R, most = ref.row_of(p.D), max(max(lens), 1)
+    e_s = (R + 8) * 2.0 ** -24 * reach[..., None] + (2.0 ** -22 * reach[..., None] if dtype == "f32" else 0)
+    e_p = 2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11)
+    bound = (e_p + most * 2.0 ** -24) * size + OUT[dtype] * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 1e-30)
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    over = np.abs(got - want) - bound
+    assert (over <= 0).all(), (np.unravel_index(over.argmax(), over.shape), over.max())
+    if w0 is not None:
+        rows = max(new) * (q.shape[1] // p.H)
+        e_w = 2 * (R + 8) * 2.0 ** -24 * reach.max(initial=0) + 2.0 ** -20 + (rows + most) * 2.0 ** -24
+        for b, n in enumerate(lens):
+            a, z = w0[b].double().cpu().numpy(), w1[b].double().cpu().numpy()
+            assert np.array_equal(a[:, n:], z[:, n:])
+            assert (np.abs(z[:, :n] - a[:, :n] - weights[b]) <= e_w * weights[b] + 2.0 ** -23 * np.abs(z[:, :n])).all()
+
+
+ATTEND = [  # lens, queries, q heads, cache heads, head_dim, options
+    ([1], [1], 1, 1, 64, {}),
+    ([200], [1], 4, 4, 128, {}),
+    ([64, 65, 63, 1, 1000], [1] * 5, 8, 2, 128, {}),
+    ([0, 5], [1, 1], 2, 1, 64, {}),                         # a row without keys
+    ([3000, 700], [1, 1], 8, 1, 128, {}),                   # long: split
+    ([2500], [1], 20, 1, 64, {}),                           # more heads than a tile has rows
+    ([300, 129], [1, 1], 5, 5, 80, dict(causal=False)),
+    ([700, 100], [3, 2], 8, 2, 96, {}),                     # a few queries
+    ([515], [4], 4, 1, 256, dict(window=100)),
+    ([130, 64], [130, 64], 4, 2, 128, {}),                  # whole prompts
+    ([300, 77, 1], [150, 77, 1], 6, 2, 192, {}),            # ragged chunks
+    ([257], [257], 3, 3, 80, dict(window=33)),
+    ([400], [140], 5, 1, 64, dict(window=1)),
+    ([90, 300], [40, 60], 4, 2, 128, dict(causal=False)),   # cross attention of another length
+    ([2000], [33], 8, 1, 128, {}),                          # few rows against many keys
+    ([50], [80], 2, 2, 64, {}),                             # queries before the first key: empty rows
+    ([40], [1], 2, 2, 13, {}),
+    ([70], [9], 2, 1, 1, {}),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hk,D,how", ATTEND)
+def test_attend(torch_cuda, lens, new, H, Hk, D, how, tracked, dtype):
+    torch = torch_cuda
+    announce(f"kv attend lens={lens} new={new} H={H}/{Hk} D={D} {how} {dtype} weights={tracked}")
+    rng = np.random.default_rng(sum(lens) + H + D)
+    p = Pool(torch, rng, lens, Hk, D)
+    cache = p.cache()
+    T = sum(new)
+    # values of a wider tensor, at an odd place: strided, not 16-byte aligned
+    wide = torch.from_numpy(rng.normal(0, 1.5, size=(T, H, D + 3)).astype(np.float32)).to(_torch_dtype(torch, dtype)).cuda()
+    q = wide[:, :, 1:D + 1]
+    out = torch.full((T, H, D), math.nan, dtype=q.dtype, device="cuda")
+    w0 = torch.from_numpy(rng.uniform(0, 1, size=(len(lens), Hk, p.width * 64 + 5)).astype(np.float32)).cuda() if tracked else None
+    w1 = None if w0 is None else w0.clone()
+    one = new == [1] * len(new)
+    st = None if one else p.dev(_starts(new))
+    args = dict(starts=st, max_q=max(new), weights=w1, **how)
+    ws = kv.attend_workspace(cache, q, p.dev(p.blocks), **args)
+    for again in range(2):                                  # the workspace is left as it was found
+        if w1 is not None:
+            w1.copy_(w0)
+        out.fill_(math.nan)
+        kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, out, ws=ws, **args)
+        torch.cuda.synchronize()
+        _check(torch, p, lens, new, q, out, dtype, w0, w1, **how)
+        if again == 0:
+            first = (out.clone(), None if w1 is None else w1.clone())
+    assert torch.equal(first[0], out) and (w1 is None or torch.equal(first[1], w1))   # bit for bit
+
+
+def test_attend_aligned_rows_and_scale(torch_cuda):
+    torch = torch_cuda
+    announce("kv attend aligned rows, own scale")
+    rng = np.random.default_rng(77)
+    lens, new, H, Hk, D = [333, 64], [200, 64], 8, 2, 128
+    p = Pool(torch, rng, lens, Hk, D)
+    cache = p.cache()
+    fused = torch.from_numpy(rng.normal(0, 1, size=(sum(new), (H + 2 * Hk) * D)).astype(np.float32)).cuda()
+    for dtype in DTYPES:
+        q = fused.to(_torch_dtype(torch, dtype))[:, :H * D].view(-1, H, D)
+        out = torch.full((sum(new), H, D), math.nan, dtype=q.dtype, device="cuda")
+        args = dict(starts=p.dev(_starts(new)), max_q=max(new))
+        ws = kv.attend_workspace(cache, q, p.dev(p.blocks), **args)
+        kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, out, scale=0.3, ws=ws, **args)
+        torch.cuda.synchronize()
+        _check(torch, p, lens, new, q, out, dtype, scale=0.3)
+
+
+@pytest.mark.parametrize("new", [1, 3, 140])
+def test_attend_large_and_small_scores(torch_cuda, new):
+    """Scores of hundreds (one key takes all), scales that differ by 2^20, a block of scale 0, queries of 1e-6 and 1e5."""
+    torch = torch_cuda
+    announce(f"kv attend extremes new={new}")
+    rng = np.random.default_rng(5)
+    lens = [450]
+    p = Pool(torch, rng, lens, 1, 64)
+    p.scales[0][p.blocks[0][1]] *= 60
+    p.scales[1][p.blocks[0][2]] *= 2.0 ** 20
+    p.scales[1][p.blocks[0][3]] = 0
+    p.scales[0][p.blocks[0][4]] = 0
+    cache = p.cache()
+    q = torch.from_numpy(rng.normal(0, 1, size=(new, 2, 64)).astype(np.float32)).cuda()
+    q[0, 1] *= 1e-6
+    q[-1, 0] *= 1e5
+    for dtype in DTYPES:
+        qd = q.to(_torch_dtype(torch, dtype)) if dtype != "f16" else q.clamp(-6e4, 6e4).half()
+        out = torch.full_like(qd, math.nan)
+        args = dict(starts=p.dev([0, new]), max_q=new)
+        ws = kv.attend_workspace(cache, qd, p.dev(p.blocks), **args)
+        kv.attend(cache, p.dev(p.blocks), p.dev(lens), qd, out, ws=ws, **args)
+        torch.cuda.synchronize()
+        if dtype == "f16":
+            out = out.float().clamp(-65504, 65504)
+        # (float16 results past its range are infinite: those are compared as its largest)
+        want, size, _, reach = ref.attend(p.codes[0], p.scales[0], p.codes[1], p.scales[1], 64, p.blocks, lens, [0, new],
+                                          qd.double().cpu().numpy())
+        e_s = 72 * 2.0 ** -24 * reach[..., None] + (2.0 ** -22 * reach[..., None] if dtype == "f32" else 0)
+        e_p = np.minimum(2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11), 2)
+        bound = (e_p + 450 * 2.0 ** -24) * size + OUT[dtype] * np.abs(want) + 2.0 ** -25
+        if dtype == "f16":
+            want = np.clip(want, -65504, 65504)
+        assert (np.abs(out.double().cpu().numpy() - want) <= bound).all(), dtype
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_attend_nan_stays_in_its_row(torch_cuda, new):
+    torch = torch_cuda
+    announce(f"kv attend NaN new={new}")
+    rng = np.random.default_rng(6)
+    p = Pool(torch, rng, [300], 1, 128)
+    cache = p.cache()
+    q = torch.from_numpy(rng.normal(0, 1, size=(new, 4, 128)).astype(np.float32)).cuda()
+    q[0, 1, 7] = math.nan
+    q[new - 1, 3, 100] = math.inf
+    bad = torch.zeros((new, 4), dtype=torch.bool)
+    bad[0, 1] = bad[new - 1, 3] = True
+    for dtype in DTYPES:
+        qd = q.to(_torch_dtype(torch, dtype))
+        out = torch.zeros_like(qd)
+        args = dict(starts=p.dev([0, new]), max_q=new)
+        ws = kv.attend_workspace(cache, qd, p.dev(p.blocks), **args)
+        kv.attend(cache, p.dev(p.blocks), p.dev([300]), qd, out, ws=ws, **args)
+        torch.cuda.synchronize()
+        nan = torch.isnan(out).cpu()
+        assert nan[bad].all() and not nan[~bad].any()
+
+
+def test_attend_captured_on_another_stream(torch_cuda):
+    """A decode step (append, then attend) captured in a graph, replayed over growing sequences between eager calls."""
+    torch = torch_cuda
+    announce("kv step captured")
+    rng = np.random.default_rng(9)
+    lens, H, Hk, D = [1030, 64], 8, 2, 128
+    p = Pool(torch, rng, [n + 8 for n in lens], Hk, D)
+    cache, eager = p.cache(), p.cache()
+    blocks, n = p.dev(p.blocks), p.dev(lens)
+    y = torch.zeros((2, H + 2 * Hk, D), device="cuda")
+    out = torch.zeros((2, H, D), device="cuda")
+    w = torch.zeros((2, Hk, p.width * 64), device="cuda")
+    ws = kv.attend_workspace(cache, y[:, :H], blocks, weights=w)
+
+    def step(c, o, wt, wsp):
+        kv.append(c, blocks, n, y[:, H:H + Hk], y[:, H + Hk:])
+        kv.attend(c, blocks, n, y[:, :H], o, weights=wt, ws=wsp)
+
+    o2, w2, ws2 = torch.zeros_like(out), torch.zeros_like(w), torch.zeros_like(ws)
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step(cache, out, w, ws)
+    for i in range(5):
+        y.copy_(torch.from_numpy(rng.normal(0, 1 + i, size=y.shape).astype(np.float32)))
+        n.add_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager, o2, w2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, o2) and torch.equal(w, w2) and torch.equal(cache.v, eager.v) and torch.equal(cache.k, eager.k)
+        assert out.abs().max() > 0
+
+
+def test_offsets_past_32_bits(torch_cuda):
+    """Blocks and rows that lie more than 2^32 bytes into their arrays."""
+    torch = torch_cuda
+    announce("kv offsets past 32 bits")
+    n_blocks, Hk, D = 70000, 8, 128                         # 4.6 GB of keys
+    cache = kv.Cache(*[torch.empty((n_blocks, Hk, 64 * D), dtype=torch.uint8, device="cuda") for _ in range(2)],
+                     *[torch.zeros((n_blocks, Hk), device="cuda") for _ in range(2)], D)
+    lens = [100]
+    blocks = torch.tensor([[n_blocks - 1, n_blocks - 3]], dtype=torch.int32, device="cuda")
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    stride = (1 << 31) // 64                                # rows 32 M elements apart: the last ones past 2^31
+    far = torch.empty(101 * stride, dtype=torch.float16, device="cuda")
+    rows = far.as_strided((100, Hk, D), (stride, D, 1))
+    rows.copy_(torch.randn((100, Hk, D), generator=g, device="cuda"))
+    st = torch.tensor([0, 100], dtype=torch.int32, device="cuda")
+    kv.append(cache, blocks, n, rows, rows, starts=st, max_new=100)
+    out = far[2 * D * Hk:].as_strided((100, Hk, D), (stride, D, 1))
+    ws = kv.attend_workspace(cache, rows, blocks, starts=st, max_q=100)
+    kv.attend(cache, blocks, n, rows, out, starts=st, max_q=100, ws=ws)
+    torch.cuda.synchronize()
+    x = rows.double().permute(1, 0, 2).contiguous()
+    s = torch.bmm(x, x.transpose(1, 2).contiguous()) / math.sqrt(D)
+    s.masked_fill_(torch.ones((100, 100), dtype=torch.bool, device="cuda").triu(1), -math.inf)
+    want = torch.bmm(torch.softmax(s, -1), x).permute(1, 0, 2)
+    # keys and values off by half a step (at most 5 / 254) each, and rounding: a wrong row would be off by about 1
+    assert (out.double() - want).abs().max() < 0.25 and (out.double() - want).square().mean().sqrt() < 0.02
+
+
+# --- eviction ----------------------------------------------------------------------
+
+EVICT = [  # lens, heads, head_dim, keep, recent, kind of weights
+    ([100], 2, 64, 40, 10, "random"), ([100, 30, 65, 0], 2, 80, 64, 0, "random"), ([130, 300], 1, 128, 65, 65, "random"),
+    ([200, 500], 2, 96, 130, 1, "ties"), ([90], 1, 192, 1000, 50, "random"), ([3000, 1500], 1, 64, 700, 100, "random"),
+    ([300], 2, 256, 100, 20, "special"), ([1], 1, 64, 1, 0, "random"), ([5000], 1, 64, 2100, 0, "ties"),
+    ([400], 1, 128, 100, 10, "equal"),
+]
+
+
+@pytest.mark.parametrize("lens,heads,D,keep,recent,kind", EVICT)
+def test_evict(torch_cuda, lens, heads, D, keep, recent, kind):
+    torch = torch_cuda
+    announce(f"kv evict lens={lens} heads={heads} D={D} keep={keep} recent={recent} {kind}")
+    rng = np.random.default_rng(keep + D)
+    counts = [-(-min(n, keep) // 64) for n in lens]
+    p = Pool(torch, rng, lens, heads, D, spare=sum(counts))
+    w = rng.exponential(1.0, size=(len(lens), heads, p.width * 64 + 3)).astype(np.float32)
+    if kind == "ties":
+        w = np.floor(w * 2).astype(np.float32)
+    elif kind == "equal":
+        w[:] = 0.25
+    elif kind == "special":
+        w[:, :, ::7], w[:, :, 1::7], w[:, :, 2::7], w[:, :, 3::7] = np.nan, -np.inf, -0.0, 0.0
+        w[:, :, 4::7] = -1.5
+        w[:, :, 5] = np.inf
+    width = max(max(counts), 1)
+    to = p.table(counts, width)
+    cache = p.cache()
+    to_lens = p.dev([-1] * len(lens))
+    to_w = torch.full((len(lens), heads, width * 64), -3.0, device="cuda")
+    index = torch.full((len(lens), heads, keep), -7, dtype=torch.int32, device="cuda")
+    kv.evict(cache, p.dev(p.blocks), p.dev(lens), torch.from_numpy(w).cuda(), keep, recent, p.dev(to), to_lens, to_w, index)
+    torch.cuda.synchronize()
+    assert to_lens.tolist() == [min(n, keep) for n in lens]
+    for b, n in enumerate(lens):
+        for h in range(heads):
+            want = ref.kept(w[b, h], n, keep, recent)
+            got = index[b, h].tolist()
+            assert got == want + [-1] * (keep - len(want)), (b, h)
+            assert np.array_equal(to_w[b, h, :len(want)].cpu().numpy().view(np.uint32), w[b, h, want].view(np.uint32))
+            for i in range(2):
+                ref.evict(p.codes[i], p.scales[i], D, i == 0, p.blocks[b], want, to[b], h)
+    at = [ref.places(D, keys) for keys in (True, False)]
+    for i, (codes, scales) in enumerate(((cache.k, cache.k_scale), (cache.v, cache.v_scale))):
+        codes, scales = codes.cpu().numpy(), scales.cpu().numpy()
+        assert np.array_equal(scales.view(np.uint32), p.scales[i].view(np.uint32))
+        for b, n in enumerate(lens):
+            for j in range(min(n, keep)):
+                blk = to[b][j // 64]
+                assert np.array_equal(codes[blk][:, at[i][j % 64]], p.codes[i][blk][:, at[i][j % 64]]), (i, b, j)
+            for blk in p.blocks[b]:
+                if blk >= 0:
+                    assert np.array_equal(codes[blk], p.codes[i][blk])
