@@ -24,7 +24,7 @@
  *         64 d + 16 ((t / 4) % 4) + 4 (t / 16) + t % 4
  * which is the order in which the matrix cores take them: 64 lanes with 16
  * bytes each read 1 KB without a gap. Bytes that no token was stored to may
- * hold anything.
+ * hold anything. Scales are not negative.
  *
  * What the GPU reads from the caller's tables is bounded there: block numbers
  * outside [0, n_blocks) are blocks that are not there (nothing is stored to

@@ -40,7 +40,8 @@ HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-fno-stric
 # not compile them, and so do the dense GEMM and the key/value cache
 # (us_kv_*.hip), which were measured with it.
 DEFAULT_SCHED_UNITS = ("us_spmm_wide8.hip", "us_spmm_perm.hip", "us_spmm_tile_plain.hip", "us_spmm_tile_perm.hip",
-                       "us_spmm_tile_w2.hip", "us_gemm.hip", "us_kv_store.hip", "us_kv_attend.hip", "us_kv_evict.hip")
+                       "us_spmm_tile_w2.hip", "us_gemm.hip", "us_kv_store.hip", "us_kv_attend.hip",
+                       "us_kv_decode.hip", "us_kv_prompt.hip", "us_kv_evict.hip")
 
 
 def hip_flags(source: str) -> list:

@@ -1,0 +1,164 @@
+// What the attention kernels share: masks, fragments of codes and queries, the
+// softmax's conventions, and the joining of a split row.
+//
+// Mathematics. With query q, key codes c_j and scales s, the score in base 2 is
+// x_j = f (q . c_j), f = scale log2(e) s / n, where n is a power of two that
+// brings the largest magnitude of q's row to [2^8, 2^9): its float16 form keeps
+// 11 bits of every value that matters, whatever the row's range. Codes are
+// whole numbers up to 127, exact in float16. The running maximum m, the
+// probabilities p_j = 2^(x_j - m + 14) and their sum l are float32; p goes to
+// the second product as float16 (the 14 keeps small ones normal), 2^-12 of
+// each on average, below the rounding of a bfloat16 or float16 result. Float32
+// rows carry the rounded-off part of q and p in a second product each, which
+// leaves 2^-22.
+#ifndef UNIONSPARSE_US_KV_ATTEND_H
+#define UNIONSPARSE_US_KV_ATTEND_H
+
+#include "us_kv_common.h"
+
+namespace us_kv {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLift = 14.0f;                             // log2 of the largest probability's form
+
+struct Mask {
+    int32_t causal, window;
+    // Keys [lo, hi) that query i of n of a sequence of len tokens sees. Both grow with i.
+    __device__ void range(int i, int n, int len, int &lo, int &hi) const {
+        lo = 0;
+        hi = len;
+        if (causal) {
+            const int at = len - n + i;
+            hi = max(at + 1, 0);
+            lo = window > 0 ? max(at - window + 1, 0) : 0;
+        }
+    }
+};
+
+// How a launch splits a row's keys, and what it leaves in the workspace: per
+// unit (sequence, cache head, row tile) and split, `rows` partial rows of R
+// floats, then their (m, l) pairs.
+struct Split {
+    int32_t chunk, splits, tiles, rows;
+    float *part;
+    float *ml;
+    int32_t *tickets;
+    float *lse;       // (row, query head): m + log2 l, +inf for a row without keys; or NULL
+    float *scores;    // decode with weights: x_j by (sequence, head, row, key); or NULL
+    int64_t scores_stride;
+};
+
+struct Args {
+    const uint8_t *k, *v;
+    const float *ks, *vs;
+    int32_t heads, D, G, vec;
+    float scale;      // log2(e) included
+    Seqs s;
+    Rows q, out;
+    Mask mask;
+    Split sp;
+};
+
+// 8 codes of two words as float16: byte u beside 0x64 is 1024 + u, and u = c + 128.
+__device__ inline f16x8 halves_of(uint32_t w0, uint32_t w1) {
+    const uint32_t a[4] = {__builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u),
+                           __builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u)};
+    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    f16x8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f16x2 h = __builtin_bit_cast(f16x2, a[i]) - bias;
+        r[2 * i] = h.x;
+        r[2 * i + 1] = h.y;
+    }
+    return r;
+}
+
+// x as float16 and, where wanted, what that leaves of it.
+template <bool SPLIT>
+__device__ inline void halve(const float (&x)[8], f16x8 &hi, f16x8 &lo) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (_Float16)x[e];
+        if constexpr (SPLIT) lo[e] = (_Float16)(x[e] - (float)hi[e]);
+    }
+}
+
+// The power of two that brings a row whose largest magnitude is mx to
+// [2^8, 2^9), and its inverse; NaN for a row that is not finite, as its result
+// is to be, and the largest for one of tiny values.
+__device__ inline float row_norm(float mx, float &inverse) {
+    uint32_t e = __float_as_uint(mx) >> 23;
+    const bool finite = e < 255u;
+    e = e < 9u ? 9u : e;
+    inverse = __uint_as_float((e - 8u) << 23);
+    return finite ? __uint_as_float((262u - e) << 23) : __uint_as_float(0x7FC00000u);
+}
+
+// Largest magnitude with infinities and NaN as an infinity.
+__device__ inline float magnitude(const float (&x)[8], float mx) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float a = fabsf(x[e]);
+        mx = a < INFINITY ? fmaxf(mx, a) : INFINITY;
+    }
+    return mx;
+}
+
+template <int DT>
+__device__ inline void load_octet_any(const typename Type<DT>::T *p, int o, int D, bool vec, float (&x)[8]) {
+    if (vec) load_octet<DT, true>(p, o, D, x);
+    else load_octet<DT, false>(p, o, D, x);
+}
+template <int DT>
+__device__ inline void store_octet_any(typename Type<DT>::T *p, int o, int D, bool vec, const float (&x)[8]) {
+    if (vec) store_octet<DT, true>(p, o, D, x);
+    else store_octet<DT, false>(p, o, D, x);
+}
+
+// What is subtracted of a score: the maximum, or 0 where there is none yet.
+__device__ inline float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// Stores a finished octet of a row: sums o of probabilities l (times 2^14).
+template <int DT>
+__device__ inline void put_octet(const Args &a, int row, int head, int oct, const float (&x)[8], float l) {
+    using T = typename Type<DT>::T;
+    float y[8];
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;         // a row without keys gives zeros
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x[e] * inv;
+    store_octet_any<DT>((T *)a.out.data + (int64_t)row * a.out.token_stride + (int64_t)head * a.out.head_stride, oct, a.D, a.vec, y);
+}
+
+__device__ inline float lse_of(float m, float l) { return l == 0.0f ? INFINITY : base_of(m) - kLift + __builtin_amdgcn_logf(l); }
+
+// Whether this workgroup is the last of `n` to arrive at `ticket`; what the
+// others wrote before is visible to the last one, which resets the ticket.
+// Called by every thread.
+__device__ inline bool last_of(int32_t *ticket, int n, int *lds) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int t = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        *lds = t == n - 1;
+        if (t == n - 1) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    const bool last = *lds != 0;
+    if (last) __threadfence();
+    return last;
+}
+
+hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream);
+hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream);
+// Adds the probabilities up: from the scores that decode left, or by the scores' product again.
+hipError_t launch_weights_saved(const Args &a, int batch, float *weights, int64_t stride, hipStream_t stream);
+hipError_t launch_weights(int dtype, const Args &a, int batch, float *weights, int64_t stride, hipStream_t stream);
+
+}  // namespace us_kv
+
+#endif  // UNIONSPARSE_US_KV_ATTEND_H

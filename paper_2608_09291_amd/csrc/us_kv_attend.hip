@@ -1,132 +1,13 @@
-// us_kv_attend: softmax attention over the 8-bit cache.
+// us_kv_attend: checks, the choice of the kernel and of its split, launches.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
-
-#include "us_kv_common.h"
+#include "us_device.h"
+#include "us_kv_attend.h"
 
 namespace {
 
 using namespace us_kv;
-
-struct Mask {
-    int32_t causal, window;
-    // Keys [lo, hi) that query i of n of a sequence of len tokens sees.
-    __device__ void range(int i, int n, int len, int &lo, int &hi) const {
-        lo = 0;
-        hi = len;
-        if (causal) {
-            const int at = len - n + i;
-            hi = max(at + 1, 0);
-            lo = window > 0 ? max(at - window + 1, 0) : 0;
-        }
-    }
-};
-
-// One wavefront per (query head, query row): 64 keys at a time, a lane per key
-// for the scores, a lane per value for the sum.
-template <int NT, int DT>
-__global__ __launch_bounds__(64) void us_kv_attend_kernel(const uint8_t *kp, const uint8_t *vp, const float *ksp,
-                                                          const float *vsp, int heads, int D, Seqs s, Rows qr, Rows outr,
-                                                          int q_heads, Mask mask, float scale, float *lse) {
-    using T = typename Type<DT>::T;
-    constexpr int R = 32 * NT;
-    __shared__ float q[R], p[64];
-    const int h = blockIdx.x, b = blockIdx.z, lane = threadIdx.x, hk = h / (q_heads / heads);
-    int r0, n;
-    s.rows(b, r0, n);
-    const int i = blockIdx.y;
-    if (i >= n) return;
-    const int len = s.len(b);
-    const T *src = (const T *)qr.data + (int64_t)(r0 + i) * qr.token_stride + (int64_t)h * qr.head_stride;
-    for (int d = lane; d < R; d += 64) q[d] = d < D ? Type<DT>::get(src[d]) : 0.0f;
-    __syncthreads();
-    int lo, hi;
-    mask.range(i, n, len, lo, hi);
-    float m = -INFINITY, l = 0.0f, o[R / 64 + 1] = {};
-    for (int blk = lo / kBlock; blk * kBlock < hi; ++blk) {
-        const int id = s.block(b, blk), j = blk * kBlock + lane;
-        if (id < 0) continue;
-        const int64_t at = (int64_t)id * heads + hk;
-        const uint8_t *k = kp + at * (kBlock * R), *v = vp + at * (kBlock * R);
-        float dot = 0.0f;
-        for (int oct = 0; oct < R / 8; ++oct) {
-            const u32x2 w = *(const u32x2 *)(k + key_octet(lane, oct));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot += code_of(w[e >> 2], e & 3) * q[8 * oct + e];
-        }
-        const float x = j >= lo && j < hi ? dot * (ksp[at] * scale) : -INFINITY;
-        float top = x;
-#pragma unroll
-        for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
-        const float m2 = fmaxf(m, top);
-        const float to = m2 == -INFINITY ? 0.0f : m2;      // (nothing seen yet, or NaN)
-        const float a = exp2f(m - to), pj = exp2f(x - to);
-        m = m2;
-        l = l * a + pj;                                    // (this lane's keys)
-        p[lane] = pj;
-        __syncthreads();
-        const float sv = vsp[at];
-        for (int c = 0; c < (R + 63) / 64; ++c) {
-            const int d = 64 * c + lane;
-            float sum = 0.0f;
-            if (d < R)
-                for (int t = 0; t < 64; ++t) sum += p[t] * ((float)v[64 * d + value_place(t)] - 128.0f);
-            o[c] = o[c] * a + sum * sv;
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
-    T *dst = (T *)outr.data + (int64_t)(r0 + i) * outr.token_stride + (int64_t)h * outr.head_stride;
-    for (int c = 0; c < (R + 63) / 64; ++c) {
-        const int d = 64 * c + lane;
-        if (d < D) dst[d] = Type<DT>::put(l == 0.0f ? 0.0f : o[c] / l);
-    }
-    if (lse && lane == 0) lse[(int64_t)(r0 + i) * q_heads + h] = l == 0.0f ? INFINITY : (m == -INFINITY ? 0.0f : m) + log2f(l);
-}
-
-// One wavefront per (64 keys, head, sequence): the probabilities again, from
-// the logarithms of their sums.
-template <int NT, int DT>
-__global__ __launch_bounds__(64) void us_kv_weights_kernel(const uint8_t *kp, const float *ksp, int heads, int D, Seqs s,
-                                                           Rows qr, int q_heads, Mask mask, float scale, const float *lse,
-                                                           float *weights, int64_t w_stride) {
-    using T = typename Type<DT>::T;
-    constexpr int R = 32 * NT;
-    __shared__ float q[R];
-    const int blk = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, lane = threadIdx.x, G = q_heads / heads;
-    int r0, n;
-    s.rows(b, r0, n);
-    const int len = s.len(b), j = blk * kBlock + lane;
-    if (blk * kBlock >= len) return;
-    const int id = s.block(b, blk);
-    if (id < 0) return;
-    const int64_t at = (int64_t)id * heads + hk;
-    const uint8_t *k = kp + at * (kBlock * R);
-    float sum = 0.0f;
-    for (int i = 0; i < n; ++i) {
-        int lo, hi;
-        mask.range(i, n, len, lo, hi);
-        if (blk * kBlock >= hi || blk * kBlock + kBlock <= lo) continue;
-        for (int g = 0; g < G; ++g) {
-            const int h = hk * G + g;
-            const T *src = (const T *)qr.data + (int64_t)(r0 + i) * qr.token_stride + (int64_t)h * qr.head_stride;
-            __syncthreads();
-            for (int d = lane; d < R; d += 64) q[d] = d < D ? Type<DT>::get(src[d]) : 0.0f;
-            __syncthreads();
-            float dot = 0.0f;
-            for (int oct = 0; oct < R / 8; ++oct) {
-                const u32x2 w = *(const u32x2 *)(k + key_octet(lane, oct));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dot += code_of(w[e >> 2], e & 3) * q[8 * oct + e];
-            }
-            if (j >= lo && j < hi) sum += exp2f(dot * (ksp[at] * scale) - lse[(int64_t)(r0 + i) * q_heads + h]);
-        }
-    }
-    if (j < len) weights[((int64_t)b * heads + hk) * w_stride + j] += sum;
-}
 
 constexpr us_kv_attend_opts kDefault = {0.0f, 1, 0, 0, nullptr, 0};
 
@@ -142,8 +23,55 @@ us_status check_opts(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, con
     return US_OK;
 }
 
-size_t bytes_needed(int q_heads, int tokens, const us_kv_attend_opts &o) {
-    return o.weights ? (size_t)q_heads * (size_t)tokens * 4 : 0;
+// What a call launches, and where its parts of the workspace lie (bytes).
+// The tickets, which have to be zero between calls, have a place of their own
+// that no other part of any call takes; calls of more units do not split.
+constexpr int64_t kTickets = 16384;
+
+struct Plan {
+    bool decode;
+    int chunk, splits, tiles, rows;
+    int64_t scores_stride;
+    size_t ml, part, lse, scores, total;
+};
+
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int tokens, const us_kv_attend_opts &o, Plan &p) {
+    const int max_len = seqs_of(c, s, o.max_len, tokens).max_len, R = row_of(c.head_dim);
+    const int64_t rows = (int64_t)s.max_new * (q_heads / c.heads), pairs = (int64_t)s.batch * c.heads;
+    if (rows > INT32_MAX / 2) return US_ERR_SHAPE;
+    p.decode = rows <= 32;
+    const int tile = p.decode ? 16 : 128;
+    p.tiles = (int)((rows + tile - 1) / tile);
+    p.rows = rows < tile && p.decode ? (int)rows : tile;
+    const int64_t units = pairs * p.tiles;
+    // Blocks that a tile's rows see at most.
+    int64_t most = up(max_len, kBlock) / kBlock;
+    if (o.window) {
+        const int64_t reach = o.window + (tile + q_heads / c.heads - 1) / (q_heads / c.heads);
+        if (reach / kBlock + 2 < most) most = reach / kBlock + 2;
+    }
+    const int cus = us_device::compute_units();
+    if (p.decode) {
+        int64_t chunk = up(units * most / (3 * cus), 4);
+        p.chunk = (int)(chunk < 4 ? 4 : chunk > 32 ? 32 : chunk);
+    } else {
+        const int64_t want = units >= 2 * cus ? 1 : (2 * cus + units - 1) / units;
+        p.chunk = (int)((most + want - 1) / want);
+        if (p.chunk < 4) p.chunk = 4;
+    }
+    if (units > kTickets || most <= p.chunk) p.chunk = (int)most;
+    p.splits = (int)((most + p.chunk - 1) / p.chunk);
+    if (units * p.splits > INT32_MAX / 256) return US_ERR_SHAPE;
+    p.scores_stride = up(max_len, kBlock);
+    const size_t parts = p.splits > 1 ? (size_t)(units * p.splits * p.rows) : 0;
+    p.ml = p.splits > 1 || o.weights ? 4 * kTickets : 0;
+    p.part = p.ml + (size_t)up(8 * (int64_t)parts, 16);
+    p.lse = p.part + parts * R * 4;
+    p.scores = p.lse + (o.weights ? (size_t)up((int64_t)q_heads * tokens * 4, 16) : 0);
+    p.total = p.scores + (o.weights && p.decode ? (size_t)(pairs * p.tiles * p.rows * p.scores_stride) * 4 : 0);
+    return US_OK;
 }
 
 }  // namespace
@@ -151,12 +79,14 @@ size_t bytes_needed(int q_heads, int tokens, const us_kv_attend_opts &o) {
 extern "C" us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                                  int32_t tokens, const us_kv_attend_opts *opts, size_t *bytes) {
     const us_kv_attend_opts &o = opts ? *opts : kDefault;
-    const us_status st = check_opts(cache, seqs, q_heads, o);
+    us_status st = check_opts(cache, seqs, q_heads, o);
     if (st != US_OK) return st;
     if (!bytes) return US_ERR_ARG;
     if (tokens < 1) return US_ERR_SHAPE;
-    *bytes = bytes_needed(q_heads, tokens, o);
-    return US_OK;
+    Plan p;
+    st = plan_of(*cache, *seqs, q_heads, tokens, o, p);
+    if (st == US_OK) *bytes = p.total;
+    return st;
 }
 
 extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
@@ -169,28 +99,27 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     if (st != US_OK) return st;
     if (q->dtype != out->dtype) return US_ERR_ARG;
     if (q->tokens != out->tokens) return US_ERR_SHAPE;
-    const size_t need = bytes_needed(q_heads, q->tokens, o);
-    if (need && (!ws || (uintptr_t)ws % 16 || ws_bytes < need)) return US_ERR_ARG;
-    const Seqs s = seqs_of(*cache, *seqs, o.max_len, q->tokens);
-    const Mask mask{o.causal, o.window};
-    const float scale = (o.scale > 0.0f ? o.scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504f;
-    const Rows qr{q->data, q->token_stride, q->head_stride}, outr{out->data, out->token_stride, out->head_stride};
-    float *lse = need ? (float *)ws : nullptr;
-    if (seqs->max_new > 65535) return US_ERR_SHAPE;
-    const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
-        return with_type(q->dtype, [&](auto dt) {
-            constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
-            hipLaunchKernelGGL((us_kv_attend_kernel<NT, DT>), dim3(q_heads, seqs->max_new, seqs->batch), dim3(64), 0,
-                               (hipStream_t)stream, cache->k, cache->v, cache->k_scale, cache->v_scale, cache->heads,
-                               cache->head_dim, s, qr, outr, q_heads, mask, scale, lse);
-            hipError_t err = hipGetLastError();
-            if (err != hipSuccess || !o.weights) return err;
-            hipLaunchKernelGGL((us_kv_weights_kernel<NT, DT>),
-                               dim3((s.max_len + kBlock - 1) / kBlock, cache->heads, seqs->batch), dim3(64), 0,
-                               (hipStream_t)stream, cache->k, cache->k_scale, cache->heads, cache->head_dim, s, qr, q_heads,
-                               mask, scale, lse, o.weights, o.weights_stride);
-            return hipGetLastError();
-        });
-    });
+    Plan p;
+    st = plan_of(*cache, *seqs, q_heads, q->tokens, o, p);
+    if (st != US_OK) return st;
+    if (p.total && (!ws || (uintptr_t)ws % 16 || ws_bytes < p.total)) return US_ERR_ARG;
+    uint8_t *w = (uint8_t *)ws;
+    Args a;
+    a.k = cache->k, a.v = cache->v, a.ks = cache->k_scale, a.vs = cache->v_scale;
+    a.heads = cache->heads, a.D = cache->head_dim, a.G = q_heads / cache->heads;
+    a.vec = octets_aligned(*q, cache->head_dim) && octets_aligned(*out, cache->head_dim);
+    a.scale = (o.scale > 0.0f ? o.scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504f;
+    a.s = seqs_of(*cache, *seqs, o.max_len, q->tokens);
+    a.q = Rows{q->data, q->token_stride, q->head_stride};
+    a.out = Rows{out->data, out->token_stride, out->head_stride};
+    a.mask = Mask{o.causal, o.window};
+    a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, (float *)(w + p.part), (float *)(w + p.ml), (int32_t *)w,
+                 o.weights ? (float *)(w + p.lse) : nullptr, o.weights && p.decode ? (float *)(w + p.scores) : nullptr,
+                 p.scores_stride};
+    const hipStream_t hs = (hipStream_t)stream;
+    hipError_t e = p.decode ? launch_decode(q->dtype, a, seqs->batch, hs) : launch_prompt(q->dtype, a, seqs->batch, hs);
+    if (e == hipSuccess && o.weights)
+        e = p.decode ? launch_weights_saved(a, seqs->batch, o.weights, o.weights_stride, hs)
+                     : launch_weights(q->dtype, a, seqs->batch, o.weights, o.weights_stride, hs);
     return e == hipSuccess ? US_OK : US_ERR_DEVICE;
 }

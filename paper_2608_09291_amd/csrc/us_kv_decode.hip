@@ -1,0 +1,312 @@
+// us_kv_attend with few query rows: every key and value is read once, for at
+// most 16 rows at a time (the query heads of a cache head, and a few tokens).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "us_kv_attend.h"
+
+namespace us_kv {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kRows = 16;
+
+template <int NT, int DT>
+__global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(Args a) {
+    using T = typename Type<DT>::T;
+    constexpr bool SPLIT = DT == US_F32;
+    constexpr int R = 32 * NT, NV = R / 16;
+    constexpr int kCols = R > 128 ? R / 2 : R;             // columns joined at a time
+    __shared__ __attribute__((aligned(16))) float sum[kWaves][kRows][kCols + 4];
+    __shared__ float wm[kWaves][kRows], wl[kWaves][kRows];
+    __shared__ int flag;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int tile = blockIdx.x % a.sp.tiles, split = blockIdx.x / a.sp.tiles, hk = blockIdx.y, b = blockIdx.z;
+    int r0, n;
+    a.s.rows(b, r0, n);
+    const int len = a.s.len(b), total = n * a.G, base = tile * kRows;
+    if (base >= total) return;
+    const int last_row = min(base + kRows, total) - 1;
+    int lo0, hi0, lo1, hi1;                                // of the tile's first and last row
+    a.mask.range(base / a.G, n, len, lo0, hi0);
+    a.mask.range(last_row / a.G, n, len, lo1, hi1);
+    const int first = lo0 / kBlock, end = (hi1 + kBlock - 1) / kBlock;
+    const int ns = max((end - first + a.sp.chunk - 1) / a.sp.chunk, 1);
+    if (split >= ns) return;
+    const int row = min(base + r, last_row), i = row / a.G, head = hk * a.G + row - i * a.G;
+    int lo, hi;
+    a.mask.range(i, n, len, lo, hi);
+
+    // This wavefront's blocks: start, start + 4, ... A lane looks one of them up.
+    const int start = first + split * a.sp.chunk + wave, stop = min(first + (split + 1) * a.sp.chunk, end);
+    const int count = start < stop ? (stop - start + kWaves - 1) / kWaves : 0;
+    int my_id;
+    float my_ks, my_vs;
+    auto look_up = [&](int c) {                            // 64 of them, from the c-th on
+        my_id = -1;
+        my_ks = my_vs = 0.0f;
+        if (c + lane < count) {
+            my_id = a.s.block(b, start + kWaves * (c + lane));
+            if (my_id >= 0) {
+                my_ks = a.ks[(int64_t)my_id * a.heads + hk];
+                my_vs = a.vs[(int64_t)my_id * a.heads + hk];
+            }
+        }
+    };
+    look_up(0);
+
+    // Queries: column r of the first product's right operand.
+    f16x8 qh[NT], ql[NT];
+    float f;
+    {
+        const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+        float x[NT][8], mx = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            load_octet_any<DT>(src, 4 * t + g, a.D, a.vec, x[t]);
+            mx = magnitude(x[t], mx);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        float inv;
+        const float norm = row_norm(mx, inv);
+        f = inv * a.scale;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[t][e] *= norm;
+            halve<SPLIT>(x[t], qh[t], ql[t]);
+        }
+    }
+
+    const int64_t page = (int64_t)kBlock * R;
+    auto at = [&](int c) {                                 // this wavefront's c-th block (block 0 where it is not there)
+        const int id = __builtin_amdgcn_readlane(my_id, c & 63);
+        return ((int64_t)max(id, 0) * a.heads + hk) * page;
+    };
+    u32x4 kr[NT][2], vr[NV];
+    auto load_k = [&](int64_t off) {
+        const uint8_t *p = a.k + off + 64 * r + 16 * g;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) kr[t][u] = __builtin_nontemporal_load((const u32x4 *)(p + 2048 * t + 1024 * u));
+    };
+    auto load_v = [&](int64_t off) {
+        const uint8_t *p = a.v + off + 64 * r + 16 * g;
+#pragma unroll
+        for (int t = 0; t < NV; ++t) vr[t] = __builtin_nontemporal_load((const u32x4 *)(p + 1024 * t));
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o[NV];
+#pragma unroll
+    for (int t = 0; t < NV; ++t) o[t] = (f32x4){0, 0, 0, 0};
+    if (count > 0) {
+        load_k(at(0));
+        load_v(at(0));
+    }
+    for (int c = 0; c < count; ++c) {
+        const int blk = start + kWaves * c;
+        const bool there = __builtin_amdgcn_readlane(my_id, c & 63) >= 0;
+        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), c & 63));
+        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), c & 63));
+        // Lane (r, g), element v of tile u: key 16 u + 4 g + v, row r.
+        f32x4 s[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const f16x8 kh = halves_of(kr[t][u >> 1][2 * (u & 1)], kr[t][u >> 1][2 * (u & 1) + 1]);
+                s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[t], s[u], 0, 0, 0);
+                if constexpr (SPLIT) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[t], s[u], 0, 0, 0);
+            }
+        if (c + 1 < count) {
+            if (((c + 1) & 63) == 0) look_up(c + 1);
+            load_k(at(c + 1));
+        }
+        const float fk = f * ks;
+        const int j0 = blk * kBlock + 4 * g;
+        const bool whole = there && blk * kBlock >= lo1 && blk * kBlock + kBlock <= hi0;
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                s[u][v] *= fk;
+                if (!whole) {
+                    const int j = j0 + 16 * u + v;
+                    if (!there || j < lo || j >= hi) s[u][v] = -INFINITY;
+                }
+                top = fmaxf(top, s[u][v]);
+            }
+        if (a.sp.scores && base + r <= last_row) {
+            float *dst = a.sp.scores + (((int64_t)b * a.heads + hk) * a.sp.rows * a.sp.tiles + row) * a.sp.scores_stride + j0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *(f32x4 *)(dst + 16 * u) = s[u];
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m2 = fmaxf(m, top), to = base_of(m2), alpha = __builtin_amdgcn_exp2f(m - to);
+        m = m2;
+        l *= alpha;
+        f16x8 ph[2], pl[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(s[2 * u + (e >> 2)][e & 3] - (to - kLift));
+                l += p[e];
+            }
+            halve<SPLIT>(p, ph[u], pl[u]);
+        }
+        // Lane (r, g) of the left operand: value 16 t + r of keys 16 u + 4 g + v.
+#pragma unroll
+        for (int t = 0; t < NV; ++t) {
+            f32x4 pv = {0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const f16x8 vh = halves_of(vr[t][2 * u], vr[t][2 * u + 1]);
+                pv = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, ph[u], pv, 0, 0, 0);
+                if constexpr (SPLIT) pv = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pl[u], pv, 0, 0, 0);
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[t][v] = fmaf(pv[v], vs, o[t][v] * alpha);
+        }
+        if (c + 1 < count) load_v(at(c + 1));
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+
+    // Join the wavefronts; lane (r, g) holds values 16 t + 4 g + v of row r.
+    if (g == 0) {
+        wm[wave][r] = m;
+        wl[wave][r] = l;
+    }
+    __syncthreads();
+    float all = wm[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, wm[w][r]);
+    const float mine = __builtin_amdgcn_exp2f(m - base_of(all));
+    const int64_t unit = ((int64_t)b * a.heads + hk) * a.sp.tiles + tile;
+    const int rows_here = last_row - base + 1;
+#pragma unroll
+    for (int c0 = 0; c0 < R; c0 += kCols) {
+        if (c0) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kCols / 16; ++t) {
+            f32x4 x = o[c0 / 16 + t];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v] *= mine;
+            *(f32x4 *)&sum[wave][r][16 * t + 4 * g] = x;
+        }
+        __syncthreads();
+        for (int q = tid; q < rows_here * (kCols / 8); q += kThreads) {
+            const int rr = q / (kCols / 8), oc = q % (kCols / 8);
+            float x[8], am = wm[0][rr], ll = 0.0f;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) am = fmaxf(am, wm[w][rr]);
+            const float bm = base_of(am);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) ll += wl[w][rr] * __builtin_amdgcn_exp2f(wm[w][rr] - bm);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += sum[w][rr][8 * oc + e];
+            const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
+            if (ns == 1) {
+                put_octet<DT>(a, r0 + ti, hd, c0 / 8 + oc, x, ll);
+                if (a.sp.lse && c0 == 0 && oc == 0) a.sp.lse[(int64_t)(r0 + ti) * (a.heads * a.G) + hd] = lse_of(am, ll);
+            } else {
+                const int64_t pr = (unit * a.sp.splits + split) * a.sp.rows + rr;
+                float *dst = a.sp.part + pr * R + c0 + 8 * oc;
+                *(f32x4 *)dst = (f32x4){x[0], x[1], x[2], x[3]};
+                *(f32x4 *)(dst + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+                if (c0 == 0 && oc == 0) {
+                    a.sp.ml[2 * pr] = am;
+                    a.sp.ml[2 * pr + 1] = ll;
+                }
+            }
+        }
+    }
+    if (ns == 1 || !last_of(a.sp.tickets + unit, ns, &flag)) return;
+    // The last workgroup joins the splits, in their order.
+    for (int q = tid; q < rows_here * (R / 8); q += kThreads) {
+        const int rr = q / (R / 8), oc = q % (R / 8);
+        const int64_t p0 = unit * a.sp.splits * a.sp.rows + rr;
+        float am = -INFINITY, ll = 0.0f, x[8];
+        for (int z = 0; z < ns; ++z) am = fmaxf(am, a.sp.ml[2 * (p0 + (int64_t)z * a.sp.rows)]);
+        const float bm = base_of(am);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+#pragma unroll 4
+        for (int z = 0; z < ns; ++z) {
+            const int64_t pr = p0 + (int64_t)z * a.sp.rows;
+            const float w = __builtin_amdgcn_exp2f(a.sp.ml[2 * pr] - bm);
+            ll += a.sp.ml[2 * pr + 1] * w;
+            const f32x4 y0 = *(const f32x4 *)(a.sp.part + pr * R + 8 * oc), y1 = *(const f32x4 *)(a.sp.part + pr * R + 8 * oc + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = fmaf(y0[e], w, x[e]);
+                x[4 + e] = fmaf(y1[e], w, x[4 + e]);
+            }
+        }
+        const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
+        put_octet<DT>(a, r0 + ti, hd, oc, x, ll);
+        if (a.sp.lse && oc == 0) a.sp.lse[(int64_t)(r0 + ti) * (a.heads * a.G) + hd] = lse_of(am, ll);
+    }
+}
+
+// weights[b, hk, j] += sum over the rows of 2^(x_j - lse): four keys per thread.
+__global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, float *weights, int64_t stride) {
+    const int hk = blockIdx.y, b = blockIdx.z;
+    int r0, n;
+    a.s.rows(b, r0, n);
+    const int len = a.s.len(b), total = n * a.G, j0 = 4 * (blockIdx.x * kThreads + threadIdx.x);
+    if (j0 >= len) return;
+    const int64_t bh = (int64_t)b * a.heads + hk;
+    float sum[4] = {0, 0, 0, 0};
+    // (no tile has stored scores of blocks ahead of its first row's window or past its last row's)
+    for (int row = 0; row < total; ++row) {
+        const int i = row / a.G, tile = row / kRows;
+        int lo, hi, x;
+        a.mask.range(tile * kRows / a.G, n, len, lo, x);
+        a.mask.range((min(tile * kRows + kRows, total) - 1) / a.G, n, len, x, hi);
+        if (j0 < lo / kBlock * kBlock || j0 >= hi) continue;
+        const float z = a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + hk * a.G + row - i * a.G];
+        const f32x4 s = *(const f32x4 *)(a.sp.scores + (bh * a.sp.rows * a.sp.tiles + row) * a.sp.scores_stride + j0);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] += __builtin_amdgcn_exp2f(s[v] - z);
+    }
+    float *w = weights + bh * stride + j0;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (j0 + v < len) w[v] += sum[v];
+}
+
+}  // namespace
+
+hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream) {
+    return with_row(a.D, [&](auto nt) {
+        return with_type(dtype, [&](auto dt) {
+            hipLaunchKernelGGL((us_kv_decode_kernel<decltype(nt)::value, decltype(dt)::value>),
+                               dim3(a.sp.splits * a.sp.tiles, a.heads, batch), dim3(kThreads), 0, stream, a);
+            return hipGetLastError();
+        });
+    });
+}
+
+hipError_t launch_weights_saved(const Args &a, int batch, float *weights, int64_t stride, hipStream_t stream) {
+    const unsigned x = (unsigned)((a.s.max_len + 4 * kThreads - 1) / (4 * kThreads));
+    hipLaunchKernelGGL(us_kv_weights_saved_kernel, dim3(x, a.heads, batch), dim3(kThreads), 0, stream, a, weights, stride);
+    return hipGetLastError();
+}
+
+}  // namespace us_kv

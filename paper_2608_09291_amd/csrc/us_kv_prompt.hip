@@ -1,0 +1,442 @@
+// us_kv_attend with many query rows: prompts and chunks of them.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+#include <type_traits>
+
+#include "us_kv_attend.h"
+
+namespace us_kv {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kRows = 128;     // 32 rows per wavefront
+
+// A block's keys and values as float16 in LDS, in the order of the operands:
+// 16 bytes (8 values of a key; 8 keys of a value) per lane.
+template <int R>
+struct Stage {
+    f16x8 k[R / 8][kBlock];        // octet of values, key
+    f16x8 v[8][R];                 // eight keys (2 j + h: 16 j + 4 h + {0..3, 8..11}), value
+};
+
+template <int NT, int DT>
+__global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
+    using T = typename Type<DT>::T;
+    constexpr bool SPLIT = DT == US_F32;
+    constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    Stage<R> *stage = (Stage<R> *)lds;
+    __shared__ int flag;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, h = lane >> 5;
+    // The tiles of a unit (sequence, cache head) follow each other on one XCD,
+    // whose L2 then serves their keys; the last tile, which sees the most, first.
+    const int per = a.sp.tiles * a.sp.splits;
+    int u = blockIdx.x / per, slot = blockIdx.x % per;
+    if (units % 8 == 0) {
+        u = (blockIdx.x >> 3) / per * 8 + (blockIdx.x & 7);
+        slot = (blockIdx.x >> 3) % per;
+    }
+    const int tile = a.sp.tiles - 1 - slot / a.sp.splits, split = slot % a.sp.splits;
+    const int b = u / a.heads, hk = u - b * a.heads;
+    int r0, n;
+    a.s.rows(b, r0, n);
+    const int len = a.s.len(b), total = n * a.G, base = tile * kRows;
+    if (base >= total) return;
+    const int last_row = min(base + kRows, total) - 1;
+    int lo0, hi0, lo1, hi1;
+    a.mask.range(base / a.G, n, len, lo0, hi0);
+    a.mask.range(last_row / a.G, n, len, lo1, hi1);
+    const int first = lo0 / kBlock, end = (hi1 + kBlock - 1) / kBlock;
+    const int ns = max((end - first + a.sp.chunk - 1) / a.sp.chunk, 1);
+    if (split >= ns) return;
+    const int start = first + split * a.sp.chunk, stop = min(start + a.sp.chunk, end);
+    // This wavefront's rows, and this lane's; the range of keys that they see.
+    const int w0 = min(base + 32 * wave, last_row), w1 = min(base + 32 * wave + 31, last_row);
+    int wlo, whi, wlo1, whi0;
+    a.mask.range(w0 / a.G, n, len, wlo, whi0);
+    a.mask.range(w1 / a.G, n, len, wlo1, whi);
+    const int row = min(base + 32 * wave + c, last_row), i = row / a.G, head = hk * a.G + row - i * a.G;
+    const bool real = base + 32 * wave + c <= last_row;
+    int lo, hi;
+    a.mask.range(i, n, len, lo, hi);
+
+    f16x8 qh[NS], ql[NS];
+    float f;
+    {
+        const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+        float mx = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            float x[8];
+            load_octet_any<DT>(src, 2 * t + h, a.D, a.vec, x);
+            mx = magnitude(x, mx);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        float inv;
+        const float norm = row_norm(mx, inv);
+        f = inv * a.scale;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            float x[8];
+            load_octet_any<DT>(src, 2 * t + h, a.D, a.vec, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= norm;
+            halve<SPLIT>(x, qh[t], ql[t]);
+        }
+    }
+
+    // Blocks on their way: 16-byte pieces of the codes in registers.
+    constexpr int kPieces = 4 * R / kThreads + (4 * R % kThreads ? 1 : 0);     // of the keys, per thread
+    constexpr int kPairs = 2 * R / kThreads + (2 * R % kThreads ? 1 : 0);      // of the values, two pieces each
+    u32x4 kr[kPieces], vr[kPairs][2];
+    float ks_next = 0.0f, vs_next = 0.0f;
+    auto fetch = [&](int blk) {
+        const int id = a.s.block(b, blk);
+        const int64_t at = (int64_t)max(id, 0) * a.heads + hk;
+        ks_next = id < 0 ? -1.0f : a.ks[at];
+        vs_next = a.vs[at];
+        const uint8_t *kp = a.k + at * (kBlock * R), *vp = a.v + at * (kBlock * R);
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+            // (64 lanes: 16 keys x 4 octets, one KB)
+            const int q = tid + kThreads * x;
+            if (4 * R % kThreads == 0 || q < 4 * R) kr[x] = *(const u32x4 *)(kp + 1024 * (q >> 6) + 64 * (q & 15) + 16 * ((q >> 4) & 3));
+        }
+#pragma unroll
+        for (int x = 0; x < kPairs; ++x) {
+            const int q = tid + kThreads * x, d = q >> 1;
+            if (2 * R % kThreads == 0 || q < 2 * R) {
+                vr[x][0] = *(const u32x4 *)(vp + 64 * d + 16 * (q & 1));
+                vr[x][1] = *(const u32x4 *)(vp + 64 * d + 16 * (q & 1) + 32);
+            }
+        }
+    };
+    auto put = [&](Stage<R> &st) {
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+            const int q = tid + kThreads * x;
+            if (4 * R % kThreads == 0 || q < 4 * R) {
+                const int oct = 4 * (q >> 7) + ((q >> 4) & 3), key = 32 * ((q >> 6) & 1) + (q & 15);
+                st.k[oct][key] = halves_of(kr[x][0], kr[x][1]);
+                st.k[oct][key + 16] = halves_of(kr[x][2], kr[x][3]);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kPairs; ++x) {
+            const int q = tid + kThreads * x, d = q >> 1;
+            if (2 * R % kThreads == 0 || q < 2 * R) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) st.v[2 * j + (q & 1)][d] = halves_of(vr[x][0][j], vr[x][1][j]);
+            }
+        }
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    f32x16 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
+    if (start < stop) {
+        fetch(start);
+        put(stage[0]);
+    }
+    __syncthreads();
+    for (int blk = start; blk < stop; ++blk) {
+        const Stage<R> &st = stage[(blk - start) & 1];
+        const float ks = ks_next, vs = vs_next;
+        if (blk + 1 < stop) fetch(blk + 1);
+        const int k0 = blk * kBlock;
+        if (k0 < whi && k0 + kBlock > wlo && ks >= 0.0f) {
+            // Lane (c, h), element v of s[y]: key 32 y + 8 (v / 4) + 4 h + v % 4, row c.
+            f32x16 s[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[y][v] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < NS; ++t) {
+                    const f16x8 kf = st.k[2 * t + h][32 * y + c];
+                    s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[t], s[y], 0, 0, 0);
+                    if constexpr (SPLIT) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[t], s[y], 0, 0, 0);
+                }
+            }
+            const float fk = f * ks;
+            if (k0 < wlo1 || k0 + kBlock > whi0) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int j = k0 + 32 * y + 8 * (v >> 2) + 4 * h + (v & 3);
+                        if (j < lo || j >= hi) s[y][v] = -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) top = fmaxf(top, s[y][v]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            // (a key scale of 0 times the -inf of a masked key would be a NaN)
+            const float m2 = fmaxf(m, top == -INFINITY ? top : top * fk), sub = base_of(m2) - kLift;
+            const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
+            m = m2;
+            l *= alpha;
+            f16x8 ph[4], pl[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = s[j >> 1][8 * (j & 1) + e];
+                    p[e] = __builtin_amdgcn_exp2f(x == -INFINITY ? x : fmaf(x, fk, -sub));
+                    l += p[e];
+                }
+                halve<SPLIT>(p, ph[j], pl[j]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f32x16 pv;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) pv[v] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f16x8 vf = st.v[2 * j + h][32 * t + c];
+                    pv = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], pv, 0, 0, 0);
+                    if constexpr (SPLIT) pv = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], pv, 0, 0, 0);
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[t][v] = fmaf(pv[v], vs, o[t][v] * alpha);
+            }
+        }
+        if (blk + 1 < stop) put(stage[(blk + 1 - start) & 1]);
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32, 64);
+
+    // Lane (c, h), element 4 z + v of o[t]: value 32 t + 8 z + 4 h + v of row c.
+    const int64_t unit = (int64_t)u * a.sp.tiles + tile;
+    if (ns > 1) {
+        const int64_t pr = (unit * a.sp.splits + split) * kRows + 32 * wave + c;
+        if (real) {
+            float *dst = a.sp.part + pr * R + 4 * h;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                    *(f32x4 *)(dst + 32 * t + 8 * z) = (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]};
+            if (h == 0) {
+                a.sp.ml[2 * pr] = m;
+                a.sp.ml[2 * pr + 1] = l;
+            }
+        }
+        if (!last_of(a.sp.tickets + unit, ns, &flag)) return;
+        const int64_t p0 = unit * a.sp.splits * kRows + 32 * wave + c;
+        if (!real) return;
+        m = -INFINITY;
+        for (int z = 0; z < ns; ++z) m = fmaxf(m, a.sp.ml[2 * (p0 + (int64_t)z * kRows)]);
+        l = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
+        for (int z = 0; z < ns; ++z) {
+            const int64_t q = p0 + (int64_t)z * kRows;
+            const float w = __builtin_amdgcn_exp2f(a.sp.ml[2 * q] - base_of(m));
+            l += a.sp.ml[2 * q + 1] * w;
+            const float *src = a.sp.part + q * R + 4 * h;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const f32x4 x = *(const f32x4 *)(src + 32 * t + 8 * y);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[t][4 * y + v] = fmaf(x[v], w, o[t][4 * y + v]);
+                }
+        }
+    }
+    if (!real) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;         // a row without keys gives zeros
+    T *dst = (T *)a.out.data + (int64_t)(r0 + i) * a.out.token_stride + (int64_t)head * a.out.head_stride;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const int d = 32 * t + 8 * z + 4 * h;
+            T y[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) y[v] = Type<DT>::put(o[t][4 * z + v] * inv);
+            if (a.vec) {
+                if (d < a.D) __builtin_memcpy(__builtin_assume_aligned(dst + d, 4 * sizeof(T)), y, 4 * sizeof(T));
+            } else {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (d + v < a.D) dst[d + v] = y[v];
+            }
+        }
+    if (a.sp.lse && h == 0) a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + head] = lse_of(m, l);
+}
+
+// The probabilities' sums over the query rows, from the logarithms of the rows'
+// sums: the first product again, the other way about. A wavefront keeps 32 keys
+// in registers; the rows pass through LDS, 64 at a time.
+template <int NT, int DT>
+__global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args a, float *weights, int64_t stride) {
+    using T = typename Type<DT>::T;
+    constexpr bool SPLIT = DT == US_F32;
+    constexpr int R = 32 * NT, NS = R / 16, kParts = SPLIT ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    f16x8(*q)[R / 8][64] = (f16x8(*)[R / 8][64])lds;       // part, octet, row
+    __shared__ float rf[64], rz[64];
+    __shared__ int rlo[64], rhi[64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, h = lane >> 5, hk = blockIdx.y, b = blockIdx.z;
+    int r0, n;
+    a.s.rows(b, r0, n);
+    const int len = a.s.len(b), j0 = blockIdx.x * 128;
+    if (j0 >= len || n == 0) return;
+    // Rows that see some of these keys.
+    int i0 = 0, i1 = n;
+    if (a.mask.causal) {
+        i0 = max(j0 - (len - n), 0);
+        if (a.mask.window > 0) i1 = (int)min((int64_t)n, (int64_t)j0 + 127 + a.mask.window - (len - n));
+    }
+    const int blk = 2 * (int)blockIdx.x + (wave >> 1);
+    const int id = blk * kBlock < len ? a.s.block(b, blk) : -1;
+    const int64_t at = (int64_t)max(id, 0) * a.heads + hk;
+    const float ks = id < 0 ? 0.0f : a.ks[at];
+    f16x8 kf[NS];
+    {
+        // key 32 (wave & 1) + c, octets 2 t + h
+        const uint8_t *p = a.k + at * (kBlock * R) + 1024 * (wave & 1) + 64 * (c & 15) + 8 * (c >> 4);
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            const u32x2 w = *(const u32x2 *)(p + 2048 * (t >> 1) + 16 * (2 * (t & 1) + h));
+            kf[t] = halves_of(w[0], w[1]);
+        }
+    }
+    const int k0 = blk * kBlock + 32 * (wave & 1);
+    f32x16 sum;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+    for (int base = i0 * a.G; base < i1 * a.G; base += 64) {
+        __syncthreads();
+        {
+            const int rr = 16 * wave + (lane & 15), g = lane >> 4, row = base + rr;
+            const bool real = row < i1 * a.G;
+            const int i = real ? row / a.G : 0, head = hk * a.G + (real ? row - i * a.G : 0);
+            const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+            float x[NT][8], mx = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                load_octet_any<DT>(src, 4 * t + g, a.D, a.vec, x[t]);
+                mx = magnitude(x[t], mx);
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            float inv;
+            const float norm = row_norm(mx, inv);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f16x8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[t][e] *= norm;
+                halve<SPLIT>(x[t], hi, lo);
+                q[0][4 * t + g][rr] = hi;
+                if constexpr (SPLIT) q[1][4 * t + g][rr] = lo;
+            }
+            if (g == 0) {
+                int lo = 0, hi = 0;
+                if (real) a.mask.range(i, n, len, lo, hi);
+                rf[rr] = inv * a.scale;
+                rz[rr] = real ? a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + head] : INFINITY;
+                rlo[rr] = lo;
+                rhi[rr] = hi;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            f32x16 s;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NS; ++t)
+#pragma unroll
+                for (int z = 0; z < kParts; ++z)
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t], q[z][2 * t + h][32 * y + c], s, 0, 0, 0);
+            const float fk = rf[32 * y + c] * ks, z = rz[32 * y + c];
+            const int lo = rlo[32 * y + c], hi = rhi[32 * y + c];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int j = k0 + 8 * (v >> 2) + 4 * h + (v & 3);
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[v], fk, -z));
+                sum[v] += j >= lo && j < hi ? p : 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) sum[v] += __shfl_xor(sum[v], w, 64);
+    if (c == 0 && id >= 0) {
+        float *dst = weights + ((int64_t)b * a.heads + hk) * stride;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int j = k0 + 8 * (v >> 2) + 4 * h + (v & 3);
+            if (j < len) dst[j] += sum[v];
+        }
+    }
+}
+
+// More than 64 KB of dynamic LDS: allowed once per kernel and device.
+template <class K>
+hipError_t allow_lds(K kern, std::atomic<unsigned long long> &set) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) dev = 0;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (set.load(std::memory_order_acquire) & bit) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024);
+    if (e == hipSuccess) set.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
+}  // namespace
+
+hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream) {
+    return with_row(a.D, [&](auto nt) {
+        return with_type(dtype, [&](auto dt) {
+            constexpr int NT = decltype(nt)::value, kLds = 2 * (int)sizeof(Stage<32 * NT>);
+            auto kern = us_kv_prompt_kernel<NT, decltype(dt)::value>;
+            if constexpr (kLds > 65536 - 1024) {
+                static std::atomic<unsigned long long> set{0};
+                const hipError_t e = allow_lds(kern, set);
+                if (e != hipSuccess) return e;
+            }
+            const int units = batch * a.heads;
+            hipLaunchKernelGGL(kern, dim3((unsigned)units * a.sp.tiles * a.sp.splits), dim3(kThreads), kLds, stream, a, units);
+            return hipGetLastError();
+        });
+    });
+}
+
+hipError_t launch_weights(int dtype, const Args &a, int batch, float *weights, int64_t stride, hipStream_t stream) {
+    return with_row(a.D, [&](auto nt) {
+        return with_type(dtype, [&](auto dt) {
+            constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
+            constexpr int kLds = (DT == US_F32 ? 2 : 1) * 64 * 32 * NT * 2;
+            auto kern = us_kv_weights_kernel<NT, DT>;
+            if constexpr (kLds > 65536 - 2048) {
+                static std::atomic<unsigned long long> set{0};
+                const hipError_t e = allow_lds(kern, set);
+                if (e != hipSuccess) return e;
+            }
+            hipLaunchKernelGGL(kern, dim3((a.s.max_len + 127) / 128, a.heads, batch), dim3(kThreads), kLds, stream, a, weights, stride);
+            return hipGetLastError();
+        });
+    });
+}
+
+}  // namespace us_kv

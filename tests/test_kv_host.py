@@ -189,3 +189,19 @@ def test_oracle_kept_by_hand():
     assert ref.kept([math.nan, -math.inf, 1.0], 3, 2, 0) == [1, 2]
     assert ref.kept([3.0, 1.0], 2, 5, 1) == [0, 1]
     assert ref.kept([3.0, 1.0, 2.0], 3, 2, 2) == [1, 2]
+
+
+def test_workspace_sizes_of_edge_shapes():
+    """Sizes exist from one token to long tables and many units, and grow with what has to be kept."""
+    L = kv.lib()
+    n = ctypes.c_size_t(0)
+    for batch, heads, width, max_new, q_heads in ((1, 1, 1, 1, 1), (1, 8, 1 << 14, 1, 64), (65535, 8, 2000, 1, 8),
+                                                  (3, 2, 100, 5000, 16), (1, 1, 1 << 20, 100, 1)):
+        c = kv.CacheStruct(P, P, P, P, 8, heads, 128)
+        s = kv.SeqsStruct(P, width, width, batch, P, P, max_new)
+        for weights in (None, P):
+            o = kv.AttendOpts(0.0, 1, 0, 0, weights, width * 64)
+            r = L.us_kv_attend_workspace_size(ctypes.byref(c), ctypes.byref(s), q_heads, batch * max_new, ctypes.byref(o),
+                                              ctypes.byref(n))
+            assert r == 0 and (n.value >= 4 * q_heads * batch * max_new or not weights), (batch, heads, width)
+            assert n.value < 1 << 42
