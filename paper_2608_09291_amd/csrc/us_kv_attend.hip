@@ -32,7 +32,7 @@ struct Plan {
     bool decode;
     int chunk, splits, tiles, rows;
     int64_t scores_stride;
-    size_t ml, part, lse, scores, total;
+    size_t part, lse, scores, total;
 };
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -61,14 +61,15 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
         p.chunk = (int)((most + want - 1) / want);
         if (p.chunk < 4) p.chunk = 4;
     }
+    // (a unit's partial rows lie within 2^31 bytes)
+    if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
     if (units > kTickets || most <= p.chunk) p.chunk = (int)most;
     p.splits = (int)((most + p.chunk - 1) / p.chunk);
     if (units * p.splits > INT32_MAX / 256) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);
-    const size_t parts = p.splits > 1 ? (size_t)(units * p.splits * p.rows) : 0;
-    p.ml = p.splits > 1 || o.weights ? 4 * kTickets : 0;
-    p.part = p.ml + (size_t)up(8 * (int64_t)parts, 16);
-    p.lse = p.part + parts * R * 4;
+    const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
+    p.part = p.splits > 1 || o.weights ? 4 * kTickets : 0;
+    p.lse = p.part + parts;
     p.scores = p.lse + (o.weights ? (size_t)up((int64_t)q_heads * tokens * 4, 16) : 0);
     p.total = p.scores + (o.weights && p.decode ? (size_t)(pairs * p.tiles * p.rows * p.scores_stride) * 4 : 0);
     return US_OK;
@@ -113,7 +114,7 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     a.q = Rows{q->data, q->token_stride, q->head_stride};
     a.out = Rows{out->data, out->token_stride, out->head_stride};
     a.mask = Mask{o.causal, o.window};
-    a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, (float *)(w + p.part), (float *)(w + p.ml), (int32_t *)w,
+    a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, (float *)(w + p.part), (int32_t *)w,
                  o.weights ? (float *)(w + p.lse) : nullptr, o.weights && p.decode ? (float *)(w + p.scores) : nullptr,
                  p.scores_stride};
     const hipStream_t hs = (hipStream_t)stream;

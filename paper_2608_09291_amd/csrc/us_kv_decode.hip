@@ -39,6 +39,10 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     int lo, hi;
     a.mask.range(i, n, len, lo, hi);
 
+    // Queries: column r of the first product's right operand.
+    RowPart<DT, NT> raw;
+    raw.load((const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride, g, 4, a.D, a.vec);
+
     // This wavefront's blocks: start, start + 4, ... A lane looks one of them up.
     const int start = first + split * a.sp.chunk + wave, stop = min(first + (split + 1) * a.sp.chunk, end);
     const int count = start < stop ? (stop - start + kWaves - 1) / kWaves : 0;
@@ -57,15 +61,13 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     };
     look_up(0);
 
-    // Queries: column r of the first product's right operand.
     f16x8 qh[NT], ql[NT];
     float f;
-    {
-        const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+    auto set_queries = [&]() {
         float x[NT][8], mx = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            load_octet_any<DT>(src, 4 * t + g, a.D, a.vec, x[t]);
+            raw.octet(t, 4 * t + g, a.D, a.D == R, x[t]);
             mx = magnitude(x[t], mx);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -79,7 +81,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
             for (int e = 0; e < 8; ++e) x[t][e] *= norm;
             halve<SPLIT>(x[t], qh[t], ql[t]);
         }
-    }
+    };
 
     const int64_t page = (int64_t)kBlock * R;
     auto at = [&](int c) {                                 // this wavefront's c-th block (block 0 where it is not there)
@@ -108,6 +110,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         load_k(at(0));
         load_v(at(0));
     }
+    set_queries();
     for (int c = 0; c < count; ++c) {
         const int blk = start + kWaves * c;
         const bool there = __builtin_amdgcn_readlane(my_id, c & 63) >= 0;
@@ -131,19 +134,20 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         }
         const float fk = f * ks;
         const int j0 = blk * kBlock + 4 * g;
-        const bool whole = there && blk * kBlock >= lo1 && blk * kBlock + kBlock <= hi0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] *= fk;
+        if (!(there && blk * kBlock >= lo1 && blk * kBlock + kBlock <= hi0)) {
+            const int from = there ? lo - j0 : kBlock, to = hi - j0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) s[u][v] = 16 * u + v >= from && 16 * u + v < to ? s[u][v] : -INFINITY;
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                s[u][v] *= fk;
-                if (!whole) {
-                    const int j = j0 + 16 * u + v;
-                    if (!there || j < lo || j >= hi) s[u][v] = -INFINITY;
-                }
-                top = fmaxf(top, s[u][v]);
-            }
+            for (int v = 0; v < 4; ++v) top = fmaxf(top, s[u][v]);
         if (a.sp.scores && base + r <= last_row) {
             float *dst = a.sp.scores + (((int64_t)b * a.heads + hk) * a.sp.rows * a.sp.tiles + row) * a.sp.scores_stride + j0;
 #pragma unroll
@@ -195,6 +199,8 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     const float mine = __builtin_amdgcn_exp2f(m - base_of(all));
     const int64_t unit = ((int64_t)b * a.heads + hk) * a.sp.tiles + tile;
     const int rows_here = last_row - base + 1;
+    const int one = (a.sp.rows * (R + 2) + 3) / 4 * 4;     // floats of a split
+    const Shared mem(a.sp.part + unit * a.sp.splits * one);
 #pragma unroll
     for (int c0 = 0; c0 < R; c0 += kCols) {
         if (c0) __syncthreads();
@@ -225,14 +231,10 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
                 put_octet<DT>(a, r0 + ti, hd, c0 / 8 + oc, x, ll);
                 if (a.sp.lse && c0 == 0 && oc == 0) a.sp.lse[(int64_t)(r0 + ti) * (a.heads * a.G) + hd] = lse_of(am, ll);
             } else {
-                const int64_t pr = (unit * a.sp.splits + split) * a.sp.rows + rr;
-                float *dst = a.sp.part + pr * R + c0 + 8 * oc;
-                *(f32x4 *)dst = (f32x4){x[0], x[1], x[2], x[3]};
-                *(f32x4 *)(dst + 4) = (f32x4){x[4], x[5], x[6], x[7]};
-                if (c0 == 0 && oc == 0) {
-                    a.sp.ml[2 * pr] = am;
-                    a.sp.ml[2 * pr + 1] = ll;
-                }
+                const uint32_t dst = split * one + rr * R + c0 + 8 * oc;
+                mem.put(dst, (f32x4){x[0], x[1], x[2], x[3]});
+                mem.put(dst + 4, (f32x4){x[4], x[5], x[6], x[7]});
+                if (c0 == 0 && oc == 0) mem.put2(split * one + a.sp.rows * R + 2 * rr, am, ll);
             }
         }
     }
@@ -240,18 +242,23 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     // The last workgroup joins the splits, in their order.
     for (int q = tid; q < rows_here * (R / 8); q += kThreads) {
         const int rr = q / (R / 8), oc = q % (R / 8);
-        const int64_t p0 = unit * a.sp.splits * a.sp.rows + rr;
         float am = -INFINITY, ll = 0.0f, x[8];
-        for (int z = 0; z < ns; ++z) am = fmaxf(am, a.sp.ml[2 * (p0 + (int64_t)z * a.sp.rows)]);
+#pragma unroll 8
+        for (int z = 0; z < ns; ++z) {
+            float mz, lz;
+            mem.get2(z * one + a.sp.rows * R + 2 * rr, mz, lz);
+            am = fmaxf(am, mz);
+        }
         const float bm = base_of(am);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
         for (int z = 0; z < ns; ++z) {
-            const int64_t pr = p0 + (int64_t)z * a.sp.rows;
-            const float w = __builtin_amdgcn_exp2f(a.sp.ml[2 * pr] - bm);
-            ll += a.sp.ml[2 * pr + 1] * w;
-            const f32x4 y0 = *(const f32x4 *)(a.sp.part + pr * R + 8 * oc), y1 = *(const f32x4 *)(a.sp.part + pr * R + 8 * oc + 4);
+            float mz, lz;
+            mem.get2(z * one + a.sp.rows * R + 2 * rr, mz, lz);
+            const f32x4 y0 = mem.get(z * one + rr * R + 8 * oc), y1 = mem.get(z * one + rr * R + 8 * oc + 4);
+            const float w = __builtin_amdgcn_exp2f(mz - bm);
+            ll += lz * w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[e] = fmaf(y0[e], w, x[e]);

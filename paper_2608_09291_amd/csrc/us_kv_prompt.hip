@@ -65,12 +65,13 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
     f16x8 qh[NS], ql[NS];
     float f;
     {
-        const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+        RowPart<DT, NS> raw;
+        raw.load((const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride, h, 2, a.D, a.vec);
         float mx = 0.0f;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
             float x[8];
-            load_octet_any<DT>(src, 2 * t + h, a.D, a.vec, x);
+            raw.octet(t, 2 * t + h, a.D, a.D == R, x);
             mx = magnitude(x, mx);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
             float x[8];
-            load_octet_any<DT>(src, 2 * t + h, a.D, a.vec, x);
+            raw.octet(t, 2 * t + h, a.D, a.D == R, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= norm;
             halve<SPLIT>(x, qh[t], ql[t]);
@@ -219,39 +220,41 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
     // Lane (c, h), element 4 z + v of o[t]: value 32 t + 8 z + 4 h + v of row c.
     const int64_t unit = (int64_t)u * a.sp.tiles + tile;
     if (ns > 1) {
-        const int64_t pr = (unit * a.sp.splits + split) * kRows + 32 * wave + c;
+        constexpr int kOne = kRows * (R + 2);              // floats of a split
+        const Shared mem(a.sp.part + unit * a.sp.splits * kOne);
+        const int rr = 32 * wave + c;
         if (real) {
-            float *dst = a.sp.part + pr * R + 4 * h;
+            const uint32_t dst = split * kOne + rr * R + 4 * h;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int z = 0; z < 4; ++z)
-                    *(f32x4 *)(dst + 32 * t + 8 * z) = (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]};
-            if (h == 0) {
-                a.sp.ml[2 * pr] = m;
-                a.sp.ml[2 * pr + 1] = l;
-            }
+                    mem.put(dst + 32 * t + 8 * z, (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]});
+            if (h == 0) mem.put2(split * kOne + kRows * R + 2 * rr, m, l);
         }
         if (!last_of(a.sp.tickets + unit, ns, &flag)) return;
-        const int64_t p0 = unit * a.sp.splits * kRows + 32 * wave + c;
         if (!real) return;
         m = -INFINITY;
-        for (int z = 0; z < ns; ++z) m = fmaxf(m, a.sp.ml[2 * (p0 + (int64_t)z * kRows)]);
+        for (int z = 0; z < ns; ++z) {
+            float mz, lz;
+            mem.get2(z * kOne + kRows * R + 2 * rr, mz, lz);
+            m = fmaxf(m, mz);
+        }
         l = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
         for (int z = 0; z < ns; ++z) {
-            const int64_t q = p0 + (int64_t)z * kRows;
-            const float w = __builtin_amdgcn_exp2f(a.sp.ml[2 * q] - base_of(m));
-            l += a.sp.ml[2 * q + 1] * w;
-            const float *src = a.sp.part + q * R + 4 * h;
+            float mz, lz;
+            mem.get2(z * kOne + kRows * R + 2 * rr, mz, lz);
+            const float w = __builtin_amdgcn_exp2f(mz - base_of(m));
+            l += lz * w;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const f32x4 x = *(const f32x4 *)(src + 32 * t + 8 * y);
+                    const f32x4 x = mem.get(z * kOne + rr * R + 4 * h + 32 * t + 8 * y);
 #pragma unroll
                     for (int v = 0; v < 4; ++v) o[t][4 * y + v] = fmaf(x[v], w, o[t][4 * y + v]);
                 }
@@ -327,11 +330,12 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_weights_kernel
             const int rr = 16 * wave + (lane & 15), g = lane >> 4, row = base + rr;
             const bool real = row < i1 * a.G;
             const int i = real ? row / a.G : 0, head = hk * a.G + (real ? row - i * a.G : 0);
-            const T *src = (const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride;
+            RowPart<DT, NT> raw;
+            raw.load((const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride, g, 4, a.D, a.vec);
             float x[NT][8], mx = 0.0f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                load_octet_any<DT>(src, 4 * t + g, a.D, a.vec, x[t]);
+                raw.octet(t, 4 * t + g, a.D, a.D == R, x[t]);
                 mx = magnitude(x[t], mx);
             }
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
