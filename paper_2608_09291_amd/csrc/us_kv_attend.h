@@ -6,11 +6,11 @@
 // brings the largest magnitude of q's row to [2^8, 2^9): its float16 form keeps
 // 11 bits of every value that matters, whatever the row's range. Codes are
 // whole numbers up to 127, exact in float16. The running maximum m, the
-// probabilities p_j = 2^(x_j - m + 14) and their sum l are float32; p goes to
-// the second product as float16 (the 14 keeps small ones normal), 2^-12 of
-// each on average, below the rounding of a bfloat16 or float16 result. Float32
-// rows carry the rounded-off part of q and p in a second product each, which
-// leaves 2^-22.
+// probabilities p_j = 2^(x_j - m + 13) and their sum l are float32; p goes to
+// the second product as float16 (the 13 keeps small ones normal), off by 2^-13
+// of each on average, below the rounding of a bfloat16 or float16 result.
+// Float32 rows carry the rounded-off part of q and p in a second product each,
+// which leaves 2^-22.
 #ifndef UNIONSPARSE_US_KV_ATTEND_H
 #define UNIONSPARSE_US_KV_ATTEND_H
 
@@ -23,7 +23,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kLift = 14.0f;                             // log2 of the largest probability's form
+constexpr float kLift = 13.0f;                             // log2 of a probability's form at m
+constexpr float kSlack = 2.0f;                             // what m may lag behind the maximum: 2^15 at most
 
 struct Mask {
     int32_t causal, window;
@@ -150,7 +151,7 @@ __device__ inline void store_octet_any(typename Type<DT>::T *p, int o, int D, bo
 // What is subtracted of a score: the maximum, or 0 where there is none yet.
 __device__ inline float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
-// Stores a finished octet of a row: sums o of probabilities l (times 2^14).
+// Stores a finished octet of a row: sums o of probabilities l (times 2^kLift).
 template <int DT>
 __device__ inline void put_octet(const Args &a, int row, int head, int oct, const float (&x)[8], float l) {
     using T = typename Type<DT>::T;

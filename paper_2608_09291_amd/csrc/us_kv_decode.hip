@@ -137,7 +137,8 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
 #pragma unroll
         for (int u = 0; u < 4; ++u) s[u] *= fk;
         if (!(there && blk * kBlock >= lo1 && blk * kBlock + kBlock <= hi0)) {
-            const int from = there ? lo - j0 : kBlock, to = hi - j0;
+            int from = there ? lo - j0 : kBlock, to = hi - j0;
+            __asm__ volatile("" : "+v"(from), "+v"(to));   // keeps the branch: most blocks have no masked keys
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll

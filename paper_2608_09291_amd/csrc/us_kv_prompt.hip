@@ -134,7 +134,10 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
         }
     };
 
-    float m = -INFINITY, l = 0.0f;
+    // o is in units of vmax, the largest value scale so far: a block's
+    // probabilities go to the second product times ratio = its scale / vmax,
+    // which the exponent takes, so that the product adds up in place.
+    float m = -INFINITY, l = 0.0f, vmax = 0.0f;
     f32x16 o[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -164,14 +167,17 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
                     if constexpr (SPLIT) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[t], s[y], 0, 0, 0);
                 }
             }
-            const float fk = f * ks;
+            // (above 0, so that a masked key's -inf stays one)
+            const float fk = fmaxf(f * ks, 1.17549435e-38f);
             if (k0 < wlo1 || k0 + kBlock > whi0) {
+                int from = lo - k0 - 4 * h, to = hi - k0 - 4 * h;
+                __asm__ volatile("" : "+v"(from), "+v"(to));   // keeps the branch: most blocks have no masked keys
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int j = k0 + 32 * y + 8 * (v >> 2) + 4 * h + (v & 3);
-                        if (j < lo || j >= hi) s[y][v] = -INFINITY;
+                        const int j = 32 * y + 8 * (v >> 2) + (v & 3);
+                        s[y][v] = j >= from && j < to ? s[y][v] : -INFINITY;
                     }
             }
             float top = -INFINITY;
@@ -180,42 +186,58 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
 #pragma unroll
                 for (int v = 0; v < 16; ++v) top = fmaxf(top, s[y][v]);
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            // (a key scale of 0 times the -inf of a masked key would be a NaN)
-            const float m2 = fmaxf(m, top == -INFINITY ? top : top * fk), sub = base_of(m2) - kLift;
-            const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
-            m = m2;
-            l *= alpha;
+            // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
+            const float m2 = fmaxf(m, top * fk);
+            float change = 1.0f;
+            if (vs > vmax) {
+                change = vmax * __builtin_amdgcn_rcpf(vs);
+                vmax = vs;
+            }
+            if (m2 > m + kSlack || m == -INFINITY) {
+                const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
+                m = m2;
+                l *= alpha;
+                change *= alpha;
+            }
+            if (__builtin_amdgcn_ballot_w64(change != 1.0f)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[t][v] *= change;
+            }
+            // (2^-60: below what any sum keeps; 1 as long as all scales are 0, where o does not count)
+            const float ratio = vmax > 0.0f ? fmaxf(vs * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
+            const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
+            float sum = 0.0f;
             f16x8 ph[4], pl[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float p[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = s[j >> 1][8 * (j & 1) + e];
-                    p[e] = __builtin_amdgcn_exp2f(x == -INFINITY ? x : fmaf(x, fk, -sub));
-                    l += p[e];
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(s[j >> 1][8 * (j & 1) + e], fk, -sub));
+                    sum += p[e];
                 }
                 halve<SPLIT>(p, ph[j], pl[j]);
             }
+            l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f32x16 pv;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) pv[v] = 0.0f;
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const f16x8 vf = st.v[2 * j + h][32 * t + c];
-                    pv = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], pv, 0, 0, 0);
-                    if constexpr (SPLIT) pv = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], pv, 0, 0, 0);
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
+                    if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
                 }
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[t][v] = fmaf(pv[v], vs, o[t][v] * alpha);
-            }
         }
         if (blk + 1 < stop) put(stage[(blk + 1 - start) & 1]);
         __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[t][v] *= vmax;
 
     // Lane (c, h), element 4 z + v of o[t]: value 32 t + 8 z + 4 h + v of row c.
     const int64_t unit = (int64_t)u * a.sp.tiles + tile;
