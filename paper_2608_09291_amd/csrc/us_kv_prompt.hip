@@ -21,7 +21,7 @@ struct Stage {
 };
 
 template <int NT, int DT>
-__global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
+__global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
@@ -92,44 +92,57 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
     constexpr int kPieces = 4 * R / kThreads + (4 * R % kThreads ? 1 : 0);     // of the keys, per thread
     constexpr int kPairs = 2 * R / kThreads + (2 * R % kThreads ? 1 : 0);      // of the values, two pieces each
     u32x4 kr[kPieces], vr[kPairs][2];
-    float ks_next = 0.0f, vs_next = 0.0f;
-    auto fetch = [&](int blk) {
-        const int id = a.s.block(b, blk);
-        const int64_t at = (int64_t)max(id, 0) * a.heads + hk;
-        ks_next = id < 0 ? -1.0f : a.ks[at];
-        vs_next = a.vs[at];
-        const uint8_t *kp = a.k + at * (kBlock * R), *vp = a.v + at * (kBlock * R);
+    // A lane looks up one of 64 blocks, the next ones when those are used up.
+    const int count = stop - start;
+    int id_k, id_v;
+    float sc_k, sc_v;                                      // of the 64 blocks whose keys (values) are in use
+    auto look_up = [&](int c, int &id, float &sc, const float *scales) {
+        id = -1;
+        sc = -1.0f;
+        if (c + lane < count) {
+            id = a.s.block(b, start + c + lane);
+            if (id >= 0) sc = scales[(int64_t)id * a.heads + hk];
+        }
+    };
+    auto lane_of = [](float x, int c) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), c & 63)); };
+    auto fetch_k = [&](int c) {
+        const uint8_t *kp = a.k + ((int64_t)max(__builtin_amdgcn_readlane(id_k, c & 63), 0) * a.heads + hk) * (kBlock * R);
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
             // (64 lanes: 16 keys x 4 octets, one KB)
             const int q = tid + kThreads * x;
             if (4 * R % kThreads == 0 || q < 4 * R) kr[x] = *(const u32x4 *)(kp + 1024 * (q >> 6) + 64 * (q & 15) + 16 * ((q >> 4) & 3));
         }
+    };
+    auto fetch_v = [&](int c) {
+        const uint8_t *vp = a.v + ((int64_t)max(__builtin_amdgcn_readlane(id_v, c & 63), 0) * a.heads + hk) * (kBlock * R);
 #pragma unroll
         for (int x = 0; x < kPairs; ++x) {
-            const int q = tid + kThreads * x, d = q >> 1;
+            const int q = tid + kThreads * x;
             if (2 * R % kThreads == 0 || q < 2 * R) {
-                vr[x][0] = *(const u32x4 *)(vp + 64 * d + 16 * (q & 1));
-                vr[x][1] = *(const u32x4 *)(vp + 64 * d + 16 * (q & 1) + 32);
+                vr[x][0] = *(const u32x4 *)(vp + 64 * (q >> 1) + 16 * (q & 1));
+                vr[x][1] = *(const u32x4 *)(vp + 64 * (q >> 1) + 16 * (q & 1) + 32);
             }
         }
     };
-    auto put = [&](Stage<R> &st) {
+    auto put_k = [&](int buf) {
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
             const int q = tid + kThreads * x;
             if (4 * R % kThreads == 0 || q < 4 * R) {
                 const int oct = 4 * (q >> 7) + ((q >> 4) & 3), key = 32 * ((q >> 6) & 1) + (q & 15);
-                st.k[oct][key] = halves_of(kr[x][0], kr[x][1]);
-                st.k[oct][key + 16] = halves_of(kr[x][2], kr[x][3]);
+                stage[buf].k[oct][key] = halves_of(kr[x][0], kr[x][1]);
+                stage[buf].k[oct][key + 16] = halves_of(kr[x][2], kr[x][3]);
             }
         }
+    };
+    auto put_v = [&](int buf) {
 #pragma unroll
         for (int x = 0; x < kPairs; ++x) {
-            const int q = tid + kThreads * x, d = q >> 1;
+            const int q = tid + kThreads * x;
             if (2 * R % kThreads == 0 || q < 2 * R) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) st.v[2 * j + (q & 1)][d] = halves_of(vr[x][0][j], vr[x][1][j]);
+                for (int j = 0; j < 4; ++j) stage[buf].v[2 * j + (q & 1)][q >> 1] = halves_of(vr[x][0][j], vr[x][1][j]);
             }
         }
     };
@@ -138,99 +151,138 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(
     // probabilities go to the second product times ratio = its scale / vmax,
     // which the exponent takes, so that the product adds up in place.
     float m = -INFINITY, l = 0.0f, vmax = 0.0f;
-    f32x16 o[NT];
+    f32x16 o[NT], s[2];                                    // s: scores of the block that is next in line
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
-    if (start < stop) {
-        fetch(start);
-        put(stage[0]);
+    // Lane (c, h), element v of s[y]: key 32 y + 8 (v / 4) + 4 h + v % 4, row c.
+    auto scores = [&](int buf, f32x16 (&x)[2]) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[y][v] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                const f16x8 kf = stage[buf].k[2 * t + h][32 * y + c];
+                x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[t], x[y], 0, 0, 0);
+                if constexpr (SPLIT) x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[t], x[y], 0, 0, 0);
+            }
+        }
+    };
+    auto hide = [&](int i, float ks, f32x16 (&x)[2]) {     // the masked keys of block i
+        const int k0 = (start + i) * kBlock;
+        if (k0 >= wlo1 && k0 + kBlock <= whi0 && ks >= 0.0f) return;
+        int from = ks < 0.0f ? kBlock : lo - k0 - 4 * h, to = hi - k0 - 4 * h;
+        __asm__ volatile("" : "+v"(from), "+v"(to));       // keeps the branch: most blocks have no masked keys
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int j = 32 * y + 8 * (v >> 2) + (v & 3);
+                x[y][v] = j >= from && j < to ? x[y][v] : -INFINITY;
+            }
+    };
+    auto largest = [&](const f32x16 (&x)[2]) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, x[y][v]);
+        return fmaxf(top, __shfl_xor(top, 32, 64));
+    };
+    // A block's keys are staged two blocks ahead of their exponentials, its
+    // values one; scores are computed one ahead. So the matrix cores work on
+    // the next scores under a block's exponentials, and on its second product
+    // under the staging of later blocks, in one wavefront.
+    float ks = 0.0f, top = -INFINITY;
+    if (count > 0) {
+        look_up(0, id_k, sc_k, a.ks);
+        look_up(0, id_v, sc_v, a.vs);
+        fetch_k(0);
+        fetch_v(0);
+        put_k(0);
+        put_v(0);
+        if (count > 1) {
+            fetch_k(1);
+            fetch_v(1);
+            put_k(1);
+        }
+        __syncthreads();
+        ks = lane_of(sc_k, 0);
+        scores(0, s);
+        hide(0, ks, s);
+        top = largest(s);
+        __syncthreads();
+        if (count > 2) fetch_k(2);
     }
-    __syncthreads();
-    for (int blk = start; blk < stop; ++blk) {
-        const Stage<R> &st = stage[(blk - start) & 1];
-        const float ks = ks_next, vs = vs_next;
-        if (blk + 1 < stop) fetch(blk + 1);
-        const int k0 = blk * kBlock;
-        if (k0 < whi && k0 + kBlock > wlo && ks >= 0.0f) {
-            // Lane (c, h), element v of s[y]: key 32 y + 8 (v / 4) + 4 h + v % 4, row c.
-            f32x16 s[2];
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[y][v] = 0.0f;
-#pragma unroll
-                for (int t = 0; t < NS; ++t) {
-                    const f16x8 kf = st.k[2 * t + h][32 * y + c];
-                    s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[t], s[y], 0, 0, 0);
-                    if constexpr (SPLIT) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[t], s[y], 0, 0, 0);
-                }
-            }
-            // (above 0, so that a masked key's -inf stays one)
-            const float fk = fmaxf(f * ks, 1.17549435e-38f);
-            if (k0 < wlo1 || k0 + kBlock > whi0) {
-                int from = lo - k0 - 4 * h, to = hi - k0 - 4 * h;
-                __asm__ volatile("" : "+v"(from), "+v"(to));   // keeps the branch: most blocks have no masked keys
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int j = 32 * y + 8 * (v >> 2) + (v & 3);
-                        s[y][v] = j >= from && j < to ? s[y][v] : -INFINITY;
-                    }
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) top = fmaxf(top, s[y][v]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
-            const float m2 = fmaxf(m, top * fk);
-            float change = 1.0f;
-            if (vs > vmax) {
-                change = vmax * __builtin_amdgcn_rcpf(vs);
-                vmax = vs;
-            }
-            if (m2 > m + kSlack || m == -INFINITY) {
-                const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
-                m = m2;
-                l *= alpha;
-                change *= alpha;
-            }
-            if (__builtin_amdgcn_ballot_w64(change != 1.0f)) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) o[t][v] *= change;
-            }
-            // (2^-60: below what any sum keeps; 1 as long as all scales are 0, where o does not count)
-            const float ratio = vmax > 0.0f ? fmaxf(vs * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
-            const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
-            float sum = 0.0f;
-            f16x8 ph[4], pl[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float p[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(fmaf(s[j >> 1][8 * (j & 1) + e], fk, -sub));
-                    sum += p[e];
-                }
-                halve<SPLIT>(p, ph[j], pl[j]);
-            }
-            l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
+    for (int i = 0; i < count; ++i) {
+        const float vs = lane_of(sc_v, i), ks_next = lane_of(sc_k, min(i + 1, count - 1));
+        // (above 0, so that a masked key's -inf stays one)
+        const float fk = fmaxf(f * fabsf(ks), 1.17549435e-38f);
+        // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
+        const float m2 = fmaxf(m, top * fk);
+        float change = 1.0f;
+        if (vs > vmax) {
+            change = vmax * __builtin_amdgcn_rcpf(vs);
+            vmax = vs;
+        }
+        if (m2 > m + kSlack || m == -INFINITY) {
+            const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
+            m = m2;
+            l *= alpha;
+            change *= alpha;
+        }
+        if (__builtin_amdgcn_ballot_w64(change != 1.0f)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f16x8 vf = st.v[2 * j + h][32 * t + c];
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
-                    if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
-                }
+                for (int v = 0; v < 16; ++v) o[t][v] *= change;
         }
-        if (blk + 1 < stop) put(stage[(blk + 1 - start) & 1]);
+        // (2^-60: below what any sum keeps; 1 as long as all scales are 0, where o does not count)
+        const float ratio = vmax > 0.0f ? fmaxf(vs * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
+        const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
+        float sum = 0.0f;
+        f16x8 ph[4], pl[4];
+        f32x16 next[2];
+        scores((i + 1) & 1, next);                         // (of no use after the last block)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf(s[j >> 1][8 * (j & 1) + e], fk, -sub));
+                sum += p[e];
+            }
+            halve<SPLIT>(p, ph[j], pl[j]);
+        }
+        l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
+        // (keeps the exponentials here, beside the scores' product)
+        __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
+        if (i + 1 < count) hide(i + 1, ks_next, next);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f16x8 vf = stage[i & 1].v[2 * j + h][32 * t + c];
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
+                if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
+            }
+        top = largest(next);
+        ks = ks_next;
+        // (past the last block: codes of an earlier one once more, which no product takes)
+        put_k(i & 1);
+        put_v((i + 1) & 1);
+        if (i + 3 < count) {
+            if (((i + 3) & 63) == 0) look_up(i + 3, id_k, sc_k, a.ks);
+            fetch_k(i + 3);
+        }
+        if (i + 2 < count) {
+            if (((i + 2) & 63) == 0) look_up(i + 2, id_v, sc_v, a.vs);
+            fetch_v(i + 2);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) s[y] = next[y];
         __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);
