@@ -47,8 +47,14 @@ struct Split {
     int32_t chunk, splits, tiles, rows;
     float *part;      // the rows of a split, then their (m, l): rows (R + 2) floats, to a multiple of 4
     int32_t *tickets;
-    float *lse;       // (row, query head): m + log2 l, +inf for a row without keys; or NULL
-    float *scores;    // decode with weights: x_j by (sequence, head, row, key); or NULL
+    // For the weights, by cache head and row_block(), 32 rows each; else NULL.
+    float *lse;       // m + log2 l, +inf for a row without keys
+    int64_t row_blocks;                                    // of a head
+    // of prompts: the rows' float16 form by (part, octet, row), and f without the key scale
+    f16x8 *qn;
+    float *qf;
+    // of decode: x_j by (sequence, head, row, key)
+    float *scores;
     int64_t scores_stride;
 };
 
@@ -205,6 +211,18 @@ __device__ inline bool last_of(int32_t *ticket, int n, int *lds) {
     __syncthreads();
     __asm__ volatile("" ::: "memory");
     return *lds != 0;
+}
+
+// Wavefronts of a prompt workgroup, 32 query rows each. Eight share the
+// conversion of a block among twice the rows (8192 causal rows, 32 heads of 128:
+// 611 us against 639 with four); wider rows and float32's two parts take the
+// registers of four.
+constexpr int prompt_waves(int row, bool f32) { return row <= 128 && !f32 ? 8 : 4; }
+
+// The block of 32 rows that holds row `row` of sequence b, whose first token row is r0 and
+// which has a.G rows to a token: every sequence begins a block of its own.
+__device__ inline int64_t row_block(const Args &a, int hk, int b, int r0, int row) {
+    return hk * a.sp.row_blocks + (int64_t)r0 * a.G / 32 + b + row / 32;
 }
 
 hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream);

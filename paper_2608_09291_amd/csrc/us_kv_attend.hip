@@ -32,17 +32,19 @@ struct Plan {
     bool decode;
     int chunk, splits, tiles, rows;
     int64_t scores_stride;
-    size_t part, lse, scores, total;
+    int64_t row_blocks;
+    size_t part, lse, qf, qn, scores, total;
 };
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int tokens, const us_kv_attend_opts &o, Plan &p) {
+us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int tokens, bool f32, const us_kv_attend_opts &o,
+                  Plan &p) {
     const int max_len = seqs_of(c, s, o.max_len, tokens).max_len, R = row_of(c.head_dim);
     const int64_t rows = (int64_t)s.max_new * (q_heads / c.heads), pairs = (int64_t)s.batch * c.heads;
     if (rows > INT32_MAX / 2) return US_ERR_SHAPE;
     p.decode = rows <= 32;
-    const int tile = p.decode ? 16 : 128;
+    const int tile = p.decode ? 16 : 32 * prompt_waves(R, f32);
     p.tiles = (int)((rows + tile - 1) / tile);
     p.rows = rows < tile && p.decode ? (int)rows : tile;
     const int64_t units = pairs * p.tiles;
@@ -70,7 +72,12 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
     p.part = p.splits > 1 || o.weights ? 4 * kTickets : 0;
     p.lse = p.part + parts;
-    p.scores = p.lse + (o.weights ? (size_t)up((int64_t)q_heads * tokens * 4, 16) : 0);
+    // (one block past the last is read)
+    p.row_blocks = (int64_t)tokens * (q_heads / c.heads) / 32 + s.batch + 2;
+    const size_t rows32 = o.weights ? (size_t)(c.heads * p.row_blocks * 32) : 0;
+    p.qf = p.lse + 4 * rows32;
+    p.qn = p.qf + (p.decode ? 0 : 4 * rows32);
+    p.scores = p.qn + (p.decode ? 0 : (f32 ? 4 : 2) * R * rows32);
     p.total = p.scores + (o.weights && p.decode ? (size_t)(pairs * p.tiles * p.rows * p.scores_stride) * 4 : 0);
     return US_OK;
 }
@@ -84,9 +91,11 @@ extern "C" us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const
     if (st != US_OK) return st;
     if (!bytes) return US_ERR_ARG;
     if (tokens < 1) return US_ERR_SHAPE;
-    Plan p;
-    st = plan_of(*cache, *seqs, q_heads, tokens, o, p);
-    if (st == US_OK) *bytes = p.total;
+    // (of either kind of rows)
+    Plan p, p32;
+    st = plan_of(*cache, *seqs, q_heads, tokens, false, o, p);
+    if (st == US_OK) st = plan_of(*cache, *seqs, q_heads, tokens, true, o, p32);
+    if (st == US_OK) *bytes = p.total > p32.total ? p.total : p32.total;
     return st;
 }
 
@@ -101,7 +110,7 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     if (q->dtype != out->dtype) return US_ERR_ARG;
     if (q->tokens != out->tokens) return US_ERR_SHAPE;
     Plan p;
-    st = plan_of(*cache, *seqs, q_heads, q->tokens, o, p);
+    st = plan_of(*cache, *seqs, q_heads, q->tokens, q->dtype == US_F32, o, p);
     if (st != US_OK) return st;
     if (p.total && (!ws || (uintptr_t)ws % 16 || ws_bytes < p.total)) return US_ERR_ARG;
     uint8_t *w = (uint8_t *)ws;
@@ -115,8 +124,9 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     a.out = Rows{out->data, out->token_stride, out->head_stride};
     a.mask = Mask{o.causal, o.window};
     a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, (float *)(w + p.part), (int32_t *)w,
-                 o.weights ? (float *)(w + p.lse) : nullptr, o.weights && p.decode ? (float *)(w + p.scores) : nullptr,
-                 p.scores_stride};
+                 o.weights ? (float *)(w + p.lse) : nullptr, p.row_blocks,
+                 o.weights && !p.decode ? (f16x8 *)(w + p.qn) : nullptr, (float *)(w + p.qf),
+                 o.weights && p.decode ? (float *)(w + p.scores) : nullptr, p.scores_stride};
     const hipStream_t hs = (hipStream_t)stream;
     hipError_t e = p.decode ? launch_decode(q->dtype, a, seqs->batch, hs) : launch_prompt(q->dtype, a, seqs->batch, hs);
     if (e == hipSuccess && o.weights)

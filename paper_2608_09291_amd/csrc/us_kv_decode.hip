@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
             const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
             if (ns == 1) {
                 put_octet<DT>(a, r0 + ti, hd, c0 / 8 + oc, x, ll);
-                if (a.sp.lse && c0 == 0 && oc == 0) a.sp.lse[(int64_t)(r0 + ti) * (a.heads * a.G) + hd] = lse_of(am, ll);
+                if (a.sp.lse && c0 == 0 && oc == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
             } else {
                 const uint32_t dst = split * one + rr * R + c0 + 8 * oc;
                 mem.put(dst, (f32x4){x[0], x[1], x[2], x[3]});
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         }
         const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
         put_octet<DT>(a, r0 + ti, hd, oc, x, ll);
-        if (a.sp.lse && oc == 0) a.sp.lse[(int64_t)(r0 + ti) * (a.heads * a.G) + hd] = lse_of(am, ll);
+        if (a.sp.lse && oc == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
     }
 }
 
@@ -283,12 +283,12 @@ __global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, f
     float sum[4] = {0, 0, 0, 0};
     // (no tile has stored scores of blocks ahead of its first row's window or past its last row's)
     for (int row = 0; row < total; ++row) {
-        const int i = row / a.G, tile = row / kRows;
+        const int tile = row / kRows;
         int lo, hi, x;
         a.mask.range(tile * kRows / a.G, n, len, lo, x);
         a.mask.range((min(tile * kRows + kRows, total) - 1) / a.G, n, len, x, hi);
         if (j0 < lo / kBlock * kBlock || j0 >= hi) continue;
-        const float z = a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + hk * a.G + row - i * a.G];
+        const float z = a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32];
         const f32x4 s = *(const f32x4 *)(a.sp.scores + (bh * a.sp.rows * a.sp.tiles + row) * a.sp.scores_stride + j0);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sum[v] += __builtin_amdgcn_exp2f(s[v] - z);

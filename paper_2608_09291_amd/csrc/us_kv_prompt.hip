@@ -10,7 +10,6 @@
 namespace us_kv {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kRows = 128;     // 32 rows per wavefront
 
 // A block's keys and values as float16 in LDS, in the order of the operands:
 // 16 bytes (8 values of a key; 8 keys of a value) per lane.
@@ -20,9 +19,10 @@ struct Stage {
     f16x8 v[8][R];                 // eight keys (2 j + h: 16 j + 4 h + {0..3, 8..11}), value
 };
 
-template <int NT, int DT>
-__global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
+template <int NT, int DT, int W>
+__global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
+    constexpr int kThreads = 64 * W, kRows = 32 * W;       // 32 rows per wavefront
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -88,6 +88,18 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
         }
     }
 
+    if (a.sp.qn && split == 0 && real) {
+        const int64_t rb = row_block(a, hk, b, r0, row);
+        constexpr int kParts = SPLIT ? 2 : 1;
+        f16x8 *dst = a.sp.qn + rb * (kParts * R / 8 * 32) + h * 32 + c;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            dst[64 * t] = qh[t];
+            if constexpr (SPLIT) dst[64 * t + R / 8 * 32] = ql[t];
+        }
+        if (h == 0) a.sp.qf[32 * rb + c] = f;
+    }
+
     // Blocks on their way: 16-byte pieces of the codes in registers.
     constexpr int kPieces = 4 * R / kThreads + (4 * R % kThreads ? 1 : 0);     // of the keys, per thread
     constexpr int kPairs = 2 * R / kThreads + (2 * R % kThreads ? 1 : 0);      // of the values, two pieces each
@@ -151,7 +163,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
     // probabilities go to the second product times ratio = its scale / vmax,
     // which the exponent takes, so that the product adds up in place.
     float m = -INFINITY, l = 0.0f, vmax = 0.0f;
-    f32x16 o[NT], s[2];                                    // s: scores of the block that is next in line
+    f32x16 o[NT], sa[2], sb[2];                            // scores of a block and of the next one, in turn
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -210,13 +222,14 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
         }
         __syncthreads();
         ks = lane_of(sc_k, 0);
-        scores(0, s);
-        hide(0, ks, s);
-        top = largest(s);
+        scores(0, sa);
+        hide(0, ks, sa);
+        top = largest(sa);
         __syncthreads();
         if (count > 2) fetch_k(2);
     }
-    for (int i = 0; i < count; ++i) {
+    auto step = [&](int i, auto odd, f32x16 (&s)[2], f32x16 (&next)[2]) {
+        constexpr int cur = decltype(odd)::value, other = 1 - cur;             // stages of blocks i and i + 1
         const float vs = lane_of(sc_v, i), ks_next = lane_of(sc_k, min(i + 1, count - 1));
         // (above 0, so that a masked key's -inf stays one)
         const float fk = fmaxf(f * fabsf(ks), 1.17549435e-38f);
@@ -244,8 +257,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
         const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
         float sum = 0.0f;
         f16x8 ph[4], pl[4];
-        f32x16 next[2];
-        scores((i + 1) & 1, next);                         // (of no use after the last block)
+        scores(other, next);                               // (of no use after the last block)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float p[8];
@@ -264,15 +276,15 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f16x8 vf = stage[i & 1].v[2 * j + h][32 * t + c];
+                const f16x8 vf = stage[cur].v[2 * j + h][32 * t + c];
                 o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
                 if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
             }
         top = largest(next);
         ks = ks_next;
         // (past the last block: codes of an earlier one once more, which no product takes)
-        put_k(i & 1);
-        put_v((i + 1) & 1);
+        put_k(cur);
+        put_v(other);
         if (i + 3 < count) {
             if (((i + 3) & 63) == 0) look_up(i + 3, id_k, sc_k, a.ks);
             fetch_k(i + 3);
@@ -281,9 +293,11 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
             if (((i + 2) & 63) == 0) look_up(i + 2, id_v, sc_v, a.vs);
             fetch_v(i + 2);
         }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) s[y] = next[y];
         __syncthreads();
+    };
+    for (int i = 0; i < count; i += 2) {
+        step(i, std::integral_constant<int, 0>(), sa, sb);
+        if (i + 1 < count) step(i + 1, std::integral_constant<int, 1>(), sb, sa);
     }
     l += __shfl_xor(l, 32, 64);
 #pragma unroll
@@ -353,119 +367,145 @@ __global__ __launch_bounds__(kThreads, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 
                     if (d + v < a.D) dst[d + v] = y[v];
             }
         }
-    if (a.sp.lse && h == 0) a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + head] = lse_of(m, l);
+    if (a.sp.lse && h == 0) a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32] = lse_of(m, l);
 }
 
 // The probabilities' sums over the query rows, from the logarithms of the rows'
-// sums: the first product again, the other way about. A wavefront keeps 32 keys
-// in registers; the rows pass through LDS, 64 at a time.
+// sums: the first product again, the other way about. A wavefront keeps a block
+// of keys in registers; the rows, in the form that the first pass left them,
+// pass through LDS, 64 at a time.
+constexpr int kKeys = 256;                                 // of a workgroup
 template <int NT, int DT>
-__global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args a, float *weights, int64_t stride) {
-    using T = typename Type<DT>::T;
+__global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args a, float *weights, int64_t stride) {
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16, kParts = SPLIT ? 2 : 1;
+    constexpr int kForm = kParts * R / 8 * 32;             // pieces of 32 rows
+    constexpr int kPieces = 2 * kForm / 256;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    f16x8(*q)[R / 8][64] = (f16x8(*)[R / 8][64])lds;       // part, octet, row
-    __shared__ float rf[64], rz[64];
-    __shared__ int rlo[64], rhi[64];
+    f16x8(*q)[2 * kForm] = (f16x8(*)[2 * kForm])lds;       // stage; row block, part, octet, row
+    __shared__ float row_f[2][64], row_z[2][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5, hk = blockIdx.y, b = blockIdx.z;
     int r0, n;
     a.s.rows(b, r0, n);
-    const int len = a.s.len(b), j0 = blockIdx.x * 128;
+    const int len = a.s.len(b), j0 = blockIdx.x * kKeys;
     if (j0 >= len || n == 0) return;
-    // Rows that see some of these keys.
+    // Queries that see some of these keys.
     int i0 = 0, i1 = n;
     if (a.mask.causal) {
         i0 = max(j0 - (len - n), 0);
-        if (a.mask.window > 0) i1 = (int)min((int64_t)n, (int64_t)j0 + 127 + a.mask.window - (len - n));
+        if (a.mask.window > 0) i1 = (int)min((int64_t)n, (int64_t)j0 + kKeys - 1 + a.mask.window - (len - n));
     }
-    const int blk = 2 * (int)blockIdx.x + (wave >> 1);
-    const int id = blk * kBlock < len ? a.s.block(b, blk) : -1;
+    if (i0 >= i1) return;
+    const int total = n * a.G, first = i0 * a.G / 32, end = (i1 * a.G + 31) / 32;   // blocks of rows
+    const int blk = 4 * (int)blockIdx.x + wave, k0 = blk * kBlock;
+    const int id = k0 < len ? a.s.block(b, blk) : -1;
     const int64_t at = (int64_t)max(id, 0) * a.heads + hk;
     const float ks = id < 0 ? 0.0f : a.ks[at];
-    f16x8 kf[NS];
+    const int64_t rb = row_block(a, hk, b, r0, 0);
+    const f16x8 *src = a.sp.qn + rb * kForm;
+    f16x8 piece[kPieces];
+    float f_next = 0.0f, z_next = 0.0f;
+    auto fetch = [&](int x) {                              // row blocks x and x + 1 (there is one past the last)
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) piece[y] = src[(int64_t)x * kForm + tid + 256 * y];
+        if (tid < 64) {
+            f_next = a.sp.qf[32 * (rb + x) + tid];
+            z_next = a.sp.lse[32 * (rb + x) + tid];
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) q[buf][tid + 256 * y] = piece[y];
+        if (tid < 64) {
+            row_f[buf][tid] = f_next;
+            row_z[buf][tid] = z_next;
+        }
+    };
+    fetch(first);
+    f16x8 kf[2][NS];
     {
-        // key 32 (wave & 1) + c, octets 2 t + h
-        const uint8_t *p = a.k + at * (kBlock * R) + 1024 * (wave & 1) + 64 * (c & 15) + 8 * (c >> 4);
+        // keys 32 u + c, octets 2 t + h
+        const uint8_t *p = a.k + at * (kBlock * R) + 64 * (c & 15) + 8 * (c >> 4);
 #pragma unroll
-        for (int t = 0; t < NS; ++t) {
-            const u32x2 w = *(const u32x2 *)(p + 2048 * (t >> 1) + 16 * (2 * (t & 1) + h));
-            kf[t] = halves_of(w[0], w[1]);
-        }
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                const u32x2 w = *(const u32x2 *)(p + 1024 * u + 2048 * (t >> 1) + 16 * (2 * (t & 1) + h));
+                kf[u][t] = halves_of(w[0], w[1]);
+            }
     }
-    const int k0 = blk * kBlock + 32 * (wave & 1);
-    f32x16 sum;
+    put(0);
+    f32x16 sum[2];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
-    for (int base = i0 * a.G; base < i1 * a.G; base += 64) {
-        __syncthreads();
-        {
-            const int rr = 16 * wave + (lane & 15), g = lane >> 4, row = base + rr;
-            const bool real = row < i1 * a.G;
-            const int i = real ? row / a.G : 0, head = hk * a.G + (real ? row - i * a.G : 0);
-            RowPart<DT, NT> raw;
-            raw.load((const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride, g, 4, a.D, a.vec);
-            float x[NT][8], mx = 0.0f;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                raw.octet(t, 4 * t + g, a.D, a.D == R, x[t]);
-                mx = magnitude(x[t], mx);
-            }
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            float inv;
-            const float norm = row_norm(mx, inv);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f16x8 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[t][e] *= norm;
-                halve<SPLIT>(x[t], hi, lo);
-                q[0][4 * t + g][rr] = hi;
-                if constexpr (SPLIT) q[1][4 * t + g][rr] = lo;
-            }
-            if (g == 0) {
-                int lo = 0, hi = 0;
-                if (real) a.mask.range(i, n, len, lo, hi);
-                rf[rr] = inv * a.scale;
-                rz[rr] = real ? a.sp.lse[(int64_t)(r0 + i) * (a.heads * a.G) + head] : INFINITY;
-                rlo[rr] = lo;
-                rhi[rr] = hi;
-            }
-        }
-        __syncthreads();
+        for (int v = 0; v < 16; ++v) sum[u][v] = 0.0f;
+    __syncthreads();
+    for (int x = first; x < end; x += 2) {
+        const int buf = ((x - first) >> 1) & 1;
+        if (x + 2 < end) fetch(x + 2);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-            f32x16 s;
+            f32x16 s[2];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[u][v] = 0.0f;
 #pragma unroll
             for (int t = 0; t < NS; ++t)
 #pragma unroll
-                for (int z = 0; z < kParts; ++z)
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t], q[z][2 * t + h][32 * y + c], s, 0, 0, 0);
-            const float fk = rf[32 * y + c] * ks, z = rz[32 * y + c];
-            const int lo = rlo[32 * y + c], hi = rhi[32 * y + c];
+                for (int z = 0; z < kParts; ++z) {
+                    const f16x8 qf = q[buf][kForm * y + (z * (R / 8) + 2 * t + h) * 32 + c];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int j = k0 + 8 * (v >> 2) + 4 * h + (v & 3);
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[v], fk, -z));
-                sum[v] += j >= lo && j < hi ? p : 0.0f;
+                    for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[u][t], qf, s[u], 0, 0, 0);
+                }
+            const float fk = row_f[buf][32 * y + c] * ks, z = row_z[buf][32 * y + c];
+            const int base = 32 * (x + y), last = min(base + 31, total - 1);
+            int lo0 = 0, hi0 = 0, lo1 = 0, hi1 = 0;
+            if (base < total) {
+                a.mask.range(base / a.G, n, len, lo0, hi0);
+                a.mask.range(last / a.G, n, len, lo1, hi1);
+            }
+            if (base + 32 > total || k0 < lo1 || k0 + kBlock > hi0) {
+                // (rows past the last hold anything)
+                int from = 0, to = 0;
+                if (base + c < total) a.mask.range((base + c) / a.G, n, len, from, to);
+                from -= k0 + 4 * h;
+                to -= k0 + 4 * h;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int j = 32 * u + 8 * (v >> 2) + (v & 3);
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
+                        sum[u][v] += j >= from && j < to ? p : 0.0f;
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sum[u][v] += __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
             }
         }
+        if (x + 2 < end) put(buf ^ 1);
+        __syncthreads();
     }
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int w = 16; w > 0; w >>= 1) sum[v] += __shfl_xor(sum[v], w, 64);
+        for (int v = 0; v < 16; ++v)
+#pragma unroll
+            for (int w = 16; w > 0; w >>= 1) sum[u][v] += __shfl_xor(sum[u][v], w, 64);
     if (c == 0 && id >= 0) {
-        float *dst = weights + ((int64_t)b * a.heads + hk) * stride;
+        float *dst = weights + ((int64_t)b * a.heads + hk) * stride + k0 + 4 * h;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int j = k0 + 8 * (v >> 2) + 4 * h + (v & 3);
-            if (j < len) dst[j] += sum[v];
-        }
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int j = 32 * u + 8 * (v >> 2) + (v & 3);
+                if (k0 + 4 * h + j < len) dst[j] += sum[u][v];
+            }
     }
 }
 
@@ -487,14 +527,15 @@ hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
             constexpr int NT = decltype(nt)::value, kLds = 2 * (int)sizeof(Stage<32 * NT>);
-            auto kern = us_kv_prompt_kernel<NT, decltype(dt)::value>;
+            constexpr int W = prompt_waves(32 * NT, decltype(dt)::value == US_F32);
+            auto kern = us_kv_prompt_kernel<NT, decltype(dt)::value, W>;
             if constexpr (kLds > 65536 - 1024) {
                 static std::atomic<unsigned long long> set{0};
                 const hipError_t e = allow_lds(kern, set);
                 if (e != hipSuccess) return e;
             }
             const int units = batch * a.heads;
-            hipLaunchKernelGGL(kern, dim3((unsigned)units * a.sp.tiles * a.sp.splits), dim3(kThreads), kLds, stream, a, units);
+            hipLaunchKernelGGL(kern, dim3((unsigned)units * a.sp.tiles * a.sp.splits), dim3(64 * W), kLds, stream, a, units);
             return hipGetLastError();
         });
     });
@@ -504,14 +545,14 @@ hipError_t launch_weights(int dtype, const Args &a, int batch, float *weights, i
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
             constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
-            constexpr int kLds = (DT == US_F32 ? 2 : 1) * 64 * 32 * NT * 2;
+            constexpr int kLds = 2 * (DT == US_F32 ? 2 : 1) * 64 * 32 * NT * 2;
             auto kern = us_kv_weights_kernel<NT, DT>;
             if constexpr (kLds > 65536 - 2048) {
                 static std::atomic<unsigned long long> set{0};
                 const hipError_t e = allow_lds(kern, set);
                 if (e != hipSuccess) return e;
             }
-            hipLaunchKernelGGL(kern, dim3((a.s.max_len + 127) / 128, a.heads, batch), dim3(kThreads), kLds, stream, a, weights, stride);
+            hipLaunchKernelGGL(kern, dim3((a.s.max_len + kKeys - 1) / kKeys, a.heads, batch), dim3(256), kLds, stream, a, weights, stride);
             return hipGetLastError();
         });
     });
