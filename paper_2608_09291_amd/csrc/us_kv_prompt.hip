@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     // A lane looks up one of 64 blocks, the next ones when those are used up.
     const int count = stop - start;
     int id_k, id_v;
-    float sc_k, sc_v;                                      // of the 64 blocks whose keys (values) are in use
+    float sc_k, sc_v;
     auto look_up = [&](int c, int &id, float &sc, const float *scales) {
         id = -1;
         sc = -1.0f;
@@ -116,8 +116,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             if (id >= 0) sc = scales[(int64_t)id * a.heads + hk];
         }
     };
+    // Blocks on their way: their keys' (values') scales leave with them.
     auto lane_of = [](float x, int c) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), c & 63)); };
-    auto fetch_k = [&](int c) {
+    auto fetch_k = [&](int c, float &scale) {
+        if (c > 0 && (c & 63) == 0) look_up(c, id_k, sc_k, a.ks);
+        scale = lane_of(sc_k, c);
         const uint8_t *kp = a.k + ((int64_t)max(__builtin_amdgcn_readlane(id_k, c & 63), 0) * a.heads + hk) * (kBlock * R);
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
@@ -126,7 +129,9 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             if (4 * R % kThreads == 0 || q < 4 * R) kr[x] = *(const u32x4 *)(kp + 1024 * (q >> 6) + 64 * (q & 15) + 16 * ((q >> 4) & 3));
         }
     };
-    auto fetch_v = [&](int c) {
+    auto fetch_v = [&](int c, float &scale) {
+        if (c > 0 && (c & 63) == 0) look_up(c, id_v, sc_v, a.vs);
+        scale = lane_of(sc_v, c);
         const uint8_t *vp = a.v + ((int64_t)max(__builtin_amdgcn_readlane(id_v, c & 63), 0) * a.heads + hk) * (kBlock * R);
 #pragma unroll
         for (int x = 0; x < kPairs; ++x) {
@@ -207,32 +212,31 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     // values one; scores are computed one ahead. So the matrix cores work on
     // the next scores under a block's exponentials, and on its second product
     // under the staging of later blocks, in one wavefront.
-    float ks = 0.0f, top = -INFINITY;
+    float top = -INFINITY;
+    float ks0 = 0.0f, ks1 = 0.0f, ks2 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;          // of blocks i, i + 1, i + 2
     if (count > 0) {
         look_up(0, id_k, sc_k, a.ks);
         look_up(0, id_v, sc_v, a.vs);
-        fetch_k(0);
-        fetch_v(0);
+        fetch_k(0, ks0);
+        fetch_v(0, vs0);
         put_k(0);
         put_v(0);
         if (count > 1) {
-            fetch_k(1);
-            fetch_v(1);
+            fetch_k(1, ks1);
+            fetch_v(1, vs1);
             put_k(1);
         }
         __syncthreads();
-        ks = lane_of(sc_k, 0);
         scores(0, sa);
-        hide(0, ks, sa);
+        hide(0, ks0, sa);
         top = largest(sa);
         __syncthreads();
-        if (count > 2) fetch_k(2);
+        if (count > 2) fetch_k(2, ks2);
     }
     auto step = [&](int i, auto odd, f32x16 (&s)[2], f32x16 (&next)[2]) {
         constexpr int cur = decltype(odd)::value, other = 1 - cur;             // stages of blocks i and i + 1
-        const float vs = lane_of(sc_v, i), ks_next = lane_of(sc_k, min(i + 1, count - 1));
         // (above 0, so that a masked key's -inf stays one)
-        const float fk = fmaxf(f * fabsf(ks), 1.17549435e-38f);
+        const float vs = vs0, fk = fmaxf(f * fabsf(ks0), 1.17549435e-38f);
         // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
         const float m2 = fmaxf(m, top * fk);
         float change = 1.0f;
@@ -271,7 +275,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
         l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
         // (keeps the exponentials here, beside the scores' product)
         __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
-        if (i + 1 < count) hide(i + 1, ks_next, next);
+        if (i + 1 < count) hide(i + 1, ks1, next);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -281,18 +285,14 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
                 if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
             }
         top = largest(next);
-        ks = ks_next;
+        ks0 = ks1;
+        ks1 = ks2;
+        vs0 = vs1;
         // (past the last block: codes of an earlier one once more, which no product takes)
         put_k(cur);
         put_v(other);
-        if (i + 3 < count) {
-            if (((i + 3) & 63) == 0) look_up(i + 3, id_k, sc_k, a.ks);
-            fetch_k(i + 3);
-        }
-        if (i + 2 < count) {
-            if (((i + 2) & 63) == 0) look_up(i + 2, id_v, sc_v, a.vs);
-            fetch_v(i + 2);
-        }
+        if (i + 3 < count) fetch_k(i + 3, ks2);
+        if (i + 2 < count) fetch_v(i + 2, vs1);
         __syncthreads();
     };
     for (int i = 0; i < count; i += 2) {

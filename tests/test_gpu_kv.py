@@ -310,6 +310,27 @@ def test_attend_aligned_rows_and_scale(torch_cuda):
         _check(torch, p, lens, new, q, out, dtype, scale=0.3)
 
 
+@pytest.mark.parametrize("lens,new,H,Hk", [
+    ([8500, 4200] + [64] * 62, [33, 40] + [1] * 62, 8, 8),           # rows over more than 64 (and 128) blocks of keys
+    ([17200] + [1] * 2099, [1] * 2100, 8, 8)])                      # single tokens over more than 256
+def test_attend_unsplit_long(torch_cuda, lens, new, H, Hk):
+    """So many sequences that no row is split: one workgroup passes over all keys of the long ones."""
+    torch = torch_cuda
+    announce(f"kv attend unsplit lens={lens[:3]}.. new={new[:3]}..")
+    rng = np.random.default_rng(12)
+    p = Pool(torch, rng, lens, Hk, 64)
+    cache = p.cache()
+    q = torch.from_numpy(rng.normal(0, 1.0, size=(sum(new), H, 64)).astype(np.float32)).cuda().half()
+    out = torch.full_like(q, math.nan)
+    w0 = torch.zeros((len(lens), Hk, p.width * 64), device="cuda")
+    w1 = w0.clone()
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w1)
+    ws = kv.attend_workspace(cache, q, p.dev(p.blocks), **args)
+    kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, out, ws=ws, **args)
+    torch.cuda.synchronize()
+    _check(torch, p, lens, new, q, out, "f16", w0, w1)
+
+
 @pytest.mark.parametrize("new", [1, 3, 140])
 def test_attend_large_and_small_scores(torch_cuda, new):
     """Scores of hundreds (one key takes all), scales that differ by 2^20, a block of scale 0, queries of 1e-6 and 1e5."""
