@@ -157,7 +157,7 @@ __device__ inline void store_octet_any(typename Type<DT>::T *p, int o, int D, bo
 // What is subtracted of a score: the maximum, or 0 where there is none yet.
 __device__ inline float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
-// Stores a finished octet of a row: sums o of probabilities l (times 2^kLift).
+// Stores finished values of a row, x / l: an octet, a quad.
 template <int DT>
 __device__ inline void put_octet(const Args &a, int row, int head, int oct, const float (&x)[8], float l) {
     using T = typename Type<DT>::T;
@@ -166,6 +166,23 @@ __device__ inline void put_octet(const Args &a, int row, int head, int oct, cons
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = x[e] * inv;
     store_octet_any<DT>((T *)a.out.data + (int64_t)row * a.out.token_stride + (int64_t)head * a.out.head_stride, oct, a.D, a.vec, y);
+}
+
+template <int DT>
+__device__ inline void put_quad(const Args &a, int row, int head, int quad, f32x4 x, float l) {
+    using T = typename Type<DT>::T;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T y[4] __attribute__((aligned(4 * sizeof(T))));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = Type<DT>::put(x[e] * inv);
+    T *dst = (T *)a.out.data + (int64_t)row * a.out.token_stride + (int64_t)head * a.out.head_stride + 4 * quad;
+    if (a.vec) {
+        if (4 * quad < a.D) __builtin_memcpy(__builtin_assume_aligned(dst, 4 * sizeof(T)), y, sizeof(y));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (4 * quad + e < a.D) dst[e] = y[e];
+    }
 }
 
 __device__ inline float lse_of(float m, float l) { return l == 0.0f ? INFINITY : base_of(m) - kLift + __builtin_amdgcn_logf(l); }

@@ -56,8 +56,8 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     }
     const int cus = us_device::compute_units();
     if (p.decode) {
-        int64_t chunk = up(units * most / (3 * cus), 4);
-        p.chunk = (int)(chunk < 4 ? 4 : chunk > 32 ? 32 : chunk);
+        int64_t chunk = up(units * most / (2 * cus), 4);
+        p.chunk = (int)(chunk < 4 ? 4 : chunk > 64 ? 64 : chunk);
     } else {
         const int64_t want = units >= 2 * cus ? 1 : (2 * cus + units - 1) / units;
         p.chunk = (int)((most + want - 1) / want);

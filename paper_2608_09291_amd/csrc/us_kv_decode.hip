@@ -20,10 +20,14 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     constexpr int kCols = R > 128 ? R / 2 : R;             // columns joined at a time
     __shared__ __attribute__((aligned(16))) float sum[kWaves][kRows][kCols + 4];
     __shared__ float wm[kWaves][kRows], wl[kWaves][kRows];
+    __shared__ float jm[16][kRows], jl[16][kRows];
     __shared__ int flag;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int tile = blockIdx.x % a.sp.tiles, split = blockIdx.x / a.sp.tiles, hk = blockIdx.y, b = blockIdx.z;
+    // Workgroups go round the XCDs in order of blockIdx, x first: heads and
+    // sequences spread over them, where splits, of which short sequences leave
+    // the later ones empty, would load a few (64 ragged sequences to 8k: 100 us).
+    const int tile = blockIdx.z % a.sp.tiles, split = blockIdx.z / a.sp.tiles, hk = blockIdx.x, b = blockIdx.y;
     int r0, n;
     a.s.rows(b, r0, n);
     const int len = a.s.len(b), total = n * a.G, base = tile * kRows;
@@ -240,35 +244,69 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         }
     }
     if (ns == 1 || !last_of(a.sp.tickets + unit, ns, &flag)) return;
-    // The last workgroup joins the splits, in their order.
-    for (int q = tid; q < rows_here * (R / 8); q += kThreads) {
-        const int rr = q / (R / 8), oc = q % (R / 8);
-        float am = -INFINITY, ll = 0.0f, x[8];
-#pragma unroll 8
-        for (int z = 0; z < ns; ++z) {
-            float mz, lz;
-            mem.get2(z * one + a.sp.rows * R + 2 * rr, mz, lz);
-            am = fmaxf(am, mz);
-        }
+    // The last workgroup joins the splits, in an order that does not depend on
+    // their arrival: first the rows' maxima and sums, 16 splits at a time, then
+    // the rows by quads of values, the splits in as many runs as there are
+    // threads for.
+    {
+        const int rr = tid & 15, z0 = tid >> 4;
+        float mj = -INFINITY, lj = 0.0f;
+        if (rr < rows_here)
+#pragma unroll 4
+            for (int z = z0; z < ns; z += 16) {
+                float mz, lz;
+                mem.get2(z * one + a.sp.rows * R + 2 * rr, mz, lz);
+                const float m2 = fmaxf(mj, mz), to = base_of(m2);
+                lj = lj * __builtin_amdgcn_exp2f(mj - to) + lz * __builtin_amdgcn_exp2f(mz - to);
+                mj = m2;
+            }
+        jm[z0][rr] = mj;
+        jl[z0][rr] = lj;
+    }
+    __syncthreads();
+    const int items = rows_here * (R / 4), runs = items < kThreads ? kThreads / items : 1;
+    const int per = (ns + runs - 1) / runs;
+    f32x4 *joined = (f32x4 *)&sum[0][0][0];                // run, item
+    float am, ll;
+    auto part = [&](int it, int z0, int z1) {              // of splits z0 .. z1 - 1, times 2^-am
+        const int rr = it / (R / 4), quad = it % (R / 4);
+        am = -INFINITY, ll = 0.0f;
+#pragma unroll
+        for (int z = 0; z < 16; ++z) am = fmaxf(am, jm[z][rr]);
         const float bm = base_of(am);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+        for (int z = 0; z < 16; ++z) ll += jl[z][rr] * __builtin_amdgcn_exp2f(jm[z][rr] - bm);
+        f32x4 x = {0, 0, 0, 0};
 #pragma unroll 8
-        for (int z = 0; z < ns; ++z) {
+        for (int z = z0; z < z1; ++z) {
             float mz, lz;
             mem.get2(z * one + a.sp.rows * R + 2 * rr, mz, lz);
-            const f32x4 y0 = mem.get(z * one + rr * R + 8 * oc), y1 = mem.get(z * one + rr * R + 8 * oc + 4);
+            const f32x4 y = mem.get(z * one + rr * R + 4 * quad);
             const float w = __builtin_amdgcn_exp2f(mz - bm);
-            ll += lz * w;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = fmaf(y0[e], w, x[e]);
-                x[4 + e] = fmaf(y1[e], w, x[4 + e]);
-            }
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], w, x[e]);
         }
-        const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
-        put_octet<DT>(a, r0 + ti, hd, oc, x, ll);
-        if (a.sp.lse && oc == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
+        return x;
+    };
+    auto finish = [&](int it, f32x4 x) {
+        const int gr = base + it / (R / 4), quad = it % (R / 4), ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
+        put_quad<DT>(a, r0 + ti, hd, quad, x, ll);
+        if (a.sp.lse && quad == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
+    };
+    if (runs > 1) {
+        f32x4 x = {0, 0, 0, 0};
+        const int run = tid / items, it = tid - run * items;
+        if (run < runs) {
+            x = part(it, run * per, min((run + 1) * per, ns));
+            joined[tid] = x;
+        }
+        __syncthreads();
+        if (run == 0) {
+            for (int z = 1; z < runs; ++z) x += joined[z * items + it];
+            finish(it, x);
+        }
+    } else {
+        for (int it = tid; it < items; it += kThreads) finish(it, part(it, 0, ns));
     }
 }
 
@@ -305,7 +343,7 @@ hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
             hipLaunchKernelGGL((us_kv_decode_kernel<decltype(nt)::value, decltype(dt)::value>),
-                               dim3(a.sp.splits * a.sp.tiles, a.heads, batch), dim3(kThreads), 0, stream, a);
+                               dim3(a.heads, batch, a.sp.splits * a.sp.tiles), dim3(kThreads), 0, stream, a);
             return hipGetLastError();
         });
     });

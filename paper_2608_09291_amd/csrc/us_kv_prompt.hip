@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     // whose L2 then serves their keys; the last tile, which sees the most, first.
     const int per = a.sp.tiles * a.sp.splits;
     int u = blockIdx.x / per, slot = blockIdx.x % per;
-    if (units % 8 == 0) {
+    if (a.heads % 8 == 0) {                                // (all XCDs then get parts of every sequence)
         u = (blockIdx.x >> 3) / per * 8 + (blockIdx.x & 7);
         slot = (blockIdx.x >> 3) % per;
     }

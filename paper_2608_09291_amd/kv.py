@@ -1,15 +1,19 @@
 """Python binding of the 8-bit key/value cache (include/us_kv.h).
 
 Argument marshalling and the checks that only the tensors can answer (types,
-shapes, strides); every computation happens in the native library.
+shapes, strides); every computation happens in the native library. A decode
+step's calls take the GPU a few microseconds, so each tensor is asked for each
+of its properties once, and the structs are packed without ctypes objects.
 """
 from __future__ import annotations
 
 import ctypes
-from dataclasses import dataclass
+import struct
+
+import torch
 
 from . import binding
-from .binding import _check, _stream_handle
+from .binding import _check
 
 BLOCK = 64           # US_KV_BLOCK: tokens of a block
 HEAD_DIM_MAX = 256   # US_KV_HEAD_DIM_MAX
@@ -55,181 +59,177 @@ def lib():
     if _ready is None:
         L = binding.lib()
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-        pc, ps, pr, po = (ctypes.POINTER(t) for t in (CacheStruct, SeqsStruct, RowsStruct, AttendOpts))
+        # (structs go as void pointers: byref() of the classes above, or their packed bytes)
         L.us_kv_row.argtypes = [i32]
-        L.us_kv_append.argtypes = [pc, ps, pr, pr, vp]
-        L.us_kv_read.argtypes = [pc, ps, pr, pr, vp]
-        L.us_kv_attend_workspace_size.argtypes = [pc, ps, i32, i32, po, ctypes.POINTER(sz)]
-        L.us_kv_attend.argtypes = [pc, ps, i32, pr, pr, po, vp, sz, vp]
-        L.us_kv_evict.argtypes = [pc, ps, vp, i64, i32, i32, i32, ctypes.POINTER(KeptStruct), vp]
+        L.us_kv_append.argtypes = [vp, vp, vp, vp, vp]
+        L.us_kv_read.argtypes = [vp, vp, vp, vp, vp]
+        L.us_kv_attend_workspace_size.argtypes = [vp, vp, i32, i32, vp, ctypes.POINTER(sz)]
+        L.us_kv_attend.argtypes = [vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.us_kv_evict.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp, vp]
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         _ready = L
     return _ready
 
 
+# The structs' layouts, padded to their size in C.
+_pack_cache = struct.Struct("@PPPPiii4x").pack
+_pack_seqs = struct.Struct("@PqiiPPi4x").pack
+_pack_rows = struct.Struct("@Pqqii").pack
+_pack_opts = struct.Struct("@fiii Pq").pack
+_pack_kept = struct.Struct("@Pqi4xPPqP").pack
+
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ROWS = {}      # us_kv_row by head_dim
+
+
 def row(head_dim: int) -> int:
     """us_kv_row: bytes of a head's key (or value) per token."""
-    r = lib().us_kv_row(head_dim)
-    if r == 0:
-        raise ValueError(f"head_dim {head_dim} is outside [1, {HEAD_DIM_MAX}]")
+    r = _ROWS.get(head_dim)
+    if r is None:
+        r = lib().us_kv_row(head_dim)
+        if r == 0:
+            raise ValueError(f"head_dim {head_dim} is outside [1, {HEAD_DIM_MAX}]")
+        _ROWS[head_dim] = r
     return r
 
 
-def _dtype(t):
-    import torch
-    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    if t.dtype not in codes:
-        raise TypeError(f"{t.dtype} rows: float32, bfloat16 or float16 are wanted")
-    return codes[t.dtype]
+def _stream(stream) -> int:
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
-def _want(t, name, dtype, ndim):
-    if t.dtype != dtype or t.dim() != ndim or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise TypeError(f"{name}: a {dtype} tensor of {ndim} dimensions, the last one contiguous, is wanted")
-    return t
-
-
-@dataclass
 class Cache:
     """A pool of blocks: uint8 codes (n_blocks, heads, BLOCK * row(head_dim)) and float32 scales (n_blocks, heads)."""
 
-    k: "object"
-    v: "object"
-    k_scale: "object"
-    v_scale: "object"
-    head_dim: int
-
-    @property
-    def n_blocks(self): return self.k.shape[0]
-
-    @property
-    def heads(self): return self.k.shape[1]
+    def __init__(self, k, v, k_scale, v_scale, head_dim: int):
+        n, heads, size = k.shape
+        if size != BLOCK * row(head_dim) or v.shape != k.shape or not (
+                k.dtype is v.dtype is _U8 and k.is_contiguous() and v.is_contiguous()):
+            raise TypeError(f"codes: contiguous uint8 tensors (blocks, heads, {BLOCK * row(head_dim)}) are wanted")
+        if k_scale.shape != (n, heads) or v_scale.shape != (n, heads) or not (
+                k_scale.dtype is v_scale.dtype is _F32 and k_scale.is_contiguous() and v_scale.is_contiguous()):
+            raise TypeError(f"scales: contiguous float32 tensors of shape {(n, heads)} are wanted")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_blocks, self.heads, self.head_dim = n, heads, head_dim
+        self._packed = _pack_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n, heads, head_dim)
 
     def struct(self) -> CacheStruct:
-        import torch
-        shape = (self.n_blocks, self.heads, BLOCK * row(self.head_dim))
-        for t in (self.k, self.v):
-            if t.dtype != torch.uint8 or tuple(t.shape) != shape or not t.is_contiguous():
-                raise TypeError(f"codes: contiguous uint8 tensors of shape {shape} are wanted")
-        for t in (self.k_scale, self.v_scale):
-            if t.dtype != torch.float32 or tuple(t.shape) != shape[:2] or not t.is_contiguous():
-                raise TypeError(f"scales: contiguous float32 tensors of shape {shape[:2]} are wanted")
-        return CacheStruct(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                           shape[0], shape[1], self.head_dim)
+        return CacheStruct.from_buffer_copy(self._packed)
 
 
 def new_cache(n_blocks: int, heads: int, head_dim: int, device="cuda") -> Cache:
     """An empty pool of n_blocks blocks per head."""
-    import torch
     shape = (n_blocks, heads, BLOCK * row(head_dim))
-    codes = [torch.full(shape, 128, dtype=torch.uint8, device=device) for _ in range(2)]
-    scales = [torch.zeros(shape[:2], dtype=torch.float32, device=device) for _ in range(2)]
+    codes = [torch.full(shape, 128, dtype=_U8, device=device) for _ in range(2)]
+    scales = [torch.zeros(shape[:2], dtype=_F32, device=device) for _ in range(2)]
     return Cache(*codes, *scales, head_dim)
 
 
-def _seqs(blocks, lens, starts, max_new) -> SeqsStruct:
-    import torch
-    _want(blocks, "blocks", torch.int32, 2)
-    _want(lens, "lens", torch.int32, 1)
-    batch = blocks.shape[0]
-    if lens.shape[0] != batch:
-        raise ValueError("lens: one length per row of blocks is wanted")
-    if starts is not None:
-        _want(starts, "starts", torch.int32, 1)
-        if starts.shape[0] != batch + 1:
-            raise ValueError("starts: one entry more than sequences is wanted")
-    return SeqsStruct(blocks.data_ptr(), blocks.stride(0) if batch > 1 else blocks.shape[1], blocks.shape[1], batch,
-                      lens.data_ptr(), None if starts is None else starts.data_ptr(), max_new)
+def _table(t, name):
+    """(rows, columns, row stride) of an int32 table with contiguous rows."""
+    rows, width = t.shape
+    stride, one = t.stride()
+    if t.dtype is not _I32 or (one != 1 and width > 1):
+        raise TypeError(f"{name}: an int32 table with contiguous rows is wanted")
+    return rows, width, stride if rows > 1 else width
 
 
-def _rows(t, heads, head_dim, name) -> RowsStruct:
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, head_dim) or (head_dim > 1 and t.stride(2) != 1):
-        raise TypeError(f"{name}: (tokens, {heads}, {head_dim}) with contiguous values is wanted")
-    return RowsStruct(t.data_ptr(), t.stride(0), t.stride(1), t.shape[0], _dtype(t))
+def _numbers(t, n, name):
+    if t.dtype is not _I32 or t.shape != (n,) or not t.is_contiguous():
+        raise TypeError(f"{name}: {n} contiguous int32 numbers are wanted")
+    return t.data_ptr()
+
+
+def _seqs(blocks, lens, starts, max_new) -> bytes:
+    batch, width, stride = _table(blocks, "blocks")
+    return _pack_seqs(blocks.data_ptr(), stride, width, batch, _numbers(lens, batch, "lens"),
+                      0 if starts is None else _numbers(starts, batch + 1, "starts"), max_new)
+
+
+def _rows(t, heads, head_dim, name) -> bytes:
+    tokens, h, d = t.shape
+    st, sh, one = t.stride()
+    dtype = _DTYPES.get(t.dtype)
+    if h != heads or d != head_dim or (one != 1 and d > 1) or dtype is None:
+        raise TypeError(f"{name}: (tokens, {heads}, {head_dim}) float32, bfloat16 or float16 with contiguous values is wanted")
+    return _pack_rows(t.data_ptr(), st, sh, tokens, dtype)
+
+
+def _weights(t, batch, heads, name):
+    """Address and row length of a float32 (sequences, heads, tokens) tensor."""
+    b, h, n = t.shape
+    if b != batch or h != heads or t.dtype is not _F32 or not t.is_contiguous():
+        raise TypeError(f"{name}: a contiguous float32 tensor ({batch}, {heads}, tokens) is wanted")
+    return t.data_ptr(), n
 
 
 def append(cache: Cache, blocks, lens, k, v, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_append: quantise the sequences' last tokens (rows of k and v) into their blocks."""
-    c, s = cache.struct(), _seqs(blocks, lens, starts, max_new)
-    kr, vr = (_rows(t, cache.heads, cache.head_dim, n) for t, n in ((k, "k"), (v, "v")))
-    _check("us_kv_append", lib().us_kv_append(ctypes.byref(c), ctypes.byref(s), ctypes.byref(kr), ctypes.byref(vr),
-                                              _stream_handle(stream)))
+    h, d = cache.heads, cache.head_dim
+    _check("us_kv_append", lib().us_kv_append(cache._packed, _seqs(blocks, lens, starts, max_new), _rows(k, h, d, "k"),
+                                              _rows(v, h, d, "v"), _stream(stream)))
 
 
 def read(cache: Cache, blocks, lens, k_out, v_out, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_read: the sequences' last tokens as dense rows."""
-    c, s = cache.struct(), _seqs(blocks, lens, starts, max_new)
-    kr, vr = (_rows(t, cache.heads, cache.head_dim, n) for t, n in ((k_out, "k_out"), (v_out, "v_out")))
-    _check("us_kv_read", lib().us_kv_read(ctypes.byref(c), ctypes.byref(s), ctypes.byref(kr), ctypes.byref(vr),
-                                          _stream_handle(stream)))
+    h, d = cache.heads, cache.head_dim
+    _check("us_kv_read", lib().us_kv_read(cache._packed, _seqs(blocks, lens, starts, max_new),
+                                          _rows(k_out, h, d, "k_out"), _rows(v_out, h, d, "v_out"), _stream(stream)))
 
 
-def _opts(scale, causal, window, max_len, weights, batch, heads) -> AttendOpts:
-    import torch
-    if weights is not None:
-        _want(weights, "weights", torch.float32, 3)
-        if tuple(weights.shape[:2]) != (batch, heads) or not weights.is_contiguous():
-            raise ValueError("weights: a contiguous (sequences, cache heads, tokens) tensor is wanted")
-    return AttendOpts(0.0 if scale is None else scale, int(bool(causal)), window, max_len or 0,
-                      None if weights is None else weights.data_ptr(), 0 if weights is None else weights.shape[2])
+def _opts(scale, causal, window, max_len, weights, batch, heads):
+    if weights is None:
+        if scale is None and causal and not window and not max_len:
+            return None
+        at, n = 0, 0
+    else:
+        at, n = _weights(weights, batch, heads, "weights")
+    return _pack_opts(0.0 if scale is None else scale, 1 if causal else 0, window, max_len or 0, at, n)
 
 
-def attend_workspace_size(cache: Cache, q_heads: int, tokens: int, blocks, lens=None, starts=None, max_q: int = 1,
-                          max_len=None, causal: bool = True, window: int = 0, weights=None) -> int:
+def attend_workspace_size(cache: Cache, q_heads: int, tokens: int, blocks, starts=None, max_q: int = 1, max_len=None,
+                          causal: bool = True, window: int = 0, weights=None) -> int:
     """us_kv_attend_workspace_size: device bytes us_kv_attend needs for these sizes."""
-    c = cache.struct()
-    # (the lengths themselves are not looked at)
-    s = SeqsStruct(blocks.data_ptr(), blocks.stride(0) if blocks.shape[0] > 1 else blocks.shape[1], blocks.shape[1],
-                   blocks.shape[0], blocks.data_ptr(), None if starts is None else starts.data_ptr(), max_q)
-    o = _opts(None, causal, window, max_len, weights, blocks.shape[0], cache.heads)
+    batch, width, stride = _table(blocks, "blocks")
+    # (what the lengths and starts are is not looked at)
+    s = _pack_seqs(blocks.data_ptr(), stride, width, batch, blocks.data_ptr(),
+                   0 if starts is None else starts.data_ptr(), max_q)
     n = ctypes.c_size_t(0)
     _check("us_kv_attend_workspace_size", lib().us_kv_attend_workspace_size(
-        ctypes.byref(c), ctypes.byref(s), q_heads, tokens, ctypes.byref(o), ctypes.byref(n)))
+        cache._packed, s, q_heads, tokens, _opts(None, causal, window, max_len, weights, batch, cache.heads),
+        ctypes.byref(n)))
     return n.value
 
 
 def attend_workspace(cache: Cache, q, blocks, starts=None, max_q: int = 1, max_len=None, causal: bool = True,
                      window: int = 0, weights=None):
     """A zero-filled workspace for attend calls of these sizes (lengths up to max_len, or the table's)."""
-    import torch
-    n = attend_workspace_size(cache, q.shape[1], q.shape[0], blocks, None, starts, max_q, max_len, causal, window,
-                              weights)
-    return torch.zeros((n + 3) // 4, dtype=torch.int32, device=q.device)
+    n = attend_workspace_size(cache, q.shape[1], q.shape[0], blocks, starts, max_q, max_len, causal, window, weights)
+    return torch.zeros((n + 3) // 4, dtype=_I32, device=q.device)
 
 
 def attend(cache: Cache, blocks, lens, q, out, starts=None, max_q: int = 1, max_len=None, scale=None,
            causal: bool = True, window: int = 0, weights=None, ws=None, stream=None) -> None:
     """us_kv_attend: out = softmax(scale q k) v over the cache; weights (if given) gain each token's probabilities."""
-    c, s = cache.struct(), _seqs(blocks, lens, starts, max_q)
-    heads = q.shape[1] if q.dim() == 3 else 0
-    qr, outr = (_rows(t, heads, cache.head_dim, n) for t, n in ((q, "q"), (out, "out")))
-    o = _opts(scale, causal, window, max_len, weights, s.batch, cache.heads)
+    heads, d = q.shape[1], cache.head_dim
     _check("us_kv_attend", lib().us_kv_attend(
-        ctypes.byref(c), ctypes.byref(s), heads, ctypes.byref(qr), ctypes.byref(outr), ctypes.byref(o),
-        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
-        _stream_handle(stream)))
+        cache._packed, _seqs(blocks, lens, starts, max_q), heads, _rows(q, heads, d, "q"), _rows(out, heads, d, "out"),
+        _opts(scale, causal, window, max_len, weights, blocks.shape[0], cache.heads),
+        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes, _stream(stream)))
 
 
 def evict(cache: Cache, blocks, lens, weights, keep: int, recent: int, to_blocks, to_lens, to_weights, index,
           max_len=None, stream=None) -> None:
     """us_kv_evict: the recent and the most attended tokens of every sequence, moved to to_blocks."""
-    import torch
-    c, s = cache.struct(), _seqs(blocks, lens, None, 1)
-    for t, name in ((weights, "weights"), (to_weights, "to_weights")):
-        if t is not None:
-            _want(t, name, torch.float32, 3)
-            if tuple(t.shape[:2]) != (s.batch, cache.heads) or not t.is_contiguous():
-                raise ValueError(f"{name}: a contiguous (sequences, cache heads, tokens) tensor is wanted")
-    _want(to_blocks, "to_blocks", torch.int32, 2)
-    _want(to_lens, "to_lens", torch.int32, 1)
-    _want(index, "index", torch.int32, 3)
-    if to_blocks.shape[0] != s.batch or to_lens.shape[0] != s.batch:
-        raise ValueError("to_blocks, to_lens: one row per sequence is wanted")
-    if tuple(index.shape) != (s.batch, cache.heads, keep) or not index.is_contiguous():
-        raise ValueError("index: a contiguous (sequences, cache heads, keep) tensor is wanted")
-    to = KeptStruct(to_blocks.data_ptr(), to_blocks.stride(0) if s.batch > 1 else to_blocks.shape[1],
-                    to_blocks.shape[1], to_lens.data_ptr(), None if to_weights is None else to_weights.data_ptr(),
-                    0 if to_weights is None else to_weights.shape[2], index.data_ptr())
-    _check("us_kv_evict", lib().us_kv_evict(ctypes.byref(c), ctypes.byref(s), weights.data_ptr(), weights.shape[2],
-                                            max_len or 0, keep, recent, ctypes.byref(to), _stream_handle(stream)))
+    heads, batch = cache.heads, blocks.shape[0]
+    w, w_stride = _weights(weights, batch, heads, "weights")
+    ow, ow_stride = (0, 0) if to_weights is None else _weights(to_weights, batch, heads, "to_weights")
+    rows, width, stride = _table(to_blocks, "to_blocks")
+    if rows != batch:
+        raise ValueError("to_blocks: one row per sequence is wanted")
+    if index.dtype is not _I32 or index.shape != (batch, heads, keep) or not index.is_contiguous():
+        raise TypeError(f"index: a contiguous int32 tensor {(batch, heads, keep)} is wanted")
+    to = _pack_kept(to_blocks.data_ptr(), stride, width, _numbers(to_lens, batch, "to_lens"), ow, ow_stride, index.data_ptr())
+    _check("us_kv_evict", lib().us_kv_evict(cache._packed, _seqs(blocks, lens, None, 1), w, w_stride, max_len or 0, keep,
+                                            recent, to, _stream(stream)))

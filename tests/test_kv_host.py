@@ -205,3 +205,15 @@ def test_workspace_sizes_of_edge_shapes():
                                               ctypes.byref(n))
             assert r == 0 and (n.value >= 4 * q_heads * batch * max_new or not weights), (batch, heads, width)
             assert n.value < 1 << 42
+
+
+def test_packed_structs_are_the_c_structs():
+    for pack, struct, values in ((kv._pack_cache, kv.CacheStruct, (1 << 40, 2, 3, 4, 5, 6, 7)),
+                                 (kv._pack_seqs, kv.SeqsStruct, (1, 1 << 40, 3, 4, 5, 6, 7)),
+                                 (kv._pack_rows, kv.RowsStruct, (1, 1 << 40, 3, 4, 2)),
+                                 (kv._pack_opts, kv.AttendOpts, (0.5, 1, 2, 3, 4, 1 << 40)),
+                                 (kv._pack_kept, kv.KeptStruct, (1, 1 << 40, 3, 4, 5, 6, 1 << 41))):
+        raw = pack(*values)
+        assert len(raw) == ctypes.sizeof(struct)
+        s = struct.from_buffer_copy(raw)
+        assert tuple(getattr(s, name) for name, _ in struct._fields_) == values
