@@ -61,10 +61,8 @@ struct Seqs {
         n = r0 < 0 || r0 >= tokens ? 0 : (int)min((int64_t)max(min(n, max_new), 0), (int64_t)tokens - r0);
     }
     // The block that holds block `i` of sequence b, or -1. i < max_len / 64, rounded up.
-    __device__ int block(int b, int i) const {
-        const int id = blocks[b * stride + i];
-        return id >= 0 && id < n_blocks ? id : -1;
-    }
+    __device__ int valid(int id) const { return id >= 0 && id < n_blocks ? id : -1; }
+    __device__ int block(int b, int i) const { return valid(blocks[b * stride + i]); }
 };
 
 struct Rows {

@@ -28,6 +28,8 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     // sequences spread over them, where splits, of which short sequences leave
     // the later ones empty, would load a few (64 ragged sequences to 8k: 100 us).
     const int tile = blockIdx.z % a.sp.tiles, split = blockIdx.z / a.sp.tiles, hk = blockIdx.x, b = blockIdx.y;
+    // Without a window the first block to look up is known before the length is.
+    const int guess = a.s.blocks[b * a.s.stride + min(split * a.sp.chunk + wave + kWaves * lane, (a.s.max_len - 1) / kBlock)];
     int r0, n;
     a.s.rows(b, r0, n);
     const int len = a.s.len(b), total = n * a.G, base = tile * kRows;
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         my_id = -1;
         my_ks = my_vs = 0.0f;
         if (c + lane < count) {
-            my_id = a.s.block(b, start + kWaves * (c + lane));
+            my_id = c == 0 && first == 0 ? a.s.valid(guess) : a.s.block(b, start + kWaves * (c + lane));
             if (my_id >= 0) {
                 my_ks = a.ks[(int64_t)my_id * a.heads + hk];
                 my_vs = a.vs[(int64_t)my_id * a.heads + hk];

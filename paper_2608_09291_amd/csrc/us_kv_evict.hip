@@ -40,9 +40,13 @@ __device__ inline int scan(int x, int *lds, int &total) {
     return before + sum - x;
 }
 
-// One workgroup per (head, sequence). The k-th largest weight by its bits, 8 at
-// a time from the top: a histogram of the next 8 bits of the weights that agree
-// with the bits found so far. Then the positions in order.
+// One workgroup per (head, sequence), a run of consecutive tokens per thread.
+// The take-th largest weight by its bits, 8 at a time from the top: a histogram
+// of the next 8 bits of the weights that agree with the bits found so far. Then
+// the positions in order: one sum over the threads' counts places every run.
+// Weights of up to kHeld tokens per thread stay in registers over the passes
+// (16384 tokens, 128 rows: 57 us with the weights read again for every pass).
+constexpr int kHeld = 32;
 __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const float *weights, int64_t w_stride, int keep,
                                                                    int recent, int heads, int32_t *to_lens,
                                                                    float *to_weights, int64_t to_w_stride,
@@ -54,113 +58,190 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
     int32_t *idx = index + ((int64_t)b * heads + h) * keep;
     float *ow = to_weights ? to_weights + ((int64_t)b * heads + h) * to_w_stride : nullptr;
     if (h == 0 && tid == 0) to_lens[b] = stay;
-
-    uint32_t bits = 0;                                     // of the smallest weight that stays
-    int equal = take;                                      // how many of that weight do
-    if (take < m && take > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
-            __syncthreads();
-            for (int i = tid; i < m; i += kSelThreads) {
-                const uint32_t u = order_of(w[i]);
-                if (shift == 24 || u >> (shift + 8) == bits >> (shift + 8)) atomicAdd(&hist[(u >> shift) & 255u], 1);
-            }
-            __syncthreads();
-            // bin of the equal-th largest: the one before whose larger bins hold fewer
-            const int mine = tid < 256 ? hist[255 - tid] : 0;
-            int total;
-            const int above = scan(mine, lds, total);
-            if (mine > 0 && above < equal && above + mine >= equal) {
-                found[0] = 255 - tid;
-                found[1] = equal - above;
-            }
-            __syncthreads();
-            bits |= (uint32_t)found[0] << shift;
-            equal = found[1];
-            __syncthreads();
-        }
-    }
-    int put = 0, same = 0;                                 // kept so far; of the smallest weight so far
-    for (int i0 = 0; i0 < m; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        const uint32_t u = i < m && take > 0 ? order_of(w[i]) : 0u;
-        const bool all = take == m, eq = i < m && !all && take > 0 && u == bits;
-        int n_eq, n_put;
-        const int before = scan(eq, lds, n_eq);
-        const bool stays = i < m && take > 0 && (all || u > bits || (eq && same + before < equal));
-        const int at = put + scan(stays, lds, n_put);
-        if (stays) {
-            idx[at] = i;
-            if (ow) ow[at] = w[i];
-        }
-        put += n_put;
-        same += n_eq;
-    }
     for (int i = tid; i < late; i += kSelThreads) {
         idx[take + i] = m + i;
         if (ow) ow[take + i] = w[m + i];
     }
-    for (int i = stay + tid; i < keep; i += kSelThreads) {
-        idx[i] = -1;
+    for (int i = stay + tid; i < keep; i += kSelThreads) idx[i] = -1;
+    if (take == 0) return;
+    if (take == m) {
+        for (int i = tid; i < m; i += kSelThreads) {
+            idx[i] = i;
+            if (ow) ow[i] = w[i];
+        }
+        return;
     }
+
+    const int run = (m + kSelThreads - 1) / kSelThreads, i0 = min(tid * run, m), n = min(run, m - i0);
+    uint32_t held[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) held[j] = j < n ? order_of(w[i0 + j]) : 0u;
+    // f(position, order) for this thread's tokens
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (j < n) f(i0 + j, held[j]);
+        for (int j = kHeld; j < n; ++j) f(i0 + j, order_of(w[i0 + j]));
+    };
+    uint32_t bits = 0;                                     // of the smallest weight that stays
+    int equal = take;                                      // how many of that weight do
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        each([&](int, uint32_t u) {
+            if (shift == 24 || (u ^ bits) >> (shift + 8) == 0) atomicAdd(&hist[(u >> shift) & 255u], 1);
+        });
+        __syncthreads();
+        if (tid < 64) {
+            // bins from the largest down, four per lane; the one that holds the equal-th
+            int c[4], sum = 0;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                c[z] = hist[255 - 4 * tid - z];
+                sum += c[z];
+            }
+            int above = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(above, o, 64);
+                if (tid >= o) above += y;
+            }
+            above -= sum;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                if (above < equal && above + c[z] >= equal) {
+                    found[0] = 255 - 4 * tid - z;
+                    found[1] = equal - above;
+                }
+                above += c[z];
+            }
+        }
+        __syncthreads();
+        bits |= (uint32_t)found[0] << shift;
+        equal = found[1];
+        __syncthreads();
+    }
+    int more = 0, same = 0, unused;
+    each([&](int, uint32_t u) {
+        more += u > bits;
+        same += u == bits;
+    });
+    int left = equal - scan(same, lds, unused);            // of that weight, for this thread and the later ones
+    int at = scan(more + min(max(left, 0), same), lds, unused);
+    each([&](int i, uint32_t u) {
+        if (u > bits || (u == bits && left-- > 0)) {
+            idx[at] = i;
+            if (ow) ow[at] = w[i];
+            ++at;
+        }
+    });
 }
 
-// One workgroup per (new block, head, sequence): the 64 tokens that the index names.
+// One workgroup per (new block, head, sequence; keys or values): the 64 tokens
+// that the index names. A key's octets are copied from where they are. Values
+// lie across their block, so that any token of it touches all its lines:
+// every block that has one passes through LDS whole.
 template <int NT>
 __global__ __launch_bounds__(kMoveThreads) void us_kv_move_kernel(uint8_t *kp, uint8_t *vp, float *ksp, float *vsp, Seqs s,
                                                                   const int32_t *index, int keep, const int32_t *to,
                                                                   int64_t to_stride, int to_width) {
-    constexpr int R = 32 * NT, kOct = R / 8;
+    constexpr int R = 32 * NT, kOct = R / 8, kPitch = kBlock + 4;
+    constexpr int kPieces = (4 * R + kMoveThreads - 1) / kMoveThreads;
+    __shared__ int token[kBlock];                          // position, -1: none
     __shared__ int64_t from[kBlock];                       // (block, head) of a token, -1: none
-    __shared__ int token[kBlock];
-    __shared__ float ratio[2][kBlock], scale[2][kBlock];
-    const int j = blockIdx.x, h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
+    __shared__ float ratio[kBlock];
+    __shared__ __attribute__((aligned(16))) uint8_t in[R * kPitch], out[R * kPitch];
+    const int j = blockIdx.x >> 1, h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
+    const bool values = blockIdx.x & 1;
     const int id = to[b * to_stride + j];
     const int left = min(min(s.len(b), keep), to_width * kBlock) - j * kBlock;
     if (id < 0 || id >= s.n_blocks || left <= 0) return;
+    float *scales = values ? vsp : ksp;
     if (tid < kBlock) {
-        int p = tid < left ? index[((int64_t)b * heads + h) * keep + j * kBlock + tid] : -1;
+        const int p = tid < left ? index[((int64_t)b * heads + h) * keep + j * kBlock + tid] : -1;
         const int src = p >= 0 ? s.block(b, p / kBlock) : -1;
         const int64_t at = src >= 0 ? (int64_t)src * heads + h : -1;
+        token[tid] = p;
         from[tid] = at;
-        token[tid] = p & (kBlock - 1);
+        const float s1 = at >= 0 ? scales[at] : 0.0f;
+        float s2 = s1;
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const float s1 = at >= 0 ? (v ? vsp : ksp)[at] : 0.0f;
-            float s2 = s1;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) s2 = fmaxf(s2, __shfl_xor(s2, o, 64));
-            ratio[v][tid] = s2 > 0.0f ? s1 / s2 : 0.0f;
-            scale[v][tid] = s2;
-        }
+        for (int o = 32; o > 0; o >>= 1) s2 = fmaxf(s2, __shfl_xor(s2, o, 64));
+        ratio[tid] = s2 > 0.0f ? s1 / s2 : 0.0f;
+        if (tid == 0) scales[(int64_t)id * heads + h] = s2;
     }
     __syncthreads();
-    const int64_t dst = (int64_t)id * heads + h;
-    if (tid == 0) {
-        ksp[dst] = scale[0][0];
-        vsp[dst] = scale[1][0];
-    }
+    const int64_t dst = ((int64_t)id * heads + h) * (kBlock * R);
+    if (!values) {
+        u32x2 w[NT];
 #pragma unroll
-    for (int i0 = 0; i0 < NT; ++i0) {
-        const int i = tid + kMoveThreads * i0, t = i / kOct, o = i % kOct;
-        u32x2 w = {0x80808080u, 0x80808080u}, q = {0, 0};
-        if (from[t] >= 0) w = *(const u32x2 *)(kp + from[t] * (kBlock * R) + key_octet(token[t], o));
-        const float r = ratio[0][t];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            q[e >> 2] |= (uint32_t)(int)(rintf(code_of(w[e >> 2], e & 3) * r) + 128.0f) << (8 * (e & 3));
-        *(u32x2 *)(kp + dst * (kBlock * R) + key_octet(t, o)) = q;
-    }
-    for (int i = tid; i < 4 * R; i += kMoveThreads) {
-        const int d = i >> 2, g = i & 3;
-        u32x4 q = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int t = (int)value_token(16 * g + e);
-            const float c = from[t] >= 0 ? (float)vp[from[t] * (kBlock * R) + 64 * d + value_place(token[t])] - 128.0f : 0.0f;
-            q[e >> 2] |= (uint32_t)(int)(rintf(c * ratio[1][t]) + 128.0f) << (8 * (e & 3));
+        for (int x = 0; x < NT; ++x) {
+            const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
+            w[x] = (u32x2){0x80808080u, 0x80808080u};
+            if (from[t] >= 0) w[x] = *(const u32x2 *)(kp + from[t] * (kBlock * R) + key_octet(token[t] & (kBlock - 1), o));
         }
-        *(u32x4 *)(vp + dst * (kBlock * R) + 16 * i) = q;
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
+            const float r = ratio[t];
+            u32x2 q = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                q[e >> 2] |= (uint32_t)(int)(rintf(code_of(w[x][e >> 2], e & 3) * r) + 128.0f) << (8 * (e & 3));
+            *(u32x2 *)(kp + dst + key_octet(t, o)) = q;
+        }
+        return;
+    }
+    for (int i = tid; i < R * kBlock / 4; i += kMoveThreads)
+        *(uint32_t *)(out + i / (kBlock / 4) * kPitch + 4 * (i % (kBlock / 4))) = 0x80808080u;
+    u32x4 piece[kPieces];
+    auto fetch = [&](int t) {                              // the block of token t
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+            const int i = tid + kMoveThreads * x;
+            if (4 * R % kMoveThreads == 0 || i < 4 * R) piece[x] = *(const u32x4 *)(vp + from[t] * (kBlock * R) + 16 * i);
+        }
+    };
+    // The tokens from t on that share its block end ahead of this one.
+    const int n = min(left, kBlock);
+    auto next_of = [&](int t) {
+        int e = t + 1;
+        while (e < n && token[e] >> 6 == token[t] >> 6) ++e;
+        return e;
+    };
+    if (from[0] >= 0) fetch(0);
+    for (int t = 0; t < n;) {                              // (uniform: all threads read the same tokens)
+        const int end = next_of(t);
+        const bool there = from[t] >= 0;
+        __syncthreads();
+        if (there)
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x) {
+                const int i = tid + kMoveThreads * x;
+                if (4 * R % kMoveThreads == 0 || i < 4 * R) {
+                    uint32_t *p = (uint32_t *)(in + (i >> 2) * kPitch + 16 * (i & 3));
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) p[z] = piece[x][z];
+                }
+            }
+        __syncthreads();
+        if (end < n && from[end] >= 0) fetch(end);
+        if (there)
+            for (int i = tid; i < (end - t) * R; i += kMoveThreads) {
+                const int e = t + i / R, d = i % R;
+                const float c = (float)in[d * kPitch + value_place(token[e] & (kBlock - 1))] - 128.0f;
+                out[d * kPitch + value_place(e)] = (uint8_t)(int)(rintf(c * ratio[e]) + 128.0f);
+            }
+        t = end;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+        const int i = tid + kMoveThreads * x;
+        if (4 * R % kMoveThreads == 0 || i < 4 * R) {
+            const uint32_t *p = (const uint32_t *)(out + (i >> 2) * kPitch + 16 * (i & 3));
+            *(u32x4 *)(vp + dst + 16 * i) = (u32x4){p[0], p[1], p[2], p[3]};
+        }
     }
 }
 
@@ -187,7 +268,7 @@ extern "C" us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seq
     if (hipGetLastError() != hipSuccess) return US_ERR_DEVICE;
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
         hipLaunchKernelGGL((us_kv_move_kernel<decltype(nt)::value>),
-                           dim3((most + kBlock - 1) / kBlock, cache->heads, seqs->batch), dim3(kMoveThreads), 0, q, cache->k,
+                           dim3(2 * ((most + kBlock - 1) / kBlock), cache->heads, seqs->batch), dim3(kMoveThreads), 0, q, cache->k,
                            cache->v, cache->k_scale, cache->v_scale, s, to->index, keep, to->blocks, to->stride, to->width);
         return hipGetLastError();
     });
