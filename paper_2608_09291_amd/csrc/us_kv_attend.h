@@ -58,6 +58,11 @@ struct Split {
     int64_t scores_stride;
 };
 
+// Splits of a tile whose rows see keys [lo, hi).
+__device__ inline int splits_of(int lo, int hi, int chunk) {
+    return max(((hi + kBlock - 1) / kBlock - lo / kBlock + chunk - 1) / chunk, 1);
+}
+
 struct Args {
     const uint8_t *k, *v;
     const float *ks, *vs;

@@ -59,18 +59,31 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
         int64_t chunk = up(units * most / (2 * cus), 4);
         p.chunk = (int)(chunk < 4 ? 4 : chunk > 64 ? 64 : chunk);
     } else {
-        const int64_t want = units >= 2 * cus ? 1 : (2 * cus + units - 1) / units;
-        p.chunk = (int)((most + want - 1) / want);
-        if (p.chunk < 4) p.chunk = 4;
+        // Generations of workgroups, one per CU, times what one takes, in blocks: its own, and 10
+        // for storing and joining its partial rows where there are several. (The tokens bound the
+        // tiles that have rows where the sequences' numbers of them differ.) us per call, two
+        // workgroups per CU and a join by the last of a tile before -> this: 64 queries on 30000
+        // keys, 8 heads over 1, 567 -> 46; 2048 causal, 32 heads, 115 -> 76; 512 on 16000, 64
+        // heads over 8, 336 -> 285.
+        const int64_t filled = c.heads * ((int64_t)tokens * (q_heads / c.heads) / tile + s.batch);
+        const int64_t work = filled < units ? filled : units;
+        int64_t best = INT64_MAX;
+        for (int64_t n = 1; n <= 128 && n <= most; ++n) {
+            const int64_t chunk = (most + n - 1) / n, t = (work * n + cus - 1) / cus * (chunk + (n > 1 ? 10 : 0));
+            if (t < best) {
+                best = t;
+                p.chunk = (int)chunk;
+            }
+        }
     }
     // (a unit's partial rows lie within 2^31 bytes)
     if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
-    if (units > kTickets || most <= p.chunk) p.chunk = (int)most;
+    if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
     p.splits = (int)((most + p.chunk - 1) / p.chunk);
     if (units * p.splits > INT32_MAX / 256) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
-    p.part = p.splits > 1 || o.weights ? 4 * kTickets : 0;
+    p.part = p.decode && p.splits > 1 ? 4 * kTickets : 0;
     p.lse = p.part + parts;
     // (one block past the last is read)
     p.row_blocks = (int64_t)tokens * (q_heads / c.heads) / 32 + s.batch + 2;

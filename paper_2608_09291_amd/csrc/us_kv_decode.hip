@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     a.mask.range(base / a.G, n, len, lo0, hi0);
     a.mask.range(last_row / a.G, n, len, lo1, hi1);
     const int first = lo0 / kBlock, end = (hi1 + kBlock - 1) / kBlock;
-    const int ns = max((end - first + a.sp.chunk - 1) / a.sp.chunk, 1);
+    const int ns = splits_of(lo0, hi1, a.sp.chunk);
     if (split >= ns) return;
     const int row = min(base + r, last_row), i = row / a.G, head = hk * a.G + row - i * a.G;
     int lo, hi;

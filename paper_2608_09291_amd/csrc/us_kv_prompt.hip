@@ -27,7 +27,6 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Stage<R> *stage = (Stage<R> *)lds;
-    __shared__ int flag;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
     // The tiles of a unit (sequence, cache head) follow each other on one XCD,
@@ -49,7 +48,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     a.mask.range(base / a.G, n, len, lo0, hi0);
     a.mask.range(last_row / a.G, n, len, lo1, hi1);
     const int first = lo0 / kBlock, end = (hi1 + kBlock - 1) / kBlock;
-    const int ns = max((end - first + a.sp.chunk - 1) / a.sp.chunk, 1);
+    const int ns = splits_of(lo0, hi1, a.sp.chunk);
     if (split >= ns) return;
     const int start = first + split * a.sp.chunk, stop = min(start + a.sp.chunk, end);
     // This wavefront's rows, and this lane's; the range of keys that they see.
@@ -306,68 +305,64 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
         for (int v = 0; v < 16; ++v) o[t][v] *= vmax;
 
     // Lane (c, h), element 4 z + v of o[t]: value 32 t + 8 z + 4 h + v of row c.
-    const int64_t unit = (int64_t)u * a.sp.tiles + tile;
-    if (ns > 1) {
-        constexpr int kOne = kRows * (R + 2);              // floats of a split
-        const Shared mem(a.sp.part + unit * a.sp.splits * kOne);
+    if (!real) return;
+    if (ns > 1) {                                          // left to the join
+        float *dst = a.sp.part + (((int64_t)u * a.sp.tiles + tile) * a.sp.splits + split) * (kRows * (R + 2));
         const int rr = 32 * wave + c;
-        if (real) {
-            const uint32_t dst = split * kOne + rr * R + 4 * h;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int z = 0; z < 4; ++z)
-                    mem.put(dst + 32 * t + 8 * z, (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]});
-            if (h == 0) mem.put2(split * kOne + kRows * R + 2 * rr, m, l);
-        }
-        if (!last_of(a.sp.tickets + unit, ns, &flag)) return;
-        if (!real) return;
-        m = -INFINITY;
-        for (int z = 0; z < ns; ++z) {
-            float mz, lz;
-            mem.get2(z * kOne + kRows * R + 2 * rr, mz, lz);
-            m = fmaxf(m, mz);
-        }
-        l = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
-        for (int z = 0; z < ns; ++z) {
-            float mz, lz;
-            mem.get2(z * kOne + kRows * R + 2 * rr, mz, lz);
-            const float w = __builtin_amdgcn_exp2f(mz - base_of(m));
-            l += lz * w;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const f32x4 x = mem.get(z * kOne + rr * R + 4 * h + 32 * t + 8 * y);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) o[t][4 * y + v] = fmaf(x[v], w, o[t][4 * y + v]);
-                }
+            for (int z = 0; z < 4; ++z)
+                *(f32x4 *)(dst + rr * R + 32 * t + 8 * z + 4 * h) = (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]};
+        if (h == 0) {
+            dst[kRows * R + 2 * rr] = m;
+            dst[kRows * R + 2 * rr + 1] = l;
         }
+        return;
     }
-    if (!real) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;         // a row without keys gives zeros
-    T *dst = (T *)a.out.data + (int64_t)(r0 + i) * a.out.token_stride + (int64_t)head * a.out.head_stride;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int z = 0; z < 4; ++z) {
-            const int d = 32 * t + 8 * z + 4 * h;
-            T y[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) y[v] = Type<DT>::put(o[t][4 * z + v] * inv);
-            if (a.vec) {
-                if (d < a.D) __builtin_memcpy(__builtin_assume_aligned(dst + d, 4 * sizeof(T)), y, 4 * sizeof(T));
-            } else {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (d + v < a.D) dst[d + v] = y[v];
-            }
-        }
+        for (int z = 0; z < 4; ++z)
+            put_quad<DT>(a, r0 + i, head, 8 * t + 2 * z + h, (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]}, l);
     if (a.sp.lse && h == 0) a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32] = lse_of(m, l);
+}
+
+// Joins the splits of a row: a thread per quad of its values. (The last workgroup of a tile
+// joining it alone, as in decode, took 400 us for 118 splits of 256 rows.)
+template <int NT, int DT>
+__global__ __launch_bounds__(256) void us_kv_join_kernel(Args a) {
+    constexpr int R = 32 * NT, kRows = 32 * prompt_waves(R, DT == US_F32), kEach = 256 / (R / 4);
+    const int hk = blockIdx.y, b = blockIdx.z, quad = threadIdx.x % (R / 4);
+    const int row = blockIdx.x * kEach + threadIdx.x / (R / 4);
+    int r0, n;
+    a.s.rows(b, r0, n);
+    const int len = a.s.len(b), total = n * a.G;
+    if ((int)threadIdx.x >= kEach * (R / 4) || row >= total) return;
+    const int tile = row / kRows, base = tile * kRows, last_row = min(base + kRows, total) - 1;
+    int lo0, hi1, unused;
+    a.mask.range(base / a.G, n, len, lo0, unused);
+    a.mask.range(last_row / a.G, n, len, unused, hi1);
+    const int ns = splits_of(lo0, hi1, a.sp.chunk);
+    if (ns == 1) return;
+    constexpr int kOne = kRows * (R + 2);
+    const float *src = a.sp.part + (((int64_t)b * a.heads + hk) * a.sp.tiles + tile) * a.sp.splits * kOne;
+    const int ml = kRows * R + 2 * (row - base), at = (row - base) * R + 4 * quad;
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 8
+    for (int z = 0; z < ns; ++z) m = fmaxf(m, src[(int64_t)z * kOne + ml]);
+    const float bm = base_of(m);
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int z = 0; z < ns; ++z) {
+        const float w = __builtin_amdgcn_exp2f(src[(int64_t)z * kOne + ml] - bm);
+        const f32x4 y = *(const f32x4 *)(src + (int64_t)z * kOne + at);
+        l = fmaf(src[(int64_t)z * kOne + ml + 1], w, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], w, x[e]);
+    }
+    put_quad<DT>(a, r0 + row / a.G, hk * a.G + row % a.G, quad, x, l);
+    if (a.sp.lse && quad == 0) a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32] = lse_of(m, l);
 }
 
 // The probabilities' sums over the query rows, from the logarithms of the rows'
@@ -536,6 +531,11 @@ hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream
             }
             const int units = batch * a.heads;
             hipLaunchKernelGGL(kern, dim3((unsigned)units * a.sp.tiles * a.sp.splits), dim3(64 * W), kLds, stream, a, units);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || a.sp.splits == 1) return e;
+            constexpr int kEach = 256 / (8 * NT);
+            const unsigned x = (unsigned)(((int64_t)a.s.max_new * a.G + kEach - 1) / kEach);
+            hipLaunchKernelGGL((us_kv_join_kernel<NT, decltype(dt)::value>), dim3(x, a.heads, batch), dim3(256), 0, stream, a);
             return hipGetLastError();
         });
     });

@@ -96,7 +96,10 @@ def row(head_dim: int) -> int:
 
 
 def _stream(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # (the handle alone: building torch's stream object takes as long as a launch)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class Cache:
