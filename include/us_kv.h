@@ -45,6 +45,9 @@ extern "C" {
 
 #define US_KV_BLOCK 64         /* tokens of a block                           */
 #define US_KV_HEAD_DIM_MAX 256 /* widest head                                 */
+#define US_KV_WIDTH_MAX (1 << 22) /* most blocks of a sequence                */
+#define US_KV_NEW_MAX (1 << 25)   /* most new tokens, or query rows of a cache
+                                     head, of a sequence in one call          */
 
 typedef enum { US_F32 = 0, US_BF16 = 1, US_F16 = 2 } us_dtype;
 
@@ -65,7 +68,7 @@ typedef struct {
 typedef struct {
     const int32_t *blocks;  /* device, batch x stride                          */
     int64_t stride;         /* >= width                                        */
-    int32_t width;          /* blocks of a sequence at most                    */
+    int32_t width;          /* blocks of a sequence at most, to US_KV_WIDTH_MAX */
     int32_t batch;          /* 1 .. 65535                                      */
     const int32_t *lens;    /* device, batch                                   */
     const int32_t *starts;  /* device, batch + 1, or NULL                      */

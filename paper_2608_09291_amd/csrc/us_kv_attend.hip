@@ -42,7 +42,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
                   Plan &p) {
     const int max_len = seqs_of(c, s, o.max_len, tokens).max_len, R = row_of(c.head_dim);
     const int64_t rows = (int64_t)s.max_new * (q_heads / c.heads), pairs = (int64_t)s.batch * c.heads;
-    if (rows > INT32_MAX / 2) return US_ERR_SHAPE;
+    if (rows > US_KV_NEW_MAX) return US_ERR_SHAPE;
     p.decode = rows <= 32;
     const int tile = p.decode ? 16 : 32 * prompt_waves(R, f32);
     p.tiles = (int)((rows + tile - 1) / tile);
@@ -80,7 +80,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
     if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
     p.splits = (int)((most + p.chunk - 1) / p.chunk);
-    if (units * p.splits > INT32_MAX / 256) return US_ERR_SHAPE;
+    if (units * p.splits > INT32_MAX / 512) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
     p.part = p.decode && p.splits > 1 ? 4 * kTickets : 0;

@@ -161,6 +161,14 @@ __device__ inline void store_octet(typename Type<DT>::T *p, int o, int D, const 
 
 __device__ inline float code_of(uint32_t word, int byte) { return (float)((word >> (8 * byte)) & 255u) - 128.0f; }
 
+// The byte of rint(c r), rounded once before it, for the code c of a byte; 0 <= r <= 1. Adding
+// 1.5 x 2^23 rounds to a whole number, halves to even, and leaves it in the lowest bits.
+__device__ inline uint32_t rescaled(uint32_t byte, float r) {
+#pragma clang fp contract(off)
+    const float x = ((float)byte - 128.0f) * r;
+    return (__float_as_uint(x + 12582912.0f) + 128u) & 255u;
+}
+
 // --- argument checks ----------------------------------------------------------
 
 inline us_status check_cache(const us_kv_cache *c) {
@@ -174,8 +182,9 @@ inline us_status check_cache(const us_kv_cache *c) {
 inline us_status check_seqs(const us_kv_seqs *s) {
     if (!s || !s->blocks || !s->lens || (uintptr_t)s->blocks % 4 || (uintptr_t)s->lens % 4 || (uintptr_t)s->starts % 4)
         return US_ERR_ARG;
-    if (s->batch < 1 || s->batch > 65535 || s->width < 1 || s->width > INT32_MAX / kBlock || s->stride < s->width ||
-        s->max_new < 1 || (!s->starts && s->max_new != 1))
+    // (so that every grid has fewer than 2^32 threads)
+    if (s->batch < 1 || s->batch > 65535 || s->width < 1 || s->width > US_KV_WIDTH_MAX || s->stride < s->width ||
+        s->max_new < 1 || s->max_new > US_KV_NEW_MAX || (!s->starts && s->max_new != 1))
         return US_ERR_SHAPE;
     return US_OK;
 }

@@ -4,13 +4,14 @@
 
 #include <type_traits>
 
+#include "us_device.h"
 #include "us_kv_common.h"
 
 namespace {
 
 using namespace us_kv;
 
-constexpr int kSelThreads = 1024, kMoveThreads = 256;
+constexpr int kMoveThreads = 256;
 
 // Orders like the weights: a NaN first, both zeros alike.
 __device__ inline uint32_t order_of(float w) {
@@ -47,6 +48,7 @@ __device__ inline int scan(int x, int *lds, int &total) {
 // Weights of up to kHeld tokens per thread stay in registers over the passes
 // (16384 tokens, 128 rows: 57 us with the weights read again for every pass).
 constexpr int kHeld = 32;
+template <int kSelThreads>
 __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const float *weights, int64_t w_stride, int keep,
                                                                    int recent, int heads, int32_t *to_lens,
                                                                    float *to_weights, int64_t to_w_stride,
@@ -137,84 +139,108 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
     });
 }
 
-// One workgroup per (new block, head, sequence; keys or values): the 64 tokens
-// that the index names. A key's octets are copied from where they are. Values
-// lie across their block, so that any token of it touches all its lines:
-// every block that has one passes through LDS whole.
+// One workgroup per (new block, head, sequence) for values, per up to four new
+// blocks for keys. The index, the block table and the scales of all its tokens
+// are looked up together: each of these steps waits for the one before, and
+// with one block of keys per workgroup the waits took most of the time. A key's
+// octets are copied from where they are. Values lie across their block, so that
+// any token of it touches all its lines: every block that has one passes
+// through LDS whole. 16 sequences of 9000-16384 tokens to 4096, 8 heads of 128:
+// 120-135 us, the values alone 105 (340 MB, 69 us at the card's copy rate); what
+// bounds them is the wait for one source block after the other.
+constexpr int kPer = kMoveThreads / kBlock;                // most new blocks of a workgroup
 template <int NT>
 __global__ __launch_bounds__(kMoveThreads) void us_kv_move_kernel(uint8_t *kp, uint8_t *vp, float *ksp, float *vsp, Seqs s,
                                                                   const int32_t *index, int keep, const int32_t *to,
-                                                                  int64_t to_stride, int to_width) {
+                                                                  int64_t to_stride, int to_width, int blocks, int key_blocks) {
     constexpr int R = 32 * NT, kOct = R / 8, kPitch = kBlock + 4;
     constexpr int kPieces = (4 * R + kMoveThreads - 1) / kMoveThreads;
-    __shared__ int token[kBlock];                          // position, -1: none
-    __shared__ int64_t from[kBlock];                       // (block, head) of a token, -1: none
-    __shared__ float ratio[kBlock];
+    __shared__ int token[kMoveThreads], from[kMoveThreads], dst[kPer];         // place in its block; block, -1: none
+    __shared__ float ratio[kMoveThreads];
     __shared__ __attribute__((aligned(16))) uint8_t in[R * kPitch], out[R * kPitch];
-    const int j = blockIdx.x >> 1, h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
-    const bool values = blockIdx.x & 1;
-    const int id = to[b * to_stride + j];
-    const int left = min(min(s.len(b), keep), to_width * kBlock) - j * kBlock;
-    if (id < 0 || id >= s.n_blocks || left <= 0) return;
+    // Values first: a block each, as they take longest.
+    const bool values = (int)blockIdx.x < blocks;
+    const int per = values ? 1 : key_blocks, j0 = values ? blockIdx.x : (blockIdx.x - blocks) * per, h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = min(min(min(s.len(b), keep), to_width * kBlock) - j0 * kBlock, per * kBlock);
+    if (n <= 0) return;
     float *scales = values ? vsp : ksp;
-    if (tid < kBlock) {
-        const int p = tid < left ? index[((int64_t)b * heads + h) * keep + j * kBlock + tid] : -1;
+    float s1 = 0.0f;
+    if (tid < per * kBlock) {                              // a wavefront per new block
+        const int p = tid < n ? index[((int64_t)b * heads + h) * keep + j0 * kBlock + tid] : -1;
         const int src = p >= 0 ? s.block(b, p / kBlock) : -1;
-        const int64_t at = src >= 0 ? (int64_t)src * heads + h : -1;
-        token[tid] = p;
-        from[tid] = at;
-        const float s1 = at >= 0 ? scales[at] : 0.0f;
-        float s2 = s1;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s2 = fmaxf(s2, __shfl_xor(s2, o, 64));
-        ratio[tid] = s2 > 0.0f ? s1 / s2 : 0.0f;
-        if (tid == 0) scales[(int64_t)id * heads + h] = s2;
+        token[tid] = p & (kBlock - 1);
+        from[tid] = src;
+        if (src >= 0) s1 = scales[(int64_t)src * heads + h];                   // (not waited for yet)
+        if (lane == 0) dst[wave] = wave * kBlock < n ? s.valid(to[b * to_stride + j0 + wave]) : -1;
     }
     __syncthreads();
-    const int64_t dst = ((int64_t)id * heads + h) * (kBlock * R);
-    if (!values) {
-        u32x2 w[NT];
+    auto set_ratios = [&]() {
+        if (tid < per * kBlock) {
+            float s2 = s1;
 #pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
-            w[x] = (u32x2){0x80808080u, 0x80808080u};
-            if (from[t] >= 0) w[x] = *(const u32x2 *)(kp + from[t] * (kBlock * R) + key_octet(token[t] & (kBlock - 1), o));
+            for (int o = 32; o > 0; o >>= 1) s2 = fmaxf(s2, __shfl_xor(s2, o, 64));
+            ratio[tid] = s2 > 0.0f ? s1 / s2 : 0.0f;
+            if (lane == 0 && dst[wave] >= 0) scales[(int64_t)dst[wave] * heads + h] = s2;
         }
+        __syncthreads();
+    };
+    auto page = [&](int block) { return ((int64_t)block * heads + h) * (kBlock * R); };
+    if (!values) {
+        u32x2 wa[NT], wb[NT];
+        auto fetch = [&](int j, u32x2 (&w)[NT]) {
 #pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
-            const float r = ratio[t];
-            u32x2 q = {0, 0};
+            for (int x = 0; x < NT; ++x) {
+                const int i = tid + kMoveThreads * x, t = j * kBlock + i / kOct, o = i % kOct;
+                w[x] = (u32x2){0x80808080u, 0x80808080u};
+                if (t < n && from[t] >= 0) w[x] = *(const u32x2 *)(kp + page(from[t]) + key_octet(token[t], o));
+            }
+        };
+        auto put = [&](int j, const u32x2 (&w)[NT]) {
+            if (dst[j] < 0) return;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                q[e >> 2] |= (uint32_t)(int)(rintf(code_of(w[x][e >> 2], e & 3) * r) + 128.0f) << (8 * (e & 3));
-            *(u32x2 *)(kp + dst + key_octet(t, o)) = q;
+            for (int x = 0; x < NT; ++x) {
+                const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
+                const float r = ratio[j * kBlock + t];
+                u32x2 q = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    q[e >> 2] |= rescaled((w[x][e >> 2] >> (8 * (e & 3))) & 255u, r) << (8 * (e & 3));
+                *(u32x2 *)(kp + page(dst[j]) + key_octet(t, o)) = q;
+            }
+        };
+        const int blocks = (n + kBlock - 1) / kBlock;
+        fetch(0, wa);
+        set_ratios();
+        for (int j = 0; j < blocks; j += 2) {
+            if (j + 1 < blocks) fetch(j + 1, wb);
+            put(j, wa);
+            if (j + 2 < blocks) fetch(j + 2, wa);
+            if (j + 1 < blocks) put(j + 1, wb);
         }
         return;
     }
-    for (int i = tid; i < R * kBlock / 4; i += kMoveThreads)
-        *(uint32_t *)(out + i / (kBlock / 4) * kPitch + 4 * (i % (kBlock / 4))) = 0x80808080u;
+    // Runs of tokens with one source and one new block. (All of this is uniform: the tables are shared.)
+    auto end_of = [&](int t) {
+        int e = t + 1;
+        while (e < n && e % kBlock != 0 && from[e] == from[t]) ++e;
+        return e;
+    };
     u32x4 piece[kPieces];
-    auto fetch = [&](int t) {                              // the block of token t
+    auto fetch = [&](int block) {
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
             const int i = tid + kMoveThreads * x;
-            if (4 * R % kMoveThreads == 0 || i < 4 * R) piece[x] = *(const u32x4 *)(vp + from[t] * (kBlock * R) + 16 * i);
+            if (4 * R % kMoveThreads == 0 || i < 4 * R) piece[x] = *(const u32x4 *)(vp + page(block) + 16 * i);
         }
     };
-    // The tokens from t on that share its block end ahead of this one.
-    const int n = min(left, kBlock);
-    auto next_of = [&](int t) {
-        int e = t + 1;
-        while (e < n && token[e] >> 6 == token[t] >> 6) ++e;
-        return e;
-    };
-    if (from[0] >= 0) fetch(0);
-    for (int t = 0; t < n;) {                              // (uniform: all threads read the same tokens)
-        const int end = next_of(t);
-        const bool there = from[t] >= 0;
-        __syncthreads();
-        if (there)
+    if (from[0] >= 0) fetch(from[0]);
+    set_ratios();
+    int have = -1;                                         // the block in LDS
+    for (int t = 0; t < n;) {
+        const int end = end_of(t), block = from[t], j = t / kBlock;
+        if (block >= 0 && block != have) {
+            __syncthreads();
 #pragma unroll
             for (int x = 0; x < kPieces; ++x) {
                 const int i = tid + kMoveThreads * x;
@@ -224,24 +250,55 @@ __global__ __launch_bounds__(kMoveThreads) void us_kv_move_kernel(uint8_t *kp, u
                     for (int z = 0; z < 4; ++z) p[z] = piece[x][z];
                 }
             }
-        __syncthreads();
-        if (end < n && from[end] >= 0) fetch(end);
-        if (there)
-            for (int i = tid; i < (end - t) * R; i += kMoveThreads) {
-                const int e = t + i / R, d = i % R;
-                const float c = (float)in[d * kPitch + value_place(token[e] & (kBlock - 1))] - 128.0f;
-                out[d * kPitch + value_place(e)] = (uint8_t)(int)(rintf(c * ratio[e]) + 128.0f);
-            }
-        t = end;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-        const int i = tid + kMoveThreads * x;
-        if (4 * R % kMoveThreads == 0 || i < 4 * R) {
-            const uint32_t *p = (const uint32_t *)(out + (i >> 2) * kPitch + 16 * (i & 3));
-            *(u32x4 *)(vp + dst + 16 * i) = (u32x4){p[0], p[1], p[2], p[3]};
+            have = block;
+            __syncthreads();
         }
+        int next = end;                                    // the first token of another block that is there
+        while (next < n && (from[next] < 0 || from[next] == have)) next = end_of(next);
+        if (next < n && block == have) fetch(from[next]);  // (once: the next run of another block stages it)
+        // A wavefront takes every fourth quad of tokens, a lane a value's row: a quad is a word of it.
+        // (A token without a block has ratio 0, which makes any byte a code of 0.)
+        const int my_token = token[j * kBlock + lane];
+        const float my_ratio = ratio[j * kBlock + lane];
+        const int ta = t - j * kBlock, tb = end - j * kBlock;
+        for (int quad = (ta >> 2) + ((wave - (ta >> 2)) & 3); 4 * quad < tb; quad += 4) {
+            uint32_t at[4];
+            float r[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int e = min(max(4 * quad + v, ta), tb - 1);
+                at[v] = value_place(__builtin_amdgcn_readlane(my_token, e));
+                r[v] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ratio), e));
+            }
+            const bool whole = 4 * quad >= ta && 4 * quad + 4 <= tb;
+            for (int d = lane; d < R; d += 64) {
+                uint8_t *p = out + d * kPitch + value_place(4 * quad);
+                uint32_t q = 0;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) q |= rescaled(in[d * kPitch + at[v]], r[v]) << (8 * v);
+                if (whole) {
+                    *(uint32_t *)p = q;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (4 * quad + v >= ta && 4 * quad + v < tb) p[v] = (uint8_t)(q >> (8 * v));
+                }
+            }
+        }
+        if (end % kBlock == 0 || end == n) {
+            __syncthreads();
+            if (dst[j] >= 0)
+#pragma unroll
+                for (int x = 0; x < kPieces; ++x) {
+                    const int i = tid + kMoveThreads * x;
+                    if (4 * R % kMoveThreads == 0 || i < 4 * R) {
+                        const uint32_t *p = (const uint32_t *)(out + (i >> 2) * kPitch + 16 * (i & 3));
+                        *(u32x4 *)(vp + page(dst[j]) + 16 * i) = (u32x4){p[0], p[1], p[2], p[3]};
+                    }
+                }
+            __syncthreads();
+        }
+        t = end;
     }
 }
 
@@ -263,13 +320,21 @@ extern "C" us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seq
         (to->weights && to->weights_stride < most))
         return US_ERR_SHAPE;
     const hipStream_t q = (hipStream_t)stream;
-    hipLaunchKernelGGL(us_kv_select_kernel, dim3(cache->heads, seqs->batch), dim3(kSelThreads), 0, q, s, weights,
-                       weights_stride, keep, recent, cache->heads, to->lens, to->weights, to->weights_stride, to->index);
+    // Four wavefronts meet at a barrier sooner than sixteen: as long as they hold all weights.
+    const auto select = [&](auto kern, int threads) {
+        hipLaunchKernelGGL(kern, dim3(cache->heads, seqs->batch), dim3(threads), 0, q, s, weights, weights_stride, keep, recent,
+                           cache->heads, to->lens, to->weights, to->weights_stride, to->index);
+    };
+    if (s.max_len <= 256 * kHeld) select(us_kv_select_kernel<256>, 256);
+    else select(us_kv_select_kernel<1024>, 1024);
     if (hipGetLastError() != hipSuccess) return US_ERR_DEVICE;
+    // (a block per workgroup as long as that leaves some CUs without one)
+    const int blocks = (most + kBlock - 1) / kBlock;
+    const int per = 2ll * blocks * cache->heads * seqs->batch > 4ll * us_device::compute_units() ? kPer : 1;
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
         hipLaunchKernelGGL((us_kv_move_kernel<decltype(nt)::value>),
-                           dim3(2 * ((most + kBlock - 1) / kBlock), cache->heads, seqs->batch), dim3(kMoveThreads), 0, q, cache->k,
-                           cache->v, cache->k_scale, cache->v_scale, s, to->index, keep, to->blocks, to->stride, to->width);
+                           dim3(blocks + (blocks + per - 1) / per, cache->heads, seqs->batch), dim3(kMoveThreads), 0, q, cache->k,
+                           cache->v, cache->k_scale, cache->v_scale, s, to->index, keep, to->blocks, to->stride, to->width, blocks, per);
         return hipGetLastError();
     });
     return e == hipSuccess ? US_OK : US_ERR_DEVICE;

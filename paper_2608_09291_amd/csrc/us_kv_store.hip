@@ -29,10 +29,6 @@ __device__ inline uint32_t byte_of(float x, float s) {
     q = q == q ? q : 0.0f;
     return (uint32_t)(int)(fminf(fmaxf(q, -127.0f), 127.0f) + 128.0f);
 }
-// The byte of rint(c r) for the code c of a byte; 0 <= r <= 1.
-__device__ inline uint32_t byte_scaled(uint32_t byte, float r) {
-    return (uint32_t)(int)(rintf(((float)byte - 128.0f) * r) + 128.0f);
-}
 
 // One workgroup per (block that gets new tokens, head, sequence; keys or
 // values). It holds the block's new values in registers, so that they are
@@ -94,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_append_kernel(uint8_t *kp, uin
             } else if (t < t0 && grown) {
                 const u32x2 old = *p;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e >> 2] |= byte_scaled((old[e >> 2] >> (8 * (e & 3))) & 255u, ratio) << (8 * (e & 3));
+                for (int e = 0; e < 8; ++e) w[e >> 2] |= rescaled((old[e >> 2] >> (8 * (e & 3))) & 255u, ratio) << (8 * (e & 3));
                 *p = w;
             }
         }
@@ -129,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_append_kernel(uint8_t *kp, uin
         for (int e = 0; e < 16; ++e) {
             const int t = (int)value_token(16 * g + e);
             const uint32_t was = (old[e >> 2] >> (8 * (e & 3))) & 255u;
-            const uint32_t now = t < t0 ? (grown ? byte_scaled(was, ratio) : was) : tile[t * (R + 8) + d];
+            const uint32_t now = t < t0 ? (grown ? rescaled(was, ratio) : was) : tile[t * (R + 8) + d];
             w[e >> 2] |= now << (8 * (e & 3));
         }
         *p = w;
