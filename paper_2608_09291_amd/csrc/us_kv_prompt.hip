@@ -19,10 +19,13 @@ struct Stage {
     f16x8 v[8][R];                 // eight keys (2 j + h: 16 j + 4 h + {0..3, 8..11}), value
 };
 
+constexpr int prompt_stages(int row) { return row <= 128 ? 4 : 2; }        // of at most 160 KB
+
 template <int NT, int DT, int W>
 __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
     constexpr int kThreads = 64 * W, kRows = 32 * W;       // 32 rows per wavefront
+    constexpr int kStages = prompt_stages(32 * NT), kAhead = kStages == 4 ? 1 : 0;
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -141,7 +144,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             }
         }
     };
-    auto put_k = [&](int buf) {
+    auto put_k = [&](int blk) {
+        const int buf = blk % kStages;
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
             const int q = tid + kThreads * x;
@@ -152,7 +156,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             }
         }
     };
-    auto put_v = [&](int buf) {
+    auto put_v = [&](int blk) {
+        const int buf = blk % kStages;
 #pragma unroll
         for (int x = 0; x < kPairs; ++x) {
             const int q = tid + kThreads * x;
@@ -173,7 +178,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[t][v] = 0.0f;
     // Lane (c, h), element v of s[y]: key 32 y + 8 (v / 4) + 4 h + v % 4, row c.
-    auto scores = [&](int buf, f32x16 (&x)[2]) {
+    auto scores = [&](int blk, f32x16 (&x)[2]) {
+        const int buf = blk % kStages;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
 #pragma unroll
@@ -207,41 +213,41 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[y][v]);
         return fmaxf(top, __shfl_xor(top, 32, 64));
     };
-    // A block's keys are staged two blocks ahead of their exponentials, its
-    // values one; scores are computed one ahead. So the matrix cores work on
-    // the next scores under a block's exponentials, and on its second product
-    // under the staging of later blocks, in one wavefront.
+    // Scores are computed one block ahead of their exponentials, so that the
+    // matrix cores work on the next scores under a block's exponentials, and on
+    // its second product under the staging of later blocks, in one wavefront.
+    // Keys are staged kAhead + 2 blocks ahead, values kAhead + 1: with four
+    // stages a barrier serves two blocks.
     float top = -INFINITY;
-    float ks0 = 0.0f, ks1 = 0.0f, ks2 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;          // of blocks i, i + 1, i + 2
+    float ks[3 + kAhead] = {}, vs[2 + kAhead] = {};        // of block i and the next ones
     if (count > 0) {
         look_up(0, id_k, sc_k, a.ks);
         look_up(0, id_v, sc_v, a.vs);
-        fetch_k(0, ks0);
-        fetch_v(0, vs0);
-        put_k(0);
-        put_v(0);
-        if (count > 1) {
-            fetch_k(1, ks1);
-            fetch_v(1, vs1);
-            put_k(1);
-        }
+#pragma unroll
+        for (int z = 0; z < 2 + kAhead; ++z)
+            if (z < count) {
+                fetch_k(z, ks[z]);
+                if (z < 1 + kAhead) fetch_v(z, vs[z]);
+                put_k(z);
+                if (z < 1 + kAhead) put_v(z);
+            }
+        if (2 + kAhead < count) fetch_k(2 + kAhead, ks[2 + kAhead]);
+        if (1 + kAhead < count) fetch_v(1 + kAhead, vs[1 + kAhead]);
         __syncthreads();
         scores(0, sa);
-        hide(0, ks0, sa);
+        hide(0, ks[0], sa);
         top = largest(sa);
-        __syncthreads();
-        if (count > 2) fetch_k(2, ks2);
+        if constexpr (kAhead == 0) __syncthreads();        // (the first step stages over block 0's keys)
     }
     auto step = [&](int i, auto odd, f32x16 (&s)[2], f32x16 (&next)[2]) {
-        constexpr int cur = decltype(odd)::value, other = 1 - cur;             // stages of blocks i and i + 1
         // (above 0, so that a masked key's -inf stays one)
-        const float vs = vs0, fk = fmaxf(f * fabsf(ks0), 1.17549435e-38f);
+        const float v_scale = vs[0], fk = fmaxf(f * fabsf(ks[0]), 1.17549435e-38f);
         // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
         const float m2 = fmaxf(m, top * fk);
         float change = 1.0f;
-        if (vs > vmax) {
-            change = vmax * __builtin_amdgcn_rcpf(vs);
-            vmax = vs;
+        if (v_scale > vmax) {
+            change = vmax * __builtin_amdgcn_rcpf(v_scale);
+            vmax = v_scale;
         }
         if (m2 > m + kSlack || m == -INFINITY) {
             const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
@@ -256,11 +262,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
                 for (int v = 0; v < 16; ++v) o[t][v] *= change;
         }
         // (2^-60: below what any sum keeps; 1 as long as all scales are 0, where o does not count)
-        const float ratio = vmax > 0.0f ? fmaxf(vs * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
+        const float ratio = vmax > 0.0f ? fmaxf(v_scale * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
         const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
         float sum = 0.0f;
         f16x8 ph[4], pl[4];
-        scores(other, next);                               // (of no use after the last block)
+        scores(i + 1, next);                               // (of no use after the last block)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float p[8];
@@ -274,25 +280,26 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
         l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
         // (keeps the exponentials here, beside the scores' product)
         __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
-        if (i + 1 < count) hide(i + 1, ks1, next);
+        if (i + 1 < count) hide(i + 1, ks[1], next);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f16x8 vf = stage[cur].v[2 * j + h][32 * t + c];
+                const f16x8 vf = stage[i % kStages].v[2 * j + h][32 * t + c];
                 o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
                 if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
             }
         top = largest(next);
-        ks0 = ks1;
-        ks1 = ks2;
-        vs0 = vs1;
+#pragma unroll
+        for (int z = 0; z < 2 + kAhead; ++z) ks[z] = ks[z + 1];
+#pragma unroll
+        for (int z = 0; z < 1 + kAhead; ++z) vs[z] = vs[z + 1];
         // (past the last block: codes of an earlier one once more, which no product takes)
-        put_k(cur);
-        put_v(other);
-        if (i + 3 < count) fetch_k(i + 3, ks2);
-        if (i + 2 < count) fetch_v(i + 2, vs1);
-        __syncthreads();
+        put_k(i + 2 + kAhead);
+        put_v(i + 1 + kAhead);
+        if (i + 3 + kAhead < count) fetch_k(i + 3 + kAhead, ks[2 + kAhead]);
+        if (i + 2 + kAhead < count) fetch_v(i + 2 + kAhead, vs[1 + kAhead]);
+        if constexpr (kAhead == 0 || decltype(odd)::value == 1) __syncthreads();
     };
     for (int i = 0; i < count; i += 2) {
         step(i, std::integral_constant<int, 0>(), sa, sb);
@@ -521,7 +528,7 @@ hipError_t allow_lds(K kern, std::atomic<unsigned long long> &set) {
 hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream) {
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
-            constexpr int NT = decltype(nt)::value, kLds = 2 * (int)sizeof(Stage<32 * NT>);
+            constexpr int NT = decltype(nt)::value, kLds = prompt_stages(32 * NT) * (int)sizeof(Stage<32 * NT>);
             constexpr int W = prompt_waves(32 * NT, decltype(dt)::value == US_F32);
             auto kern = us_kv_prompt_kernel<NT, decltype(dt)::value, W>;
             if constexpr (kLds > 65536 - 1024) {
