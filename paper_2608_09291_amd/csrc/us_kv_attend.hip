@@ -43,7 +43,13 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     const int max_len = seqs_of(c, s, o.max_len, tokens).max_len, R = row_of(c.head_dim);
     const int64_t rows = (int64_t)s.max_new * (q_heads / c.heads), pairs = (int64_t)s.batch * c.heads;
     if (rows > US_KV_NEW_MAX) return US_ERR_SHAPE;
-    p.decode = rows <= 32;
+    // Rows of a cache head up to which the decode kernel reads the cache once per 16 of them, rather
+    // than the prompt kernel once per 128 or 256. us per call, decode against prompt: 64 rows of 4000
+    // keys, 8 heads of 128, 8 sequences 33 and 52, 16 61 and 91, 40 210 and 222; 128 rows, 8 sequences
+    // (64 MB of cache) 51 and 55, 16 (131 MB) 128 and 94; 128 rows of 500 keys, one sequence, 12 and 23.
+    // (60 rows of 2000 keys, 32 heads, 32 sequences, 524 MB: 351 and 315.)
+    const int64_t cached = pairs * up(max_len, kBlock) * 2 * R;
+    p.decode = rows <= 64 || (rows <= 128 && cached <= (64 << 20));
     const int tile = p.decode ? 16 : 32 * prompt_waves(R, f32);
     p.tiles = (int)((rows + tile - 1) / tile);
     p.rows = rows < tile && p.decode ? (int)rows : tile;
