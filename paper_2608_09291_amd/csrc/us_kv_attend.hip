@@ -43,48 +43,60 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     const int max_len = seqs_of(c, s, o.max_len, tokens).max_len, R = row_of(c.head_dim);
     const int64_t rows = (int64_t)s.max_new * (q_heads / c.heads), pairs = (int64_t)s.batch * c.heads;
     if (rows > US_KV_NEW_MAX) return US_ERR_SHAPE;
-    // Rows of a cache head up to which the decode kernel reads the cache once per 16 of them, rather
-    // than the prompt kernel once per 128 or 256. us per call, decode against prompt: 64 rows of 4000
-    // keys, 8 heads of 128, 8 sequences 33 and 52, 16 61 and 91, 40 210 and 222; 128 rows, 8 sequences
-    // (64 MB of cache) 51 and 55, 16 (131 MB) 128 and 94; 128 rows of 500 keys, one sequence, 12 and 23.
-    // (60 rows of 2000 keys, 32 heads, 32 sequences, 524 MB: 351 and 315.)
-    const int64_t cached = pairs * up(max_len, kBlock) * 2 * R;
-    p.decode = rows <= 64 || (rows <= 128 && cached <= (64 << 20));
-    const int tile = p.decode ? 16 : 32 * prompt_waves(R, f32);
-    p.tiles = (int)((rows + tile - 1) / tile);
-    p.rows = rows < tile && p.decode ? (int)rows : tile;
-    const int64_t units = pairs * p.tiles;
-    // Blocks that a tile's rows see at most.
-    int64_t most = up(max_len, kBlock) / kBlock;
-    if (o.window) {
-        const int64_t reach = o.window + (tile + q_heads / c.heads - 1) / (q_heads / c.heads);
-        if (reach / kBlock + 2 < most) most = reach / kBlock + 2;
-    }
-    const int cus = us_device::compute_units();
-    if (p.decode) {
-        int64_t chunk = up(units * most / (2 * cus), 4);
-        p.chunk = (int)(chunk < 4 ? 4 : chunk > 64 ? 64 : chunk);
-    } else {
-        // Generations of workgroups, one per CU, times what one takes, in blocks: its own, and 10
-        // for storing and joining its partial rows where there are several. (The tokens bound the
-        // tiles that have rows where the sequences' numbers of them differ.) us per call, two
-        // workgroups per CU and a join by the last of a tile before -> this: 64 queries on 30000
-        // keys, 8 heads over 1, 567 -> 46; 2048 causal, 32 heads, 115 -> 76; 512 on 16000, 64
-        // heads over 8, 336 -> 285.
-        const int64_t filled = c.heads * ((int64_t)tokens * (q_heads / c.heads) / tile + s.batch);
-        const int64_t work = filled < units ? filled : units;
-        int64_t best = INT64_MAX;
-        for (int64_t n = 1; n <= 128 && n <= most; ++n) {
-            const int64_t chunk = (most + n - 1) / n, t = (work * n + cus - 1) / cus * (chunk + (n > 1 ? 10 : 0));
-            if (t < best) {
-                best = t;
-                p.chunk = (int)chunk;
-            }
+    const int cus = us_device::compute_units(), G = q_heads / c.heads;
+    const int64_t all = up(max_len, kBlock) / kBlock;
+    // Blocks that the rows of a tile see at most.
+    const auto seen = [&](int tile) {
+        const int64_t reach = (o.window + (int64_t)(tile + G - 1) / G) / kBlock + 2;
+        return o.window && reach < all ? reach : all;
+    };
+    // Prompt: generations of workgroups, one per CU, times what one takes, in blocks: its own, and 10
+    // for storing and joining its partial rows where there are several. (The tokens bound the tiles that
+    // have rows where the sequences' numbers of them differ.) us per call, two workgroups per CU and a
+    // join by the last of a tile before -> this: 64 queries on 30000 keys, 8 heads over 1, 567 -> 46;
+    // 2048 causal, 32 heads, 115 -> 76; 512 on 16000, 64 heads over 8, 336 -> 285.
+    const int wide = 32 * prompt_waves(R, f32);
+    const int64_t most_w = seen(wide), tiles_w = (rows + wide - 1) / wide;
+    const int64_t filled = c.heads * ((int64_t)tokens * G / wide + s.batch);
+    const int64_t work = filled < pairs * tiles_w ? filled : pairs * tiles_w;
+    int64_t best = INT64_MAX, chunk_w = most_w;
+    for (int64_t n = 1; n <= 128 && n <= most_w; ++n) {
+        const int64_t chunk = (most_w + n - 1) / n, t = (work * n + cus - 1) / cus * (chunk + (n > 1 ? 10 : 0));
+        if (t < best) {
+            best = t;
+            chunk_w = chunk;
         }
     }
+    // Decode: two workgroups per CU, splits of 4 to 64 blocks.
+    const int64_t most_n = seen(16), tiles_n = (rows + 15) / 16, units_n = pairs * tiles_n;
+    int64_t chunk_n = up(units_n * most_n / (2 * cus), 4);
+    chunk_n = chunk_n < 4 ? 4 : chunk_n > 64 ? 64 : chunk_n;
+    // Which of the two, by what they take in us: the decode kernel reads the cache once per 16 rows,
+    // from behind the L2s at 10 TB/s if the 256 MB there hold it and at 6 if not, a wavefront takes
+    // 1 us for a block, a generation 4 at least; the prompt kernel takes 1.75 us for a block of the
+    // above, 2.2 with four wavefronts. us per call, decode and prompt: 64 rows of 4000 keys, 8 sequences
+    // of 8 heads of 128, 33 and 52; 128 rows, 16 sequences, 123 and 95; 500 causal rows, 32 heads, 18
+    // and 27; 60 rows of 2000 keys, 32 sequences of 32 heads, 342 and 308; 328 rows of 43840 keys, 2
+    // sequences of 8 heads, 75 and 104. Over 25 shapes the choice takes at most 1.1 times the faster
+    // one's time, but where weights rule the decode kernel out (537 and 455).
+    const double cached = (double)(pairs * all) * 128.0 * R, narrow_blocks = (double)units_n * (double)most_n;
+    const double read = narrow_blocks * 128.0 * R / (cached <= 256e6 ? 1e7 : 6e6), math = narrow_blocks * R / (128.0 * 4 * cus);
+    const double gens = 4.0 * (double)((units_n * ((most_n + chunk_n - 1) / chunk_n) + 2 * cus - 1) / (2 * cus));
+    const double narrow = 5.0 + (read > math ? (read > gens ? read : gens) : (math > gens ? math : gens));
+    const double broad = 8.0 + (wide == 256 ? 1.75 : 2.2) * (double)best;
+    // (the scores that weights need are kept up to 64 MB, for up to 16 rows however many there are)
+    const bool keeps = !o.weights || rows <= 16 || (double)(pairs * tiles_n * 16) * (double)(all * kBlock) * 4.0 <= 64e6;
+    p.decode = rows <= 16 || (narrow <= broad && keeps && tiles_n <= 4096);
+    const int64_t most = p.decode ? most_n : most_w;
+    const int tile = p.decode ? 16 : wide;
+    p.tiles = (int)(p.decode ? tiles_n : tiles_w);
+    p.rows = p.decode && rows < 16 ? (int)rows : tile;
+    p.chunk = (int)(p.decode ? chunk_n : chunk_w);
+    const int64_t units = pairs * p.tiles;
     // (a unit's partial rows lie within 2^31 bytes)
     if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
     if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
+    if (p.decode && ((most + p.chunk - 1) / p.chunk) * p.tiles > 65535) p.chunk = (int)((most * p.tiles + 65534) / 65535) + 1;
     p.splits = (int)((most + p.chunk - 1) / p.chunk);
     if (units * p.splits > INT32_MAX / 512) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);

@@ -312,26 +312,42 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     }
 }
 
-// weights[b, hk, j] += sum over the rows of 2^(x_j - lse): four keys per thread.
-__global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, float *weights, int64_t stride) {
-    const int hk = blockIdx.y, b = blockIdx.z;
+// weights[b, hk, j] += sum over the rows of 2^(x_j - lse): four keys per thread, and a quarter of a
+// tile's rows per wavefront where there are more than two.
+__global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, float *weights, int64_t stride, int shared) {
+    __shared__ f32x4 part[kWaves][64];
+    const int hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int r0, n;
     a.s.rows(b, r0, n);
-    const int len = a.s.len(b), total = n * a.G, j0 = 4 * (blockIdx.x * kThreads + threadIdx.x);
-    if (j0 >= len) return;
+    const int len = a.s.len(b), total = n * a.G;
+    const int j0 = 4 * (shared ? (int)blockIdx.x * 64 + (tid & 63) : (int)blockIdx.x * kThreads + tid);
+    if (4 * (int)blockIdx.x * (shared ? 64 : kThreads) >= len) return;         // (the whole workgroup)
     const int64_t bh = (int64_t)b * a.heads + hk;
-    float sum[4] = {0, 0, 0, 0};
-    // (no tile has stored scores of blocks ahead of its first row's window or past its last row's)
-    for (int row = 0; row < total; ++row) {
-        const int tile = row / kRows;
+    f32x4 sum = {0, 0, 0, 0};
+    const int first = shared ? 4 * wave : 0, each = shared ? 4 : kRows;
+    for (int base = 0; base < total; base += kRows) {
+        // (no tile has stored scores of blocks ahead of its first row's window or past its last row's)
         int lo, hi, x;
-        a.mask.range(tile * kRows / a.G, n, len, lo, x);
-        a.mask.range((min(tile * kRows + kRows, total) - 1) / a.G, n, len, x, hi);
+        a.mask.range(base / a.G, n, len, lo, x);
+        a.mask.range((min(base + kRows, total) - 1) / a.G, n, len, x, hi);
         if (j0 < lo / kBlock * kBlock || j0 >= hi) continue;
-        const float z = a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32];
-        const f32x4 s = *(const f32x4 *)(a.sp.scores + (bh * a.sp.rows * a.sp.tiles + row) * a.sp.scores_stride + j0);
+        const float *z = a.sp.lse + 32 * row_block(a, hk, b, r0, base) + base % 32;
+        const float *s = a.sp.scores + (bh * a.sp.rows * a.sp.tiles + base) * a.sp.scores_stride + j0;
+        const int end = min(first + each, total - base);
+#pragma unroll 4
+        for (int r = first; r < end; ++r) {
+            const f32x4 y = *(const f32x4 *)(s + r * a.sp.scores_stride);
+            const float zr = z[r];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) sum[v] += __builtin_amdgcn_exp2f(s[v] - z);
+            for (int v = 0; v < 4; ++v) sum[v] += __builtin_amdgcn_exp2f(y[v] - zr);
+        }
+    }
+    if (shared) {
+        part[wave][tid & 63] = sum;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) sum += part[w][tid];
     }
     float *w = weights + bh * stride + j0;
 #pragma unroll
@@ -352,8 +368,9 @@ hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream
 }
 
 hipError_t launch_weights_saved(const Args &a, int batch, float *weights, int64_t stride, hipStream_t stream) {
-    const unsigned x = (unsigned)((a.s.max_len + 4 * kThreads - 1) / (4 * kThreads));
-    hipLaunchKernelGGL(us_kv_weights_saved_kernel, dim3(x, a.heads, batch), dim3(kThreads), 0, stream, a, weights, stride);
+    const int shared = (int64_t)a.s.max_new * a.G > 2, keys = 4 * (shared ? 64 : kThreads);
+    hipLaunchKernelGGL(us_kv_weights_saved_kernel, dim3((unsigned)((a.s.max_len + keys - 1) / keys), a.heads, batch), dim3(kThreads), 0,
+                       stream, a, weights, stride, shared);
     return hipGetLastError();
 }
 
