@@ -508,3 +508,18 @@ def test_evict(torch_cuda, lens, heads, D, keep, recent, kind):
             for blk in p.blocks[b]:
                 if blk >= 0:
                     assert np.array_equal(codes[blk], p.codes[i][blk])
+
+
+def test_example_layer(torch_cuda):
+    """The operators together, as a decoder layer uses them: projections, cache, attention, eviction."""
+    import importlib.util
+    import os
+    announce("kv example")
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "kv_decode.py")
+    spec = importlib.util.spec_from_file_location("kv_decode", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    off, evictions = m.main(["--batch", "3", "--tokens", "170", "--budget", "100"])
+    assert evictions == 2
+    # float32 queries: scores of at most 64 products off by 72 * 2^-24 of about 10, probabilities by twice that
+    assert off < 2.0 ** -13
