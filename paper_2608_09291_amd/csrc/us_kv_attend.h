@@ -45,6 +45,7 @@ struct Mask {
 // floats, then their (m, l) pairs.
 struct Split {
     int32_t chunk, splits, tiles, rows;
+    int32_t mix;      // of prompts: units of an XCD whose tiles run side by side; divides their number
     float *part;      // the rows of a split, then their (m, l): rows (R + 2) floats, to a multiple of 4
     int32_t *tickets;
     // For the weights, by cache head and row_block(), 32 rows each; else NULL.

@@ -30,7 +30,7 @@ constexpr int64_t kTickets = 16384;
 
 struct Plan {
     bool decode;
-    int chunk, splits, tiles, rows;
+    int chunk, splits, tiles, rows, mix;
     int64_t scores_stride;
     int64_t row_blocks;
     size_t part, lse, qf, qn, scores, total;
@@ -93,6 +93,14 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     p.rows = p.decode && rows < 16 ? (int)rows : tile;
     p.chunk = (int)(p.decode ? chunk_n : chunk_w);
     const int64_t units = pairs * p.tiles;
+    // Heads of a sequence side by side on an XCD, up to 18 MB of cache. us per call, one by one and so:
+    // 8192 causal rows, 32 heads, 655 and 619; 4096, 229 and 164; 2048, 4 sequences, 258 and 203; 16384,
+    // 64 heads, 4527 and 4446. (Sequences differ in length: 4 of them side by side 1160 and 1376.)
+    const int64_t share = c.heads % 8 == 0 ? c.heads / 8 : 1;
+    int64_t mix = 18000000 / (all * 128 * R);
+    mix = mix < 1 ? 1 : mix > share ? share : mix;
+    while (share % mix) --mix;
+    p.mix = (int)mix;
     // (a unit's partial rows lie within 2^31 bytes)
     if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
     if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
@@ -154,7 +162,7 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     a.q = Rows{q->data, q->token_stride, q->head_stride};
     a.out = Rows{out->data, out->token_stride, out->head_stride};
     a.mask = Mask{o.causal, o.window};
-    a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, (float *)(w + p.part), (int32_t *)w,
+    a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, p.mix, (float *)(w + p.part), (int32_t *)w,
                  o.weights ? (float *)(w + p.lse) : nullptr, p.row_blocks,
                  o.weights && !p.decode ? (f16x8 *)(w + p.qn) : nullptr, (float *)(w + p.qf),
                  o.weights && p.decode ? (float *)(w + p.scores) : nullptr, p.scores_stride};

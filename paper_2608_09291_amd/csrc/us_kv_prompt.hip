@@ -19,6 +19,7 @@ struct Stage {
     f16x8 v[8][R];                 // eight keys (2 j + h: 16 j + 4 h + {0..3, 8..11}), value
 };
 
+constexpr int weights_blocks(int row, bool f32) { return row <= 192 || !f32 ? 2 : 1; }     // three stages of at most 160 KB
 constexpr int prompt_stages(int row) { return row <= 128 ? 4 : 2; }        // of at most 160 KB
 
 template <int NT, int DT, int W>
@@ -32,13 +33,15 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     Stage<R> *stage = (Stage<R> *)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
-    // The tiles of a unit (sequence, cache head) follow each other on one XCD,
-    // whose L2 then serves their keys; the last tile, which sees the most, first.
+    // The tiles of a unit (sequence, cache head) run on one XCD, whose L2 then
+    // serves their keys; of `mix` units together the last tiles, which see the most,
+    // first, so that short ones fill the end.
     const int per = a.sp.tiles * a.sp.splits;
     int u = blockIdx.x / per, slot = blockIdx.x % per;
     if (a.heads % 8 == 0) {                                // (all XCDs then get parts of every sequence)
-        u = (blockIdx.x >> 3) / per * 8 + (blockIdx.x & 7);
-        slot = (blockIdx.x >> 3) % per;
+        const int s = blockIdx.x >> 3, turn = s / (per * a.sp.mix), in = s % (per * a.sp.mix);
+        u = (turn * a.sp.mix + in % a.sp.mix) * 8 + (blockIdx.x & 7);
+        slot = in / a.sp.mix;
     }
     const int tile = a.sp.tiles - 1 - slot / a.sp.splits, split = slot % a.sp.splits;
     const int b = u / a.heads, hk = u - b * a.heads;
@@ -375,17 +378,22 @@ __global__ __launch_bounds__(256) void us_kv_join_kernel(Args a) {
 // The probabilities' sums over the query rows, from the logarithms of the rows'
 // sums: the first product again, the other way about. A wavefront keeps a block
 // of keys in registers; the rows, in the form that the first pass left them,
-// pass through LDS, 64 at a time.
+// pass through LDS, in three stages. Scores are computed 32 rows ahead of their
+// exponentials, so that the matrix cores work under these. Chunks of 512 on
+// 16000 keys, 64 heads over 8: 455 us without that and with a division per 32
+// rows for the mask.
 constexpr int kKeys = 256;                                 // of a workgroup
 template <int NT, int DT>
-__global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args a, float *weights, int64_t stride) {
+__global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) void us_kv_weights_kernel(Args a, float *weights, int64_t stride) {
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16, kParts = SPLIT ? 2 : 1;
     constexpr int kForm = kParts * R / 8 * 32;             // pieces of 32 rows
-    constexpr int kPieces = 2 * kForm / 256;
+    constexpr int kBlocks = weights_blocks(R, SPLIT);      // blocks of 32 rows of a stage
+    constexpr int kPieces = kBlocks * kForm / 256;
+    static_assert(kBlocks * kForm % 256 == 0);
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    f16x8(*q)[2 * kForm] = (f16x8(*)[2 * kForm])lds;       // stage; row block, part, octet, row
-    __shared__ float row_f[2][64], row_z[2][64];
+    f16x8(*q)[kBlocks * kForm] = (f16x8(*)[kBlocks * kForm])lds;               // stage; row block, part, octet, row
+    __shared__ float row_f[3][64], row_z[3][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5, hk = blockIdx.y, b = blockIdx.z;
     int r0, n;
@@ -401,6 +409,14 @@ __global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args
     if (i0 >= i1) return;
     const int total = n * a.G, first = i0 * a.G / 32, end = (i1 * a.G + 31) / 32;   // blocks of rows
     const int blk = 4 * (int)blockIdx.x + wave, k0 = blk * kBlock;
+    // Rows [all0, all1) see all of this wavefront's keys.
+    int all0 = 0, all1 = total;
+    if (a.mask.causal) {
+        all0 = (int)min((int64_t)total, (int64_t)max(k0 + kBlock - 1 - (len - n), 0) * a.G);
+        if (a.mask.window > 0) all1 = (int)min((int64_t)total, max((int64_t)k0 + a.mask.window - (len - n), (int64_t)0) * a.G);
+    } else if (k0 + kBlock > len) {
+        all1 = 0;
+    }
     const int id = k0 < len ? a.s.block(b, blk) : -1;
     const int64_t at = (int64_t)max(id, 0) * a.heads + hk;
     const float ks = id < 0 ? 0.0f : a.ks[at];
@@ -408,10 +424,10 @@ __global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args
     const f16x8 *src = a.sp.qn + rb * kForm;
     f16x8 piece[kPieces];
     float f_next = 0.0f, z_next = 0.0f;
-    auto fetch = [&](int x) {                              // row blocks x and x + 1 (there is one past the last)
+    auto fetch = [&](int x) {                              // row blocks x .. (there is one past the last)
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) piece[y] = src[(int64_t)x * kForm + tid + 256 * y];
-        if (tid < 64) {
+        if (tid < 32 * kBlocks) {
             f_next = a.sp.qf[32 * (rb + x) + tid];
             z_next = a.sp.lse[32 * (rb + x) + tid];
         }
@@ -419,7 +435,7 @@ __global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args
     auto put = [&](int buf) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) q[buf][tid + 256 * y] = piece[y];
-        if (tid < 64) {
+        if (tid < 32 * kBlocks) {
             row_f[buf][tid] = f_next;
             row_z[buf][tid] = z_next;
         }
@@ -437,60 +453,78 @@ __global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void us_kv_weights_kernel(Args
                 kf[u][t] = halves_of(w[0], w[1]);
             }
     }
-    put(0);
-    f32x16 sum[2];
+    f32x16 sum[2], sa[2], sb[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int v = 0; v < 16; ++v) sum[u][v] = 0.0f;
-    __syncthreads();
-    for (int x = first; x < end; x += 2) {
-        const int buf = ((x - first) >> 1) & 1;
-        if (x + 2 < end) fetch(x + 2);
+    auto scores = [&](int buf, int y, f32x16 (&s)[2]) {    // of row block y of a stage
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            f32x16 s[2];
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[u][v] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int z = 0; z < kParts; ++z) {
+                const f16x8 qf = q[buf][kForm * y + (z * (R / 8) + 2 * t + h) * 32 + c];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[u][t], qf, s[u], 0, 0, 0);
+            }
+    };
+    auto add = [&](int x, float fk, float z, const f32x16 (&s)[2]) {           // row block x
+        const int base = 32 * x;
+        if (base >= all0 && base + 32 <= all1) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s[u][v] = 0.0f;
+                for (int v = 0; v < 16; ++v) sum[u][v] += __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
+        } else {
+            // (rows past the last hold anything)
+            int from = 0, to = 0;
+            if (base + c < total) a.mask.range((base + c) / a.G, n, len, from, to);
+            from -= k0 + 4 * h;
+            to -= k0 + 4 * h;
 #pragma unroll
-            for (int t = 0; t < NS; ++t)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int z = 0; z < kParts; ++z) {
-                    const f16x8 qf = q[buf][kForm * y + (z * (R / 8) + 2 * t + h) * 32 + c];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[u][t], qf, s[u], 0, 0, 0);
+                for (int v = 0; v < 16; ++v) {
+                    const int j = 32 * u + 8 * (v >> 2) + (v & 3);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
+                    sum[u][v] += j >= from && j < to ? p : 0.0f;
                 }
-            const float fk = row_f[buf][32 * y + c] * ks, z = row_z[buf][32 * y + c];
-            const int base = 32 * (x + y), last = min(base + 31, total - 1);
-            int lo0 = 0, hi0 = 0, lo1 = 0, hi1 = 0;
-            if (base < total) {
-                a.mask.range(base / a.G, n, len, lo0, hi0);
-                a.mask.range(last / a.G, n, len, lo1, hi1);
-            }
-            if (base + 32 > total || k0 < lo1 || k0 + kBlock > hi0) {
-                // (rows past the last hold anything)
-                int from = 0, to = 0;
-                if (base + c < total) a.mask.range((base + c) / a.G, n, len, from, to);
-                from -= k0 + 4 * h;
-                to -= k0 + 4 * h;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int j = 32 * u + 8 * (v >> 2) + (v & 3);
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
-                        sum[u][v] += j >= from && j < to ? p : 0.0f;
-                    }
-            } else {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sum[u][v] += __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
-            }
         }
-        if (x + 2 < end) put(buf ^ 1);
+    };
+    // Stage i % 3 holds chunk i: while chunk i is added up and the first scores of
+    // chunk i + 1 are taken, chunk i + 2 is put, and i + 3 is on its way.
+    const int chunks = (end - first + kBlocks - 1) / kBlocks;
+    put(0);
+    if (chunks > 1) {
+        fetch(first + kBlocks);
+        put(1);
+    }
+    if (chunks > 2) fetch(first + 2 * kBlocks);
+    __syncthreads();
+    scores(0, 0, sa);
+    auto turn = [&](int i, int x, int y, f32x16 (&s)[2], f32x16 (&next)[2]) {  // row block y of chunk i, the x-th
+        const int buf = i % 3;
+        const float fk = row_f[buf][32 * y + c] * ks, z = row_z[buf][32 * y + c];
+        if (y + 1 < kBlocks) scores(buf, y + 1, next);
+        else scores((i + 1) % 3, 0, next);                 // (of no use after the last chunk)
+        add(x, fk, z, s);
+    };
+    for (int i = 0; i < chunks; ++i) {
+        const int x = first + i * kBlocks;
+        if constexpr (kBlocks == 2) {
+            turn(i, x, 0, sa, sb);
+            turn(i, x + 1, 1, sb, sa);
+        } else {
+            turn(i, x, 0, sa, sb);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) sa[u] = sb[u];
+        }
+        if (i + 2 < chunks) put((i + 2) % 3);
+        if (i + 3 < chunks) fetch(x + 3 * kBlocks);
         __syncthreads();
     }
 #pragma unroll
@@ -552,7 +586,7 @@ hipError_t launch_weights(int dtype, const Args &a, int batch, float *weights, i
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
             constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
-            constexpr int kLds = 2 * (DT == US_F32 ? 2 : 1) * 64 * 32 * NT * 2;
+            constexpr int kLds = 3 * (DT == US_F32 ? 2 : 1) * 32 * weights_blocks(32 * NT, DT == US_F32) * 32 * NT * 2;
             auto kern = us_kv_weights_kernel<NT, DT>;
             if constexpr (kLds > 65536 - 2048) {
                 static std::atomic<unsigned long long> set{0};
