@@ -237,10 +237,10 @@ __device__ inline bool last_of(int32_t *ticket, int n, int *lds) {
 }
 
 // Wavefronts of a prompt workgroup, 32 query rows each. Eight share the
-// conversion of a block among twice the rows (8192 causal rows, 32 heads of 128:
-// 611 us against 639 with four); wider rows and float32's two parts take the
-// registers of four.
-constexpr int prompt_waves(int row, bool f32) { return row <= 128 && !f32 ? 8 : 4; }
+// conversion of a block among twice the rows (us, four and eight: 8192 causal
+// rows, 32 heads of 128, 639 and 611; 4096 float32 rows, heads of 64, 290 and
+// 187, of 128 362 and 310); wider rows take the registers of four.
+constexpr int prompt_waves(int row) { return row <= 128 ? 8 : 4; }
 
 // The block of 32 rows that holds row `row` of sequence b, whose first token row is r0 and
 // which has a.G rows to a token: every sequence begins a block of its own.

@@ -55,7 +55,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     // have rows where the sequences' numbers of them differ.) us per call, two workgroups per CU and a
     // join by the last of a tile before -> this: 64 queries on 30000 keys, 8 heads over 1, 567 -> 46;
     // 2048 causal, 32 heads, 115 -> 76; 512 on 16000, 64 heads over 8, 336 -> 285.
-    const int wide = 32 * prompt_waves(R, f32);
+    const int wide = 32 * prompt_waves(R);
     const int64_t most_w = seen(wide), tiles_w = (rows + wide - 1) / wide;
     const int64_t filled = c.heads * ((int64_t)tokens * G / wide + s.batch);
     const int64_t work = filled < pairs * tiles_w ? filled : pairs * tiles_w;
@@ -74,7 +74,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     // Which of the two, by what they take in us: the decode kernel reads the cache once per 16 rows,
     // from behind the L2s at 10 TB/s if the 256 MB there hold it and at 6 if not, a wavefront takes
     // 1 us for a block, a generation 4 at least; the prompt kernel takes 1.75 us for a block of the
-    // above, 2.2 with four wavefronts. us per call, decode and prompt: 64 rows of 4000 keys, 8 sequences
+    // above, 2.6 with float32 rows, 2.2 with four wavefronts. us per call, decode and prompt: 64 rows of 4000 keys, 8 sequences
     // of 8 heads of 128, 33 and 52; 128 rows, 16 sequences, 123 and 95; 500 causal rows, 32 heads, 18
     // and 27; 60 rows of 2000 keys, 32 sequences of 32 heads, 342 and 308; 328 rows of 43840 keys, 2
     // sequences of 8 heads, 75 and 104. Over 25 shapes the choice takes at most 1.1 times the faster
@@ -83,7 +83,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     const double read = narrow_blocks * 128.0 * R / (cached <= 256e6 ? 1e7 : 6e6), math = narrow_blocks * R / (128.0 * 4 * cus);
     const double gens = 4.0 * (double)((units_n * ((most_n + chunk_n - 1) / chunk_n) + 2 * cus - 1) / (2 * cus));
     const double narrow = 5.0 + (read > math ? (read > gens ? read : gens) : (math > gens ? math : gens));
-    const double broad = 8.0 + (wide == 256 ? 1.75 : 2.2) * (double)best;
+    const double broad = 8.0 + (wide < 256 ? 2.2 : f32 ? 2.6 : 1.75) * (double)best;
     // (the scores that weights need are kept up to 64 MB, for up to 16 rows however many there are)
     const bool keeps = !o.weights || rows <= 16 || (double)(pairs * tiles_n * 16) * (double)(all * kBlock) * 4.0 <= 64e6;
     p.decode = rows <= 16 || (narrow <= broad && keeps && tiles_n <= 4096);

@@ -20,15 +20,20 @@ struct Stage {
 };
 
 constexpr int weights_blocks(int row, bool f32) { return row <= 192 || !f32 ? 2 : 1; }     // three stages of at most 160 KB
-constexpr int prompt_stages(int row) { return row <= 128 ? 4 : 2; }        // of at most 160 KB
+// Stages of blocks, within 160 KB; beside them, of float32 rows above 64, the low parts of the queries.
+constexpr bool prompt_low(int row, bool f32) { return f32 && row > 64 && row <= 128; }
+constexpr int prompt_stages(int row, bool f32) { return row <= 128 && !prompt_low(row, f32) ? 4 : 2; }
 
 template <int NT, int DT, int W>
-__global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
+__global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
     constexpr int kThreads = 64 * W, kRows = 32 * W;       // 32 rows per wavefront
-    constexpr int kStages = prompt_stages(32 * NT), kAhead = kStages == 4 ? 1 : 0;
+    constexpr int kStages = prompt_stages(32 * NT, DT == US_F32), kAhead = kStages == 4 ? 1 : 0;
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
+    // Float32 rows above 64: the queries' low parts wait in LDS, and scores are not taken
+    // ahead, so that two wavefronts fit a SIMD.
+    constexpr bool kLow = prompt_low(R, SPLIT), kEarly = !kLow;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Stage<R> *stage = (Stage<R> *)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -67,7 +72,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     int lo, hi;
     a.mask.range(i, n, len, lo, hi);
 
-    f16x8 qh[NS], ql[NS];
+    f16x8 qh[NS], ql[kLow ? 1 : NS];
+    f16x8 *low = (f16x8 *)(lds + kStages * sizeof(Stage<R>)) + wave * NS * 64 + lane;
     float f;
     {
         RowPart<DT, NS> raw;
@@ -89,7 +95,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
             raw.octet(t, 2 * t + h, a.D, a.D == R, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= norm;
-            halve<SPLIT>(x, qh[t], ql[t]);
+            halve<SPLIT>(x, qh[t], ql[kLow ? 0 : t]);
+            if constexpr (kLow) low[64 * t] = ql[0];       // (for this lane alone)
         }
     }
 
@@ -100,7 +107,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
             dst[64 * t] = qh[t];
-            if constexpr (SPLIT) dst[64 * t + R / 8 * 32] = ql[t];
+            if constexpr (SPLIT) dst[64 * t + R / 8 * 32] = kLow ? low[64 * t] : ql[kLow ? 0 : t];
         }
         if (h == 0) a.sp.qf[32 * rb + c] = f;
     }
@@ -184,15 +191,26 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
     auto scores = [&](int blk, f32x16 (&x)[2]) {
         const int buf = blk % kStages;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[y][v] = 0.0f;
+        const auto product = [&](int y, int t, f16x8 lo) {
+            const f16x8 kf = stage[buf].k[2 * t + h][32 * y + c];
+            x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[t], x[y], 0, 0, 0);
+            if constexpr (SPLIT) x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, lo, x[y], 0, 0, 0);
+        };
+        if constexpr (kLow) {
 #pragma unroll
             for (int t = 0; t < NS; ++t) {
-                const f16x8 kf = stage[buf].k[2 * t + h][32 * y + c];
-                x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[t], x[y], 0, 0, 0);
-                if constexpr (SPLIT) x[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[t], x[y], 0, 0, 0);
+                const f16x8 lo = low[64 * t];
+                product(0, t, lo);
+                product(1, t, lo);
             }
+        } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int t = 0; t < NS; ++t) product(y, t, ql[kLow ? 0 : t]);
         }
     };
     auto hide = [&](int i, float ks, f32x16 (&x)[2]) {     // the masked keys of block i
@@ -269,7 +287,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
         const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
         float sum = 0.0f;
         f16x8 ph[4], pl[4];
-        scores(i + 1, next);                               // (of no use after the last block)
+        if constexpr (kEarly) scores(i + 1, next);         // (of no use after the last block)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float p[8];
@@ -283,7 +301,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
         l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
         // (keeps the exponentials here, beside the scores' product)
         __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
-        if (i + 1 < count) hide(i + 1, ks[1], next);
+        if (kEarly && i + 1 < count) hide(i + 1, ks[1], next);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -292,6 +310,10 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
                 o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[j], o[t], 0, 0, 0);
                 if constexpr (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[j], o[t], 0, 0, 0);
             }
+        if constexpr (!kEarly) {
+            scores(i + 1, next);
+            if (i + 1 < count) hide(i + 1, ks[1], next);
+        }
         top = largest(next);
 #pragma unroll
         for (int z = 0; z < 2 + kAhead; ++z) ks[z] = ks[z + 1];
@@ -342,7 +364,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 || (NT > 2 && DT == US_F32) ? 1 : 2)
 // joining it alone, as in decode, took 400 us for 118 splits of 256 rows.)
 template <int NT, int DT>
 __global__ __launch_bounds__(256) void us_kv_join_kernel(Args a) {
-    constexpr int R = 32 * NT, kRows = 32 * prompt_waves(R, DT == US_F32), kEach = 256 / (R / 4);
+    constexpr int R = 32 * NT, kRows = 32 * prompt_waves(R), kEach = 256 / (R / 4);
     const int hk = blockIdx.y, b = blockIdx.z, quad = threadIdx.x % (R / 4);
     const int row = blockIdx.x * kEach + threadIdx.x / (R / 4);
     int r0, n;
@@ -562,8 +584,10 @@ hipError_t allow_lds(K kern, std::atomic<unsigned long long> &set) {
 hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream) {
     return with_row(a.D, [&](auto nt) {
         return with_type(dtype, [&](auto dt) {
-            constexpr int NT = decltype(nt)::value, kLds = prompt_stages(32 * NT) * (int)sizeof(Stage<32 * NT>);
-            constexpr int W = prompt_waves(32 * NT, decltype(dt)::value == US_F32);
+            constexpr int NT = decltype(nt)::value, R = 32 * NT;
+            constexpr bool f32 = decltype(dt)::value == US_F32;
+            constexpr int W = prompt_waves(R);
+            constexpr int kLds = prompt_stages(R, f32) * (int)sizeof(Stage<R>) + (prompt_low(R, f32) ? W * R / 16 * 64 * 16 : 0);
             auto kern = us_kv_prompt_kernel<NT, decltype(dt)::value, W>;
             if constexpr (kLds > 65536 - 1024) {
                 static std::atomic<unsigned long long> set{0};

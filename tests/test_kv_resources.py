@@ -57,7 +57,7 @@ def test_registers_leave_the_waves_that_the_kernels_count_on(kernels):
     for (w, t, *_), (vgpr, _) in _of(kernels, "us_kv_decode_kernel").items():
         assert vgpr <= (256 if w <= 4 else 512), (w, t)          # two wavefronts per SIMD, or one
     for (w, t, waves), (vgpr, _) in _of(kernels, "us_kv_prompt_kernel").items():
-        assert waves == (8 if w <= 4 and t != 0 else 4)
+        assert waves == (8 if w <= 4 else 4)
         assert vgpr <= (256 if waves == 8 else 512), (w, t)
 
 
