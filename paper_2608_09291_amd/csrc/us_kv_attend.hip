@@ -109,7 +109,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     if (units * p.splits > INT32_MAX / 512) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
-    p.part = p.decode && p.splits > 1 ? 4 * kTickets : 0;
+    p.part = parts || o.weights ? 4 * kTickets : 0;        // (also where this call draws none)
     p.lse = p.part + parts;
     // (one block past the last is read)
     p.row_blocks = (int64_t)tokens * (q_heads / c.heads) / 32 + s.batch + 2;

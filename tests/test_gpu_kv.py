@@ -390,6 +390,30 @@ def test_attend_nan_stays_in_its_row(torch_cuda, new):
         assert nan[bad].all() and not nan[~bad].any()
 
 
+@pytest.mark.parametrize("tracked", [False, True])
+def test_workspace_serves_calls_of_other_kinds(torch_cuda, tracked):
+    """One workspace for a prompt's call, decode calls that split and others that do not, in turn: as with fresh ones."""
+    torch = torch_cuda
+    announce(f"kv workspace shared weights={tracked}")
+    rng = np.random.default_rng(31)
+    lens, H, Hk, D = [6000, 900], 8, 2, 128
+    p = Pool(torch, rng, lens, Hk, D)
+    cache, blocks, n = p.cache(), p.dev(p.blocks), p.dev(lens)
+    kinds = [[400, 300], [1, 1], [3, 2], [200, 10], [2, 1]]
+    qs = [torch.from_numpy(rng.normal(0, 1, size=(sum(k), H, D)).astype(np.float32)).cuda().half() for k in kinds]
+    w0 = torch.zeros((2, Hk, p.width * 64), device="cuda") if tracked else None
+    args = [dict(starts=p.dev(_starts(k)), max_q=max(k)) for k in kinds]
+    size = max(kv.attend_workspace(cache, q, blocks, weights=w0, **a).numel() for q, a in zip(qs, args))
+    shared = torch.zeros(size, dtype=torch.int32, device="cuda")
+    for q, a, k in zip(qs, args, kinds):
+        got, want = torch.full_like(q, math.nan), torch.full_like(q, math.nan)
+        w1, w2 = (torch.zeros_like(w0), torch.zeros_like(w0)) if tracked else (None, None)
+        kv.attend(cache, blocks, n, q, got, weights=w1, ws=shared, **a)
+        kv.attend(cache, blocks, n, q, want, weights=w2, ws=kv.attend_workspace(cache, q, blocks, weights=w0, **a), **a)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and (not tracked or torch.equal(w1, w2)), k
+
+
 def test_attend_captured_on_another_stream(torch_cuda):
     """A decode step (append, then attend) captured in a graph, replayed over growing sequences between eager calls."""
     torch = torch_cuda
