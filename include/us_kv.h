@@ -136,7 +136,9 @@ typedef struct {
  * float32. A query with an infinity or a NaN gives a NaN row.
  * ws: us_kv_attend_workspace_size bytes, 16-byte aligned, zero-filled before
  * its first use and left so that any later call can use it again; calls that
- * may overlap need workspaces of their own. opts = NULL: causal, the rest 0.
+ * may overlap need workspaces of their own. The size for a call without a
+ * window (or without the causal mask) serves the same call with one.
+ * opts = NULL: causal, the rest 0.
  */
 us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                       int32_t tokens, const us_kv_attend_opts *opts, size_t *bytes);

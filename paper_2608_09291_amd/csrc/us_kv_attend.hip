@@ -151,6 +151,16 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     Plan p;
     st = plan_of(*cache, *seqs, q_heads, q->tokens, q->dtype == US_F32, o, p);
     if (st != US_OK) return st;
+    if (o.window && p.total && (!ws || ws_bytes < p.total)) {
+        // A workspace of the size for calls without a window (or with another one) serves as well: the
+        // plan for all keys is right for any part of them, if with other splits.
+        us_kv_attend_opts all = o;
+        all.window = 0;
+        Plan wide;
+        st = plan_of(*cache, *seqs, q_heads, q->tokens, q->dtype == US_F32, all, wide);
+        if (st != US_OK) return st;
+        p = wide;
+    }
     if (p.total && (!ws || (uintptr_t)ws % 16 || ws_bytes < p.total)) return US_ERR_ARG;
     uint8_t *w = (uint8_t *)ws;
     Args a;

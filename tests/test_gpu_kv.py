@@ -414,6 +414,26 @@ def test_workspace_serves_calls_of_other_kinds(torch_cuda, tracked):
         assert torch.equal(got, want) and (not tracked or torch.equal(w1, w2)), k
 
 
+@pytest.mark.parametrize("lens,new,H,Hk,D,dtype,how", [
+    ([41889, 15028, 20000, 30000, 16000], [1] * 5, 4, 1, 64, "f16", dict(window=30356)),
+    ([13249, 2162, 9000, 5000], [7, 3, 4, 5], 40, 8, 128, "f32", dict(window=1549)),
+    ([2580, 1335], [1, 1], 256, 32, 64, "f16", dict(window=1575)),
+    ([300], [150], 2, 1, 64, "bf16", dict(causal=False))])
+def test_workspace_without_the_mask_serves_calls_with_it(torch_cuda, lens, new, H, Hk, D, dtype, how):
+    torch = torch_cuda
+    announce(f"kv workspace of a call without a window: lens={lens} new={new} H={H}/{Hk} D={D} {dtype} {how}")
+    rng = np.random.default_rng(len(lens) + D)
+    p = Pool(torch, rng, lens, Hk, D)
+    cache, blocks = p.cache(), p.dev(p.blocks)
+    q = torch.from_numpy(rng.normal(0, 1, size=(sum(new), H, D)).astype(np.float32)).cuda().to(_torch_dtype(torch, dtype))
+    out = torch.full_like(q, math.nan)
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new))
+    ws = kv.attend_workspace(cache, q, blocks, **args)
+    kv.attend(cache, blocks, p.dev(lens), q, out, ws=ws, **args, **how)
+    torch.cuda.synchronize()
+    _check(torch, p, lens, new, q, out, dtype, **how)
+
+
 def test_attend_captured_on_another_stream(torch_cuda):
     """A decode step (append, then attend) captured in a graph, replayed over growing sequences between eager calls."""
     torch = torch_cuda
