@@ -178,10 +178,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         }
     };
 
-    // o is in units of vmax, the largest value scale so far: a block's
-    // probabilities go to the second product times ratio = its scale / vmax,
-    // which the exponent takes, so that the product adds up in place.
-    float m = -INFINITY, l = 0.0f, vmax = 0.0f;
+    // A block's value scale goes into its exponents, so that the second product
+    // adds up in place: o is in units of 2^mo, mo the largest score plus log2 of
+    // its block's value scale that this row has seen. Neither a block that is
+    // masked for the row nor one of large values and no weight moves it.
+    float m = -INFINITY, l = 0.0f, mo = -INFINITY;
     f32x16 o[NT], sa[2], sb[2];                            // scores of a block and of the next one, in turn
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -262,19 +263,21 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
     }
     auto step = [&](int i, auto odd, f32x16 (&s)[2], f32x16 (&next)[2]) {
         // (above 0, so that a masked key's -inf stays one)
-        const float v_scale = vs[0], fk = fmaxf(f * fabsf(ks[0]), 1.17549435e-38f);
-        // The maximum may lag behind by 2^kSlack before sums are brought to a new one.
-        const float m2 = fmaxf(m, top * fk);
-        float change = 1.0f;
-        if (v_scale > vmax) {
-            change = vmax * __builtin_amdgcn_rcpf(v_scale);
-            vmax = v_scale;
-        }
-        if (m2 > m + kSlack || m == -INFINITY) {
-            const float alpha = __builtin_amdgcn_exp2f(m - base_of(m2));
+        const float fk = fmaxf(f * fabsf(ks[0]), 1.17549435e-38f);
+        // (-200: of a scale of 0, whose values count for nothing)
+        const float lv = fmaxf(__builtin_amdgcn_logf(vs[0]), -200.0f);
+        // The maxima may lag behind by 2^kSlack before sums are brought to new ones.
+        const float t1 = top * fk, t2 = t1 + lv;
+        if (t1 > m + kSlack || m == -INFINITY) {
+            const float m2 = fmaxf(m, t1);
+            l *= __builtin_amdgcn_exp2f(m - base_of(m2));
             m = m2;
-            l *= alpha;
-            change *= alpha;
+        }
+        float change = 1.0f;
+        if (t2 > mo + kSlack || mo == -INFINITY) {
+            const float m2 = fmaxf(mo, t2);
+            change = __builtin_amdgcn_exp2f(mo - base_of(m2));
+            mo = m2;
         }
         if (__builtin_amdgcn_ballot_w64(change != 1.0f)) {
 #pragma unroll
@@ -282,9 +285,8 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[t][v] *= change;
         }
-        // (2^-60: below what any sum keeps; 1 as long as all scales are 0, where o does not count)
-        const float ratio = vmax > 0.0f ? fmaxf(v_scale * __builtin_amdgcn_rcpf(vmax), 8.67361738e-19f) : 1.0f;
-        const float sub = base_of(m) - kLift - __builtin_amdgcn_logf(ratio);
+        // (60: values of less than 2^-60 of what o holds are lost in it, weights are not)
+        const float bm = base_of(m), unit = fminf(base_of(mo) - lv, bm + 60.0f), sub = unit - kLift;
         float sum = 0.0f;
         f16x8 ph[4], pl[4];
         if constexpr (kEarly) scores(i + 1, next);         // (of no use after the last block)
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
             }
             halve<SPLIT>(p, ph[j], pl[j]);
         }
-        l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
+        l = fmaf(sum, __builtin_amdgcn_exp2f(unit - bm), l);
         // (keeps the exponentials here, beside the scores' product)
         __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
         if (kEarly && i + 1 < count) hide(i + 1, ks[1], next);
@@ -331,10 +333,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         if (i + 1 < count) step(i + 1, std::integral_constant<int, 1>(), sb, sa);
     }
     l += __shfl_xor(l, 32, 64);
+    const float to_m = __builtin_amdgcn_exp2f(mo - base_of(m));
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[t][v] *= vmax;
+        for (int v = 0; v < 16; ++v) o[t][v] *= to_m;
 
     // Lane (c, h), element 4 z + v of o[t]: value 32 t + 8 z + 4 h + v of row c.
     if (!real) return;

@@ -367,6 +367,44 @@ def test_attend_large_and_small_scores(torch_cuda, new):
         assert (np.abs(out.double().cpu().numpy() - want) <= bound).all(), dtype
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("where", ["masked", "unseen", "first"])
+def test_attend_values_of_other_rows_and_blocks_do_not_matter(torch_cuda, where, D):
+    """A block of values 2^70 times the others': masked for the rows before it, or with scores that leave it no weight."""
+    torch = torch_cuda
+    announce(f"kv attend a block of huge values, {where}, D={D}")
+    rng = np.random.default_rng(15)
+    # (so many heads that the kernel for prompts takes it; two of them are looked at)
+    lens, new, Hk = [460], [330], 64
+    p = Pool(torch, rng, lens, Hk, D)
+    huge = {"masked": 4, "unseen": 3, "first": 0}[where]
+    p.scales[1][p.blocks[0][huge]] *= np.float32(2.0 ** 70)
+    if where != "masked":
+        # keys of one sign: -127 in the block of huge values, above 0 elsewhere
+        for j, blk in enumerate(p.blocks[0]):
+            c = p.codes[0][blk].astype(np.int32) - 128
+            p.codes[0][blk] = 1 if j == huge else (129 + np.minimum(np.abs(c), 60)).astype(np.uint8)
+    cache = p.cache()
+    base = rng.normal(0, 1, size=(new[0], 2 * Hk, D)) if where == "masked" else rng.uniform(6, 8, size=(new[0], 2 * Hk, D))
+    for dtype in DTYPES:
+        q = torch.from_numpy(base.astype(np.float32)).cuda().to(_torch_dtype(torch, dtype))
+        out = torch.full_like(q, math.nan)
+        args = dict(starts=p.dev(_starts(new)), max_q=new[0])
+        ws = kv.attend_workspace(cache, q, p.dev(p.blocks), **args)
+        kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, out, ws=ws, **args)
+        torch.cuda.synchronize()
+        rows = slice(0, 256 - 130) if where == "masked" else slice(None)       # those that see none of the block
+        for h in (0, Hk - 1):
+            of = [x[:, h:h + 1] for x in (p.codes[0], p.scales[0], p.codes[1], p.scales[1])]
+            want, size, _, reach = ref.attend(*of, D, p.blocks, lens, _starts(new), q[:, 2 * h:2 * h + 2].double().cpu().numpy())
+            e_s = (ref.row_of(D) + 8) * 2.0 ** -24 * reach[..., None] + (2.0 ** -22 * reach[..., None] if dtype == "f32" else 0)
+            e_p = 2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11)
+            assert np.abs(want[rows]).max() < 1e3              # the block has no weight in them
+            bound = (e_p + 460 * 2.0 ** -24) * size + OUT[dtype] * np.abs(want) + 2.0 ** -25
+            got = out[:, 2 * h:2 * h + 2].double().cpu().numpy()
+            assert (np.abs(got - want) <= bound)[rows].all(), (dtype, h)
+
+
 @pytest.mark.parametrize("new", [1, 70])
 def test_attend_nan_stays_in_its_row(torch_cuda, new):
     torch = torch_cuda
