@@ -292,6 +292,75 @@ def test_attend(torch_cuda, lens, new, H, Hk, D, how, tracked, dtype):
     assert torch.equal(first[0], out) and (w1 is None or torch.equal(first[1], w1))   # bit for bit
 
 
+PROMPTS = [  # as ATTEND, with rows and heads that the kernel for prompts takes; whether rows lie at odd places
+    ([330, 200, 77, 0], [330, 140, 60, 0], 96, 96, 96, {}, True),
+    ([700, 100], [500, 100], 96, 48, 80, dict(window=90), False),
+    ([400, 300], [200, 300], 120, 24, 128, {}, True),
+    ([333, 200], [250, 170], 64, 32, 192, {}, False),
+    ([300, 250], [300, 250], 48, 24, 256, dict(causal=False), True),
+    ([4000], [700], 64, 8, 128, dict(causal=False), False),
+    ([6000], [500], 64, 8, 64, {}, False),                  # split
+    ([5000, 4000], [260, 300], 64, 4, 256, {}, False),      # split
+    ([4100], [600], 64, 4, 96, dict(window=3000), True),
+    ([100], [2000], 64, 32, 128, {}, False),                # most rows are before the first key
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hk,D,how,odd", PROMPTS)
+def test_attend_prompts(torch_cuda, lens, new, H, Hk, D, how, odd, tracked, dtype):
+    """Two cache heads of every call against float64 on the GPU, within the bounds above."""
+    torch = torch_cuda
+    announce(f"kv attend prompts lens={lens} new={new} H={H}/{Hk} D={D} {how} odd={odd} {dtype} weights={tracked}")
+    rng = np.random.default_rng(sum(lens) + H + D)
+    p = Pool(torch, rng, lens, Hk, D)
+    cache, T, G, R = p.cache(), sum(new), H // Hk, ref.row_of(D)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(sum(lens) + D)
+    wide = (torch.randn((T, H, D + 3 if odd else D), generator=gen, device="cuda") * 1.5).to(_torch_dtype(torch, dtype))
+    q = wide[:, :, 1:D + 1] if odd else wide
+    out = torch.full((T, H, D), math.nan, dtype=q.dtype, device="cuda")
+    w0 = torch.rand((len(lens), Hk, p.width * 64), generator=gen, device="cuda") if tracked else None
+    w1 = None if w0 is None else w0.clone()
+    st = _starts(new)
+    args = dict(starts=p.dev(st), max_q=max(new), weights=w1, **how)
+    ws = kv.attend_workspace(cache, q, p.dev(p.blocks), **args)
+    kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, out, ws=ws, **args)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    for b, n in enumerate(lens):
+        if w0 is not None:
+            assert torch.equal(w0[b, :, n:], w1[b, :, n:])
+        if n == 0 or new[b] == 0:
+            continue
+        rows = slice(st[b], st[b + 1])
+        lo, hi = (torch.tensor(x, device="cuda")[:, None] for x in zip(*[
+            ref.visible(i, new[b], n, how.get("causal", True), how.get("window", 0)) for i in range(new[b])]))
+        j = torch.arange(n, device="cuda")
+        seen = ((j >= lo) & (j < hi)).repeat_interleave(G, dim=0)
+        for hk in (0, Hk - 1):
+            (kc, ks), (vc, vs) = [[torch.from_numpy(x).cuda() for x in ref.tokens(p.codes[i], p.scales[i], D, i == 0, p.blocks[b], n, hk)]
+                                  for i in range(2)]
+            key, val = kc * ks[:, None], vc * vs[:, None]
+            x = q[rows, hk * G:hk * G + G].double().reshape(-1, D)
+            scores = (x @ key.t().contiguous()) / math.sqrt(D)
+            reach = ((x.abs() @ key.abs().t().contiguous()) / math.sqrt(D)).masked_fill(~seen, 0).amax(1, keepdim=True)
+            scores = scores.masked_fill(~seen, -math.inf)
+            prob = torch.softmax(scores, dim=1).masked_fill(~seen, 0)           # (zeros for a row without keys)
+            want, size = prob @ val, prob @ val.abs()
+            e_s = (R + 8) * 2.0 ** -24 * reach + (2.0 ** -22 * reach if dtype == "f32" else 0)
+            e_p = 2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11)
+            bound = (e_p + n * 2.0 ** -24) * size + OUT[dtype] * want.abs() + (2.0 ** -25 if dtype == "f16" else 1e-30)
+            got = out[rows, hk * G:hk * G + G].double().reshape(-1, D)
+            assert ((got - want).abs() <= bound).all(), (b, hk, ((got - want).abs() - bound).max())
+            if w0 is not None:
+                add = prob.sum(0)
+                e_w = 2 * (R + 8) * 2.0 ** -24 * reach.max() + 2.0 ** -20 + (new[b] * G + n) * 2.0 ** -24
+                a, z = w0[b, hk, :n].double(), w1[b, hk, :n].double()
+                assert ((z - a - add).abs() <= e_w * add + 2.0 ** -23 * z.abs()).all(), (b, hk)
+
+
 def test_attend_aligned_rows_and_scale(torch_cuda):
     torch = torch_cuda
     announce("kv attend aligned rows, own scale")
