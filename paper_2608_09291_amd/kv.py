@@ -2,12 +2,14 @@
 
 Argument marshalling and the checks that only the tensors can answer (types,
 shapes, strides); every computation happens in the native library. A decode
-step's calls take the GPU a few microseconds, so each tensor is asked for each
-of its properties once, and the structs are packed without ctypes objects.
+step's calls take the GPU a few microseconds, so tensors are looked at in
+compiled code (csrc/python), one call for each argument, and the structs are
+packed without ctypes objects.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib
 import struct
 
 import torch
@@ -50,14 +52,18 @@ class KeptStruct(ctypes.Structure):
                 ("index", ctypes.c_void_p)]
 
 
-_ready = None
+_ready = _args = None
 
 
 def lib():
-    """The native library with the signatures of us_kv.h; raises if it was not built."""
-    global _ready
+    """The native library with the signatures of us_kv.h; raises if it (or the tensors' checks) was not built."""
+    global _ready, _args
     if _ready is None:
         L = binding.lib()
+        try:
+            _args = importlib.import_module("._kv_args", __package__)
+        except ModuleNotFoundError as e:
+            raise RuntimeError("_kv_args.so is missing: run `python -m paper_2608_09291_amd.build_args`") from e
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         # (structs go as void pointers: byref() of the classes above, or their packed bytes)
         L.us_kv_row.argtypes = [i32]
@@ -79,8 +85,7 @@ _pack_rows = struct.Struct("@Pqqii").pack
 _pack_opts = struct.Struct("@fiii Pq").pack
 _pack_kept = struct.Struct("@Pqi4xPPqP").pack
 
-_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_I32, _F32 = torch.int32, torch.float32
 _ROWS = {}      # us_kv_row by head_dim
 
 
@@ -106,16 +111,14 @@ class Cache:
     """A pool of blocks: uint8 codes (n_blocks, heads, BLOCK * row(head_dim)) and float32 scales (n_blocks, heads)."""
 
     def __init__(self, k, v, k_scale, v_scale, head_dim: int):
-        n, heads, size = k.shape
-        if size != BLOCK * row(head_dim) or v.shape != k.shape or not (
-                k.dtype is v.dtype is _U8 and k.is_contiguous() and v.is_contiguous()):
-            raise TypeError(f"codes: contiguous uint8 tensors (blocks, heads, {BLOCK * row(head_dim)}) are wanted")
-        if k_scale.shape != (n, heads) or v_scale.shape != (n, heads) or not (
-                k_scale.dtype is v_scale.dtype is _F32 and k_scale.is_contiguous() and v_scale.is_contiguous()):
-            raise TypeError(f"scales: contiguous float32 tensors of shape {(n, heads)} are wanted")
+        size = BLOCK * row(head_dim)
+        ak, av, aks, avs, n, heads, bytes_, cuda = _args.cache(k, v, k_scale, v_scale)
+        if bytes_ != size:
+            raise TypeError(f"codes: contiguous uint8 tensors (blocks, heads, {size}) are wanted")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_blocks, self.heads, self.head_dim = n, heads, head_dim
-        self._packed = _pack_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n, heads, head_dim)
+        self._packed = _pack_cache(ak, av, aks, avs, n, heads, head_dim)
+        self._there = self._packed if cuda else None       # what calls are given: they refuse None
 
     def struct(self) -> CacheStruct:
         return CacheStruct.from_buffer_copy(self._packed)
@@ -124,7 +127,7 @@ class Cache:
 def new_cache(n_blocks: int, heads: int, head_dim: int, device="cuda") -> Cache:
     """An empty pool of n_blocks blocks per head."""
     shape = (n_blocks, heads, BLOCK * row(head_dim))
-    codes = [torch.full(shape, 128, dtype=_U8, device=device) for _ in range(2)]
+    codes = [torch.full(shape, 128, dtype=torch.uint8, device=device) for _ in range(2)]
     scales = [torch.zeros(shape[:2], dtype=_F32, device=device) for _ in range(2)]
     return Cache(*codes, *scales, head_dim)
 
@@ -145,18 +148,12 @@ def _numbers(t, n, name):
 
 
 def _seqs(blocks, lens, starts, max_new) -> bytes:
-    batch, width, stride = _table(blocks, "blocks")
-    return _pack_seqs(blocks.data_ptr(), stride, width, batch, _numbers(lens, batch, "lens"),
-                      0 if starts is None else _numbers(starts, batch + 1, "starts"), max_new)
+    at, stride, width, batch, at_lens, at_starts = _args.seqs(blocks, lens, starts)
+    return _pack_seqs(at, stride, width, batch, at_lens, at_starts, max_new)
 
 
 def _rows(t, heads, head_dim, name) -> bytes:
-    tokens, h, d = t.shape
-    st, sh, one = t.stride()
-    dtype = _DTYPES.get(t.dtype)
-    if h != heads or d != head_dim or (one != 1 and d > 1) or dtype is None:
-        raise TypeError(f"{name}: (tokens, {heads}, {head_dim}) float32, bfloat16 or float16 with contiguous values is wanted")
-    return _pack_rows(t.data_ptr(), st, sh, tokens, dtype)
+    return _pack_rows(*_args.rows(t, heads, head_dim, name))
 
 
 def _weights(t, batch, heads, name):
@@ -164,20 +161,22 @@ def _weights(t, batch, heads, name):
     b, h, n = t.shape
     if b != batch or h != heads or t.dtype is not _F32 or not t.is_contiguous():
         raise TypeError(f"{name}: a contiguous float32 tensor ({batch}, {heads}, tokens) is wanted")
+    if not t.is_cuda:
+        raise TypeError(f"{name}: a tensor on the GPU is wanted")
     return t.data_ptr(), n
 
 
 def append(cache: Cache, blocks, lens, k, v, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_append: quantise the sequences' last tokens (rows of k and v) into their blocks."""
     h, d = cache.heads, cache.head_dim
-    _check("us_kv_append", lib().us_kv_append(cache._packed, _seqs(blocks, lens, starts, max_new), _rows(k, h, d, "k"),
+    _check("us_kv_append", lib().us_kv_append(cache._there, _seqs(blocks, lens, starts, max_new), _rows(k, h, d, "k"),
                                               _rows(v, h, d, "v"), _stream(stream)))
 
 
 def read(cache: Cache, blocks, lens, k_out, v_out, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_read: the sequences' last tokens as dense rows."""
     h, d = cache.heads, cache.head_dim
-    _check("us_kv_read", lib().us_kv_read(cache._packed, _seqs(blocks, lens, starts, max_new),
+    _check("us_kv_read", lib().us_kv_read(cache._there, _seqs(blocks, lens, starts, max_new),
                                           _rows(k_out, h, d, "k_out"), _rows(v_out, h, d, "v_out"), _stream(stream)))
 
 
@@ -216,8 +215,10 @@ def attend(cache: Cache, blocks, lens, q, out, starts=None, max_q: int = 1, max_
            causal: bool = True, window: int = 0, weights=None, ws=None, stream=None) -> None:
     """us_kv_attend: out = softmax(scale q k) v over the cache; weights (if given) gain each token's probabilities."""
     heads, d = q.shape[1], cache.head_dim
+    if ws is not None and not (ws.is_cuda and ws.is_contiguous()):
+        raise TypeError("ws: a contiguous tensor on the GPU is wanted")
     _check("us_kv_attend", lib().us_kv_attend(
-        cache._packed, _seqs(blocks, lens, starts, max_q), heads, _rows(q, heads, d, "q"), _rows(out, heads, d, "out"),
+        cache._there, _seqs(blocks, lens, starts, max_q), heads, _rows(q, heads, d, "q"), _rows(out, heads, d, "out"),
         _opts(scale, causal, window, max_len, weights, blocks.shape[0], cache.heads),
         0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes, _stream(stream)))
 
@@ -233,6 +234,8 @@ def evict(cache: Cache, blocks, lens, weights, keep: int, recent: int, to_blocks
         raise ValueError("to_blocks: one row per sequence is wanted")
     if index.dtype is not _I32 or index.shape != (batch, heads, keep) or not index.is_contiguous():
         raise TypeError(f"index: a contiguous int32 tensor {(batch, heads, keep)} is wanted")
+    if not (to_blocks.is_cuda and to_lens.is_cuda and index.is_cuda):
+        raise TypeError("to_blocks, to_lens, index: tensors on the GPU are wanted")
     to = _pack_kept(to_blocks.data_ptr(), stride, width, _numbers(to_lens, batch, "to_lens"), ow, ow_stride, index.data_ptr())
-    _check("us_kv_evict", lib().us_kv_evict(cache._packed, _seqs(blocks, lens, None, 1), w, w_stride, max_len or 0, keep,
+    _check("us_kv_evict", lib().us_kv_evict(cache._there, _seqs(blocks, lens, None, 1), w, w_stride, max_len or 0, keep,
                                             recent, to, _stream(stream)))

@@ -167,6 +167,31 @@ def test_append_of_extremes(torch_cuda, case):
         assert np.array_equal(codes[blk, 0].cpu().numpy()[at], p.codes[i][blk, 0][at])
 
 
+def test_binding_refuses_tensors_on_the_gpu(torch_cuda):
+    """As on the host, where nothing is launched: types, shapes and strides, and a mixture of places."""
+    torch = torch_cuda
+    announce("kv binding refusals")
+    c = kv.new_cache(4, 2, 80)
+    blocks, lens = torch.zeros((3, 2), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    x = torch.zeros((3, 2, 80), device="cuda")
+    good = dict(blocks=blocks, lens=lens, k=x, v=x)
+    for bad in (dict(blocks=blocks.long()), dict(blocks=blocks[0]), dict(blocks=blocks.t()), dict(blocks=blocks.cpu()),
+                dict(lens=lens[:2]), dict(lens=lens.float()), dict(lens=lens.cpu()), dict(lens=None), dict(k=x.double()),
+                dict(k=x[:, :1]), dict(k=x[..., :79]), dict(k=x.cpu()), dict(k=x[0]), dict(v=3), dict(starts=lens),
+                dict(starts=lens.long()), dict(starts=torch.zeros(4, dtype=torch.int32)),
+                dict(k=torch.zeros((3, 2, 160), device="cuda")[..., ::2])):
+        with pytest.raises(TypeError):
+            kv.append(c, **{**good, **bad})
+    host = kv.new_cache(4, 2, 80, device="cpu")
+    with pytest.raises(binding.UsError):
+        kv.append(host, **good)
+    with pytest.raises(TypeError):
+        kv.attend(c, blocks, lens, x, x, ws=torch.zeros(1 << 20, dtype=torch.int32))
+    kv.append(c, **good)                                    # (lengths of 0: nothing is stored)
+    torch.cuda.synchronize()
+    assert (c.k == 128).all() and (c.k_scale == 0).all()
+
+
 def test_tables_out_of_range_are_left_alone(torch_cuda):
     """Blocks that are not in the pool, lengths past the table, rows past the arrays: nothing outside is touched."""
     torch = torch_cuda

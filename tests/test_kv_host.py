@@ -152,6 +152,31 @@ def test_binding_refuses_tensors():
         kv.Cache(c.k, c.v, c.k_scale, c.v_scale, 128).struct()
 
 
+def test_binding_refuses_host_tensors():
+    """Nothing on the host gets as far as a launch."""
+    torch = pytest.importorskip("torch")
+    c = kv.new_cache(4, 2, 80, device="cpu")
+    blocks, lens = torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    x, w = torch.zeros((3, 2, 80)), torch.zeros((3, 2, 128))
+    for call in (lambda: kv.append(c, blocks, lens, x, x), lambda: kv.read(c, blocks, lens, x, x),
+                 lambda: kv.attend(c, blocks, lens, x, x), lambda: kv.attend(c, blocks, lens, x, x, weights=w),
+                 lambda: kv.attend(c, blocks, lens, x, x, ws=w),
+                 lambda: kv.evict(c, blocks, lens, w, 64, 1, blocks, lens, None, torch.zeros((3, 2, 64), dtype=torch.int32)),
+                 lambda: kv.append(c, blocks, None, x, x), lambda: kv.append(c, blocks, lens, x, 3)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(TypeError):
+        kv.Cache(c.k, c.v[:3], c.k_scale, c.v_scale, 80)
+    with pytest.raises(TypeError):
+        kv.Cache(c.k, c.v.transpose(0, 1), c.k_scale, c.v_scale, 80)
+    with pytest.raises(TypeError):
+        kv.Cache(c.k, c.v, c.k_scale, c.v_scale.half(), 80)
+    # a cache on the host is refused by the library
+    assert c._there is None
+    _, s, r, _ = _valid()
+    assert kv.lib().us_kv_read(c._there, ctypes.byref(s), ctypes.byref(r), ctypes.byref(r), None) == ARG
+
+
 # --- the oracle against hand-worked cases --------------------------------------
 
 def test_oracle_append_by_hand():
