@@ -145,26 +145,124 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
 // with one block of keys per workgroup the waits took most of the time. A key's
 // octets are copied from where they are. Values lie across their block, so that
 // any token of it touches all its lines: every block that has one passes
-// through LDS whole. 16 sequences of 9000-16384 tokens to 4096, 8 heads of 128:
-// 120-135 us, the values alone 105 (340 MB, 69 us at the card's copy rate); what
-// bounds them is the wait for one source block after the other.
+// through LDS whole. A wavefront does that for its quarter of the values alone,
+// four source blocks on their way and no barrier (with the workgroup together,
+// one block ahead: 4 sequences of 700-1100 tokens to 512, 8 heads of 128, 30 us
+// for the whole call and its read, 24 so; 16 of 9000-16384 to 4096 230 and 227,
+// where the 340 MB that the values' lines make bound it).
+// What a wavefront's lanes have stored to LDS, its other lanes find after this.
+__device__ inline void in_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 constexpr int kPer = kMoveThreads / kBlock;                // most new blocks of a workgroup
 template <int NT>
 __global__ __launch_bounds__(kMoveThreads) void us_kv_move_kernel(uint8_t *kp, uint8_t *vp, float *ksp, float *vsp, Seqs s,
                                                                   const int32_t *index, int keep, const int32_t *to,
                                                                   int64_t to_stride, int to_width, int blocks, int key_blocks) {
     constexpr int R = 32 * NT, kOct = R / 8, kPitch = kBlock + 4;
-    constexpr int kPieces = (4 * R + kMoveThreads - 1) / kMoveThreads;
     __shared__ int token[kMoveThreads], from[kMoveThreads], dst[kPer];         // place in its block; block, -1: none
     __shared__ float ratio[kMoveThreads];
     __shared__ __attribute__((aligned(16))) uint8_t in[R * kPitch], out[R * kPitch];
-    // Values first: a block each, as they take longest.
-    const bool values = (int)blockIdx.x < blocks;
-    const int per = values ? 1 : key_blocks, j0 = values ? blockIdx.x : (blockIdx.x - blocks) * per, h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
+    __shared__ __attribute__((aligned(16))) uint32_t place[kMoveThreads / 64][kBlock];
+    __shared__ __attribute__((aligned(16))) float part[kMoveThreads / 64][kBlock];
+    const int h = blockIdx.y, b = blockIdx.z, heads = gridDim.y, tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = min(min(min(s.len(b), keep), to_width * kBlock) - j0 * kBlock, per * kBlock);
+    const int total = min(min(s.len(b), keep), to_width * kBlock);
+    auto page = [&](int block) { return ((int64_t)block * heads + h) * (kBlock * R); };
+    // Values first: a block each, as they take longest.
+    if ((int)blockIdx.x < blocks) {
+        const int j = blockIdx.x, n = min(total - j * kBlock, kBlock);
+        if (n <= 0) return;
+        // Every wavefront for itself: a lane per token, then the rows of R / 4 values.
+        const int p = lane < n ? index[((int64_t)b * heads + h) * keep + j * kBlock + lane] : -1;
+        const int from = p >= 0 ? s.block(b, p / kBlock) : -1, into = s.valid(to[b * to_stride + j]);
+        const float s1 = from >= 0 ? vsp[(int64_t)from * heads + h] : 0.0f;    // (not waited for yet)
+        place[wave][lane] = value_place(p & (kBlock - 1));
+        const int before = __shfl_up(from, 1, 64);
+        const uint64_t runs = __builtin_amdgcn_ballot_w64(lane == 0 || from != before);    // first tokens of runs of one source
+        constexpr int kOwn = R / 4, kPieces = (4 * kOwn + 63) / 64, kStages = 4, kQuads = 64 / kOwn;
+        u32x4 piece[kStages][kPieces];
+        uint64_t ahead = runs, left = runs;
+        auto fetch = [&](u32x4 (&w)[kPieces]) {            // of the next run, if there is one
+            if (!ahead) return;
+            const int block = __builtin_amdgcn_readlane(from, __builtin_ctzll(ahead));
+            ahead &= ahead - 1;
+            if (block < 0) return;
+            const u32x4 *src = (const u32x4 *)(vp + page(block)) + 4 * kOwn * wave;
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x)
+                if (4 * kOwn % 64 == 0 || lane + 64 * x < 4 * kOwn) w[x] = src[lane + 64 * x];
+        };
+#pragma unroll
+        for (int z = 0; z < kStages; ++z) fetch(piece[z]);
+        float s2 = s1;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) s2 = fmaxf(s2, __shfl_xor(s2, o, 64));
+        // (a token without a block, or past the last: 0, which makes any byte a code of 0)
+        part[wave][lane] = s2 > 0.0f ? s1 / s2 : 0.0f;
+        if (into < 0) return;
+        if (tid == 0) vsp[(int64_t)into * heads + h] = s2;
+        uint8_t *mine_in = in + kOwn * kPitch * wave, *mine_out = out + kOwn * kPitch * wave;
+        const int d = lane % kOwn, first = lane / kOwn;    // this lane's row, and which of kQuads quads at a time
+        auto move = [&](const u32x4 (&w)[kPieces]) {
+            const int t = __builtin_ctzll(left);
+            left &= left - 1;
+            const int end = left ? __builtin_ctzll(left) : kBlock;
+            in_order();
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x) {
+                const int i = lane + 64 * x;
+                if (4 * kOwn % 64 == 0 || i < 4 * kOwn) {
+                    uint32_t *q = (uint32_t *)(mine_in + (i >> 2) * kPitch + 16 * (i & 3));
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) q[z] = w[x][z];
+                }
+            }
+            in_order();
+            if (first >= kQuads) return;
+            for (int quad = (t >> 2) + first; 4 * quad < end; quad += kQuads) {
+                const u32x4 at = *(const u32x4 *)&place[wave][4 * quad];
+                const float4 r = *(const float4 *)&part[wave][4 * quad];
+                const float rv[4] = {r.x, r.y, r.z, r.w};
+                uint8_t *q = mine_out + d * kPitch + value_place(4 * quad);
+                uint32_t word = 0;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) word |= rescaled(mine_in[d * kPitch + at[v]], rv[v]) << (8 * v);
+                if (4 * quad >= t && 4 * quad + 4 <= end) {
+                    *(uint32_t *)q = word;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (4 * quad + v >= t && 4 * quad + v < end) q[v] = (uint8_t)(word >> (8 * v));
+                }
+            }
+        };
+        while (left) {
+#pragma unroll
+            for (int z = 0; z < kStages; ++z)
+                if (left) {
+                    move(piece[z]);
+                    fetch(piece[z]);
+                }
+        }
+        in_order();
+        u32x4 *dst = (u32x4 *)(vp + page(into)) + 4 * kOwn * wave;
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+            const int i = lane + 64 * x;
+            if (4 * kOwn % 64 == 0 || i < 4 * kOwn) {
+                const uint32_t *q = (const uint32_t *)(mine_out + (i >> 2) * kPitch + 16 * (i & 3));
+                dst[i] = (u32x4){q[0], q[1], q[2], q[3]};
+            }
+        }
+        return;
+    }
+    const int per = key_blocks, j0 = ((int)blockIdx.x - blocks) * per, n = min(total - j0 * kBlock, per * kBlock);
     if (n <= 0) return;
-    float *scales = values ? vsp : ksp;
+    float *scales = ksp;
     float s1 = 0.0f;
     if (tid < per * kBlock) {                              // a wavefront per new block
         const int p = tid < n ? index[((int64_t)b * heads + h) * keep + j0 * kBlock + tid] : -1;
@@ -185,120 +283,36 @@ __global__ __launch_bounds__(kMoveThreads) void us_kv_move_kernel(uint8_t *kp, u
         }
         __syncthreads();
     };
-    auto page = [&](int block) { return ((int64_t)block * heads + h) * (kBlock * R); };
-    if (!values) {
-        u32x2 wa[NT], wb[NT];
-        auto fetch = [&](int j, u32x2 (&w)[NT]) {
+    u32x2 wa[NT], wb[NT];
+    auto fetch = [&](int j, u32x2 (&w)[NT]) {
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                const int i = tid + kMoveThreads * x, t = j * kBlock + i / kOct, o = i % kOct;
-                w[x] = (u32x2){0x80808080u, 0x80808080u};
-                if (t < n && from[t] >= 0) w[x] = *(const u32x2 *)(kp + page(from[t]) + key_octet(token[t], o));
-            }
-        };
-        auto put = [&](int j, const u32x2 (&w)[NT]) {
-            if (dst[j] < 0) return;
-#pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
-                const float r = ratio[j * kBlock + t];
-                u32x2 q = {0, 0};
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    q[e >> 2] |= rescaled((w[x][e >> 2] >> (8 * (e & 3))) & 255u, r) << (8 * (e & 3));
-                *(u32x2 *)(kp + page(dst[j]) + key_octet(t, o)) = q;
-            }
-        };
-        const int blocks = (n + kBlock - 1) / kBlock;
-        fetch(0, wa);
-        set_ratios();
-        for (int j = 0; j < blocks; j += 2) {
-            if (j + 1 < blocks) fetch(j + 1, wb);
-            put(j, wa);
-            if (j + 2 < blocks) fetch(j + 2, wa);
-            if (j + 1 < blocks) put(j + 1, wb);
-        }
-        return;
-    }
-    // Runs of tokens with one source and one new block. (All of this is uniform: the tables are shared.)
-    auto end_of = [&](int t) {
-        int e = t + 1;
-        while (e < n && e % kBlock != 0 && from[e] == from[t]) ++e;
-        return e;
-    };
-    u32x4 piece[kPieces];
-    auto fetch = [&](int block) {
-#pragma unroll
-        for (int x = 0; x < kPieces; ++x) {
-            const int i = tid + kMoveThreads * x;
-            if (4 * R % kMoveThreads == 0 || i < 4 * R) piece[x] = *(const u32x4 *)(vp + page(block) + 16 * i);
+        for (int x = 0; x < NT; ++x) {
+            const int i = tid + kMoveThreads * x, t = j * kBlock + i / kOct, o = i % kOct;
+            w[x] = (u32x2){0x80808080u, 0x80808080u};
+            if (t < n && from[t] >= 0) w[x] = *(const u32x2 *)(kp + page(from[t]) + key_octet(token[t], o));
         }
     };
-    if (from[0] >= 0) fetch(from[0]);
+    auto put = [&](int j, const u32x2 (&w)[NT]) {
+        if (dst[j] < 0) return;
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int i = tid + kMoveThreads * x, t = i / kOct, o = i % kOct;
+            const float r = ratio[j * kBlock + t];
+            u32x2 q = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                q[e >> 2] |= rescaled((w[x][e >> 2] >> (8 * (e & 3))) & 255u, r) << (8 * (e & 3));
+            *(u32x2 *)(kp + page(dst[j]) + key_octet(t, o)) = q;
+        }
+    };
+    const int count = (n + kBlock - 1) / kBlock;
+    fetch(0, wa);
     set_ratios();
-    int have = -1;                                         // the block in LDS
-    for (int t = 0; t < n;) {
-        const int end = end_of(t), block = from[t], j = t / kBlock;
-        if (block >= 0 && block != have) {
-            __syncthreads();
-#pragma unroll
-            for (int x = 0; x < kPieces; ++x) {
-                const int i = tid + kMoveThreads * x;
-                if (4 * R % kMoveThreads == 0 || i < 4 * R) {
-                    uint32_t *p = (uint32_t *)(in + (i >> 2) * kPitch + 16 * (i & 3));
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) p[z] = piece[x][z];
-                }
-            }
-            have = block;
-            __syncthreads();
-        }
-        int next = end;                                    // the first token of another block that is there
-        while (next < n && (from[next] < 0 || from[next] == have)) next = end_of(next);
-        if (next < n && block == have) fetch(from[next]);  // (once: the next run of another block stages it)
-        // A wavefront takes every fourth quad of tokens, a lane a value's row: a quad is a word of it.
-        // (A token without a block has ratio 0, which makes any byte a code of 0.)
-        const int my_token = token[j * kBlock + lane];
-        const float my_ratio = ratio[j * kBlock + lane];
-        const int ta = t - j * kBlock, tb = end - j * kBlock;
-        for (int quad = (ta >> 2) + ((wave - (ta >> 2)) & 3); 4 * quad < tb; quad += 4) {
-            uint32_t at[4];
-            float r[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int e = min(max(4 * quad + v, ta), tb - 1);
-                at[v] = value_place(__builtin_amdgcn_readlane(my_token, e));
-                r[v] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ratio), e));
-            }
-            const bool whole = 4 * quad >= ta && 4 * quad + 4 <= tb;
-            for (int d = lane; d < R; d += 64) {
-                uint8_t *p = out + d * kPitch + value_place(4 * quad);
-                uint32_t q = 0;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) q |= rescaled(in[d * kPitch + at[v]], r[v]) << (8 * v);
-                if (whole) {
-                    *(uint32_t *)p = q;
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        if (4 * quad + v >= ta && 4 * quad + v < tb) p[v] = (uint8_t)(q >> (8 * v));
-                }
-            }
-        }
-        if (end % kBlock == 0 || end == n) {
-            __syncthreads();
-            if (dst[j] >= 0)
-#pragma unroll
-                for (int x = 0; x < kPieces; ++x) {
-                    const int i = tid + kMoveThreads * x;
-                    if (4 * R % kMoveThreads == 0 || i < 4 * R) {
-                        const uint32_t *p = (const uint32_t *)(out + (i >> 2) * kPitch + 16 * (i & 3));
-                        *(u32x4 *)(vp + page(dst[j]) + 16 * i) = (u32x4){p[0], p[1], p[2], p[3]};
-                    }
-                }
-            __syncthreads();
-        }
-        t = end;
+    for (int j = 0; j < count; j += 2) {
+        if (j + 1 < count) fetch(j + 1, wb);
+        put(j, wa);
+        if (j + 2 < count) fetch(j + 2, wa);
+        if (j + 1 < count) put(j + 1, wb);
     }
 }
 
