@@ -46,7 +46,9 @@ __device__ inline int scan(int x, int *lds, int &total) {
 // of the next 8 bits of the weights that agree with the bits found so far. Then
 // the positions in order: one sum over the threads' counts places every run.
 // Weights of up to kHeld tokens per thread stay in registers over the passes
-// (16384 tokens, 128 rows: 57 us with the weights read again for every pass).
+// (16384 tokens, 128 rows: 57 us with the weights read again for every pass, 31
+// so); the loops over them end where the longest run does (700-1100 tokens, 32
+// rows: 11.6 us without, 9.0 so).
 constexpr int kHeld = 32;
 template <int kSelThreads>
 __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const float *weights, int64_t w_stride, int keep,
@@ -74,15 +76,20 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
         return;
     }
 
-    const int run = (m + kSelThreads - 1) / kSelThreads, i0 = min(tid * run, m), n = min(run, m - i0);
+    const int run = __builtin_amdgcn_readfirstlane((m + kSelThreads - 1) / kSelThreads), i0 = min(tid * run, m), n = min(run, m - i0);
     uint32_t held[kHeld];
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) held[j] = j < n ? order_of(w[i0 + j]) : 0u;
+    for (int j = 0; j < kHeld; ++j) {
+        if (j >= run) break;                               // (of all threads at once)
+        held[j] = j < n ? order_of(w[i0 + j]) : 0u;
+    }
     // f(position, order) for this thread's tokens
     auto each = [&](auto f) {
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
+        for (int j = 0; j < kHeld; ++j) {
+            if (j >= run) break;
             if (j < n) f(i0 + j, held[j]);
+        }
         for (int j = kHeld; j < n; ++j) f(i0 + j, order_of(w[i0 + j]));
     };
     uint32_t bits = 0;                                     // of the smallest weight that stays
@@ -147,9 +154,9 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
 // any token of it touches all its lines: every block that has one passes
 // through LDS whole. A wavefront does that for its quarter of the values alone,
 // four source blocks on their way and no barrier (with the workgroup together,
-// one block ahead: 4 sequences of 700-1100 tokens to 512, 8 heads of 128, 30 us
-// for the whole call and its read, 24 so; 16 of 9000-16384 to 4096 230 and 227,
-// where the 340 MB that the values' lines make bound it).
+// one block ahead: 4 sequences of 700-1100 tokens to 512, 8 heads of 128, 13 us
+// and 7.7 so; 16 of 9000-16384 to 4096 120, 3 less, where the lines of values
+// and keys that it has to touch, some 550 MB, bound it).
 // What a wavefront's lanes have stored to LDS, its other lanes find after this.
 __device__ inline void in_order() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
