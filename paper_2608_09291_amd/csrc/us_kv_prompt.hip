@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "us_kv_attend.h"
+#include "us_kv_rules.h"
 
 namespace us_kv {
 namespace {
@@ -28,7 +29,8 @@ template <int NT, int DT, int W>
 __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
     constexpr int kThreads = 64 * W, kRows = 32 * W;       // 32 rows per wavefront
-    constexpr int kStages = prompt_stages(32 * NT, DT == US_F32), kAhead = kStages == 4 ? 1 : 0;
+    constexpr StageOrder kOrder{prompt_stages(32 * NT, DT == US_F32)};
+    constexpr int kStages = kOrder.stages, kAhead = kOrder.ahead();
     constexpr bool SPLIT = DT == US_F32;
     constexpr int R = 32 * NT, NS = R / 16;                // NS: steps of the first product
     // Float32 rows above 64: the queries' low parts wait in LDS, and scores are not taken
@@ -246,12 +248,12 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         look_up(0, id_k, sc_k, a.ks);
         look_up(0, id_v, sc_v, a.vs);
 #pragma unroll
-        for (int z = 0; z < 2 + kAhead; ++z)
+        for (int z = 0; z < kOrder.first_keys(); ++z)
             if (z < count) {
                 fetch_k(z, ks[z]);
-                if (z < 1 + kAhead) fetch_v(z, vs[z]);
+                if (z < kOrder.first_values()) fetch_v(z, vs[z]);
                 put_k(z);
-                if (z < 1 + kAhead) put_v(z);
+                if (z < kOrder.first_values()) put_v(z);
             }
         if (2 + kAhead < count) fetch_k(2 + kAhead, ks[2 + kAhead]);
         if (1 + kAhead < count) fetch_v(1 + kAhead, vs[1 + kAhead]);
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         scores(0, sa);
         hide(0, ks[0], sa);
         top = largest(sa);
-        if constexpr (kAhead == 0) __syncthreads();        // (the first step stages over block 0's keys)
+        if constexpr (kOrder.barrier_after_first()) __syncthreads();
     }
     auto step = [&](int i, auto odd, f32x16 (&s)[2], f32x16 (&next)[2]) {
         // (above 0, so that a masked key's -inf stays one)
@@ -322,11 +324,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
 #pragma unroll
         for (int z = 0; z < 1 + kAhead; ++z) vs[z] = vs[z + 1];
         // (past the last block: codes of an earlier one once more, which no product takes)
-        put_k(i + 2 + kAhead);
-        put_v(i + 1 + kAhead);
+        put_k(kOrder.puts_keys(i));
+        put_v(kOrder.puts_values(i));
         if (i + 3 + kAhead < count) fetch_k(i + 3 + kAhead, ks[2 + kAhead]);
         if (i + 2 + kAhead < count) fetch_v(i + 2 + kAhead, vs[1 + kAhead]);
-        if constexpr (kAhead == 0 || decltype(odd)::value == 1) __syncthreads();
+        if constexpr (kOrder.barrier_after(decltype(odd)::value)) __syncthreads();
     };
     for (int i = 0; i < count; i += 2) {
         step(i, std::integral_constant<int, 0>(), sa, sb);
