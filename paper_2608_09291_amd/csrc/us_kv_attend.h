@@ -15,6 +15,7 @@
 #define UNIONSPARSE_US_KV_ATTEND_H
 
 #include "us_kv_common.h"
+#include "us_kv_rules.h"
 
 namespace us_kv {
 
@@ -25,20 +26,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLift = 13.0f;                             // log2 of a probability's form at m
 constexpr float kSlack = 2.0f;                             // what m may lag behind the maximum: 2^15 at most
-
-struct Mask {
-    int32_t causal, window;
-    // Keys [lo, hi) that query i of n of a sequence of len tokens sees. Both grow with i.
-    __device__ void range(int i, int n, int len, int &lo, int &hi) const {
-        lo = 0;
-        hi = len;
-        if (causal) {
-            const int at = len - n + i;
-            hi = max(at + 1, 0);
-            lo = window > 0 ? max(at - window + 1, 0) : 0;
-        }
-    }
-};
 
 // How a launch splits a row's keys, and what it leaves in the workspace: per
 // unit (sequence, cache head, row tile) and split, `rows` partial rows of R

@@ -6,7 +6,6 @@
 #include <type_traits>
 
 #include "us_kv_attend.h"
-#include "us_kv_rules.h"
 
 namespace us_kv {
 namespace {

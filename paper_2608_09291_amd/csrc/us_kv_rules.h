@@ -8,6 +8,20 @@
 
 namespace us_kv {
 
+struct Mask {
+    int32_t causal, window;
+    // Keys [lo, hi) that query i of n of a sequence of len tokens sees. Both grow with i.
+    __host__ __device__ void range(int i, int n, int len, int &lo, int &hi) const {
+        lo = 0;
+        hi = len;
+        if (causal) {
+            const int at = len - n + i;
+            hi = at < 0 ? 0 : at + 1;
+            lo = window > 0 && at >= window ? at - window + 1 : 0;             // (no window is too wide for 32 bits)
+        }
+    }
+};
+
 // How a prompt workgroup passes the blocks of a row tile through its LDS stages:
 // block i lies in stage i % stages, keys and values apart. Ahead of step 0 the
 // first blocks are staged, then a barrier, then block 0's scores are taken. Step

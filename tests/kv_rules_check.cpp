@@ -60,9 +60,34 @@ static int stages() {
     return 0;
 }
 
+// The keys that a query sees, against the definition in 64 bits: positions up to its own, the last `window` of them.
+static int masks() {
+    const int lens[] = {0, 1, 2, 50, 64, 4000, 1 << 28}, counts[] = {1, 2, 80, 5000, 1 << 25};
+    const int windows[] = {0, 1, 2, 49, 50, 64, 4001, 1 << 28, INT32_MAX - 2, INT32_MAX - 1, INT32_MAX};
+    for (int len : lens)
+        for (int n : counts)
+            for (int window : windows)
+                for (int causal = window ? 1 : 0; causal <= 1; ++causal)
+                    for (int i : {0, 1, n / 2, n - 2, n - 1}) {
+                        if (i < 0 || i >= n) continue;
+                        const int64_t at = (int64_t)len - n + i;
+                        int64_t from = causal && window ? at - window + 1 : 0, end = causal ? at + 1 : len;
+                        from = from < 0 ? 0 : from;
+                        end = end < 0 ? 0 : end;
+                        int lo, hi;
+                        Mask{causal, window}.range(i, n, len, lo, hi);
+                        if (lo != from || hi != end) {
+                            std::printf("FAIL len=%d n=%d window=%d causal=%d i=%d: [%d, %d)\n", len, n, window, causal, i, lo, hi);
+                            return 1;
+                        }
+                    }
+    return 0;
+}
+
 int main(int argc, char **argv) {
     int r = 1;
     if (argc == 2 && !std::strcmp(argv[1], "stages")) r = stages();
+    if (argc == 2 && !std::strcmp(argv[1], "masks")) r = masks();
     if (r == 0) std::printf("ok\n");
     return r;
 }

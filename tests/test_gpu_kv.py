@@ -317,6 +317,35 @@ def test_attend(torch_cuda, lens, new, H, Hk, D, how, tracked, dtype):
     assert torch.equal(first[0], out) and (w1 is None or torch.equal(first[1], w1))   # bit for bit
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,H,Hk,D", [
+    ([50], [80], 2, 1, 64), ([50, 4], [80, 9], 4, 2, 128),
+    ([100, 64], [2000, 80], 64, 32, 64)])                   # (the last one for the kernel for prompts)
+def test_attend_widest_windows(torch_cuda, lens, new, H, Hk, D, dtype):
+    """Windows up to the largest number, with queries before the first key: as without one."""
+    torch = torch_cuda
+    announce(f"kv attend widest windows lens={lens} new={new} H={H}/{Hk} D={D} {dtype}")
+    rng = np.random.default_rng(sum(lens) + D)
+    p = Pool(torch, rng, lens, Hk, D)
+    cache, blocks, n = p.cache(), p.dev(p.blocks), p.dev(lens)
+    q = torch.from_numpy(rng.normal(0, 1.5, size=(sum(new), H, D)).astype(np.float32)).cuda().to(_torch_dtype(torch, dtype))
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new))
+    w0 = torch.zeros((len(lens), Hk, p.width * 64), device="cuda")
+    got = []
+    for window in (0, max(lens), 2 ** 31 - 3, 2 ** 31 - 1):
+        w, out = w0.clone(), torch.full_like(q, math.nan)
+        ws = kv.attend_workspace(cache, q, blocks, window=window, weights=w, **args)
+        kv.attend(cache, blocks, n, q, out, window=window, weights=w, ws=ws, **args)
+        torch.cuda.synchronize()
+        got.append((out, w))
+    if H == 64:
+        assert all(torch.equal(o, got[0][0]) and torch.equal(w, got[0][1]) for o, w in got[1:])
+        assert (got[0][0][new[0] - 1] != 0).all()
+    else:
+        for out, w in got:
+            _check(torch, p, lens, new, q, out, dtype, w0, w)
+
+
 PROMPTS = [  # as ATTEND, with rows and heads that the kernel for prompts takes; whether rows lie at odd places
     ([330, 200, 77, 0], [330, 140, 60, 0], 96, 96, 96, {}, True),
     ([700, 100], [500, 100], 96, 48, 80, dict(window=90), False),

@@ -1,5 +1,6 @@
 """What the key/value cache's attention kernels decide by whole numbers (paper_2608_09291_amd/csrc/us_kv_rules.h),
-compiled for the host: the order in which blocks pass through the LDS stages of the prompt kernel."""
+compiled for the host: the order in which blocks pass through the LDS stages of the prompt kernel,
+and the range of keys that a query sees."""
 import os
 import shutil
 import subprocess
@@ -27,3 +28,7 @@ def check(tmp_path_factory):
 
 def test_no_stage_is_overwritten_while_it_may_be_read(check):
     check("stages")
+
+
+def test_ranges_of_keys(check):
+    check("masks")
