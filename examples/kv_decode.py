@@ -76,7 +76,7 @@ class Layer:
     def evict(self):
         """Half of the budget stays, a quarter of that for being recent."""
         keep = self.budget // 2
-        lens, weights = torch.empty_like(self.lens), torch.zeros_like(self.weights)
+        lens, weights = torch.empty_like(self.lens), torch.empty_like(self.weights)
         kv.evict(self.cache, self.tables[0], self.lens, self.weights, keep, keep // 4, self.tables[1], lens, weights, self.index)
         self.tables.reverse()
         self.lens, self.weights, self.length = lens, weights, min(self.length, keep)

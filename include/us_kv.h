@@ -152,7 +152,9 @@ typedef struct {
     int64_t stride;
     int32_t width;          /* width * US_KV_BLOCK >= keep, or >= every length */
     int32_t *lens;          /* device, batch: min(length, keep)                */
-    float *weights;         /* device, batch x heads x weights_stride, or NULL */
+    float *weights;         /* device, batch x heads x weights_stride, or NULL:
+                               of the kept tokens in order, then zeros for the
+                               tokens that the blocks have room for            */
     int64_t weights_stride; /* >= min(keep, width * US_KV_BLOCK)               */
     int32_t *index;         /* device, batch x heads x keep: the kept positions,
                                ascending, then -1                              */

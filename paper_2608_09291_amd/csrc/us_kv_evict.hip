@@ -53,7 +53,7 @@ constexpr int kHeld = 32;
 template <int kSelThreads>
 __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const float *weights, int64_t w_stride, int keep,
                                                                    int recent, int heads, int32_t *to_lens,
-                                                                   float *to_weights, int64_t to_w_stride,
+                                                                   float *to_weights, int64_t to_w_stride, int to_w_end,
                                                                    int32_t *index) {
     __shared__ int hist[256], lds[16], found[2];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
@@ -67,6 +67,9 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
         if (ow) ow[take + i] = w[m + i];
     }
     for (int i = stay + tid; i < keep; i += kSelThreads) idx[i] = -1;
+    // (tokens still to come: us_kv_attend adds to what is there)
+    if (ow)
+        for (int i = stay + tid; i < to_w_end; i += kSelThreads) ow[i] = 0.0f;
     if (take == 0) return;
     if (take == m) {
         for (int i = tid; i < m; i += kSelThreads) {
@@ -342,9 +345,11 @@ extern "C" us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seq
         return US_ERR_SHAPE;
     const hipStream_t q = (hipStream_t)stream;
     // Four wavefronts meet at a barrier sooner than sixteen: as long as they hold all weights.
+    const int64_t to_tokens = (int64_t)to->width * kBlock < to->weights_stride ? (int64_t)to->width * kBlock : to->weights_stride;
+    const int to_w_end = (int)(to_tokens < (int64_t)US_KV_WIDTH_MAX * kBlock ? to_tokens : (int64_t)US_KV_WIDTH_MAX * kBlock);
     const auto select = [&](auto kern, int threads) {
         hipLaunchKernelGGL(kern, dim3(cache->heads, seqs->batch), dim3(threads), 0, q, s, weights, weights_stride, keep, recent,
-                           cache->heads, to->lens, to->weights, to->weights_stride, to->index);
+                           cache->heads, to->lens, to->weights, to->weights_stride, to_w_end, to->index);
     };
     if (s.max_len <= 256 * kHeld) select(us_kv_select_kernel<256>, 256);
     else select(us_kv_select_kernel<1024>, 1024);

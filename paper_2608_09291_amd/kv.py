@@ -225,7 +225,8 @@ def attend(cache: Cache, blocks, lens, q, out, starts=None, max_q: int = 1, max_
 
 def evict(cache: Cache, blocks, lens, weights, keep: int, recent: int, to_blocks, to_lens, to_weights, index,
           max_len=None, stream=None) -> None:
-    """us_kv_evict: the recent and the most attended tokens of every sequence, moved to to_blocks."""
+    """us_kv_evict: the recent and the most attended tokens of every sequence, moved to to_blocks; to_weights gets
+    their weights, and zeros for the tokens still to come."""
     heads, batch = cache.heads, blocks.shape[0]
     w, w_stride = _weights(weights, batch, heads, "weights")
     ow, ow_stride = (0, 0) if to_weights is None else _weights(to_weights, batch, heads, "to_weights")

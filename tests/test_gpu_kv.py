@@ -715,6 +715,66 @@ def test_evict(torch_cuda, lens, heads, D, keep, recent, kind):
                     assert np.array_equal(codes[blk], p.codes[i][blk])
 
 
+@pytest.mark.parametrize("lens,keep,recent", [([300, 40, 0], 100, 10), ([200], 64, 0), ([130], 500, 500), ([90, 70], 65, 65)])
+def test_evict_clears_the_weights_behind_the_kept(torch_cuda, lens, keep, recent):
+    """Weights of tokens still to come start from zero, whatever the buffer held; past the new table it is not touched."""
+    torch = torch_cuda
+    announce(f"kv evict tails lens={lens} keep={keep} recent={recent}")
+    rng = np.random.default_rng(sum(lens))
+    heads, width = 2, 3 if keep < 300 else 8                # (wider than what is kept)
+    p = Pool(torch, rng, lens, heads, 64, spare=width * len(lens))
+    cache, w = p.cache(), torch.rand((len(lens), heads, p.width * 64), device="cuda")
+    to = p.dev(p.table([width] * len(lens), width))
+    for room in (width * 64 - 20, width * 64, width * 64 + 37):
+        to_w = torch.full((len(lens), heads, room), math.nan, device="cuda")
+        to_lens, index = p.dev([-1] * len(lens)), torch.zeros((len(lens), heads, keep), dtype=torch.int32, device="cuda")
+        kv.evict(cache, p.dev(p.blocks), p.dev(lens), w, keep, recent, to, to_lens, to_w, index)
+        torch.cuda.synchronize()
+        for b, n in enumerate(lens):
+            stay = min(n, keep)
+            for h in range(heads):
+                assert torch.equal(to_w[b, h, :stay], w[b, h][index[b, h, :stay].long()])
+            assert (to_w[b, :, stay:width * 64] == 0).all() and torch.isnan(to_w[b, :, width * 64:]).all()
+
+
+def test_two_buffers_of_weights_in_turn(torch_cuda):
+    """Append, attend and evict with two tables and two buffers that change places: the same as with fresh zeros."""
+    torch = torch_cuda
+    announce("kv evict buffers in turn")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    B, H, Hk, D, width, keep = 2, 4, 2, 64, 3, 100
+    q = torch.randn((3 * 192, B, H, D), generator=gen, device="cuda") * 4
+    x = torch.randn((3 * 192, B, Hk, D), generator=gen, device="cuda")
+    kept = []
+    for fresh in (True, False):
+        cache = kv.new_cache(2 * B * width, Hk, D)
+        tables = list(torch.arange(2 * B * width, dtype=torch.int32, device="cuda").view(2, B, width))
+        lens, length = torch.zeros(B, dtype=torch.int32, device="cuda"), 0
+        w = [torch.zeros((B, Hk, width * 64), device="cuda") for _ in range(2)]
+        out, kept_now = torch.empty((B, H, D), device="cuda"), []
+        for t in range(3 * 192):
+            if length == width * 64:
+                index = torch.empty((B, Hk, keep), dtype=torch.int32, device="cuda")
+                to_lens = torch.empty_like(lens)
+                if fresh:
+                    w[1] = torch.zeros_like(w[1])
+                kv.evict(cache, tables[0], lens, w[0], keep, 20, tables[1], to_lens, w[1], index)
+                tables.reverse()
+                w.reverse()
+                lens, length = to_lens, keep
+                kept_now.append(index)
+            lens.add_(1)
+            length += 1
+            kv.append(cache, tables[0], lens, x[t], x[t])
+            kv.attend(cache, tables[0], lens, q[t], out, weights=w[0], ws=kv.attend_workspace(cache, out, tables[0], weights=w[0]))
+        torch.cuda.synchronize()
+        kept.append(kept_now)
+    assert len(kept[0]) == 5
+    for a, b in zip(*kept):
+        assert torch.equal(a, b)
+
+
 def test_example_layer(torch_cuda):
     """The operators together, as a decoder layer uses them: projections, cache, attention, eviction."""
     import importlib.util
