@@ -339,7 +339,10 @@ __global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, f
             const f32x4 y = *(const f32x4 *)(s + r * a.sp.scores_stride);
             const float zr = z[r];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sum[v] += __builtin_amdgcn_exp2f(y[v] - zr);
+            for (int v = 0; v < 4; ++v) {
+                const float e = __builtin_amdgcn_exp2f(y[v] - zr);
+                sum[v] += y[v] == -INFINITY ? 0.0f : e;    // (a masked key, whatever the row's sum is)
+            }
         }
     }
     if (shared) {

@@ -551,6 +551,37 @@ def test_attend_nan_stays_in_its_row(torch_cuda, new):
         assert nan[bad].all() and not nan[~bad].any()
 
 
+@pytest.mark.parametrize("lens,new,H,Hk,how", [
+    ([300, 70], [5, 3], 4, 2, {}), ([200], [9], 2, 1, dict(window=3)), ([130], [2], 1, 1, {}), ([64], [64], 2, 1, {}),
+    ([600], [400], 64, 32, {}), ([600], [400], 64, 32, dict(window=70))])    # (the last two for the kernel for prompts)
+def test_weights_of_keys_that_a_nan_query_does_not_see(torch_cuda, lens, new, H, Hk, how):
+    """A query with a NaN or an infinity leaves NaN in the weights of the keys that it sees, and nothing in the others'."""
+    torch = torch_cuda
+    announce(f"kv attend weights beside NaN lens={lens} new={new} H={H}/{Hk} {how}")
+    rng = np.random.default_rng(sum(lens))
+    p = Pool(torch, rng, lens, Hk, 64)
+    cache, blocks, n = p.cache(), p.dev(p.blocks), p.dev(lens)
+    clean = torch.from_numpy(rng.normal(0, 1, size=(sum(new), H, 64)).astype(np.float32)).cuda()
+    bad = 1                                                 # the second query, of every head: the last ones see more
+    for dtype in DTYPES:
+        for value in (math.nan, math.inf):
+            got = []
+            for spoilt in (False, True):
+                q = clean.to(_torch_dtype(torch, dtype)).clone()
+                if spoilt:
+                    q[bad, :, 7] = value
+                w, out = torch.zeros((len(lens), Hk, p.width * 64), device="cuda"), torch.empty_like(q)
+                args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w, **how)
+                kv.attend(cache, blocks, n, q, out, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+                torch.cuda.synchronize()
+                got.append(w)
+            lo, hi = ref.visible(bad, new[0], lens[0], True, how.get("window", 0))
+            seen = torch.zeros_like(got[0], dtype=torch.bool)
+            seen[0, :, lo:hi] = True
+            assert torch.isnan(got[1][seen]).all(), (dtype, value)
+            assert torch.equal(got[1][~seen], got[0][~seen]), (dtype, value)
+
+
 @pytest.mark.parametrize("tracked", [False, True])
 def test_workspace_serves_calls_of_other_kinds(torch_cuda, tracked):
     """One workspace for a prompt's call, decode calls that split and others that do not, in turn: as with fresh ones."""
