@@ -150,7 +150,8 @@ typedef struct {
     const int32_t *blocks;  /* device, batch x stride: blocks of the same pool,
                                none of them one of the sequences' own          */
     int64_t stride;
-    int32_t width;          /* width * US_KV_BLOCK >= keep, or >= every length */
+    int32_t width;          /* width * US_KV_BLOCK >= keep, or >= every length;
+                               to US_KV_WIDTH_MAX                              */
     int32_t *lens;          /* device, batch: min(length, keep)                */
     float *weights;         /* device, batch x heads x weights_stride, or NULL:
                                of the kept tokens in order, then zeros for the

@@ -340,13 +340,13 @@ extern "C" us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seq
     if (max_len < 0 || keep < 1 || recent < 0 || recent > keep) return US_ERR_SHAPE;
     const Seqs s = seqs_of(*cache, *seqs, max_len, 0);
     const int most = keep < s.max_len ? keep : s.max_len;
-    if (to->width < 1 || to->stride < to->width || (int64_t)to->width * kBlock < most || weights_stride < s.max_len ||
+    if (to->width < 1 || to->width > US_KV_WIDTH_MAX || to->stride < to->width || (int64_t)to->width * kBlock < most || weights_stride < s.max_len ||
         (to->weights && to->weights_stride < most))
         return US_ERR_SHAPE;
     const hipStream_t q = (hipStream_t)stream;
     // Four wavefronts meet at a barrier sooner than sixteen: as long as they hold all weights.
     const int64_t to_tokens = (int64_t)to->width * kBlock < to->weights_stride ? (int64_t)to->width * kBlock : to->weights_stride;
-    const int to_w_end = (int)(to_tokens < (int64_t)US_KV_WIDTH_MAX * kBlock ? to_tokens : (int64_t)US_KV_WIDTH_MAX * kBlock);
+    const int to_w_end = (int)to_tokens;                   // (at most 2^28: the widest table's)
     const auto select = [&](auto kern, int threads) {
         hipLaunchKernelGGL(kern, dim3(cache->heads, seqs->batch), dim3(threads), 0, q, s, weights, weights_stride, keep, recent,
                            cache->heads, to->lens, to->weights, to->weights_stride, to_w_end, to->index);

@@ -132,6 +132,13 @@ def test_evict_refuses(change, status):
     assert r == status
 
 
+def test_evict_refuses_tables_wider_than_any():
+    c, s, _, _ = _valid()
+    for width in ((1 << 22) + 1, 1 << 25, 1 << 26, (1 << 31) - 1):
+        to = kv.KeptStruct(P, width, width, P, P, 256, P)
+        assert kv.lib().us_kv_evict(ctypes.byref(c), ctypes.byref(s), P, 256, 0, 100, 10, ctypes.byref(to), None) == SHAPE
+
+
 def test_binding_refuses_tensors():
     torch = pytest.importorskip("torch")
     c = kv.new_cache(4, 2, 80, device="cpu")
