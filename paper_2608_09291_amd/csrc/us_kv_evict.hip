@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kSelThreads) void us_kv_select_kernel(Seqs s, const
         idx[take + i] = m + i;
         if (ow) ow[take + i] = w[m + i];
     }
-    for (int i = stay + tid; i < keep; i += kSelThreads) idx[i] = -1;
+    for (uint32_t i = stay + tid; i < (uint32_t)keep; i += kSelThreads) idx[i] = -1;      // (keep goes up to 2^31 - 1)
     // (tokens still to come: us_kv_attend adds to what is there)
     if (ow)
         for (int i = stay + tid; i < to_w_end; i += kSelThreads) ow[i] = 0.0f;

@@ -746,6 +746,22 @@ def test_evict(torch_cuda, lens, heads, D, keep, recent, kind):
                     assert np.array_equal(codes[blk], p.codes[i][blk])
 
 
+def test_evict_keeps_as_many_as_a_number_holds(torch_cuda):
+    """keep = 2^31 - 1: every token stays, and the index is filled to its end and no further."""
+    torch = torch_cuda
+    announce("kv evict keep=2^31-1")
+    p = Pool(torch, np.random.default_rng(2), [70], 1, 64, spare=2)
+    cache, keep, guard = p.cache(), 2 ** 31 - 1, 4096
+    to, to_lens = p.dev(p.table([2], 2)), p.dev([-1])
+    around = torch.full((keep + 2 * guard,), -7, dtype=torch.int32, device="cuda")     # 8.6 GB
+    index = around[guard:guard + keep].view(1, 1, keep)
+    kv.evict(cache, p.dev(p.blocks), p.dev([70]), torch.rand((1, 1, 128), device="cuda"), keep, 5, to, to_lens, None, index)
+    torch.cuda.synchronize()
+    assert to_lens.tolist() == [70] and index[0, 0, :70].tolist() == list(range(70))
+    assert all((x == -1).all() for x in index[0, 0, 70:].split(1 << 28))
+    assert (around[:guard] == -7).all() and (around[guard + keep:] == -7).all()
+
+
 @pytest.mark.parametrize("lens,keep,recent", [([300, 40, 0], 100, 10), ([200], 64, 0), ([130], 500, 500), ([90, 70], 65, 65)])
 def test_evict_clears_the_weights_behind_the_kept(torch_cuda, lens, keep, recent):
     """Weights of tokens still to come start from zero, whatever the buffer held; past the new table it is not touched."""
