@@ -145,7 +145,7 @@ us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs
 us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
                        const us_rows *out, const us_kv_attend_opts *opts, void *ws, size_t ws_bytes, void *stream);
 
-/* Where an eviction leaves what it keeps. */
+/* Where an eviction leaves what it keeps; none of it overlaps what the call reads. */
 typedef struct {
     const int32_t *blocks;  /* device, batch x stride: blocks of the same pool,
                                none of them one of the sequences' own          */

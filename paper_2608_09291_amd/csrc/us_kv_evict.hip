@@ -343,6 +343,8 @@ extern "C" us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seq
     if (to->width < 1 || to->width > US_KV_WIDTH_MAX || to->stride < to->width || (int64_t)to->width * kBlock < most || weights_stride < s.max_len ||
         (to->weights && to->weights_stride < most))
         return US_ERR_SHAPE;
+    // (some heads would be cut by the new length, some weights chosen by moved ones)
+    if (to->lens == seqs->lens || to->weights == weights) return US_ERR_ARG;
     const hipStream_t q = (hipStream_t)stream;
     // Four wavefronts meet at a barrier sooner than sixteen: as long as they hold all weights.
     const int64_t to_tokens = (int64_t)to->width * kBlock < to->weights_stride ? (int64_t)to->width * kBlock : to->weights_stride;

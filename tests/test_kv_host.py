@@ -139,6 +139,15 @@ def test_evict_refuses_tables_wider_than_any():
         assert kv.lib().us_kv_evict(ctypes.byref(c), ctypes.byref(s), P, 256, 0, 100, 10, ctypes.byref(to), None) == SHAPE
 
 
+def test_evict_refuses_to_write_what_it_reads():
+    """Lengths and weights of what is kept have places of their own: other workgroups still read the sequences'."""
+    c, s, _, _ = _valid()
+    s.lens = 2 * P
+    for lens, weights in ((2 * P, 4 * P), (2 * P, None), (5 * P, 3 * P)):
+        to = kv.KeptStruct(P, 4, 4, lens, weights, 256, 6 * P)
+        assert kv.lib().us_kv_evict(ctypes.byref(c), ctypes.byref(s), 3 * P, 256, 0, 100, 10, ctypes.byref(to), None) == ARG
+
+
 def test_binding_refuses_tensors():
     torch = pytest.importorskip("torch")
     c = kv.new_cache(4, 2, 80, device="cpu")
