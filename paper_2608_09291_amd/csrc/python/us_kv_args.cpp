@@ -36,12 +36,15 @@ PyObject *guarded(PyObject *(*f)(PyObject *const *, Py_ssize_t), PyObject *const
     }
 }
 
-// (k, v, k_scale, v_scale) -> addresses, blocks, heads, bytes of a block, whether all are on the GPU
+// Whether t is on GPU `device`, or on any where that is negative.
+bool on(const at::Tensor &t, long long device) { return t.is_cuda() && (device < 0 || t.get_device() == device); }
+
+// (k, v, k_scale, v_scale) -> addresses, blocks, heads, bytes of a block, number of the GPU that holds them (-1: not all are on one)
 PyObject *cache_of(PyObject *const *args, Py_ssize_t n) {
     if (!count(n, 4)) return nullptr;
     const char *names[4] = {"k", "v", "k_scale", "v_scale"};
     const at::Tensor *t[4];
-    bool cuda = true;
+    bool one = true;
     for (int i = 0; i < 4; ++i) {
         t[i] = tensor(args, i, names[i]);
         if (!t[i]) return nullptr;
@@ -50,18 +53,20 @@ PyObject *cache_of(PyObject *const *args, Py_ssize_t n) {
             t[i]->size(0) != t[0]->size(0) || t[i]->size(1) != t[0]->size(1) || (codes && t[i]->size(2) != t[0]->size(2)))
             return refuse(names[i], codes ? "a contiguous uint8 tensor (blocks, heads, bytes of a block) is wanted"
                                           : "a contiguous float32 tensor (blocks, heads) is wanted");
-        cuda = cuda && t[i]->is_cuda();
+        one = one && t[i]->is_cuda() && t[i]->get_device() == t[0]->get_device();
     }
-    return Py_BuildValue("KKKKLLLO", address(*t[0]), address(*t[1]), address(*t[2]), address(*t[3]), (long long)t[0]->size(0),
-                         (long long)t[0]->size(1), (long long)t[0]->size(2), cuda ? Py_True : Py_False);
+    return Py_BuildValue("KKKKLLLL", address(*t[0]), address(*t[1]), address(*t[2]), address(*t[3]), (long long)t[0]->size(0),
+                         (long long)t[0]->size(1), (long long)t[0]->size(2), one ? (long long)t[0]->get_device() : -1ll);
 }
 
-// (blocks, lens, starts or None) -> address of blocks, stride, width, batch, addresses of lens and starts
+// (blocks, lens, starts or None, device) -> address of blocks, stride, width, batch, addresses of lens and starts
 PyObject *seqs_of(PyObject *const *args, Py_ssize_t n) {
-    if (!count(n, 3)) return nullptr;
+    if (!count(n, 4)) return nullptr;
     const at::Tensor *blocks = tensor(args, 0, "blocks"), *lens = blocks ? tensor(args, 1, "lens") : nullptr, *starts = nullptr;
     if (!lens) return nullptr;
     if (args[2] != Py_None && !(starts = tensor(args, 2, "starts"))) return nullptr;
+    const long long device = PyLong_AsLongLong(args[3]);
+    if (PyErr_Occurred()) return nullptr;
     if (blocks->dim() != 2 || blocks->scalar_type() != at::kInt || (blocks->size(1) > 1 && blocks->stride(1) != 1))
         return refuse("blocks", "an int32 table with contiguous rows is wanted");
     const int64_t batch = blocks->size(0), width = blocks->size(1);
@@ -70,26 +75,26 @@ PyObject *seqs_of(PyObject *const *args, Py_ssize_t n) {
     };
     if (!numbers(*lens, batch)) return refuse("lens", "a contiguous int32 number for every sequence is wanted");
     if (starts && !numbers(*starts, batch + 1)) return refuse("starts", "contiguous int32 numbers, one more than sequences, are wanted");
-    if (!blocks->is_cuda() || !lens->is_cuda() || (starts && !starts->is_cuda()))
-        return refuse("blocks, lens, starts", "tensors on the GPU are wanted");
+    if (!on(*blocks, device) || !on(*lens, device) || (starts && !on(*starts, device)))
+        return refuse("blocks, lens, starts", "tensors on the cache's GPU are wanted");
     return Py_BuildValue("KLLLKK", address(*blocks), (long long)(batch > 1 ? blocks->stride(0) : width), (long long)width,
                          (long long)batch, address(*lens), starts ? address(*starts) : 0ull);
 }
 
-// (rows, heads, head_dim, name) -> address, token stride, head stride, tokens, type
+// (rows, heads, head_dim, name, device) -> address, token stride, head stride, tokens, type
 PyObject *rows_of(PyObject *const *args, Py_ssize_t n) {
-    if (!count(n, 4)) return nullptr;
+    if (!count(n, 5)) return nullptr;
     const char *name = PyUnicode_AsUTF8(args[3]);
     const at::Tensor *t = name ? tensor(args, 0, name) : nullptr;
     if (!t) return nullptr;
-    const long long heads = PyLong_AsLongLong(args[1]), head_dim = PyLong_AsLongLong(args[2]);
+    const long long heads = PyLong_AsLongLong(args[1]), head_dim = PyLong_AsLongLong(args[2]), device = PyLong_AsLongLong(args[4]);
     if (PyErr_Occurred()) return nullptr;
     const auto type = t->scalar_type();
     const int dtype = type == at::kFloat ? 0 : type == at::kBFloat16 ? 1 : type == at::kHalf ? 2 : -1;
     if (dtype < 0 || t->dim() != 3 || t->size(1) != heads || t->size(2) != head_dim || (head_dim > 1 && t->stride(2) != 1))
         return PyErr_Format(PyExc_TypeError, "%s: (tokens, %lld, %lld) float32, bfloat16 or float16 with contiguous values is wanted",
                             name, heads, head_dim);
-    if (!t->is_cuda()) return refuse(name, "a tensor on the GPU is wanted");
+    if (!on(*t, device)) return refuse(name, "a tensor on the cache's GPU is wanted");
     return Py_BuildValue("KLLLi", address(*t), (long long)t->stride(0), (long long)t->stride(1), (long long)t->size(0), dtype);
 }
 

@@ -100,11 +100,17 @@ def row(head_dim: int) -> int:
     return r
 
 
-def _stream(stream) -> int:
-    if stream is not None:
-        return stream.cuda_stream
-    # (the handle alone: building torch's stream object takes as long as a launch)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _stream(stream, cache) -> int:
+    """A call's stream. The library launches on the current device, which has to be the cache's and the stream's."""
+    now = torch.cuda.current_device()
+    if cache.device >= 0 and now != cache.device:
+        raise ValueError(f"the cache is on cuda:{cache.device}, the current device is cuda:{now}")
+    if stream is None:
+        # (the handle alone: building torch's stream object takes as long as a launch)
+        return torch._C._cuda_getCurrentRawStream(now)
+    if stream.device.index != now:
+        raise ValueError(f"a stream of cuda:{now}, the current device, is wanted")
+    return stream.cuda_stream
 
 
 class Cache:
@@ -112,13 +118,14 @@ class Cache:
 
     def __init__(self, k, v, k_scale, v_scale, head_dim: int):
         size = BLOCK * row(head_dim)
-        ak, av, aks, avs, n, heads, bytes_, cuda = _args.cache(k, v, k_scale, v_scale)
+        ak, av, aks, avs, n, heads, bytes_, self.device = _args.cache(k, v, k_scale, v_scale)
         if bytes_ != size:
             raise TypeError(f"codes: contiguous uint8 tensors (blocks, heads, {size}) are wanted")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_blocks, self.heads, self.head_dim = n, heads, head_dim
         self._packed = _pack_cache(ak, av, aks, avs, n, heads, head_dim)
-        self._there = self._packed if cuda else None       # what calls are given: they refuse None
+        # what calls are given: they refuse None, a cache that is not on one GPU
+        self._there = self._packed if self.device >= 0 else None
 
     def struct(self) -> CacheStruct:
         return CacheStruct.from_buffer_copy(self._packed)
@@ -147,46 +154,51 @@ def _numbers(t, n, name):
     return t.data_ptr()
 
 
-def _seqs(blocks, lens, starts, max_new) -> bytes:
-    at, stride, width, batch, at_lens, at_starts = _args.seqs(blocks, lens, starts)
+def _on(t, device) -> bool:
+    """Whether t is on GPU `device`, or on any where that is negative."""
+    return t.is_cuda and (device < 0 or t.get_device() == device)
+
+
+def _seqs(blocks, lens, starts, max_new, device) -> bytes:
+    at, stride, width, batch, at_lens, at_starts = _args.seqs(blocks, lens, starts, device)
     return _pack_seqs(at, stride, width, batch, at_lens, at_starts, max_new)
 
 
-def _rows(t, heads, head_dim, name) -> bytes:
-    return _pack_rows(*_args.rows(t, heads, head_dim, name))
+def _rows(t, heads, head_dim, name, device) -> bytes:
+    return _pack_rows(*_args.rows(t, heads, head_dim, name, device))
 
 
-def _weights(t, batch, heads, name):
+def _weights(t, batch, heads, name, device):
     """Address and row length of a float32 (sequences, heads, tokens) tensor."""
     b, h, n = t.shape
     if b != batch or h != heads or t.dtype is not _F32 or not t.is_contiguous():
         raise TypeError(f"{name}: a contiguous float32 tensor ({batch}, {heads}, tokens) is wanted")
-    if not t.is_cuda:
-        raise TypeError(f"{name}: a tensor on the GPU is wanted")
+    if not _on(t, device):
+        raise TypeError(f"{name}: a tensor on the cache's GPU is wanted")
     return t.data_ptr(), n
 
 
 def append(cache: Cache, blocks, lens, k, v, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_append: quantise the sequences' last tokens (rows of k and v) into their blocks."""
-    h, d = cache.heads, cache.head_dim
-    _check("us_kv_append", lib().us_kv_append(cache._there, _seqs(blocks, lens, starts, max_new), _rows(k, h, d, "k"),
-                                              _rows(v, h, d, "v"), _stream(stream)))
+    h, d, on = cache.heads, cache.head_dim, cache.device
+    _check("us_kv_append", lib().us_kv_append(cache._there, _seqs(blocks, lens, starts, max_new, on), _rows(k, h, d, "k", on),
+                                              _rows(v, h, d, "v", on), _stream(stream, cache)))
 
 
 def read(cache: Cache, blocks, lens, k_out, v_out, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_read: the sequences' last tokens as dense rows."""
-    h, d = cache.heads, cache.head_dim
-    _check("us_kv_read", lib().us_kv_read(cache._there, _seqs(blocks, lens, starts, max_new),
-                                          _rows(k_out, h, d, "k_out"), _rows(v_out, h, d, "v_out"), _stream(stream)))
+    h, d, on = cache.heads, cache.head_dim, cache.device
+    _check("us_kv_read", lib().us_kv_read(cache._there, _seqs(blocks, lens, starts, max_new, on), _rows(k_out, h, d, "k_out", on),
+                                          _rows(v_out, h, d, "v_out", on), _stream(stream, cache)))
 
 
-def _opts(scale, causal, window, max_len, weights, batch, heads):
+def _opts(scale, causal, window, max_len, weights, batch, heads, device):
     if weights is None:
         if scale is None and causal and not window and not max_len:
             return None
         at, n = 0, 0
     else:
-        at, n = _weights(weights, batch, heads, "weights")
+        at, n = _weights(weights, batch, heads, "weights", device)
     return _pack_opts(0.0 if scale is None else scale, 1 if causal else 0, window, max_len or 0, at, n)
 
 
@@ -199,7 +211,7 @@ def attend_workspace_size(cache: Cache, q_heads: int, tokens: int, blocks, start
                    0 if starts is None else starts.data_ptr(), max_q)
     n = ctypes.c_size_t(0)
     _check("us_kv_attend_workspace_size", lib().us_kv_attend_workspace_size(
-        cache._packed, s, q_heads, tokens, _opts(None, causal, window, max_len, weights, batch, cache.heads),
+        cache._packed, s, q_heads, tokens, _opts(None, causal, window, max_len, weights, batch, cache.heads, cache.device),
         ctypes.byref(n)))
     return n.value
 
@@ -214,29 +226,29 @@ def attend_workspace(cache: Cache, q, blocks, starts=None, max_q: int = 1, max_l
 def attend(cache: Cache, blocks, lens, q, out, starts=None, max_q: int = 1, max_len=None, scale=None,
            causal: bool = True, window: int = 0, weights=None, ws=None, stream=None) -> None:
     """us_kv_attend: out = softmax(scale q k) v over the cache; weights (if given) gain each token's probabilities."""
-    heads, d = q.shape[1], cache.head_dim
-    if ws is not None and not (ws.is_cuda and ws.is_contiguous()):
-        raise TypeError("ws: a contiguous tensor on the GPU is wanted")
+    heads, d, on = q.shape[1], cache.head_dim, cache.device
+    if ws is not None and not (_on(ws, on) and ws.is_contiguous()):
+        raise TypeError("ws: a contiguous tensor on the cache's GPU is wanted")
     _check("us_kv_attend", lib().us_kv_attend(
-        cache._there, _seqs(blocks, lens, starts, max_q), heads, _rows(q, heads, d, "q"), _rows(out, heads, d, "out"),
-        _opts(scale, causal, window, max_len, weights, blocks.shape[0], cache.heads),
-        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes, _stream(stream)))
+        cache._there, _seqs(blocks, lens, starts, max_q, on), heads, _rows(q, heads, d, "q", on),
+        _rows(out, heads, d, "out", on), _opts(scale, causal, window, max_len, weights, blocks.shape[0], cache.heads, on),
+        0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes, _stream(stream, cache)))
 
 
 def evict(cache: Cache, blocks, lens, weights, keep: int, recent: int, to_blocks, to_lens, to_weights, index,
           max_len=None, stream=None) -> None:
     """us_kv_evict: the recent and the most attended tokens of every sequence, moved to to_blocks; to_weights gets
     their weights, and zeros for the tokens still to come."""
-    heads, batch = cache.heads, blocks.shape[0]
-    w, w_stride = _weights(weights, batch, heads, "weights")
-    ow, ow_stride = (0, 0) if to_weights is None else _weights(to_weights, batch, heads, "to_weights")
+    heads, batch, on = cache.heads, blocks.shape[0], cache.device
+    w, w_stride = _weights(weights, batch, heads, "weights", on)
+    ow, ow_stride = (0, 0) if to_weights is None else _weights(to_weights, batch, heads, "to_weights", on)
     rows, width, stride = _table(to_blocks, "to_blocks")
     if rows != batch:
         raise ValueError("to_blocks: one row per sequence is wanted")
     if index.dtype is not _I32 or index.shape != (batch, heads, keep) or not index.is_contiguous():
         raise TypeError(f"index: a contiguous int32 tensor {(batch, heads, keep)} is wanted")
-    if not (to_blocks.is_cuda and to_lens.is_cuda and index.is_cuda):
-        raise TypeError("to_blocks, to_lens, index: tensors on the GPU are wanted")
+    if not (_on(to_blocks, on) and _on(to_lens, on) and _on(index, on)):
+        raise TypeError("to_blocks, to_lens, index: tensors on the cache's GPU are wanted")
     to = _pack_kept(to_blocks.data_ptr(), stride, width, _numbers(to_lens, batch, "to_lens"), ow, ow_stride, index.data_ptr())
-    _check("us_kv_evict", lib().us_kv_evict(cache._there, _seqs(blocks, lens, None, 1), w, w_stride, max_len or 0, keep,
-                                            recent, to, _stream(stream)))
+    _check("us_kv_evict", lib().us_kv_evict(cache._there, _seqs(blocks, lens, None, 1, on), w, w_stride, max_len or 0,
+                                            keep, recent, to, _stream(stream, cache)))

@@ -192,6 +192,48 @@ def test_binding_refuses_tensors_on_the_gpu(torch_cuda):
     assert (c.k == 128).all() and (c.k_scale == 0).all()
 
 
+def test_binding_refuses_another_gpu(torch_cuda, monkeypatch):
+    """All of a call is on the cache's GPU, and that is the current one. (The cache's number is changed: one GPU will do.)"""
+    torch = torch_cuda
+    announce("kv binding on another GPU")
+    c = kv.new_cache(4, 2, 80)
+    here = torch.cuda.current_device()
+    assert c.device == here and kv.new_cache(1, 1, 80, device="cpu").device == -1
+    dev = dict(dtype=torch.int32, device="cuda")
+    blocks, lens, index = torch.zeros((3, 2), **dev), torch.zeros(3, **dev), torch.zeros((3, 2, 64), **dev)
+    x, w, ws = torch.zeros((3, 2, 80), device="cuda"), torch.zeros((3, 2, 128), device="cuda"), torch.zeros(1 << 16, **dev)
+    calls = (lambda **a: kv.append(c, blocks, lens, x, x, **a), lambda **a: kv.read(c, blocks, lens, x, x, **a),
+             lambda **a: kv.attend(c, blocks, lens, x, x, **a), lambda **a: kv.attend(c, blocks, lens, x, x, weights=w, **a),
+             lambda **a: kv.attend(c, blocks, lens, x, x, ws=ws, **a),
+             lambda **a: kv.evict(c, blocks, lens, w, 64, 1, blocks.clone(), lens.clone(), None, index, **a))
+
+    class Elsewhere:
+        cuda_stream, device = 0, torch.device("cuda", here + 1)
+
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(stream=Elsewhere)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: here + 1)
+        for call in calls:
+            with pytest.raises(ValueError):
+                call()
+    c.device = here + 1
+    for call in calls:
+        with pytest.raises(TypeError):
+            call()
+    for args in ((x, 2, 80, "q", here + 1), (x, 2, 80, "q")):
+        with pytest.raises(TypeError):
+            kv._args.rows(*args)
+    with pytest.raises(TypeError):
+        kv._args.seqs(blocks, lens, None, here + 1)
+    c.device = here
+    kv.append(c, blocks, lens, x, x, stream=torch.cuda.current_stream())       # (lengths of 0: nothing is stored)
+    kv.append(c, blocks, lens, x, x, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert (c.k == 128).all() and (c.k_scale == 0).all()
+
+
 def test_tables_out_of_range_are_left_alone(torch_cuda):
     """Blocks that are not in the pool, lengths past the table, rows past the arrays: nothing outside is touched."""
     torch = torch_cuda
