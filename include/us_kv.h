@@ -138,7 +138,9 @@ typedef struct {
  * its first use and left so that any later call can use it again; calls that
  * may overlap need workspaces of their own. The size for a call without a
  * window (or without the causal mask) serves the same call with one.
- * opts = NULL: causal, the rest 0.
+ * opts = NULL: causal, the rest 0. US_ERR_SHAPE also for more than 2^25 query
+ * rows of a cache head (max_new x q_heads / heads), and for calls of many rows
+ * if batch x heads x rows / 256 (128 for head_dim above 128) passes 2^22.
  */
 us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                       int32_t tokens, const us_kv_attend_opts *opts, size_t *bytes);

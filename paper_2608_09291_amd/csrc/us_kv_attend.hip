@@ -27,6 +27,8 @@ us_status check_opts(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, con
 // The tickets, which have to be zero between calls, have a place of their own
 // that no other part of any call takes; calls of more units do not split.
 constexpr int64_t kTickets = 16384;
+// Workgroups of the prompt kernel, whose grid has one dimension of 512 threads each.
+constexpr int64_t kMostPrompt = INT32_MAX / 512;
 
 struct Plan {
     bool decode;
@@ -60,7 +62,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     const int64_t filled = c.heads * ((int64_t)tokens * G / wide + s.batch);
     const int64_t work = filled < pairs * tiles_w ? filled : pairs * tiles_w;
     int64_t best = INT64_MAX, chunk_w = most_w;
-    for (int64_t n = 1; n <= 128 && n <= most_w; ++n) {
+    for (int64_t n = 1; n <= 128 && n <= most_w && (n == 1 || n * pairs * tiles_w <= kMostPrompt); ++n) {
         const int64_t chunk = (most_w + n - 1) / n, t = (work * n + cus - 1) / cus * (chunk + (n > 1 ? 10 : 0));
         if (t < best) {
             best = t;
@@ -106,7 +108,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
     if (p.decode && ((most + p.chunk - 1) / p.chunk) * p.tiles > 65535) p.chunk = (int)((most * p.tiles + 65534) / 65535) + 1;
     p.splits = (int)((most + p.chunk - 1) / p.chunk);
-    if (units * p.splits > INT32_MAX / 512) return US_ERR_SHAPE;
+    if (!p.decode && units * p.splits > kMostPrompt) return US_ERR_SHAPE;
     p.scores_stride = up(max_len, kBlock);
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
     p.part = parts || o.weights ? 4 * kTickets : 0;        // (also where this call draws none)

@@ -496,6 +496,47 @@ def test_attend_unsplit_long(torch_cuda, lens, new, H, Hk):
     _check(torch, p, lens, new, q, out, "f16", w0, w1)
 
 
+def test_attend_many_sequences(torch_cuda):
+    """More than 2^22 cache heads in a call, a token each: every row gets its head's value."""
+    torch = torch_cuda
+    announce("kv attend 40000 sequences of 128 heads")
+    B, Hk, D = 40000, 128, 64
+    p = Pool(torch, np.random.default_rng(21), [1, 1], Hk, D)
+    cache = p.cache()
+    which = torch.randint(0, 2, (B,), device="cuda")
+    blocks = p.dev(p.blocks)[which].contiguous()            # (sequences may share blocks that are only read)
+    q = torch.randn((B, Hk, D), device="cuda", dtype=torch.bfloat16)
+    out = torch.full_like(q, math.nan)
+    kv.attend(cache, blocks, torch.ones(B, dtype=torch.int32, device="cuda"), q, out, ws=kv.attend_workspace(cache, q, blocks))
+    torch.cuda.synchronize()
+    # (the one key's probability and its sum are rounded apart: the bounds above, of one token)
+    (key, val) = (torch.stack([torch.from_numpy((p.codes[i][r[0]][:, ref.places(D, i == 0)[0]].astype(np.float64) - 128)
+                                                * p.scales[i][r[0]][:, None]) for r in p.blocks]).cuda()[which] for i in range(2))
+    reach = (q.double() * key).abs().sum(-1, keepdim=True) / math.sqrt(D)
+    e_p = 2 * (64 + 8) * 2.0 ** -24 * reach + 2.0 ** -21 + 2.0 ** -11
+    assert ((out.double() - val).abs() <= (e_p + 2.0 ** -24 + OUT["bf16"]) * val.abs() + 1e-30).all()
+
+
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("Hk,new", [(8, [300]), (2, [250, 1])])
+def test_attend_with_a_high_bound_of_rows(torch_cuda, Hk, new, tracked):
+    """max_q far above the rows that there are: the grid is bounded, the rows are right."""
+    torch = torch_cuda
+    announce(f"kv attend max_q=2^20 heads={Hk} new={new} weights={tracked}")
+    rng = np.random.default_rng(22)
+    lens = [3000, 700][:len(new)]
+    p = Pool(torch, rng, lens, Hk, 64)
+    cache, blocks = p.cache(), p.dev(p.blocks)
+    q = torch.from_numpy(rng.normal(0, 1.5, size=(sum(new), Hk, 64)).astype(np.float32)).cuda().half()
+    out = torch.full_like(q, math.nan)
+    w0 = torch.zeros((len(lens), Hk, p.width * 64), device="cuda") if tracked else None
+    w1 = None if w0 is None else w0.clone()
+    args = dict(starts=p.dev(_starts(new)), max_q=1 << 20, weights=w1)
+    kv.attend(cache, blocks, p.dev(lens), q, out, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+    torch.cuda.synchronize()
+    _check(torch, p, lens, new, q, out, "f16", w0, w1)
+
+
 @pytest.mark.parametrize("new", [1, 3, 140])
 def test_attend_large_and_small_scores(torch_cuda, new):
     """Scores of hundreds (one key takes all), scales that differ by 2^20, a block of scale 0, queries of 1e-6 and 1e5."""

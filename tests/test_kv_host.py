@@ -248,6 +248,17 @@ def test_workspace_sizes_of_edge_shapes():
             assert n.value < 1 << 42
 
 
+@pytest.mark.parametrize("batch,heads,width,max_new,tokens,q_heads", [
+    (65535, 128, 10, 1, 65535, 128), (65535, 65535, 1, 1, 65535, 65535),   # single tokens: as many as batch and heads allow
+    (1, 8, 1000, 1 << 25, 100, 8), (3, 64, 4000, 1 << 20, 50, 64),         # a high bound of the new tokens, few rows
+    (2, 4, 2000, 1 << 23, 1000, 16)])
+def test_large_calls_have_a_plan(batch, heads, width, max_new, tokens, q_heads):
+    c = kv.CacheStruct(P, P, P, P, 8, heads, 128)
+    s = kv.SeqsStruct(P, width, width, batch, P, P, max_new)
+    n = ctypes.c_size_t(0)
+    assert kv.lib().us_kv_attend_workspace_size(ctypes.byref(c), ctypes.byref(s), q_heads, tokens, None, ctypes.byref(n)) == 0
+
+
 def test_packed_structs_are_the_c_structs():
     for pack, struct, values in ((kv._pack_cache, kv.CacheStruct, (1 << 40, 2, 3, 4, 5, 6, 7)),
                                  (kv._pack_seqs, kv.SeqsStruct, (1, 1 << 40, 3, 4, 5, 6, 7)),
