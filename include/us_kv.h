@@ -147,6 +147,21 @@ us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs
 us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
                        const us_rows *out, const us_kv_attend_opts *opts, void *ws, size_t ws_bytes, void *stream);
 
+typedef struct {
+    int32_t prompt;      /* 0: the kernel for few rows of a cache head, 1: for many */
+    int32_t tile_rows;   /* rows of a workgroup                                     */
+    int32_t split_keys;  /* parts that the longest sequence's keys may be cut into  */
+    int32_t part_blocks; /* blocks of such a part                                   */
+} us_kv_attend_route_info;
+
+/*
+ * us_kv_attend_route - what us_kv_attend launches for these sizes and this
+ * type of rows on the current device (256 CUs when no device is visible).
+ * Host only; for reporting and tests. Refusals as the workspace's size.
+ */
+us_status us_kv_attend_route(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, int32_t tokens,
+                             int32_t dtype, const us_kv_attend_opts *opts, us_kv_attend_route_info *out);
+
 /* Where an eviction leaves what it keeps; none of it overlaps what the call reads. */
 typedef struct {
     const int32_t *blocks;  /* device, batch x stride: blocks of the same pool,

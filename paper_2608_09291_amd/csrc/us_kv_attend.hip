@@ -140,6 +140,19 @@ extern "C" us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const
     return st;
 }
 
+extern "C" us_status us_kv_attend_route(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, int32_t tokens,
+                                        int32_t dtype, const us_kv_attend_opts *opts, us_kv_attend_route_info *out) {
+    const us_kv_attend_opts &o = opts ? *opts : kDefault;
+    us_status st = check_opts(cache, seqs, q_heads, o);
+    if (st != US_OK) return st;
+    if (!out || dtype < US_F32 || dtype > US_F16) return US_ERR_ARG;
+    if (tokens < 1) return US_ERR_SHAPE;
+    Plan p;
+    st = plan_of(*cache, *seqs, q_heads, tokens, dtype == US_F32, o, p);
+    if (st == US_OK) *out = us_kv_attend_route_info{!p.decode, p.decode ? 16 : p.rows, p.splits, p.chunk};
+    return st;
+}
+
 extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
                                   const us_rows *out, const us_kv_attend_opts *opts, void *ws, size_t ws_bytes,
                                   void *stream) {

@@ -21,7 +21,8 @@ BLOCK = 64           # US_KV_BLOCK: tokens of a block
 HEAD_DIM_MAX = 256   # US_KV_HEAD_DIM_MAX
 
 #: Every symbol us_kv.h declares.
-EXPORTS = ("us_kv_row", "us_kv_append", "us_kv_read", "us_kv_attend_workspace_size", "us_kv_attend", "us_kv_evict")
+EXPORTS = ("us_kv_row", "us_kv_append", "us_kv_read", "us_kv_attend_workspace_size", "us_kv_attend_route",
+           "us_kv_attend", "us_kv_evict")
 
 
 class CacheStruct(ctypes.Structure):
@@ -44,6 +45,10 @@ class RowsStruct(ctypes.Structure):
 class AttendOpts(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
                 ("max_len", ctypes.c_int32), ("weights", ctypes.c_void_p), ("weights_stride", ctypes.c_int64)]
+
+
+class AttendRouteInfo(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("prompt", "tile_rows", "split_keys", "part_blocks")]
 
 
 class KeptStruct(ctypes.Structure):
@@ -70,6 +75,7 @@ def lib():
         L.us_kv_append.argtypes = [vp, vp, vp, vp, vp]
         L.us_kv_read.argtypes = [vp, vp, vp, vp, vp]
         L.us_kv_attend_workspace_size.argtypes = [vp, vp, i32, i32, vp, ctypes.POINTER(sz)]
+        L.us_kv_attend_route.argtypes = [vp, vp, i32, i32, i32, vp, ctypes.POINTER(AttendRouteInfo)]
         L.us_kv_attend.argtypes = [vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.us_kv_evict.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp, vp]
         for name in EXPORTS:
@@ -202,18 +208,34 @@ def _opts(scale, causal, window, max_len, weights, batch, heads, device):
     return _pack_opts(0.0 if scale is None else scale, 1 if causal else 0, window, max_len or 0, at, n)
 
 
+def _sizes(blocks, starts, max_q) -> bytes:
+    """The sequences of a call whose sizes alone matter: what the lengths and starts are is not looked at."""
+    batch, width, stride = _table(blocks, "blocks")
+    return _pack_seqs(blocks.data_ptr(), stride, width, batch, blocks.data_ptr(),
+                      0 if starts is None else starts.data_ptr(), max_q)
+
+
 def attend_workspace_size(cache: Cache, q_heads: int, tokens: int, blocks, starts=None, max_q: int = 1, max_len=None,
                           causal: bool = True, window: int = 0, weights=None) -> int:
     """us_kv_attend_workspace_size: device bytes us_kv_attend needs for these sizes."""
-    batch, width, stride = _table(blocks, "blocks")
-    # (what the lengths and starts are is not looked at)
-    s = _pack_seqs(blocks.data_ptr(), stride, width, batch, blocks.data_ptr(),
-                   0 if starts is None else starts.data_ptr(), max_q)
-    n = ctypes.c_size_t(0)
+    s, batch, n = _sizes(blocks, starts, max_q), blocks.shape[0], ctypes.c_size_t(0)
     _check("us_kv_attend_workspace_size", lib().us_kv_attend_workspace_size(
         cache._packed, s, q_heads, tokens, _opts(None, causal, window, max_len, weights, batch, cache.heads, cache.device),
         ctypes.byref(n)))
     return n.value
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # us_dtype
+
+
+def attend_route(cache: Cache, q, blocks, starts=None, max_q: int = 1, max_len=None, causal: bool = True, window: int = 0,
+                 weights=None) -> dict:
+    """us_kv_attend_route: what attend launches for these sizes."""
+    r, s, batch = AttendRouteInfo(), _sizes(blocks, starts, max_q), blocks.shape[0]
+    _check("us_kv_attend_route", lib().us_kv_attend_route(
+        cache._packed, s, q.shape[1], q.shape[0], _TYPES[q.dtype],
+        _opts(None, causal, window, max_len, weights, batch, cache.heads, cache.device), ctypes.byref(r)))
+    return {name: getattr(r, name) for name, _ in AttendRouteInfo._fields_}
 
 
 def attend_workspace(cache: Cache, q, blocks, starts=None, max_q: int = 1, max_len=None, causal: bool = True,

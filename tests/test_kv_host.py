@@ -259,6 +259,25 @@ def test_large_calls_have_a_plan(batch, heads, width, max_new, tokens, q_heads):
     assert kv.lib().us_kv_attend_workspace_size(ctypes.byref(c), ctypes.byref(s), q_heads, tokens, None, ctypes.byref(n)) == 0
 
 
+def test_route():
+    """Single tokens go to the kernel for few rows, whole prompts to the other; refusals as elsewhere."""
+    torch = pytest.importorskip("torch")
+    c = kv.new_cache(4, 8, 128, device="cpu")
+    blocks, starts = torch.zeros((2, 100), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        r = kv.attend_route(c, torch.zeros((2, 32, 128), dtype=dtype), blocks)
+        assert r["prompt"] == 0 and r["tile_rows"] == 16 and (r["split_keys"] - 1) * r["part_blocks"] < 100
+        r = kv.attend_route(c, torch.zeros((8000, 32, 128), dtype=dtype), blocks, starts=starts, max_q=6000)
+        assert r == dict(prompt=1, tile_rows=256, split_keys=1, part_blocks=100)
+    a, out = _valid(), kv.AttendRouteInfo()
+    r = [ctypes.byref(x) for x in a]
+    f = kv.lib().us_kv_attend_route
+    assert f(r[0], r[1], 2, 9, 1, None, ctypes.byref(out)) == 0
+    assert f(r[0], r[1], 2, 9, 1, None, None) == ARG and f(r[0], r[1], 2, 9, 3, None, ctypes.byref(out)) == ARG
+    assert f(None, r[1], 2, 9, 1, None, ctypes.byref(out)) == ARG and f(r[0], None, 2, 9, 1, None, ctypes.byref(out)) == ARG
+    assert f(r[0], r[1], 3, 9, 1, None, ctypes.byref(out)) == SHAPE and f(r[0], r[1], 2, 0, 1, None, ctypes.byref(out)) == SHAPE
+
+
 def test_packed_structs_are_the_c_structs():
     for pack, struct, values in ((kv._pack_cache, kv.CacheStruct, (1 << 40, 2, 3, 4, 5, 6, 7)),
                                  (kv._pack_seqs, kv.SeqsStruct, (1, 1 << 40, 3, 4, 5, 6, 7)),
