@@ -377,6 +377,7 @@ def test_attend_widest_windows(torch_cuda, lens, new, H, Hk, D, dtype):
     for window in (0, max(lens), 2 ** 31 - 3, 2 ** 31 - 1):
         w, out = w0.clone(), torch.full_like(q, math.nan)
         ws = kv.attend_workspace(cache, q, blocks, window=window, weights=w, **args)
+        assert kv.attend_route(cache, q, blocks, window=window, weights=w, **args)["prompt"] == (H >= 64)
         kv.attend(cache, blocks, n, q, out, window=window, weights=w, ws=ws, **args)
         torch.cuda.synchronize()
         got.append((out, w))
@@ -455,6 +456,246 @@ def test_attend_prompts(torch_cuda, lens, new, H, Hk, D, how, odd, tracked, dtyp
                 e_w = 2 * (R + 8) * 2.0 ** -24 * reach.max() + 2.0 ** -20 + (new[b] * G + n) * 2.0 ** -24
                 a, z = w0[b, hk, :n].double(), w1[b, hk, :n].double()
                 assert ((z - a - add).abs() <= e_w * add + 2.0 ** -23 * z.abs()).all(), (b, hk)
+
+
+# The kernel for prompts at the values where it has code of its own. Shapes that it takes, as the tests assert, one
+# workgroup per row tile or the keys split and joined.
+WHOLE = [([600], [500], 128, 64, 64), ([900, 70], [700, 70], 64, 16, 128), ([900], [600], 48, 24, 256)]
+SPLIT = [([6000], [500], 64, 8, 64), ([3000], [300], 64, 4, 128), ([5000, 4000], [260, 300], 64, 4, 256)]
+
+
+def _takes_prompts(q, cache, blocks, split, args):
+    r = kv.attend_route(cache, q, blocks, **args)
+    assert r["prompt"] == 1 and (r["split_keys"] > 1) == split, r
+
+
+def _check_heads(torch, p, lens, new, q, out, dtype, heads, w0=None, w1=None, scale=None, causal=True, window=0, rows=None):
+    """Cache heads `heads` of a call against float64 on the GPU. Blocks that are not in the pool are seen by no query.
+
+    The bounds are those at the top, worked out row by row, and one more: in this kernel a probability is held in
+    units of the row's largest product of probability and value scale, as float16 down to half of 2^-24 with 2^13 for
+    one, so that each key adds at most 127 2^-38 of that product."""
+    D, G, R, st = p.D, q.shape[1] // p.H, ref.row_of(p.D), _starts(new)
+    scale = 1 / math.sqrt(D) if scale is None else scale
+    top = 65504.0 if dtype == "f16" else math.inf           # (results past float16's range are infinite: compared as its largest)
+    for b, n in enumerate(lens):
+        if n == 0 or new[b] == 0:
+            continue
+        here = slice(st[b], st[b + 1])
+        ids = [blk if 0 <= blk < p.n else -1 for blk in p.blocks[b][:-(-n // 64)]]
+        there = torch.tensor(ids, device="cuda").repeat_interleave(64)[:n] >= 0
+        lo, hi = (torch.tensor(x, device="cuda")[:, None] for x in zip(*[ref.visible(i, new[b], n, causal, window)
+                                                                         for i in range(new[b])]))
+        j = torch.arange(n, device="cuda")
+        seen = ((j >= lo) & (j < hi) & there).repeat_interleave(G, dim=0)
+        for hk in heads:
+            (kc, ks), (vc, vs) = [[torch.from_numpy(x).cuda() for x in ref.tokens(p.codes[i], p.scales[i], D, i == 0,
+                                                                                  [max(x, p.good) if x < 0 else x for x in ids], n, hk)]
+                                  for i in range(2)]
+            ks, vs = torch.where(there, ks, 0.0), torch.where(there, vs, 0.0)
+            key, val = kc * ks[:, None], vc * vs[:, None]
+            x = q[here, hk * G:hk * G + G].double().reshape(-1, D)
+            scores = ((x @ key.t().contiguous()) * scale).masked_fill(~seen, -math.inf)
+            reach = ((x.abs() @ key.abs().t().contiguous()) * scale).masked_fill(~seen, 0).amax(1, keepdim=True)
+            prob = torch.softmax(scores, dim=1).masked_fill(~seen, 0)
+            want, size = prob @ val, prob @ val.abs()
+            e_s = (R + 8) * 2.0 ** -24 * reach + (2.0 ** -22 * reach if dtype == "f32" else 0)
+            e_p = (2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11)).clamp(max=2)
+            small = 127 * n * 2.0 ** -38 * (prob * vs).amax(1, keepdim=True)
+            bound = (e_p + n * 2.0 ** -24) * size + small + OUT[dtype] * want.abs() + (2.0 ** -25 if dtype == "f16" else 1e-30)
+            got = out[here, hk * G:hk * G + G].double().reshape(-1, D).clamp(-top, top)
+            assert not torch.isnan(got).any()
+            over = (got - want.clamp(-top, top)).abs() - bound
+            assert (over <= 0).all(), (b, hk, over.max())
+            if w0 is not None:
+                e_w = (torch.expm1(2 * e_s) + 2.0 ** -20 + (new[b] * G + n) * 2.0 ** -24)
+                a, z = w0[b, hk, :n].double(), w1[b, hk, :n].double()
+                assert ((z - a - prob.sum(0)).abs() <= (e_w * prob).sum(0) + 2.0 ** -23 * z.abs()).all(), (b, hk)
+                assert torch.equal(w0[b, hk, :n][~there], w1[b, hk, :n][~there]) and torch.equal(w0[b, hk, n:], w1[b, hk, n:])
+
+
+def _prompt(torch, lens, new, H, Hk, D, split, tracked, dtype, spoil, **how):
+    """A call of the kernel for prompts after `spoil(pool, q)`, which returns the cache heads to look at."""
+    rng = np.random.default_rng(sum(lens) + D)
+    p = Pool(torch, rng, lens, Hk, D)
+    p.good = p.blocks[0][0]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(sum(lens) + D)
+    q = torch.randn((sum(new), H, D), generator=gen, device="cuda")
+    heads = spoil(p, q)
+    cache, blocks = p.cache(), p.dev(p.blocks)
+    q = q.to(_torch_dtype(torch, dtype)) if dtype != "f16" else q.clamp(-6e4, 6e4).half()
+    out = torch.full_like(q, 5.0)
+    w0 = torch.rand((len(lens), Hk, p.width * 64), generator=gen, device="cuda") if tracked else None
+    w1 = None if w0 is None else w0.clone()
+    scale = how.pop("scale", None)
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w1, **how)
+    _takes_prompts(q, cache, blocks, split, args)
+    kv.attend(cache, blocks, p.dev(lens), q, out, scale=scale, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+    torch.cuda.synchronize()
+    _check_heads(torch, p, lens, new, q, out, dtype, heads, w0, w1, scale=scale, **how)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hk,D", WHOLE + SPLIT)
+def test_prompts_over_blocks_that_are_not_there(torch_cuda, lens, new, H, Hk, D, tracked, dtype):
+    """Entries outside the pool at the start (rows that see nothing else come out as zeros), in between and at the end."""
+    announce(f"kv prompts missing blocks lens={lens} new={new} H={H}/{Hk} D={D} {dtype} weights={tracked}")
+    def spoil(p, q):
+        p.good = p.blocks[0][1]
+        for row in p.blocks:
+            row[0] = p.n
+            if len(row) > 8 and row[8] >= 0:
+                row[3], row[4], row[-(-min(lens) // 64) - 1 if len(lens) == 1 else 6] = -1, -7, 1 << 30
+        return (0, Hk - 1)
+    _prompt(torch_cuda, lens, new, H, Hk, D, (lens, new, H, Hk, D) in SPLIT, tracked, dtype, spoil)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,H,Hk,D,how", [
+    (*WHOLE[0], dict(scale=0.3)), (*WHOLE[1], dict(scale=0.01)), (*SPLIT[0], dict(scale=0.2)), (*SPLIT[1], dict(scale=1e-30)),
+    (*WHOLE[0], dict(causal=False, scale=0.5)), (*WHOLE[2], dict(window=40, scale=2.0))])
+def test_prompts_with_a_scale_of_their_own(torch_cuda, lens, new, H, Hk, D, how, dtype):
+    announce(f"kv prompts lens={lens} new={new} H={H}/{Hk} D={D} {dtype} {how}")
+    _prompt(torch_cuda, lens, new, H, Hk, D, (lens, new, H, Hk, D) in SPLIT, True, dtype, lambda p, q: (0, Hk - 1), **dict(how))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,H,Hk,D", [WHOLE[0], WHOLE[1], WHOLE[2], SPLIT[0], SPLIT[1]])
+def test_prompts_keep_a_nan_in_its_row(torch_cuda, lens, new, H, Hk, D, dtype):
+    """A NaN or an infinity makes its own row NaN; every other row is the same bit for bit."""
+    torch = torch_cuda
+    announce(f"kv prompts NaN lens={lens} new={new} H={H}/{Hk} D={D} {dtype}")
+    p = Pool(torch, np.random.default_rng(6), lens, Hk, D)
+    cache, blocks, n = p.cache(), p.dev(p.blocks), p.dev(lens)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(8)
+    q = torch.randn((sum(new), H, D), generator=gen, device="cuda").to(_torch_dtype(torch, dtype))
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new))
+    _takes_prompts(q, cache, blocks, (lens, new, H, Hk, D) in SPLIT, args)
+    bad = torch.zeros((sum(new), H), dtype=torch.bool, device="cuda")
+    bad[0, 1] = bad[new[0] // 2, H - 1] = bad[new[0] - 1, 3] = True
+    got = []
+    for value in (None, math.nan, math.inf):
+        x = q.clone()
+        if value is not None:
+            x[:, :, D - 1] = torch.where(bad, value, x[:, :, D - 1])
+        out = torch.zeros_like(q)
+        kv.attend(cache, blocks, n, x, out, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+        torch.cuda.synchronize()
+        got.append(out)
+    for out in got[1:]:
+        assert torch.isnan(out[bad]).all() and torch.equal(out[~bad], got[0][~bad])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,H,Hk,D", [WHOLE[0], SPLIT[1]])
+def test_prompts_cut_to_their_arrays(torch_cuda, lens, new, H, Hk, D, dtype):
+    """Fewer rows in the array than the sequences' ranges name, or more than max_q: those there are, and no others."""
+    torch = torch_cuda
+    announce(f"kv prompts cut lens={lens} new={new} H={H}/{Hk} D={D} {dtype}")
+    p = Pool(torch, np.random.default_rng(11), lens, Hk, D)
+    cache, blocks, n = p.cache(), p.dev(p.blocks), p.dev(lens)
+    q = torch.randn((new[0] + 9, H, D), device="cuda").to(_torch_dtype(torch, dtype))
+    for rows, most, first in ((new[0], new[0], 0), (new[0] + 9, new[0], 0), (new[0] + 9, new[0] + 50, 9)):
+        out = torch.full_like(q, 7.0)
+        args = dict(starts=p.dev([first, first + new[0] + 500]), max_q=most)
+        _takes_prompts(q[:rows], cache, blocks, H == 64 and D == 128, args)
+        kv.attend(cache, blocks, n, q[:rows], out[:rows], ws=kv.attend_workspace(cache, q[:rows], blocks, **args), **args)
+        torch.cuda.synchronize()
+        assert (out[:first] == 7).all() and (out[first + new[0]:] == 7).all()
+        _check_heads(torch, p, lens, new, q[first:first + new[0]], out[first:first + new[0]], dtype, (0, Hk - 1))
+
+
+@pytest.mark.parametrize("split", [False, True])
+def test_prompts_with_offsets_past_32_bits(torch_cuda, split):
+    """Blocks and rows that lie more than 2^32 bytes into their arrays, with weights."""
+    torch = torch_cuda
+    announce(f"kv prompts offsets past 32 bits split={split}")
+    n_blocks, Hk, D, H = 70000, 8, 128, 64                  # 4.6 GB of keys
+    n, new = (2000, 400) if split else (700, 600)
+    cache = kv.Cache(*[torch.empty((n_blocks, Hk, 64 * D), dtype=torch.uint8, device="cuda") for _ in range(2)],
+                     *[torch.zeros((n_blocks, Hk), device="cuda") for _ in range(2)], D)
+    small = kv.new_cache(-(-n // 64), Hk, D)
+    far_blocks = torch.arange(n_blocks - 1, n_blocks - 1 - 2 * small.n_blocks, -2, dtype=torch.int32, device="cuda")[None].contiguous()
+    near_blocks = torch.arange(small.n_blocks, dtype=torch.int32, device="cuda")[None].contiguous()
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    x = torch.randn((n, Hk, D), generator=gen, device="cuda", dtype=torch.float16)
+    q = torch.randn((new, H, D), generator=gen, device="cuda", dtype=torch.float16)
+    stride = (1 << 32) // new                               # (elements: the last rows past 2^33 bytes)
+    stride -= stride % 8
+    far = torch.empty(new * stride + 2 * H * D, dtype=torch.float16, device="cuda")
+    q_far = far.as_strided((new, H, D), (stride, D, 1))
+    out_far = far[H * D:].as_strided((new, H, D), (stride, D, 1))
+    q_far.copy_(q)
+    got = []
+    for c, blocks, rows, out in ((small, near_blocks, q, torch.empty_like(q)), (cache, far_blocks, q_far, out_far)):
+        kv.append(c, blocks, lens, x, x, starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"), max_new=n)
+        w = torch.zeros((1, Hk, 64 * small.n_blocks), device="cuda")
+        args = dict(starts=torch.tensor([0, new], dtype=torch.int32, device="cuda"), max_q=new, weights=w)
+        _takes_prompts(rows, c, blocks, split, args)
+        kv.attend(c, blocks, lens, rows, out, ws=kv.attend_workspace(c, rows, blocks, **args), **args)
+        torch.cuda.synchronize()
+        got.append((out.clone(), w))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and got[0][0].abs().max() > 0
+    assert abs(got[0][1].double().sum().item() / (new * H) - 1) < 2.0 ** -12      # (every query gives away 1)
+
+
+def test_prompts_captured_on_another_stream(torch_cuda):
+    """A chunk (append, then attend with weights, split and not) captured in a graph, replayed between eager calls."""
+    torch = torch_cuda
+    for lens, new, H, Hk, D in (WHOLE[1], SPLIT[0]):
+        announce(f"kv prompts captured lens={lens} new={new}")
+        rng = np.random.default_rng(9)
+        p = Pool(torch, rng, [x + 64 for x in lens], Hk, D)
+        cache, eager = p.cache(), p.cache()
+        blocks, n, st = p.dev(p.blocks), p.dev(lens), p.dev(_starts(new))
+        y = torch.zeros((sum(new), H + 2 * Hk, D), device="cuda")
+        w, w2 = (torch.zeros((len(lens), Hk, p.width * 64), device="cuda") for _ in range(2))
+        out, o2 = (torch.zeros((sum(new), H, D), device="cuda") for _ in range(2))
+        args = dict(starts=st, max_q=max(new))
+        _takes_prompts(y[:, :H], cache, blocks, len(lens) == 1, dict(weights=w, **args))
+        ws, ws2 = (kv.attend_workspace(cache, y[:, :H], blocks, weights=w, **args) for _ in range(2))
+
+        def chunk(c, o, wt, wsp):
+            kv.append(c, blocks, n, y[:, H:H + Hk], y[:, H + Hk:], starts=st, max_new=max(new))
+            kv.attend(c, blocks, n, y[:, :H], o, weights=wt, ws=wsp, **args)
+
+        torch.cuda.synchronize()
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            chunk(cache, out, w, ws)
+        for i in range(4):
+            y.copy_(torch.from_numpy(rng.normal(0, 1 + i, size=y.shape).astype(np.float32)))
+            n.add_(11)
+            graph.replay()
+            torch.cuda.synchronize()
+            chunk(eager, o2, w2, ws2)
+            torch.cuda.synchronize()
+            assert torch.equal(out, o2) and torch.equal(w, w2) and torch.equal(cache.v, eager.v) and torch.equal(cache.k, eager.k)
+            assert out.abs().max() > 0
+
+
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hk,D,window", [(*SPLIT[0], 900), (*SPLIT[1], 130), (*WHOLE[1], 300)])
+def test_prompts_with_a_window_in_a_workspace_without(torch_cuda, lens, new, H, Hk, D, window, tracked):
+    """A workspace sized without a window serves the same call with one."""
+    torch = torch_cuda
+    announce(f"kv prompts windowed, workspace without: lens={lens} new={new} D={D} window={window} weights={tracked}")
+    p = Pool(torch, np.random.default_rng(13), lens, Hk, D)
+    p.good = p.blocks[0][0]
+    cache, blocks = p.cache(), p.dev(p.blocks)
+    q = torch.randn((sum(new), H, D), device="cuda").bfloat16()
+    w0 = torch.rand((len(lens), Hk, p.width * 64), device="cuda") if tracked else None
+    w1, out = None if w0 is None else w0.clone(), torch.full_like(q, math.nan)
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w1)
+    assert kv.attend_route(cache, q, blocks, **args)["prompt"] == 1
+    kv.attend(cache, blocks, p.dev(lens), q, out, ws=kv.attend_workspace(cache, q, blocks, **args), window=window, **args)
+    torch.cuda.synchronize()
+    _check_heads(torch, p, lens, new, q, out, "bf16", (0, Hk - 1), w0, w1, window=window)
 
 
 def test_attend_aligned_rows_and_scale(torch_cuda):
@@ -636,7 +877,7 @@ def test_attend_nan_stays_in_its_row(torch_cuda, new):
 
 @pytest.mark.parametrize("lens,new,H,Hk,how", [
     ([300, 70], [5, 3], 4, 2, {}), ([200], [9], 2, 1, dict(window=3)), ([130], [2], 1, 1, {}), ([64], [64], 2, 1, {}),
-    ([600], [400], 64, 32, {}), ([600], [400], 64, 32, dict(window=70))])    # (the last two for the kernel for prompts)
+    ([600], [500], 128, 64, {}), ([600], [500], 128, 64, dict(window=70))])    # (the last two for the kernel for prompts)
 def test_weights_of_keys_that_a_nan_query_does_not_see(torch_cuda, lens, new, H, Hk, how):
     """A query with a NaN or an infinity leaves NaN in the weights of the keys that it sees, and nothing in the others'."""
     torch = torch_cuda
@@ -655,6 +896,7 @@ def test_weights_of_keys_that_a_nan_query_does_not_see(torch_cuda, lens, new, H,
                     q[bad, :, 7] = value
                 w, out = torch.zeros((len(lens), Hk, p.width * 64), device="cuda"), torch.empty_like(q)
                 args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w, **how)
+                assert kv.attend_route(cache, q, blocks, **args)["prompt"] == (H >= 64)
                 kv.attend(cache, blocks, n, q, out, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
                 torch.cuda.synchronize()
                 got.append(w)
