@@ -180,10 +180,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
     };
 
     // A block's value scale goes into its exponents, so that the second product
-    // adds up in place: o is in units of 2^mo, mo the largest score plus log2 of
-    // its block's value scale that this row has seen. Neither a block that is
-    // masked for the row nor one of large values and no weight moves it.
-    float m = -INFINITY, l = 0.0f, mo = -INFINITY;
+    // adds up in place: o is in units of 2^(m + mv), m + mv the largest score plus
+    // log2 of its block's value scale that this row has seen. Neither a block that
+    // is masked for the row nor one of large values and no weight moves it. mv is
+    // kept apart from m, so that no score is large enough to take the scale's bits.
+    float m = -INFINITY, l = 0.0f, mv = -INFINITY;
     f32x16 o[NT], sa[2], sb[2];                            // scores of a block and of the next one, in turn
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -236,6 +237,18 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[y][v]);
         return fmaxf(top, __shfl_xor(top, 32, 64));
     };
+    // Past 2^18 the lift and the unit would be rounded off beside a score: there scores go down by
+    // m first, rounded as its own product was, so that none is above it.
+    auto hold_large = [&](f32x16 (&x)[2], float fk, float bm, float &fs, float &sub, float rest) {
+#pragma clang fp contract(off)
+        if (NT <= 4 && !__builtin_amdgcn_ballot_w64(fabsf(bm) > 262144.0f)) return;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[y][v] = x[y][v] * fk - bm;
+        fs = 1.0f;
+        sub = rest;
+    };
     // Scores are computed one block ahead of their exponentials, so that the
     // matrix cores work on the next scores under a block's exponentials, and on
     // its second product under the staging of later blocks, in one wavefront.
@@ -268,17 +281,19 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         // (-200: of a scale of 0, whose values count for nothing)
         const float lv = fmaxf(__builtin_amdgcn_logf(vs[0]), -200.0f);
         // The maxima may lag behind by 2^kSlack before sums are brought to new ones.
-        const float t1 = top * fk, t2 = t1 + lv;
+        const float t1 = top * fk;
         if (t1 > m + kSlack || m == -INFINITY) {
-            const float m2 = fmaxf(m, t1);
-            l *= __builtin_amdgcn_exp2f(m - base_of(m2));
+            const float m2 = fmaxf(m, t1), down = m - base_of(m2);
+            l *= __builtin_amdgcn_exp2f(down);
+            mv += down;                                    // (o as it is, in units of the new m)
             m = m2;
         }
+        const float bm = base_of(m), t2 = t1 - bm + lv;
         float change = 1.0f;
-        if (t2 > mo + kSlack || mo == -INFINITY) {
-            const float m2 = fmaxf(mo, t2);
-            change = __builtin_amdgcn_exp2f(mo - base_of(m2));
-            mo = m2;
+        if (t2 > mv + kSlack || mv == -INFINITY) {
+            const float m2 = fmaxf(mv, t2);
+            change = __builtin_amdgcn_exp2f(mv - base_of(m2));
+            mv = m2;
         }
         if (__builtin_amdgcn_ballot_w64(change != 1.0f)) {
 #pragma unroll
@@ -287,8 +302,9 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
                 for (int v = 0; v < 16; ++v) o[t][v] *= change;
         }
         // (60: values of less than 2^-60 of what o holds are lost in it, weights are not)
-        const float bm = base_of(m), unit = fminf(base_of(mo) - lv, bm + 60.0f), sub = unit - kLift;
-        float sum = 0.0f;
+        const float unit = fminf(base_of(mv) - lv, 60.0f);                     // of p, over 2^m
+        float fs = fk, sub = bm + (unit - kLift), sum = 0.0f;
+        hold_large(s, fk, bm, fs, sub, unit - kLift);
         f16x8 ph[4], pl[4];
         if constexpr (kEarly) scores(i + 1, next);         // (of no use after the last block)
 #pragma unroll
@@ -296,12 +312,12 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
             float p[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                p[e] = __builtin_amdgcn_exp2f(fmaf(s[j >> 1][8 * (j & 1) + e], fk, -sub));
+                p[e] = __builtin_amdgcn_exp2f(fmaf(s[j >> 1][8 * (j & 1) + e], fs, -sub));
                 sum += p[e];
             }
             halve<SPLIT>(p, ph[j], pl[j]);
         }
-        l = fmaf(sum, __builtin_amdgcn_exp2f(unit - bm), l);
+        l = fmaf(sum, __builtin_amdgcn_exp2f(unit), l);
         // (keeps the exponentials here, beside the scores' product)
         __asm__ volatile("" : "+v"(ph[0]), "+v"(ph[1]), "+v"(ph[2]), "+v"(ph[3]), "+v"(l));
         if (kEarly && i + 1 < count) hide(i + 1, ks[1], next);
@@ -334,7 +350,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         if (i + 1 < count) step(i + 1, std::integral_constant<int, 1>(), sb, sa);
     }
     l += __shfl_xor(l, 32, 64);
-    const float to_m = __builtin_amdgcn_exp2f(mo - base_of(m));
+    const float to_m = __builtin_amdgcn_exp2f(mv);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll

@@ -539,6 +539,78 @@ def _prompt(torch, lens, new, H, Hk, D, split, tracked, dtype, spoil, **how):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("tracked", [False, True])
 @pytest.mark.parametrize("lens,new,H,Hk,D", WHOLE + SPLIT)
+def test_prompts_of_large_and_small_scores(torch_cuda, lens, new, H, Hk, D, tracked, dtype):
+    """Scores of hundreds (one key takes all), scales that differ by 2^20, blocks of scale 0, queries of 1e-6 and 100."""
+    announce(f"kv prompts extremes lens={lens} new={new} H={H}/{Hk} D={D} {dtype} weights={tracked}")
+    def spoil(p, q):
+        for row in p.blocks:
+            for j, (i, by) in enumerate(((0, 60.0), (1, 2.0 ** 20), (1, 0.0), (0, 0.0))):
+                if row[min(1 + j, len(row) - 1)] >= 0:
+                    p.scales[i][row[min(1 + j, len(row) - 1)]] *= np.float32(by)
+        q[0, 1] *= 1e-6
+        q[-1, 0] *= 1e2
+        q[new[0] // 2, -1] *= 1e-6
+        q[new[0] // 2 + 1, -2] *= 1e2
+        return (0, Hk - 1)
+    _prompt(torch_cuda, lens, new, H, Hk, D, (lens, new, H, Hk, D) in SPLIT, tracked, dtype, spoil)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("factor", [3e3, 1e5, 1e7, 1e10])
+@pytest.mark.parametrize("lens,new,H,Hk,D", WHOLE + SPLIT)
+def test_attend_scores_of_millions(torch_cuda, lens, new, H, Hk, D, factor, dtype):
+    """Scores up to 10^12. Where one key is ahead by more than scores can be off, the row is that key's value.
+
+    Off by the roundings of its probability, of the sums and of the result, and by what the others may add: keys that
+    lag behind by 20 and twice the error of both scores have less than e^-20 of its probability each."""
+    torch = torch_cuda
+    announce(f"kv attend large scores lens={lens} new={new} H={H}/{Hk} D={D} factor={factor} {dtype}")
+    if dtype == "f16" and factor > 1e5:
+        pytest.skip("past float16's range")
+    p = Pool(torch, np.random.default_rng(sum(lens)), lens, Hk, D)
+    for row in p.blocks:                                    # scales of values that no power of two makes alike
+        for j, blk in enumerate(row):
+            if blk >= 0:
+                p.scales[1][blk] = np.float32(0.01 * 1.37 ** (j % 11))
+    cache, blocks, R, G = p.cache(), p.dev(p.blocks), ref.row_of(D), H // Hk
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(17)
+    q = torch.randn((sum(new), H, D), generator=gen, device="cuda") * factor
+    q = q.clamp(-6e4, 6e4).half() if dtype == "f16" else q.to(_torch_dtype(torch, dtype))
+    out = torch.full_like(q, math.nan)
+    st = _starts(new)
+    args = dict(starts=p.dev(st), max_q=max(new))
+    assert kv.attend_route(cache, q, blocks, **args)["prompt"] == (sum(new) > 10)
+    kv.attend(cache, blocks, p.dev(lens), q, out, ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+    torch.cuda.synchronize()
+    clear = rows = 0
+    for b, n in enumerate(lens):
+        for hk in {0, Hk - 1}:
+            (kc, ks), (vc, vs) = [[torch.from_numpy(x).cuda() for x in ref.tokens(p.codes[i], p.scales[i], D, i == 0,
+                                                                                  p.blocks[b][:-(-n // 64)], n, hk)] for i in range(2)]
+            key, val = kc * ks[:, None], vc * vs[:, None]
+            x = q[st[b]:st[b + 1], hk * G:hk * G + G].double().reshape(-1, D)
+            at = (n - new[b] + torch.arange(new[b], device="cuda")).repeat_interleave(G)[:, None]
+            seen = torch.arange(n, device="cuda") <= at
+            scores = ((x @ key.t().contiguous()) / math.sqrt(D)).masked_fill(~seen, -math.inf)
+            reach = ((x.abs() @ key.abs().t().contiguous()) / math.sqrt(D)).masked_fill(~seen, 0).amax(1)
+            e_s = (R + 8) * 2.0 ** -24 * reach + (2.0 ** -22 * reach if dtype == "f32" else 0)
+            top = scores.topk(min(2, n), dim=1)
+            lead = top.values[:, 0] - (top.values[:, 1] if n > 1 else -math.inf)
+            ok = lead > 20 + 4 * e_s
+            want = val[top.indices[:, 0]][ok]
+            got = out[st[b]:st[b + 1], hk * G:hk * G + G].double().reshape(-1, D)[ok]
+            assert torch.isfinite(out[st[b]:st[b + 1], hk * G:hk * G + G]).all()
+            bound = ((2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11) + n * 2.0 ** -24 + OUT[dtype]) * want.abs()
+                     + n * math.exp(-20) * val.abs().max() + 2.0 ** -25)
+            assert ((got - want).abs() <= bound).all(), (b, hk, ((got - want).abs() - bound).max())
+            clear, rows = clear + int(ok.sum()), rows + ok.numel()
+    assert clear > 0.9 * rows
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tracked", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hk,D", WHOLE + SPLIT)
 def test_prompts_over_blocks_that_are_not_there(torch_cuda, lens, new, H, Hk, D, tracked, dtype):
     """Entries outside the pool at the start (rows that see nothing else come out as zeros), in between and at the end."""
     announce(f"kv prompts missing blocks lens={lens} new={new} H={H}/{Hk} D={D} {dtype} weights={tracked}")
