@@ -25,6 +25,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLift = 13.0f;                             // log2 of a probability's form at m
+constexpr float kLarge = 262144.0f;                        // scores past which the lift is not added to the maximum
 constexpr float kSlack = 2.0f;                             // what m may lag behind the maximum: 2^15 at most
 
 // How a launch splits a row's keys, and what it leaves in the workspace: per

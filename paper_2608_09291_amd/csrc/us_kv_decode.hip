@@ -166,12 +166,19 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         m = m2;
         l *= alpha;
         f16x8 ph[2], pl[2];
+        float sub = to - kLift;
+        // (beside larger scores the lift would be rounded, past float16 from 2^25 on)
+        if (__builtin_amdgcn_ballot_w64(fabsf(to) > kLarge)) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] -= to;
+            sub = -kLift;
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float p[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                p[e] = __builtin_amdgcn_exp2f(s[2 * u + (e >> 2)][e & 3] - (to - kLift));
+                p[e] = __builtin_amdgcn_exp2f(s[2 * u + (e >> 2)][e & 3] - sub);
                 l += p[e];
             }
             halve<SPLIT>(p, ph[u], pl[u]);

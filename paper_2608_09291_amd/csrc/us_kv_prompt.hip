@@ -237,11 +237,11 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[y][v]);
         return fmaxf(top, __shfl_xor(top, 32, 64));
     };
-    // Past 2^18 the lift and the unit would be rounded off beside a score: there scores go down by
+    // Past kLarge the lift and the unit would be rounded off beside a score: there scores go down by
     // m first, rounded as its own product was, so that none is above it.
     auto hold_large = [&](f32x16 (&x)[2], float fk, float bm, float &fs, float &sub, float rest) {
 #pragma clang fp contract(off)
-        if (NT <= 4 && !__builtin_amdgcn_ballot_w64(fabsf(bm) > 262144.0f)) return;
+        if (NT <= 4 && !__builtin_amdgcn_ballot_w64(fabsf(bm) > kLarge)) return;
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
