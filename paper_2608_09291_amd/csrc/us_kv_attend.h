@@ -25,7 +25,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLift = 13.0f;                             // log2 of a probability's form at m
-constexpr float kLarge = 262144.0f;                        // scores past which the lift is not added to the maximum
+constexpr float kLarge = 1024.0f;                          // scores past which the lift is not added to the maximum
 constexpr float kSlack = 2.0f;                             // what m may lag behind the maximum: 2^15 at most
 
 // How a launch splits a row's keys, and what it leaves in the workspace: per
@@ -37,7 +37,7 @@ struct Split {
     float *part;      // the rows of a split, then their (m, l): rows (R + 2) floats, to a multiple of 4
     int32_t *tickets;
     // For the weights, by cache head and row_block(), 32 rows each; else NULL.
-    float *lse;       // m + log2 l, +inf for a row without keys
+    float2 *ml;       // m and 2^13 / l, apart: the logarithm of l would lose its bits in m; zeros for a row without keys
     int64_t row_blocks;                                    // of a head
     // of prompts: the rows' float16 form by (part, octet, row), and f without the key scale
     f16x8 *qn;
@@ -179,7 +179,7 @@ __device__ inline void put_quad(const Args &a, int row, int head, int quad, f32x
     }
 }
 
-__device__ inline float lse_of(float m, float l) { return l == 0.0f ? INFINITY : base_of(m) - kLift + __builtin_amdgcn_logf(l); }
+__device__ inline float2 ml_of(float m, float l) { return make_float2(base_of(m), l == 0.0f ? 0.0f : 8192.0f / l); }
 
 // Partial results pass from one workgroup to another, on another XCD with an L2
 // of its own: they are stored through to memory and loaded past the L2 (sc1, the

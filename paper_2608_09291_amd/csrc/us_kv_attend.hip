@@ -35,7 +35,7 @@ struct Plan {
     int chunk, splits, tiles, rows, mix;
     int64_t scores_stride;
     int64_t row_blocks;
-    size_t part, lse, qf, qn, scores, total;
+    size_t part, ml, qf, qn, scores, total;
 };
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -112,11 +112,11 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     p.scores_stride = up(max_len, kBlock);
     const size_t parts = p.splits > 1 ? (size_t)(units * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4 : 0;
     p.part = parts || o.weights ? 4 * kTickets : 0;        // (also where this call draws none)
-    p.lse = p.part + parts;
+    p.ml = p.part + parts;
     // (one block past the last is read)
     p.row_blocks = (int64_t)tokens * (q_heads / c.heads) / 32 + s.batch + 2;
     const size_t rows32 = o.weights ? (size_t)(c.heads * p.row_blocks * 32) : 0;
-    p.qf = p.lse + 4 * rows32;
+    p.qf = p.ml + 8 * rows32;
     p.qn = p.qf + (p.decode ? 0 : 4 * rows32);
     p.scores = p.qn + (p.decode ? 0 : (f32 ? 4 : 2) * R * rows32);
     p.total = p.scores + (o.weights && p.decode ? (size_t)(pairs * p.tiles * p.rows * p.scores_stride) * 4 : 0);
@@ -188,7 +188,7 @@ extern "C" us_status us_kv_attend(const us_kv_cache *cache, const us_kv_seqs *se
     a.out = Rows{out->data, out->token_stride, out->head_stride};
     a.mask = Mask{o.causal, o.window};
     a.sp = Split{p.chunk, p.splits, p.tiles, p.rows, p.mix, (float *)(w + p.part), (int32_t *)w,
-                 o.weights ? (float *)(w + p.lse) : nullptr, p.row_blocks,
+                 o.weights ? (float2 *)(w + p.ml) : nullptr, p.row_blocks,
                  o.weights && !p.decode ? (f16x8 *)(w + p.qn) : nullptr, (float *)(w + p.qf),
                  o.weights && p.decode ? (float *)(w + p.scores) : nullptr, p.scores_stride};
     const hipStream_t hs = (hipStream_t)stream;

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
         l *= alpha;
         f16x8 ph[2], pl[2];
         float sub = to - kLift;
-        // (beside larger scores the lift would be rounded, past float16 from 2^25 on)
+        // (beside larger ones the lift would be rounded, past float16's range from 2^25 on)
         if (__builtin_amdgcn_ballot_w64(fabsf(to) > kLarge)) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) s[u] -= to;
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
             const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
             if (ns == 1) {
                 put_octet<DT>(a, r0 + ti, hd, c0 / 8 + oc, x, ll);
-                if (a.sp.lse && c0 == 0 && oc == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
+                if (a.sp.ml && c0 == 0 && oc == 0) a.sp.ml[32 * row_block(a, hk, b, r0, gr) + gr % 32] = ml_of(am, ll);
             } else {
                 const uint32_t dst = split * one + rr * R + c0 + 8 * oc;
                 mem.put(dst, (f32x4){x[0], x[1], x[2], x[3]});
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     auto finish = [&](int it, f32x4 x) {
         const int gr = base + it / (R / 4), quad = it % (R / 4), ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
         put_quad<DT>(a, r0 + ti, hd, quad, x, ll);
-        if (a.sp.lse && quad == 0) a.sp.lse[32 * row_block(a, hk, b, r0, gr) + gr % 32] = lse_of(am, ll);
+        if (a.sp.ml && quad == 0) a.sp.ml[32 * row_block(a, hk, b, r0, gr) + gr % 32] = ml_of(am, ll);
     };
     if (runs > 1) {
         f32x4 x = {0, 0, 0, 0};
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kThreads, NT > 4 ? 1 : 2) void us_kv_decode_kernel(
     }
 }
 
-// weights[b, hk, j] += sum over the rows of 2^(x_j - lse): four keys per thread, and a quarter of a
+// weights[b, hk, j] += sum over the rows of 2^(x_j - m) / l: four keys per thread, and a quarter of a
 // tile's rows per wavefront where there are more than two.
 __global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, float *weights, int64_t stride, int shared) {
     __shared__ f32x4 part[kWaves][64];
@@ -338,17 +338,17 @@ __global__ __launch_bounds__(kThreads) void us_kv_weights_saved_kernel(Args a, f
         a.mask.range(base / a.G, n, len, lo, x);
         a.mask.range((min(base + kRows, total) - 1) / a.G, n, len, x, hi);
         if (j0 < lo / kBlock * kBlock || j0 >= hi) continue;
-        const float *z = a.sp.lse + 32 * row_block(a, hk, b, r0, base) + base % 32;
+        const float2 *row_ml = a.sp.ml + 32 * row_block(a, hk, b, r0, base) + base % 32;
         const float *s = a.sp.scores + (bh * a.sp.rows * a.sp.tiles + base) * a.sp.scores_stride + j0;
         const int end = min(first + each, total - base);
 #pragma unroll 4
         for (int r = first; r < end; ++r) {
             const f32x4 y = *(const f32x4 *)(s + r * a.sp.scores_stride);
-            const float zr = z[r];
+            const float2 ml = row_ml[r];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float e = __builtin_amdgcn_exp2f(y[v] - zr);
-                sum[v] += y[v] == -INFINITY ? 0.0f : e;    // (a masked key, whatever the row's sum is)
+                const float e = fmaf(__builtin_amdgcn_exp2f(y[v] - ml.x), ml.y, sum[v]);
+                sum[v] = y[v] == -INFINITY ? sum[v] : e;   // (a masked key, whatever the row's sum is)
             }
         }
     }

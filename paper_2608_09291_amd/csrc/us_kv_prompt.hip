@@ -24,6 +24,10 @@ constexpr int weights_blocks(int row, bool f32) { return row <= 192 || !f32 ? 2 
 constexpr bool prompt_low(int row, bool f32) { return f32 && row > 64 && row <= 128; }
 constexpr int prompt_stages(int row, bool f32) { return row <= 128 && !prompt_low(row, f32) ? 4 : 2; }
 
+// A score's distance from m as that of its own float: x is the same before its rounding. Both
+// passes take a large score's like this, so that the largest one's is 0.
+__device__ inline float above(float x, float m) { return (x + m) - m; }
+
 template <int NT, int DT, int W>
 __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
     using T = typename Type<DT>::T;
@@ -237,15 +241,14 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[y][v]);
         return fmaxf(top, __shfl_xor(top, 32, 64));
     };
-    // Past kLarge the lift and the unit would be rounded off beside a score: there scores go down by
-    // m first, rounded as its own product was, so that none is above it.
+    // Past kLarge the lift and the unit would be rounded off beside a score: there scores go down by m
+    // first.
     auto hold_large = [&](f32x16 (&x)[2], float fk, float bm, float &fs, float &sub, float rest) {
-#pragma clang fp contract(off)
         if (NT <= 4 && !__builtin_amdgcn_ballot_w64(fabsf(bm) > kLarge)) return;
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[y][v] = x[y][v] * fk - bm;
+            for (int v = 0; v < 16; ++v) x[y][v] = above(fmaf(x[y][v], fk, -bm), bm);
         fs = 1.0f;
         sub = rest;
     };
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
         const float lv = fmaxf(__builtin_amdgcn_logf(vs[0]), -200.0f);
         // The maxima may lag behind by 2^kSlack before sums are brought to new ones.
         const float t1 = top * fk;
-        if (t1 > m + kSlack || m == -INFINITY) {
+        if (t1 - m > kSlack || m == -INFINITY) {
             const float m2 = fmaxf(m, t1), down = m - base_of(m2);
             l *= __builtin_amdgcn_exp2f(down);
             mv += down;                                    // (o as it is, in units of the new m)
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
 #pragma unroll
         for (int z = 0; z < 4; ++z)
             put_quad<DT>(a, r0 + i, head, 8 * t + 2 * z + h, (f32x4){o[t][4 * z], o[t][4 * z + 1], o[t][4 * z + 2], o[t][4 * z + 3]}, l);
-    if (a.sp.lse && h == 0) a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32] = lse_of(m, l);
+    if (a.sp.ml && h == 0) a.sp.ml[32 * row_block(a, hk, b, r0, row) + row % 32] = ml_of(m, l);
 }
 
 // Joins the splits of a row: a thread per quad of its values. (The last workgroup of a tile
@@ -414,11 +417,11 @@ __global__ __launch_bounds__(256) void us_kv_join_kernel(Args a) {
         for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], w, x[e]);
     }
     put_quad<DT>(a, r0 + row / a.G, hk * a.G + row % a.G, quad, x, l);
-    if (a.sp.lse && quad == 0) a.sp.lse[32 * row_block(a, hk, b, r0, row) + row % 32] = lse_of(m, l);
+    if (a.sp.ml && quad == 0) a.sp.ml[32 * row_block(a, hk, b, r0, row) + row % 32] = ml_of(m, l);
 }
 
-// The probabilities' sums over the query rows, from the logarithms of the rows'
-// sums: the first product again, the other way about. A wavefront keeps a block
+// The probabilities' sums over the query rows, from the rows' maxima and sums:
+// the first product again, the other way about. A wavefront keeps a block
 // of keys in registers; the rows, in the form that the first pass left them,
 // pass through LDS, in three stages. Scores are computed 32 rows ahead of their
 // exponentials, so that the matrix cores work under these. Chunks of 512 on
@@ -435,7 +438,8 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
     static_assert(kBlocks * kForm % 256 == 0);
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     f16x8(*q)[kBlocks * kForm] = (f16x8(*)[kBlocks * kForm])lds;               // stage; row block, part, octet, row
-    __shared__ float row_f[3][64], row_z[3][64];
+    __shared__ float row_f[3][64];
+    __shared__ float2 row_ml[3][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5, hk = blockIdx.y, b = blockIdx.z;
     int r0, n;
@@ -465,22 +469,24 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
     const int64_t rb = row_block(a, hk, b, r0, 0);
     const f16x8 *src = a.sp.qn + rb * kForm;
     f16x8 piece[kPieces];
-    float f_next = 0.0f, z_next = 0.0f;
+    float f_next = 0.0f;
+    float2 ml_next = make_float2(0.0f, 0.0f);
     auto fetch = [&](int x) {                              // row blocks x .. (there is one past the last)
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) piece[y] = src[(int64_t)x * kForm + tid + 256 * y];
-        if (tid < 32 * kBlocks) {
-            f_next = a.sp.qf[32 * (rb + x) + tid];
-            z_next = a.sp.lse[32 * (rb + x) + tid];
-        }
+        if (tid < 32 * kBlocks) f_next = a.sp.qf[32 * (rb + x) + tid];
+        if (lane < 32 * kBlocks) ml_next = a.sp.ml[32 * (rb + x) + lane];      // (by every wavefront, for put)
     };
-    auto put = [&](int buf) {
+    // Returns how many rows of these, from row block x on, have a maximum past kLarge.
+    auto put = [&](int buf, int x) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) q[buf][tid + 256 * y] = piece[y];
         if (tid < 32 * kBlocks) {
             row_f[buf][tid] = f_next;
-            row_z[buf][tid] = z_next;
+            row_ml[buf][tid] = ml_next;
         }
+        // (rows past the last hold anything)
+        return __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < 32 * kBlocks && 32 * x + lane < total && fabsf(ml_next.x) > kLarge));
     };
     fetch(first);
     f16x8 kf[2][NS];
@@ -514,15 +520,25 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
                 for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[u][t], qf, s[u], 0, 0, 0);
             }
     };
-    auto add = [&](int x, float fk, float z, const f32x16 (&s)[2]) {           // row block x
+    auto add = [&](int x, float fk, float2 ml, int large, f32x16 (&s)[2]) {    // row block x
         const int base = 32 * x;
+        // (ahead of the branches, so that they go beside the next scores' product: 6 % of the kernel)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[u][v] = fmaf(s[u][v], fk, -ml.x);
+        if (__builtin_expect(large != 0, 0)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[u][v] = above(s[u][v], ml.x);
+        }
         if (base >= all0 && base + 32 <= all1) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sum[u][v] += __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
+                for (int v = 0; v < 16; ++v) sum[u][v] = fmaf(__builtin_amdgcn_exp2f(s[u][v]), ml.y, sum[u][v]);
         } else {
-            // (rows past the last hold anything)
             int from = 0, to = 0;
             if (base + c < total) a.mask.range((base + c) / a.G, n, len, from, to);
             from -= k0 + 4 * h;
@@ -532,7 +548,7 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int j = 32 * u + 8 * (v >> 2) + (v & 3);
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[u][v], fk, -z));
+                    const float p = __builtin_amdgcn_exp2f(s[u][v]) * ml.y;
                     sum[u][v] += j >= from && j < to ? p : 0.0f;
                 }
         }
@@ -540,20 +556,21 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
     // Stage i % 3 holds chunk i: while chunk i is added up and the first scores of
     // chunk i + 1 are taken, chunk i + 2 is put, and i + 3 is on its way.
     const int chunks = (end - first + kBlocks - 1) / kBlocks;
-    put(0);
+    int large = put(0, first), large1 = 0, large2 = 0;     // of this chunk and the next ones
     if (chunks > 1) {
         fetch(first + kBlocks);
-        put(1);
+        large1 = put(1, first + kBlocks);
     }
     if (chunks > 2) fetch(first + 2 * kBlocks);
     __syncthreads();
     scores(0, 0, sa);
     auto turn = [&](int i, int x, int y, f32x16 (&s)[2], f32x16 (&next)[2]) {  // row block y of chunk i, the x-th
         const int buf = i % 3;
-        const float fk = row_f[buf][32 * y + c] * ks, z = row_z[buf][32 * y + c];
+        const float fk = row_f[buf][32 * y + c] * ks;
+        const float2 ml = row_ml[buf][32 * y + c];
         if (y + 1 < kBlocks) scores(buf, y + 1, next);
         else scores((i + 1) % 3, 0, next);                 // (of no use after the last chunk)
-        add(x, fk, z, s);
+        add(x, fk, ml, large, s);
     };
     for (int i = 0; i < chunks; ++i) {
         const int x = first + i * kBlocks;
@@ -565,7 +582,9 @@ __global__ __launch_bounds__(256, NT > 4 || (NT > 3 && DT == US_F32) ? 1 : 2) vo
 #pragma unroll
             for (int u = 0; u < 2; ++u) sa[u] = sb[u];
         }
-        if (i + 2 < chunks) put((i + 2) % 3);
+        if (i + 2 < chunks) large2 = put((i + 2) % 3, x + 2 * kBlocks);
+        large = large1;
+        large1 = large2;
         if (i + 3 < chunks) fetch(x + 3 * kBlocks);
         __syncthreads();
     }
@@ -632,7 +651,7 @@ hipError_t launch_weights(int dtype, const Args &a, int batch, float *weights, i
             constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
             constexpr int kLds = 3 * (DT == US_F32 ? 2 : 1) * 32 * weights_blocks(32 * NT, DT == US_F32) * 32 * NT * 2;
             auto kern = us_kv_weights_kernel<NT, DT>;
-            if constexpr (kLds > 65536 - 2048) {
+            if constexpr (kLds > 65536 - 4096) {
                 static std::atomic<unsigned long long> set{0};
                 const hipError_t e = allow_lds(kern, set);
                 if (e != hipSuccess) return e;

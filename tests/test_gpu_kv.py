@@ -609,6 +609,32 @@ def test_attend_scores_of_millions(torch_cuda, lens, new, H, Hk, D, factor, dtyp
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("factor", [1.0, 3e3, 1e5, 1e7])
+@pytest.mark.parametrize("lens,new,H,Hk,D", [([450], [3], 2, 1, 64), ([5000, 300], [1, 1], 8, 1, 128), ([700], [9], 6, 3, 256)] + WHOLE + SPLIT)
+def test_weights_of_a_query_add_up_to_one(torch_cuda, lens, new, H, Hk, D, factor, dtype):
+    """However large the scores are: off by 2^-20 of each for the exponentials, and by the roundings of the sums."""
+    torch = torch_cuda
+    announce(f"kv weights of large scores lens={lens} new={new} H={H}/{Hk} D={D} factor={factor} {dtype}")
+    if dtype == "f16" and factor > 1e5:
+        pytest.skip("past float16's range")
+    p = Pool(torch, np.random.default_rng(sum(lens)), lens, Hk, D)
+    cache, blocks, G = p.cache(), p.dev(p.blocks), H // Hk
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(19)
+    q = torch.randn((sum(new), H, D), generator=gen, device="cuda") * factor
+    q = q.clamp(-6e4, 6e4).half() if dtype == "f16" else q.to(_torch_dtype(torch, dtype))
+    w = torch.zeros((len(lens), Hk, p.width * 64), device="cuda")
+    args = dict(starts=p.dev(_starts(new)), max_q=max(new), weights=w)
+    assert kv.attend_route(cache, q, blocks, **args)["prompt"] == (sum(new) > 10)
+    kv.attend(cache, blocks, p.dev(lens), q, torch.empty_like(q), ws=kv.attend_workspace(cache, q, blocks, **args), **args)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        rows = min(new[b], n) * G                           # (a query before the first key gives nothing)
+        got = w[b].double().sum(-1)
+        assert ((got / rows - 1).abs() <= 2.0 ** -20 + (n + rows) * 2.0 ** -24).all(), (b, (got / rows - 1).abs().max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("tracked", [False, True])
 @pytest.mark.parametrize("lens,new,H,Hk,D", WHOLE + SPLIT)
 def test_prompts_over_blocks_that_are_not_there(torch_cuda, lens, new, H, Hk, D, tracked, dtype):
