@@ -10,7 +10,6 @@
 namespace us_kv {
 namespace {
 
-
 // A block's keys and values as float16 in LDS, in the order of the operands:
 // 16 bytes (8 values of a key; 8 keys of a value) per lane.
 template <int R>
@@ -29,7 +28,7 @@ constexpr int prompt_stages(int row, bool f32) { return row <= 128 && !prompt_lo
 __device__ inline float above(float x, float m) { return (x + m) - m; }
 
 template <int NT, int DT, int W>
-__global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a, int units) {
+__global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Args a) {
     using T = typename Type<DT>::T;
     constexpr int kThreads = 64 * W, kRows = 32 * W;       // 32 rows per wavefront
     constexpr StageOrder kOrder{prompt_stages(32 * NT, DT == US_F32)};
@@ -67,11 +66,12 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
     const int ns = splits_of(lo0, hi1, a.sp.chunk);
     if (split >= ns) return;
     const int start = first + split * a.sp.chunk, stop = min(start + a.sp.chunk, end);
-    // This wavefront's rows, and this lane's; the range of keys that they see.
+    // This wavefront's first and last row: keys [all0, all1) are seen by both, and so by all between.
+    // Then this lane's row and the keys that it sees.
     const int w0 = min(base + 32 * wave, last_row), w1 = min(base + 32 * wave + 31, last_row);
-    int wlo, whi, wlo1, whi0;
-    a.mask.range(w0 / a.G, n, len, wlo, whi0);
-    a.mask.range(w1 / a.G, n, len, wlo1, whi);
+    int all0, all1, unused;
+    a.mask.range(w0 / a.G, n, len, unused, all1);
+    a.mask.range(w1 / a.G, n, len, all0, unused);
     const int row = min(base + 32 * wave + c, last_row), i = row / a.G, head = hk * a.G + row - i * a.G;
     const bool real = base + 32 * wave + c <= last_row;
     int lo, hi;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * W, NT > 4 ? 1 : 2) void us_kv_prompt_kernel(Ar
     };
     auto hide = [&](int i, float ks, f32x16 (&x)[2]) {     // the masked keys of block i
         const int k0 = (start + i) * kBlock;
-        if (k0 >= wlo1 && k0 + kBlock <= whi0 && ks >= 0.0f) return;
+        if (k0 >= all0 && k0 + kBlock <= all1 && ks >= 0.0f) return;
         int from = ks < 0.0f ? kBlock : lo - k0 - 4 * h, to = hi - k0 - 4 * h;
         __asm__ volatile("" : "+v"(from), "+v"(to));       // keeps the branch: most blocks have no masked keys
 #pragma unroll
@@ -633,8 +633,7 @@ hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream
                 const hipError_t e = allow_lds(kern, set);
                 if (e != hipSuccess) return e;
             }
-            const int units = batch * a.heads;
-            hipLaunchKernelGGL(kern, dim3((unsigned)units * a.sp.tiles * a.sp.splits), dim3(64 * W), kLds, stream, a, units);
+            hipLaunchKernelGGL(kern, dim3((unsigned)batch * a.heads * a.sp.tiles * a.sp.splits), dim3(64 * W), kLds, stream, a);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess || a.sp.splits == 1) return e;
             constexpr int kEach = 256 / (8 * NT);
