@@ -135,6 +135,51 @@ def test_append_and_read(torch_cuda, lens, new, heads, D, dtype):
                 assert (off <= step * (0.5 + 127 * 2.0 ** -22)).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("growth", ["every", "some", "first"])
+def test_blocks_filled_token_by_token(torch_cuda, growth, dtype):
+    """What a step stores stays near its source while the block's scale grows under it, up to 63 times.
+
+    A code is off by half a step when stored, and by half a step of the new scale each time that it is rounded again;
+    each of these roundings is done on a float32 quotient or product, off by 127 2^-23 of a step at most."""
+    torch = torch_cuda
+    announce(f"kv append token by token, growth={growth} {dtype}")
+    rng = np.random.default_rng(41)
+    B, heads, D, n = 2, 3, 96, 150
+    p = Pool(torch, rng, [n] * B, heads, D)
+    cache, blocks, lens = p.cache(), p.dev(p.blocks), p.dev([0] * B)
+    size = {"every": 1.05 ** (np.arange(n) % 64), "some": np.where(np.arange(n) % 13 == 12, 1.0 + np.arange(n) % 64, 0.5),
+            "first": np.where(np.arange(n) % 64 == 0, 5.0, 0.7)}[growth]
+    x = (rng.uniform(0.5, 1.0, size=(n, 2, B, heads, D)) * rng.choice([-1.0, 1.0], size=(n, 2, B, heads, D)) * size[:, None, None, None, None])
+    x = torch.from_numpy(x.astype(np.float32)).to(_torch_dtype(torch, dtype))
+    scales = []
+    for t in range(n):
+        lens.add_(1)
+        kv.append(cache, blocks, lens, x[t, 0].cuda(), x[t, 1].cuda())
+        torch.cuda.synchronize()
+        scales.append([s.cpu().numpy()[[row[t // 64] for row in p.blocks]].astype(np.float64)       # of the block of token t
+                       for s in (cache.k_scale, cache.v_scale)])
+        for i in range(2):                                  # the oracle, step by step
+            ref.append(p.codes[i], p.scales[i], D, i == 0, p.blocks, [t + 1] * B, None, x[t, i].float().numpy())
+    out = [torch.empty((B * n, heads, D), dtype=torch.float32, device="cuda") for _ in range(2)]
+    kv.read(cache, blocks, lens, *out, starts=p.dev(_starts([n] * B)), max_new=n)
+    torch.cuda.synchronize()
+    for i, (codes, keys) in enumerate(((cache.k, True), (cache.v, False))):
+        at, codes = ref.places(D, keys), codes.cpu().numpy()
+        got = out[i].view(B, n, heads, D).cpu().double().numpy()
+        for b in range(B):
+            for t in range(n):
+                blk = p.blocks[b][t // 64]
+                assert np.array_equal(codes[blk][:, at[t % 64]], p.codes[i][blk][:, at[t % 64]]), (i, b, t)
+            for t in range(n):
+                later = [scales[u][i][b] for u in range(t, min(n, t // 64 * 64 + 64))]
+                rounded = later[0] + sum((np.where(s != was, s, 0) for was, s in zip(later, later[1:])), np.zeros(heads))
+                off = np.abs(got[b, t] - x[t, i, b].double().numpy())
+                assert (off <= rounded[:, None] * (0.5 + 127 * 2.0 ** -22)).all(), (i, b, t)
+    grown = sum((scales[t][0] != scales[t - 1][0]).all() for t in range(1, 64))
+    assert grown >= {"every": 60, "some": 4, "first": 0}[growth]
+
+
 @pytest.mark.parametrize("case", ["zeros", "nan", "inf", "tiny", "huge"])
 def test_append_of_extremes(torch_cuda, case):
     torch = torch_cuda
