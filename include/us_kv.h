@@ -98,7 +98,10 @@ int32_t us_kv_row(int32_t head_dim);
  * rint(x / s'), halves to even; where s' > s the earlier codes c become
  * rint(c (s / s')). Infinities and NaN do not count for amax; an infinity is
  * stored as +-127, a NaN as 0. All in float32; a block of zeros has scale 0.
- * k, v: rows of heads x head_dim, of one type.
+ * A code is off by half a step when stored, and by half a step of the new scale
+ * each time that the block's scale grows afterwards.
+ * k, v: rows of heads x head_dim, of one type. A block that a call stores to
+ * belongs to one of its sequences.
  */
 us_status us_kv_append(const us_kv_cache *cache, const us_kv_seqs *seqs, const us_rows *k, const us_rows *v,
                        void *stream);
@@ -132,12 +135,21 @@ typedef struct {
  * heads; head h reads cache head h / (q_heads / heads)),
  *   out = sum_j p_j v_j,  p = softmax over the visible j of scale (q . k_j).
  * A query that sees no key gets zeros. Query i of a sequence's n is at
- * position lens - n + i. q and out have one type; sums and the softmax are in
- * float32. A query with an infinity or a NaN gives a NaN row.
+ * position lens - n + i. q and out have one type. Scores, their maximum, sums
+ * and results are in float32. A probability meets the values as float16 where
+ * the rows are bfloat16 or float16 (off by at most 2^-12 of itself, less than
+ * their own rounding), as two float16 parts where they are float32 (2^-22); one
+ * below 2^-27 (2^-16) of the row's largest, in calls of many rows both times
+ * their blocks' value scales, keeps fewer bits. Sums are held with probabilities times
+ * up to 2^15: values times keys have to stay below 2^113. A query with an
+ * infinity or a NaN gives a NaN row, also in the weights of the keys it sees.
  * ws: us_kv_attend_workspace_size bytes, 16-byte aligned, zero-filled before
  * its first use and left so that any later call can use it again; calls that
  * may overlap need workspaces of their own. The size for a call without a
- * window (or without the causal mask) serves the same call with one.
+ * window (or without the causal mask) serves the same call with one. Calls of
+ * few rows with weights keep their scores there: batch x q_heads x max_new x
+ * max_len floats, without a limit up to 16 rows of a cache head, up to 64 MB past
+ * that.
  * opts = NULL: causal, the rest 0. US_ERR_SHAPE also for more than 2^25 query
  * rows of a cache head (max_new x q_heads / heads), and for calls of many rows
  * if batch x heads x rows / 256 (128 for head_dim above 128) passes 2^22.

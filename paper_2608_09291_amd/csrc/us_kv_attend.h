@@ -10,7 +10,9 @@
 // the second product as float16 (the 13 keeps small ones normal), off by 2^-13
 // of each on average, below the rounding of a bfloat16 or float16 result.
 // Float32 rows carry the rounded-off part of q and p in a second product each,
-// which leaves 2^-22.
+// which leaves 2^-22. In prompts p is held times the value scale of its block,
+// over the row's largest such product (us_kv_prompt.hip): beside it a smaller one
+// keeps these bits down to 2^-27 of it, and adds at most 127 2^-38 of it below.
 #ifndef UNIONSPARSE_US_KV_ATTEND_H
 #define UNIONSPARSE_US_KV_ATTEND_H
 

@@ -76,11 +76,12 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     // Which of the two, by what they take in us: the decode kernel reads the cache once per 16 rows,
     // from behind the L2s at 10 TB/s if the 256 MB there hold it and at 6 if not, a wavefront takes
     // 1 us for a block, a generation 4 at least; the prompt kernel takes 1.75 us for a block of the
-    // above, 2.6 with float32 rows, 2.2 with four wavefronts. us per call, decode and prompt: 64 rows of 4000 keys, 8 sequences
-    // of 8 heads of 128, 33 and 52; 128 rows, 16 sequences, 123 and 95; 500 causal rows, 32 heads, 18
-    // and 27; 60 rows of 2000 keys, 32 sequences of 32 heads, 342 and 308; 328 rows of 43840 keys, 2
-    // sequences of 8 heads, 75 and 104. Over 25 shapes the choice takes at most 1.1 times the faster
-    // one's time, but where weights rule the decode kernel out (537 and 455).
+    // above, 2.6 with float32 rows, 2.2 with four wavefronts. us per call, decode and prompt: 64 rows of
+    // 4000 keys, 8 sequences of 8 heads of 128, 31 and 46; 128 rows, 16 sequences, 122 and 82; 500
+    // causal rows, 32 heads, 17 and 26; 60 rows of 2000 keys, 32 sequences of 32 heads, 347 and 291; 328
+    // rows of 43840 keys, 2 sequences of 8 heads, 311 and 192. Of 25 shapes the choice takes the faster
+    // one 22 times, and else 1.1 (256 rows of 2000 keys, heads of 256), 1.3 (1000 causal float32 rows, 32
+    // heads of 128) and 1.4 times its time (300 rows of 3000 keys, 2 sequences of 8 heads of 192).
     const double cached = (double)(pairs * all) * 128.0 * R, narrow_blocks = (double)units_n * (double)most_n;
     const double read = narrow_blocks * 128.0 * R / (cached <= 256e6 ? 1e7 : 6e6), math = narrow_blocks * R / (128.0 * 4 * cus);
     const double gens = 4.0 * (double)((units_n * ((most_n + chunk_n - 1) / chunk_n) + 2 * cus - 1) / (2 * cus));
