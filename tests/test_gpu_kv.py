@@ -506,7 +506,13 @@ def test_attend_prompts(torch_cuda, lens, new, H, Hk, D, how, odd, tracked, dtyp
 # The kernel for prompts at the values where it has code of its own. Shapes that it takes, as the tests assert, one
 # workgroup per row tile or the keys split and joined.
 WHOLE = [([600], [500], 128, 64, 64), ([900, 70], [700, 70], 64, 16, 128), ([900], [600], 48, 24, 256)]
+FEW = [([450], [3], 2, 1, 64), ([5000, 300], [1, 1], 8, 1, 128), ([700], [9], 6, 3, 256)]     # for the other kernel
 SPLIT = [([6000], [500], 64, 8, 64), ([3000], [300], 64, 4, 128), ([5000, 4000], [260, 300], 64, 4, 256)]
+
+
+def _factors(*factors):
+    """Factors of queries, within float16's range where the rows are float16."""
+    return [(f, dtype) for f in factors for dtype in DTYPES if dtype != "f16" or f <= 1e5]
 
 
 def _takes_prompts(q, cache, blocks, split, args):
@@ -600,9 +606,8 @@ def test_prompts_of_large_and_small_scores(torch_cuda, lens, new, H, Hk, D, trac
     _prompt(torch_cuda, lens, new, H, Hk, D, (lens, new, H, Hk, D) in SPLIT, tracked, dtype, spoil)
 
 
-@pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("factor", [3e3, 1e5, 1e7, 1e10])
-@pytest.mark.parametrize("lens,new,H,Hk,D", [([450], [3], 2, 1, 64), ([5000, 300], [1, 1], 8, 1, 128), ([700], [9], 6, 3, 256)] + WHOLE + SPLIT)
+@pytest.mark.parametrize("factor,dtype", _factors(3e3, 1e5, 1e7, 1e10))
+@pytest.mark.parametrize("lens,new,H,Hk,D", FEW + WHOLE + SPLIT)
 def test_attend_scores_of_millions(torch_cuda, lens, new, H, Hk, D, factor, dtype):
     """Scores up to 10^12. Where one key is ahead by more than scores can be off, the row is that key's value.
 
@@ -610,8 +615,6 @@ def test_attend_scores_of_millions(torch_cuda, lens, new, H, Hk, D, factor, dtyp
     lag behind by 20 and twice the error of both scores have less than e^-20 of its probability each."""
     torch = torch_cuda
     announce(f"kv attend large scores lens={lens} new={new} H={H}/{Hk} D={D} factor={factor} {dtype}")
-    if dtype == "f16" and factor > 1e5:
-        pytest.skip("past float16's range")
     p = Pool(torch, np.random.default_rng(sum(lens)), lens, Hk, D)
     for row in p.blocks:                                    # scales of values that no power of two makes alike
         for j, blk in enumerate(row):
@@ -653,15 +656,12 @@ def test_attend_scores_of_millions(torch_cuda, lens, new, H, Hk, D, factor, dtyp
     assert clear > 0.9 * rows
 
 
-@pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("factor", [1.0, 3e3, 1e5, 1e7])
-@pytest.mark.parametrize("lens,new,H,Hk,D", [([450], [3], 2, 1, 64), ([5000, 300], [1, 1], 8, 1, 128), ([700], [9], 6, 3, 256)] + WHOLE + SPLIT)
+@pytest.mark.parametrize("factor,dtype", _factors(1.0, 3e3, 1e5, 1e7))
+@pytest.mark.parametrize("lens,new,H,Hk,D", FEW + WHOLE + SPLIT)
 def test_weights_of_a_query_add_up_to_one(torch_cuda, lens, new, H, Hk, D, factor, dtype):
     """However large the scores are: off by 2^-20 of each for the exponentials, and by the roundings of the sums."""
     torch = torch_cuda
     announce(f"kv weights of large scores lens={lens} new={new} H={H}/{Hk} D={D} factor={factor} {dtype}")
-    if dtype == "f16" and factor > 1e5:
-        pytest.skip("past float16's range")
     p = Pool(torch, np.random.default_rng(sum(lens)), lens, Hk, D)
     cache, blocks, G = p.cache(), p.dev(p.blocks), H // Hk
     gen = torch.Generator(device="cuda")
@@ -1212,6 +1212,56 @@ def test_evict(torch_cuda, lens, heads, D, keep, recent, kind):
             for blk in p.blocks[b]:
                 if blk >= 0:
                     assert np.array_equal(codes[blk], p.codes[i][blk])
+
+
+@pytest.mark.parametrize("D", [64, 96, 256])
+def test_evict_over_tables_out_of_range(torch_cuda, D):
+    """Blocks that are not in the pool, lengths past the table and below zero, a bound of the lengths, rows of the new table
+    that are not there: nothing outside is read or written, tokens of missing blocks move as zeros."""
+    torch = torch_cuda
+    announce(f"kv evict tables out of range D={D}")
+    rng = np.random.default_rng(D)
+    p = Pool(torch, rng, [256, 200, 192, 100], 2, D, spare=12)
+    tables = [list(r) for r in p.blocks]
+    tables[0][1], tables[1][0] = p.n, -3
+    to = p.table([3, 3, 3, 3], 3)
+    into = [list(r) for r in to]
+    into[0][2], into[2][0] = 1 << 30, -1
+    lens, keep, max_len = [5000, 200, 192, -7], 150, 230    # (cut to 230, as they are, none)
+    real = [230, 200, 192, 0]
+    w = torch.rand((4, 2, p.width * 64), device="cuda")
+    cache, to_lens = p.cache(), p.dev([-1] * 4)
+    to_w, index = torch.full((4, 2, 192), -3.0, device="cuda"), torch.full((4, 2, keep), -7, dtype=torch.int32, device="cuda")
+    kv.evict(cache, p.dev(tables), p.dev(lens), w, keep, 20, p.dev(into), to_lens, to_w, index, max_len=max_len)
+    torch.cuda.synchronize()
+    assert to_lens.tolist() == [min(n, keep) for n in real]
+    at = [ref.places(D, keys) for keys in (True, False)]
+    got = [(c.cpu().numpy(), s.cpu().numpy()) for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale))]
+    written = set()
+    for b, n in enumerate(real):
+        for h in range(2):
+            want = ref.kept(w[b, h].cpu().numpy(), n, keep, 20)
+            assert index[b, h].tolist() == want + [-1] * (keep - len(want))
+            for first in range(0, len(want), 64):
+                blk = into[b][first // 64]
+                if not 0 <= blk < p.n:
+                    continue
+                written.add(blk)
+                part = want[first:first + 64]
+                src = [tables[b][j // 64] for j in part]
+                src = [x if 0 <= x < p.n else -1 for x in src]
+                for i in range(2):
+                    s1 = np.array([p.scales[i][x, h] if x >= 0 else np.float32(0) for x in src], dtype=np.float32)
+                    s2 = s1.max()
+                    assert got[i][1][blk, h] == s2
+                    for t, (j, x) in enumerate(zip(part, src)):
+                        c = p.codes[i][x, h][at[i][j % 64]].astype(np.float32) - 128 if x >= 0 else np.zeros(D, np.float32)
+                        r = np.float32(s1[t] / s2) if s2 > 0 else np.float32(0)
+                        assert np.array_equal(got[i][0][blk, h][at[i][t]], (np.rint(c * r) + 128).astype(np.uint8)), (b, h, first, t)
+    others = [i for i in range(p.n) if i not in written]
+    for i in range(2):
+        assert np.array_equal(got[i][0][others], p.codes[i][others])
+        assert np.array_equal(got[i][1][others].view(np.uint32), p.scales[i][others].view(np.uint32))
 
 
 def test_evict_keeps_as_many_as_a_number_holds(torch_cuda):
