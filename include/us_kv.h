@@ -7,6 +7,13 @@
  * and a sequence's cache can be cut to its recent and most attended tokens.
  * Attention and caches are not part of the paper.
  *
+ * Around the cache: queries and keys are normed and rotated by their positions
+ * on the way there (us_kv_rotate); sequences continue others without copying what
+ * they have in common (us_kv_fork), which attention then reads once for all of
+ * them (us_kv_attend_shared); and a long cache is attended to in the blocks alone
+ * whose keys can matter to a query (us_kv_summarise, us_kv_choose,
+ * us_kv_attend_chosen).
+ *
  * Conventions are those of us.h: arguments are checked before any work, device
  * pointers belong to the caller, every call is asynchronous on its stream,
  * allocates nothing, never synchronises, and can be captured in a HIP graph.
@@ -46,6 +53,8 @@ extern "C" {
 #define US_KV_BLOCK 64         /* tokens of a block                           */
 #define US_KV_HEAD_DIM_MAX 256 /* widest head                                 */
 #define US_KV_WIDTH_MAX (1 << 22) /* most blocks of a sequence                */
+#define US_KV_AXES_MAX 4       /* position axes of a rotation                 */
+#define US_KV_CHOSEN_MAX (1 << 16) /* most blocks that a query chooses        */
 #define US_KV_NEW_MAX (1 << 25)   /* most new tokens, or query rows of a cache
                                      head, of a sequence in one call          */
 
@@ -202,6 +211,156 @@ typedef struct {
  */
 us_status us_kv_evict(const us_kv_cache *cache, const us_kv_seqs *seqs, const float *weights, int64_t weights_stride,
                       int32_t max_len, int32_t keep, int32_t recent, const us_kv_kept *to, void *stream);
+
+/* How us_kv_rotate turns a row. */
+typedef struct {
+    const float *freq;         /* device, axes x pairs, contiguous              */
+    int32_t pairs;             /* 0 .. head_dim / 2; 0: no rotation             */
+    int32_t axes;              /* 1 .. US_KV_AXES_MAX                           */
+    const int32_t *positions;  /* device, axes x positions_stride: of every row */
+    int64_t positions_stride;  /* >= tokens                                     */
+    int32_t offset;            /* added to every position (lengths are the positions
+                                  of the newest tokens with an offset of -1)    */
+    int32_t adjacent;          /* pair i is values (2 i, 2 i + 1), not (i, pairs + i) */
+    int32_t norm;              /* 1: rows are normed first                      */
+    float eps;                 /* with norm: > 0                                */
+    const float *q_weight, *k_weight; /* with norm: device, head_dim, or NULL (ones) */
+} us_kv_rotation;
+
+/*
+ * us_kv_rotate - norms of query and key heads and their rotation, in one pass.
+ * A row x (a token's head) becomes, where `norm`,
+ *   n = x w / sqrt(mean(x^2) + eps),
+ * then pair i of its first 2 pairs values (n1, n2) becomes
+ *   (n1 cos a_i - n2 sin a_i, n2 cos a_i + n1 sin a_i),
+ *   a_i = sum over the axes of (positions[axis, row] + offset) freq[axis, i],
+ * and the rest stays. (An axis that does not turn a pair has frequency 0 there.)
+ * Angles are taken in 64 bits, the rest in float32, rounded once. q_out may be q
+ * and k_out may be k, with the same strides; otherwise they overlap nothing. All
+ * rows have one type and number. k = k_out = NULL with k_heads = 0: queries alone.
+ */
+us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head_dim, const us_rows *q, const us_rows *q_out,
+                       const us_rows *k, const us_rows *k_out, const us_kv_rotation *how, void *stream);
+
+/* The sequences that a fork makes; none of it overlaps what the call reads. */
+typedef struct {
+    int32_t *blocks;        /* device, batch x stride                           */
+    int64_t stride;
+    int32_t width;          /* >= that of the old table, to US_KV_WIDTH_MAX     */
+    int32_t batch;          /* 1 .. 65535                                       */
+    int32_t *lens;          /* device, batch                                    */
+} us_kv_forked;
+
+/*
+ * us_kv_fork - sequences that continue others, in tables of their own. New
+ * sequence b has the tokens of the old one parents[b] (NULL: b; a number outside
+ * the old ones: none) and blocks for room[b] more (NULL or below 0: none), as far
+ * as the table is wide. refs[i] is how often the tables name block i; 0 is a free
+ * block. Full blocks are shared by all children of a sequence. The block that a
+ * sequence's next token goes to, and those behind it, stay with its first child
+ * (the lowest b) if refs is 1; any other child is given a block for each of
+ * them, a copy of the started one. Blocks that are given are the free ones of
+ * lowest number, in the order of sequences and of their tables. Then the old
+ * tables count for nothing any more, over their whole width: entries without a
+ * block have to be outside [0, n_blocks). So a call frees what no child
+ * continues, and gives a growing sequence its next block.
+ * Where there are too few free blocks, missing (device, one number) is how many
+ * are lacking, the new sequences are empty, and the old tables, refs and blocks
+ * stay as they are and count on; else missing is 0.
+ * A started block that is not there stays so. Only the blocks of seqs count:
+ * its starts and max_new are not looked at.
+ * ws: us_kv_fork_workspace_size bytes, as us_kv_attend's. US_ERR_SHAPE for more
+ * than 32767 heads.
+ */
+us_status us_kv_fork_workspace_size(const us_kv_cache *cache, int32_t batch, int32_t to_batch, size_t *bytes);
+us_status us_kv_fork(const us_kv_cache *cache, int32_t *refs, const us_kv_seqs *seqs, const int32_t *parents,
+                     const int32_t *room, const us_kv_forked *to, int32_t *missing, void *ws, size_t ws_bytes, void *stream);
+
+/* Groups of sequences that have their first blocks in common: group g is
+ * sequences starts[g] .. starts[g + 1] - 1, which have shared[g] blocks in
+ * common. Sequences of no group have none. */
+typedef struct {
+    const int32_t *starts;  /* device, groups + 1, ascending                    */
+    const int32_t *shared;  /* device, groups                                   */
+    int32_t groups;         /* 1 .. 65535                                       */
+    int32_t max_group;      /* no group has more sequences; 1 .. 65535          */
+    int32_t max_shared;     /* nor more blocks in common; 0 = the table's width */
+} us_kv_groups;
+
+/*
+ * us_kv_attend_shared - us_kv_attend for sequences with their first blocks in
+ * common, which are read once for a group: those of its first sequence. (Where
+ * another sequence's table differs there, its own blocks are not looked at.)
+ * Queries see what us_kv_attend shows them, also if a sequence is shorter than
+ * the common blocks, and results are off by as much. Sequences past max_group
+ * in a group count as sequences of none. opts->window has to be 0 and
+ * opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, 16-byte
+ * aligned, which need not be zero; calls that may overlap need their own.
+ * US_ERR_SHAPE as us_kv_attend, for groups as for sequences: for more than 2^25
+ * query rows of a group and cache head.
+ */
+us_status us_kv_attend_shared_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
+                                             int32_t tokens, const us_kv_groups *groups, const us_kv_attend_opts *opts,
+                                             size_t *bytes);
+us_status us_kv_attend_shared(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
+                              const us_rows *out, const us_kv_groups *groups, const us_kv_attend_opts *opts, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/*
+ * us_kv_summarise - the extremes of keys, for us_kv_choose. For every block that
+ * holds some of the sequences' last tokens (those of starts and max_new),
+ * summary (n_blocks x heads x 2 x us_kv_row(head_dim) bytes, 16-byte aligned)
+ * gets the smallest byte of each value over the sequence's tokens in the block,
+ * then the largest. Called after the append of these tokens, also because that
+ * may change a block's scale and with it older codes.
+ */
+us_status us_kv_summarise(const us_kv_cache *cache, const us_kv_seqs *seqs, uint8_t *summary, void *stream);
+
+typedef struct {
+    float *scores;          /* device, tokens x heads x scores_stride           */
+    int64_t scores_stride;  /* >= the blocks of max_len tokens                  */
+    int32_t *chosen;        /* device, tokens x heads x top                     */
+    int32_t top;            /* 1 .. US_KV_CHOSEN_MAX                            */
+    int32_t sinks, recent;  /* blocks taken in any case; together at most top   */
+    int32_t max_len;        /* no sequence is longer; 0 = width * US_KV_BLOCK   */
+} us_kv_choice;
+
+/*
+ * us_kv_choose - for every query row and cache head, the blocks of its sequence
+ * whose keys can have the largest score. With lo and hi the codes of a block's
+ * summary and s its keys' scale, its score is
+ *   s max over the query heads of sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d,
+ * no less than any q . k_j of it, taken in 64 bits and rounded once to float32;
+ * a query head with an infinity or a NaN does not count, -infinity if none does.
+ * Row i of a sequence's n is at position p = lens - n + i and looks at the
+ * blocks up to that of p. chosen gets, ascending, then -1, `top` of them: the
+ * first `sinks` and the last `recent` ones, then those of largest score (equal
+ * scores: the earlier one; a NaN counts as the smallest). Blocks that are not
+ * there are not chosen. scores gets the scores of the blocks that a row looks
+ * at (-infinity for one that is not there). Rows that are none of the sequences'
+ * are left as they were. ws: us_kv_choose_workspace_size bytes, as us_kv_attend's.
+ * US_ERR_SHAPE for more than 65535 rows.
+ */
+us_status us_kv_choose_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t tokens, int32_t top,
+                                      size_t *bytes);
+us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *seqs, const uint8_t *summary, int32_t q_heads,
+                       const us_rows *q, const us_kv_choice *choice, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * us_kv_attend_chosen - us_kv_attend (causal) over the chosen blocks alone:
+ * row t and head h of cache head k sees the keys up to its position in blocks
+ * chosen[t, k, :] (tokens x heads x top). Numbers outside the sequence's blocks
+ * up to that position count for nothing, a number that is there twice counts
+ * twice. Rows without any key get zeros. For single tokens and a few drafted
+ * ones: a row's blocks are read for it alone. opts: causal, without window and
+ * weights. ws: us_kv_attend_chosen_workspace_size bytes, as us_kv_attend's; one
+ * zero-filled workspace serves both in turn. US_ERR_SHAPE for more than 65535 rows.
+ */
+us_status us_kv_attend_chosen_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
+                                             int32_t tokens, int32_t top, size_t *bytes);
+us_status us_kv_attend_chosen(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads, const us_rows *q,
+                              const us_rows *out, const int32_t *chosen, int32_t top, const us_kv_attend_opts *opts, void *ws,
+                              size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

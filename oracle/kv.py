@@ -138,3 +138,122 @@ def evict(codes, scales, head_dim, keys, blocks, positions, to_blocks, h):
             r = F32(s / s2) if s2 > 0 else F32(0)
             codes[blk, h][at[t]] = (np.rint(c * r) + F32(128)).astype(np.uint8)
         scales[blk, h] = s2
+
+
+# --- rotations, forks, and blocks that a query chooses ------------------------------
+
+def rotate(x, freq=None, positions=None, offset=0, adjacent=False, weight=None, eps=None):
+    """float64 norms (with eps) and rotations of rows x (tokens, heads, head_dim); freq (axes, pairs), positions (axes, tokens)."""
+    x = x.astype(np.float64).copy()
+    if eps is not None:
+        x /= np.sqrt((x * x).mean(-1, keepdims=True) + float(F32(eps)))
+        if weight is not None:
+            x *= weight.astype(np.float64)
+    if freq is None:
+        return x
+    pairs = freq.shape[1]
+    for t in range(x.shape[0]):
+        for i in range(pairs):
+            a = math.fsum((int(positions[j][t]) + offset) * float(freq[j][i]) for j in range(freq.shape[0]))
+            one, two = (2 * i, 2 * i + 1) if adjacent else (i, pairs + i)
+            n1, n2 = x[t, :, one].copy(), x[t, :, two].copy()
+            x[t, :, one] = n1 * math.cos(a) - n2 * math.sin(a)
+            x[t, :, two] = n2 * math.cos(a) + n1 * math.sin(a)
+    return x
+
+
+def fork(refs, blocks, lens, parents, room, to_width):
+    """A fork of the sequences in `blocks` (lists of numbers); parents a list, room one or None.
+
+    Returns (to_blocks, to_lens, refs, copies, missing): copies a list of (from, to) blocks; with missing > 0
+    empty sequences and refs as they were."""
+    n_blocks, batch, width = len(refs), len(blocks), len(blocks[0])
+    free = [i for i in range(n_blocks) if refs[i] == 0]
+    taken = set()
+    new, copies, want, to_lens = [], [], 0, []
+    for b, p in enumerate(parents):
+        p = p if 0 <= p < batch else None
+        row = [-1] * to_width
+        length = min(max(lens[p], 0), width * BLOCK) if p is not None else 0
+        more = 0 if room is None else max(room[b], 0)
+        need = min(-(-(length + more) // BLOCK), to_width)
+        heir = p is not None and p not in taken
+        taken.add(p)
+        for i in range(need):
+            old = blocks[p][i] if p is not None and i < width and 0 <= blocks[p][i] < n_blocks else -1
+            started = i * BLOCK < length
+            if i < length // BLOCK or (heir and old >= 0 and refs[old] == 1):
+                row[i] = old
+            elif old >= 0 or not started:
+                got = free[want] if want < len(free) else None
+                want += 1
+                row[i] = got
+                if started:
+                    copies.append((old, got))
+        new.append(row)
+        to_lens.append(length)
+    if want > len(free):
+        return [[-1] * to_width for _ in parents], [0] * len(parents), list(refs), [], want - len(free)
+    after = list(refs)
+    for row in blocks:
+        for x in row:
+            if 0 <= x < n_blocks:
+                after[x] -= 1
+    for row in new:
+        for x in row:
+            if x >= 0:
+                after[x] += 1
+    return new, to_lens, after, copies, 0
+
+
+def extremes(codes, head_dim, block, h, tokens_there):
+    """Smallest and largest byte of each value over the first tokens of a key block: (2, head_dim)."""
+    c = codes[block, h][places(head_dim, True)[:tokens_there]]
+    return np.stack((c.min(0), c.max(0)))
+
+
+def score(summary, scale, q):
+    """float32 score of a block for the query heads q (heads, head_dim) of its cache head, rounded once."""
+    lo, hi = summary.astype(np.float64) - 128
+    q = q.astype(np.float64)
+    ok = np.isfinite(q).all(-1)
+    if not ok.any():
+        return F32(-np.inf)
+    q = q[ok]
+    return F32((np.maximum(q, 0) @ hi + np.minimum(q, 0) @ lo).max() * float(scale))
+
+
+def choose(scores, there, top, sinks, recent):
+    """Places of the blocks to take, ascending: `there` says which of the scored blocks exist."""
+    n = len(scores)
+
+    def rank(i):
+        if i < sinks or i >= n - recent:
+            return (0, 0.0, i)
+        return (2, 0.0, i) if math.isnan(scores[i]) else (1, -float(scores[i]), i)
+
+    return sorted(sorted((i for i in range(n) if there[i]), key=rank)[:top])
+
+
+def attend_chosen(k, ks, v, vs, head_dim, blocks, at, places_, q, h, scale=None):
+    """float64 attention of one query (head_dim) at position `at` over the blocks at places_ of its sequence.
+
+    Returns (out, out_abs, reach) as attend does."""
+    scale = 1 / math.sqrt(head_dim) if scale is None else scale
+    q = q.astype(np.float64)
+    key, val = [], []
+    for i in places_:
+        n = min(BLOCK, at + 1 - i * BLOCK) if i >= 0 else 0
+        if n <= 0 or i >= len(blocks) or not 0 <= blocks[i] < len(k):
+            continue
+        kc, kscale = tokens(k, ks, head_dim, True, [blocks[i]], n, h)
+        vc, vscale = tokens(v, vs, head_dim, False, [blocks[i]], n, h)
+        key.append(kc * kscale[:, None])
+        val.append(vc * vscale[:, None])
+    if not key:
+        return np.zeros(head_dim), np.zeros(head_dim), 0.0
+    key, val = np.concatenate(key), np.concatenate(val)
+    x = scale * (key @ q)
+    p = np.exp(x - x.max())
+    p /= p.sum()
+    return p @ val, p @ np.abs(val), (scale * (np.abs(key) @ np.abs(q))).max()

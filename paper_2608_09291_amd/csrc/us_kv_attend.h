@@ -238,6 +238,21 @@ __device__ inline int64_t row_block(const Args &a, int hk, int b, int r0, int ro
     return hk * a.sp.row_blocks + (int64_t)r0 * a.G / 32 + b + row / 32;
 }
 
+// What an attention call launches, and where its parts of the workspace lie (bytes).
+struct Plan {
+    bool decode;
+    int chunk, splits, tiles, rows, mix;
+    int64_t scores_stride;
+    int64_t row_blocks;
+    size_t part, ml, qf, qn, scores, total;
+};
+
+__host__ __device__ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+us_status check_opts(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, const us_kv_attend_opts &o);
+us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int tokens, bool f32, const us_kv_attend_opts &o,
+                  Plan &p);
+
 hipError_t launch_decode(int dtype, const Args &a, int batch, hipStream_t stream);
 hipError_t launch_prompt(int dtype, const Args &a, int batch, hipStream_t stream);
 // Adds the probabilities up: from the scores that decode left, or by the scores' product again.

@@ -11,6 +11,17 @@ using namespace us_kv;
 
 constexpr us_kv_attend_opts kDefault = {0.0f, 1, 0, 0, nullptr, 0};
 
+// What a call launches, and where its parts of the workspace lie (bytes).
+// The tickets, which have to be zero between calls, have a place of their own
+// that no other part of any call takes; calls of more units do not split.
+constexpr int64_t kTickets = 16384;
+// Workgroups of the prompt kernel, whose grid has one dimension of 512 threads each.
+constexpr int64_t kMostPrompt = INT32_MAX / 512;
+
+}  // namespace
+
+namespace us_kv {
+
 us_status check_opts(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, const us_kv_attend_opts &o) {
     us_status st = check_cache(c);
     if (st == US_OK) st = check_seqs(s);
@@ -22,23 +33,6 @@ us_status check_opts(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, con
     if (o.weights && o.weights_stride < seqs_of(*c, *s, o.max_len, 0).max_len) return US_ERR_SHAPE;
     return US_OK;
 }
-
-// What a call launches, and where its parts of the workspace lie (bytes).
-// The tickets, which have to be zero between calls, have a place of their own
-// that no other part of any call takes; calls of more units do not split.
-constexpr int64_t kTickets = 16384;
-// Workgroups of the prompt kernel, whose grid has one dimension of 512 threads each.
-constexpr int64_t kMostPrompt = INT32_MAX / 512;
-
-struct Plan {
-    bool decode;
-    int chunk, splits, tiles, rows, mix;
-    int64_t scores_stride;
-    int64_t row_blocks;
-    size_t part, ml, qf, qn, scores, total;
-};
-
-int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int tokens, bool f32, const us_kv_attend_opts &o,
                   Plan &p) {
@@ -124,7 +118,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     return US_OK;
 }
 
-}  // namespace
+}  // namespace us_kv
 
 extern "C" us_status us_kv_attend_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                                  int32_t tokens, const us_kv_attend_opts *opts, size_t *bytes) {

@@ -1,0 +1,371 @@
+// us_kv_summarise and us_kv_choose: the extremes of each block's keys, and the
+// blocks of highest possible score for every query.
+//
+// With lo_d <= k_jd <= hi_d for all keys j of a block, q . k_j is at most
+//   sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d,
+// which is a product of 2 D values per block and query head: MFMA's 16 x 16 x 4
+// of float64, 16 blocks by 16 query heads. In 64 bits two blocks' scores change
+// places only where they agree to the last bits, and the choice is that of the
+// definition; the matrix cores take as long for it as the loads of the extremes.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "us_device.h"
+#include "us_kv_others.h"
+
+namespace {
+
+using namespace us_kv;
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// --- summaries ----------------------------------------------------------------
+
+__device__ inline u16x2 pair_of(uint32_t x) { return __builtin_bit_cast(u16x2, x); }
+__device__ inline uint32_t bits_of(u16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+
+// A workgroup per (block, head, sequence), a wavefront per 32 values: lane
+// (t % 16, octet) has those of 16 byte pieces, tokens t and t + 16.
+template <int NT>
+__global__ __launch_bounds__(kThreads) void us_kv_summarise_kernel(const uint8_t *kp, uint8_t *summary, Seqs s) {
+    constexpr int R = 32 * NT;
+    const int b = blockIdx.z, h = blockIdx.y, heads = gridDim.y, tid = threadIdx.x, lane = tid & 63;
+    int r0, n;
+    s.rows(b, r0, n);
+    const int len = s.len(b), p0 = len - n, blk = max(p0, 0) / kBlock + blockIdx.x;
+    const int tokens = min(len - blk * kBlock, kBlock);
+    if (n <= 0 || tokens <= 0) return;
+    const int id = s.block(b, blk);
+    if (id < 0) return;
+    const int64_t at = (int64_t)id * heads + h;
+    const int t0 = lane >> 2;
+    for (int c = __builtin_amdgcn_readfirstlane(tid >> 6); c < NT; c += kWaves) {
+        const u32x4 *src = (const u32x4 *)(kp + at * (kBlock * R) + 2048 * c) + lane;
+        const u32x4 raw[2] = {src[0], src[64]};
+        u16x2 lo[4], hi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lo[i] = pair_of(0x00FF00FFu), hi[i] = pair_of(0);
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bool here = t0 + 16 * u + 32 * y < tokens;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w = raw[y][2 * u + (i >> 1)];
+                    const u16x2 x = pair_of(__builtin_amdgcn_perm(0, w, i & 1 ? 0x0C030C02u : 0x0C010C00u));
+                    const u16x2 a = here ? x : pair_of(0x00FF00FFu), z = here ? x : pair_of(0);
+                    lo[i] = __builtin_elementwise_min(lo[i], a);
+                    hi[i] = __builtin_elementwise_max(hi[i], z);
+                }
+            }
+#pragma unroll
+        for (int z = 4; z < 64; z <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo[i] = __builtin_elementwise_min(lo[i], pair_of(__shfl_xor(bits_of(lo[i]), z, 64)));
+                hi[i] = __builtin_elementwise_max(hi[i], pair_of(__shfl_xor(bits_of(hi[i]), z, 64)));
+            }
+        if (lane < 4) {
+            u32x2 *dst = (u32x2 *)(summary + at * (2 * R) + 32 * c) + lane;
+            dst[0] = (u32x2){__builtin_amdgcn_perm(bits_of(lo[1]), bits_of(lo[0]), 0x06040200u),
+                             __builtin_amdgcn_perm(bits_of(lo[3]), bits_of(lo[2]), 0x06040200u)};
+            dst[R / 8] = (u32x2){__builtin_amdgcn_perm(bits_of(hi[1]), bits_of(hi[0]), 0x06040200u),
+                                 __builtin_amdgcn_perm(bits_of(hi[3]), bits_of(hi[2]), 0x06040200u)};
+        }
+    }
+}
+
+// --- scores and the choice ------------------------------------------------------
+
+struct ChooseArgs {
+    const uint8_t *summary;
+    const float *ks;
+    int32_t heads, D, G, vec;
+    Seqs s;
+    Rows q;
+    Others more;
+    float *scores;                                         // tokens x heads x stride
+    int64_t stride;
+    int32_t *chosen;                                       // tokens x heads x top
+    int32_t top, sinks, recent;
+    int32_t *tickets;                                      // tokens x heads
+};
+
+constexpr int kHeld = 16;                                  // scores of a thread that stay in registers
+
+// Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
+__device__ inline uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);          // (no -0)
+    return x != x ? 1u : b >> 31 ? ~b : b | 0x80000000u;
+}
+
+__device__ inline int sum_before(int x, int *lds, int &all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int run = x;
+#pragma unroll
+    for (int z = 1; z < 64; z <<= 1) {
+        const int y = __shfl_up(run, z, 64);
+        if (lane >= z) run += y;
+    }
+    __syncthreads();                                       // (of an earlier call)
+    if (lane == 63) lds[wave] = run;
+    __syncthreads();
+    int sum = run - x;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) sum += lds[w];
+        all += lds[w];
+    }
+    return sum;
+}
+
+// The places of the largest `top` of n keys to `out`, ascending, ties to the first; keys of 0 count for
+// nothing. each(f) calls f(place, key) for a thread's own run of places, in order.
+template <class E>
+__device__ inline void select(E each, int top, int *out, int *lds, int *hist) {
+    const int tid = threadIdx.x;
+    int there = 0, all;
+    each([&](int, uint32_t k) { there += k != 0; });
+    sum_before(there, lds, all);
+    const int take = min(top, all);
+    // The take-th largest key, 8 bits at a time.
+    uint32_t limit = 0;
+    int rest = take;                                       // of the keys that agree with limit so far
+    if (take < all) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            __syncthreads();
+            hist[tid] = 0;
+            __syncthreads();
+            each([&](int, uint32_t k) {
+                if (k && (shift == 24 || (k ^ limit) >> (shift + 8) == 0)) atomicAdd(hist + ((k >> shift) & 255), 1);
+            });
+            __syncthreads();
+            // thread z: keys of digit 255 - z, and of the larger ones
+            const int mine = hist[255 - tid];
+            int unused;
+            const int above = sum_before(mine, lds, unused);
+            __syncthreads();
+            if (above < rest && above + mine >= rest) {    // (one thread; rest >= 1)
+                lds[kWaves] = 255 - tid;
+                lds[kWaves + 1] = rest - above;
+            }
+            __syncthreads();
+            limit |= (uint32_t)lds[kWaves] << shift;
+            rest = lds[kWaves + 1];
+        }
+    }
+    int more = 0, same = 0;
+    each([&](int, uint32_t k) {
+        more += k > limit;
+        same += k && k == limit;
+    });
+    int at = sum_before(more, lds, all), eq = sum_before(same, lds, all);
+    each([&](int i, uint32_t k) {
+        const bool tie = k && k == limit;
+        if (k > limit || (tie && eq < rest)) out[at + min(eq, rest)] = i;
+        at += k > limit;
+        eq += tie;
+    });
+    for (int i = take + tid; i < top; i += kThreads) out[i] = -1;
+}
+
+template <int NT, int DT>
+__global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
+    using T = typename Type<DT>::T;
+    constexpr int R = 32 * NT, kSteps = 2 * R / 64;        // of 64 values of a summary, 16 products each
+    // The queries as the products' right operand: step, product, lane.
+    __shared__ double qs[kSteps * 16 * 64];
+    __shared__ double total[kWaves][16];                   // of a query's values
+    __shared__ int lds[kWaves + 2], hist[256], flag;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, kk = lane >> 4, t = blockIdx.x, hk = blockIdx.y;
+    int b, at;
+    if (!a.more.place(a.s, t, b, at)) return;
+    const int64_t unit = (int64_t)t * a.heads + hk;
+    const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + 63) / 64, parts = min(max(chunks, 1), (int)gridDim.z);
+    if ((int)blockIdx.z >= parts) return;
+    float *scores = a.scores + unit * a.stride;
+    const T *q = (const T *)a.q.data + (int64_t)t * a.q.token_stride + (int64_t)hk * a.G * a.q.head_stride;
+    const auto load_queries = [&](int g0) {
+        double sum = 0.0;
+        __syncthreads();                                   // (of the heads before these)
+        for (int o = tid >> 4; o < R / 8; o += kThreads / 16) {
+            float x[8];
+            if (g0 + n < a.G) {
+                const T *p = q + (int64_t)(g0 + n) * a.q.head_stride;
+                if (a.vec) load_octet<DT, true>(p, o, a.D, x);
+                else load_octet<DT, false>(p, o, a.D, x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int lo = 8 * o + e, hi = R + lo;
+                sum += x[e];
+                qs[((lo >> 6) * 16 + (lo & 15)) * 64 + ((lo >> 4) & 3) * 16 + n] = x[e] < 0.0f ? x[e] : 0.0f;
+                qs[((hi >> 6) * 16 + (hi & 15)) * 64 + ((hi >> 4) & 3) * 16 + n] = x[e] > 0.0f ? x[e] : 0.0f;
+            }
+        }
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (kk == 0) total[wave][n] = sum;
+        __syncthreads();
+    };
+    if (a.G <= 16) load_queries(0);
+    for (int c = blockIdx.z; c < chunks; c += parts) {
+        const int m0 = 64 * c + 16 * wave, mine = m0 + n;  // a wavefront's 16 blocks; lane n's
+        const int id = mine < blocks ? a.s.block(b, mine) : -1;
+        const int64_t where = (int64_t)max(id, 0) * a.heads + hk;
+        const u32x4 *src = (const u32x4 *)(a.summary + where * (2 * R)) + kk;
+        u32x4 raw[kSteps];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) raw[j] = src[4 * j];
+        const float ks = a.ks[where];
+        double best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        for (int g0 = 0; g0 < a.G; g0 += 16) {
+            if (a.G > 16) load_queries(g0);
+            f64x4 x = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const double code = (double)((raw[j][e >> 2] >> (8 * (e & 3))) & 255u);
+                    x = __builtin_amdgcn_mfma_f64_16x16x4f64(code, qs[(j * 16 + e) * 64 + lane], x, 0, 0, 0);
+                }
+            // Lane (n, kk), element v: block 4 v + kk, query head n. The bytes are codes + 128.
+            const double bias = 128.0 * (total[0][n] + total[1][n] + total[2][n] + total[3][n]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const double y = x[v] - bias;
+                best[v] = g0 + n < a.G && y > best[v] ? y : best[v];
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int z = 1; z < 16; z <<= 1) {
+                const double y = __shfl_xor(best[v], z, 64);
+                best[v] = y > best[v] ? y : best[v];
+            }
+        double y = best[0];
+#pragma unroll
+        for (int v = 1; v < 4; ++v) y = n == v ? best[v] : y;
+        const int m = 4 * (n & 3) + kk;                    // of the 16, this lane's to store
+        const float scale = __shfl(ks, m, 64);
+        const bool there = __shfl(id, m, 64) >= 0;
+        if (n < 4 && m0 + m < blocks) {
+            const float score = there ? (float)(y * (double)scale) : -INFINITY;
+            __hip_atomic_store(scores + m0 + m, score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (parts > 1) {
+        if (!last_of(a.tickets + unit, parts, &flag)) return;
+    } else {
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
+    const auto key_of = [&](int i) {
+        if (a.s.block(b, i) < 0) return 0u;
+        if (i < a.sinks || i >= blocks - a.recent) return 0xFFFFFFFFu;
+        return order_of(__hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    };
+    const int per = (blocks + kThreads - 1) / kThreads, i0 = min(tid * per, blocks), i1 = min(i0 + per, blocks);
+    int *out = a.chosen + unit * a.top;
+    if (per <= kHeld) {
+        uint32_t held[kHeld];
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) held[e] = i0 + e < i1 ? key_of(i0 + e) : 0u;
+        select([&](auto f) {
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e)
+                if (e < per) f(i0 + e, held[e]);           // (past i1 a key of 0)
+        }, a.top, out, lds, hist);
+    } else {
+        select([&](auto f) {
+            for (int i = i0; i < i1; ++i) f(i, key_of(i));
+        }, a.top, out, lds, hist);
+    }
+}
+
+us_status check_summary(const us_kv_cache *c, const us_kv_seqs *s, const uint8_t *summary) {
+    us_status st = check_cache(c);
+    if (st == US_OK) st = check_seqs(s);
+    if (st != US_OK) return st;
+    return !summary || (uintptr_t)summary % 16 ? US_ERR_ARG : US_OK;
+}
+
+us_status check_units(const us_kv_cache &c, int tokens, int top) {
+    return tokens < 1 || tokens > 65535 || top < 1 || top > US_KV_CHOSEN_MAX ? US_ERR_SHAPE : US_OK;
+}
+
+}  // namespace
+
+extern "C" us_status us_kv_summarise(const us_kv_cache *cache, const us_kv_seqs *seqs, uint8_t *summary, void *stream) {
+    const us_status st = check_summary(cache, seqs, summary);
+    if (st != US_OK) return st;
+    const Seqs s = seqs_of(*cache, *seqs, 0, INT32_MAX);
+    const int most = seqs->max_new < seqs->width * kBlock ? seqs->max_new : seqs->width * kBlock;
+    const dim3 grid((most + kBlock - 2) / kBlock + 1, cache->heads, seqs->batch);
+    const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
+        hipLaunchKernelGGL(us_kv_summarise_kernel<decltype(nt)::value>, grid, dim3(kThreads), 0, (hipStream_t)stream, cache->k, summary, s);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? US_OK : US_ERR_DEVICE;
+}
+
+extern "C" us_status us_kv_choose_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t tokens, int32_t top,
+                                                 size_t *bytes) {
+    us_status st = check_cache(cache);
+    if (st == US_OK) st = check_seqs(seqs);
+    if (st != US_OK) return st;
+    if (!bytes) return US_ERR_ARG;
+    st = check_units(*cache, tokens, top);
+    if (st == US_OK) *bytes = (size_t)up((int64_t)tokens * cache->heads * 4, 16);
+    return st;
+}
+
+extern "C" us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *seqs, const uint8_t *summary, int32_t q_heads,
+                                  const us_rows *q, const us_kv_choice *choice, void *ws, size_t ws_bytes, void *stream) {
+    us_status st = check_summary(cache, seqs, summary);
+    if (st == US_OK) st = check_rows(q);
+    if (st != US_OK) return st;
+    if (!choice || !choice->scores || !choice->chosen || (uintptr_t)choice->scores % 4 || (uintptr_t)choice->chosen % 4) return US_ERR_ARG;
+    st = check_units(*cache, q->tokens, choice->top);
+    if (st != US_OK) return st;
+    if (q_heads < 1 || q_heads % cache->heads || q_heads > 65535 || choice->max_len < 0) return US_ERR_SHAPE;
+    if (choice->sinks < 0 || choice->recent < 0 || (int64_t)choice->sinks + choice->recent > choice->top) return US_ERR_SHAPE;
+    ChooseArgs a;
+    a.s = seqs_of(*cache, *seqs, choice->max_len, q->tokens);
+    const int most = (int)(up(a.s.max_len, kBlock) / kBlock);
+    if (choice->scores_stride < most) return US_ERR_SHAPE;
+    const int64_t units = (int64_t)q->tokens * cache->heads;
+    if (!ws || (uintptr_t)ws % 16 || ws_bytes < (size_t)up(units * 4, 16)) return US_ERR_ARG;
+    a.summary = summary, a.ks = cache->k_scale, a.heads = cache->heads, a.D = cache->head_dim, a.G = q_heads / cache->heads;
+    a.vec = octets_aligned(*q, cache->head_dim);
+    a.q = Rows{q->data, q->token_stride, q->head_stride};
+    a.more = Others{};
+    a.more.batch = seqs->batch;
+    a.scores = choice->scores, a.stride = choice->scores_stride, a.chosen = choice->chosen;
+    a.top = choice->top, a.sinks = choice->sinks, a.recent = choice->recent, a.tickets = (int32_t *)ws;
+    // Workgroups of 64 blocks, but no more of them than fill the GPU a few times: each has its queries to lay out.
+    const int64_t room = 8 * us_device::compute_units() / units;
+    int64_t parts = (most + 63) / 64;
+    if (parts > room) parts = room < 1 ? 1 : room;
+    const dim3 grid(q->tokens, cache->heads, (unsigned)parts);
+    const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
+        return with_type(q->dtype, [&](auto dt) {
+            hipLaunchKernelGGL((us_kv_choose_kernel<decltype(nt)::value, decltype(dt)::value>), grid, dim3(kThreads), 0,
+                               (hipStream_t)stream, a);
+            return hipGetLastError();
+        });
+    });
+    return e == hipSuccess ? US_OK : US_ERR_DEVICE;
+}

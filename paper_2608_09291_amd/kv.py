@@ -19,10 +19,14 @@ from .binding import _check
 
 BLOCK = 64           # US_KV_BLOCK: tokens of a block
 HEAD_DIM_MAX = 256   # US_KV_HEAD_DIM_MAX
+AXES_MAX = 4         # US_KV_AXES_MAX
+CHOSEN_MAX = 1 << 16  # US_KV_CHOSEN_MAX
 
 #: Every symbol us_kv.h declares.
 EXPORTS = ("us_kv_row", "us_kv_append", "us_kv_read", "us_kv_attend_workspace_size", "us_kv_attend_route",
-           "us_kv_attend", "us_kv_evict")
+           "us_kv_attend", "us_kv_evict", "us_kv_rotate", "us_kv_fork_workspace_size", "us_kv_fork",
+           "us_kv_attend_shared_workspace_size", "us_kv_attend_shared", "us_kv_summarise", "us_kv_choose_workspace_size",
+           "us_kv_choose", "us_kv_attend_chosen_workspace_size", "us_kv_attend_chosen")
 
 
 class CacheStruct(ctypes.Structure):
@@ -57,6 +61,28 @@ class KeptStruct(ctypes.Structure):
                 ("index", ctypes.c_void_p)]
 
 
+class RotationStruct(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64), ("offset", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class ForkedStruct(ctypes.Structure):
+    _fields_ = [("blocks", ctypes.c_void_p), ("stride", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("lens", ctypes.c_void_p)]
+
+
+class GroupsStruct(ctypes.Structure):
+    _fields_ = [("starts", ctypes.c_void_p), ("shared", ctypes.c_void_p), ("groups", ctypes.c_int32),
+                ("max_group", ctypes.c_int32), ("max_shared", ctypes.c_int32)]
+
+
+class ChoiceStruct(ctypes.Structure):
+    _fields_ = [("scores", ctypes.c_void_p), ("scores_stride", ctypes.c_int64), ("chosen", ctypes.c_void_p),
+                ("top", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
 _ready = _args = None
 
 
@@ -78,6 +104,16 @@ def lib():
         L.us_kv_attend_route.argtypes = [vp, vp, i32, i32, i32, vp, ctypes.POINTER(AttendRouteInfo)]
         L.us_kv_attend.argtypes = [vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.us_kv_evict.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp, vp]
+        L.us_kv_rotate.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.us_kv_fork_workspace_size.argtypes = [vp, i32, i32, ctypes.POINTER(sz)]
+        L.us_kv_fork.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.us_kv_attend_shared_workspace_size.argtypes = [vp, vp, i32, i32, vp, vp, ctypes.POINTER(sz)]
+        L.us_kv_attend_shared.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.us_kv_summarise.argtypes = [vp, vp, vp, vp]
+        L.us_kv_choose_workspace_size.argtypes = [vp, vp, i32, i32, ctypes.POINTER(sz)]
+        L.us_kv_choose.argtypes = [vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.us_kv_attend_chosen_workspace_size.argtypes = [vp, vp, i32, i32, i32, ctypes.POINTER(sz)]
+        L.us_kv_attend_chosen.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, vp, sz, vp]
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         _ready = L
@@ -90,6 +126,10 @@ _pack_seqs = struct.Struct("@PqiiPPi4x").pack
 _pack_rows = struct.Struct("@Pqqii").pack
 _pack_opts = struct.Struct("@fiii Pq").pack
 _pack_kept = struct.Struct("@Pqi4xPPqP").pack
+_pack_rotation = struct.Struct("@PiiPqiiifPP").pack
+_pack_forked = struct.Struct("@PqiiP").pack
+_pack_groups = struct.Struct("@PPiii4x").pack
+_pack_choice = struct.Struct("@PqPiiii").pack
 
 _I32, _F32 = torch.int32, torch.float32
 _ROWS = {}      # us_kv_row by head_dim
@@ -108,9 +148,13 @@ def row(head_dim: int) -> int:
 
 def _stream(stream, cache) -> int:
     """A call's stream. The library launches on the current device, which has to be the cache's and the stream's."""
+    return _stream_on(stream, cache.device, "the cache")
+
+
+def _stream_on(stream, device: int, what: str) -> int:
     now = torch.cuda.current_device()
-    if cache.device >= 0 and now != cache.device:
-        raise ValueError(f"the cache is on cuda:{cache.device}, the current device is cuda:{now}")
+    if device >= 0 and now != device:
+        raise ValueError(f"{what} is on cuda:{device}, the current device is cuda:{now}")
     if stream is None:
         # (the handle alone: building torch's stream object takes as long as a launch)
         return torch._C._cuda_getCurrentRawStream(now)
@@ -274,3 +318,185 @@ def evict(cache: Cache, blocks, lens, weights, keep: int, recent: int, to_blocks
     to = _pack_kept(to_blocks.data_ptr(), stride, width, _numbers(to_lens, batch, "to_lens"), ow, ow_stride, index.data_ptr())
     _check("us_kv_evict", lib().us_kv_evict(cache._there, _seqs(blocks, lens, None, 1, on), w, w_stride, max_len or 0,
                                             keep, recent, to, _stream(stream, cache)))
+
+
+def _workspace(ws, device):
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return 0, 0
+    if not (_on(ws, device) and ws.is_contiguous()):
+        raise TypeError("ws: a contiguous tensor on the cache's GPU is wanted")
+    return ws.data_ptr(), ws.nbytes
+
+
+def _zeros(n: int, device):
+    """A zero-filled workspace of n bytes."""
+    return torch.zeros((n + 3) // 4, dtype=_I32, device=device)
+
+
+def _vector(t, n, dtype, name, device) -> int:
+    """Address of n contiguous numbers on GPU `device`; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise TypeError(f"{name}: {n} contiguous {str(dtype)[6:]} numbers are wanted")
+    if not _on(t, device):
+        raise TypeError(f"{name}: a tensor on the call's GPU is wanted")
+    return t.data_ptr()
+
+
+def rotate(q, k, freq, positions, q_out=None, k_out=None, adjacent: bool = False, norm: bool = False, q_weight=None,
+           k_weight=None, eps: float = 1e-6, offset: int = 0, stream=None) -> None:
+    """us_kv_rotate: norms (norm=True) of query and key heads, and their rotation by freq (axes, pairs) times
+    positions (axes, tokens); in place where no q_out and k_out are given. k may be None, and freq (no rotation)."""
+    L = lib()
+    tokens, heads, d = q.shape
+    on = q.get_device() if q.is_cuda else -1
+    if on < 0:
+        raise TypeError("q: a tensor on a GPU is wanted")
+    rows = _rows(q, heads, d, "q", on)
+    rows_out = rows if q_out is None else _rows(q_out, heads, d, "q_out", on)
+    k_heads, k_rows, k_rows_out = 0, None, None
+    if k is not None:
+        k_heads = k.shape[1]
+        k_rows = _rows(k, k_heads, d, "k", on)
+        k_rows_out = k_rows if k_out is None else _rows(k_out, k_heads, d, "k_out", on)
+    elif k_out is not None:
+        raise TypeError("k_out: there is no k")
+    axes, pairs, at, at_pos, stride = 0, 0, 0, 0, 0
+    if freq is not None:
+        axes, pairs = (1, freq.shape[0]) if freq.dim() == 1 else freq.shape
+        if freq.dtype is not _F32 or freq.dim() > 2 or not freq.is_contiguous() or not _on(freq, on):
+            raise TypeError("freq: a contiguous float32 tensor (axes, pairs) on the rows' GPU is wanted")
+        shape = (tokens,) if positions.dim() == 1 else (axes, tokens)
+        if positions.dtype is not _I32 or positions.shape != shape or (positions.stride(-1) != 1 and tokens > 1) or \
+                (positions.dim() == 1 and axes != 1) or not _on(positions, on):
+            raise TypeError(f"positions: int32 numbers ({axes}, {tokens}) in contiguous rows on the rows' GPU are wanted")
+        at, at_pos = freq.data_ptr(), positions.data_ptr()
+        stride = positions.stride(0) if positions.dim() == 2 and axes > 1 else tokens
+    how = _pack_rotation(at, pairs, axes, at_pos, stride, offset, 1 if adjacent else 0, 1 if norm else 0, eps,
+                         _vector(q_weight, d, _F32, "q_weight", on), _vector(k_weight, d, _F32, "k_weight", on))
+    _check("us_kv_rotate", L.us_kv_rotate(heads, k_heads, d, rows, rows_out, k_rows, k_rows_out, how,
+                                          _stream_on(stream, on, "q")))
+
+
+def fork_workspace(cache: Cache, blocks, to_blocks):
+    """A zero-filled workspace for fork calls between tables of these sizes."""
+    n = ctypes.c_size_t(0)
+    _check("us_kv_fork_workspace_size", lib().us_kv_fork_workspace_size(cache._packed, blocks.shape[0], to_blocks.shape[0],
+                                                                        ctypes.byref(n)))
+    return _zeros(n.value, cache.k.device)
+
+
+def fork(cache: Cache, refs, blocks, lens, parents, to_blocks, to_lens, missing, room=None, ws=None, stream=None) -> None:
+    """us_kv_fork: new sequences (to_blocks, to_lens) that go on from the old ones `parents` (None: each from its own),
+    with blocks for `room` more tokens each; refs counts the tables' references to every block."""
+    on = cache.device
+    batch, width, stride = _table(to_blocks, "to_blocks")
+    seqs = _seqs(blocks, lens, None, 1, on)
+    if not _on(to_blocks, on):
+        raise TypeError("to_blocks: a tensor on the cache's GPU is wanted")
+    to = _pack_forked(to_blocks.data_ptr(), stride, width, batch, _vector(to_lens, batch, _I32, "to_lens", on))
+    at, n = _workspace(ws, on)
+    _check("us_kv_fork", lib().us_kv_fork(
+        cache._there, _vector(refs, cache.n_blocks, _I32, "refs", on), seqs, _vector(parents, batch, _I32, "parents", on),
+        _vector(room, batch, _I32, "room", on), to, _vector(missing, 1, _I32, "missing", on), at, n, _stream(stream, cache)))
+
+
+def _groups(group_starts, shared, max_group, max_shared, device) -> bytes:
+    n = group_starts.shape[0] - 1
+    return _pack_groups(_vector(group_starts, n + 1, _I32, "group_starts", device), _vector(shared, n, _I32, "shared", device),
+                        n, max_group, max_shared or 0)
+
+
+def attend_shared_workspace(cache: Cache, q, blocks, group_starts, starts=None, max_q: int = 1, max_group=None,
+                            max_shared=None, max_len=None, causal: bool = True):
+    """A workspace for attend_shared calls of these sizes (groups of up to max_group sequences, or of all)."""
+    batch, n = blocks.shape[0], ctypes.c_size_t(0)
+    at, count = group_starts.data_ptr(), group_starts.shape[0] - 1
+    _check("us_kv_attend_shared_workspace_size", lib().us_kv_attend_shared_workspace_size(
+        cache._packed, _sizes(blocks, starts, max_q), q.shape[1], q.shape[0],
+        _pack_groups(at, at, count, max_group or batch, max_shared or 0),
+        _opts(None, causal, 0, max_len, None, batch, cache.heads, cache.device), ctypes.byref(n)))
+    return _zeros(n.value, cache.k.device)
+
+
+def attend_shared(cache: Cache, blocks, lens, q, out, group_starts, shared, starts=None, max_q: int = 1, max_group=None,
+                  max_shared=None, max_len=None, scale=None, causal: bool = True, ws=None, stream=None) -> None:
+    """us_kv_attend_shared: attend, with the first shared[g] blocks of group g's sequences (group_starts[g] ..
+    group_starts[g + 1] - 1) read once for all of them."""
+    heads, d, on, batch = q.shape[1], cache.head_dim, cache.device, blocks.shape[0]
+    at, n = _workspace(ws, on)
+    _check("us_kv_attend_shared", lib().us_kv_attend_shared(
+        cache._there, _seqs(blocks, lens, starts, max_q, on), heads, _rows(q, heads, d, "q", on), _rows(out, heads, d, "out", on),
+        _groups(group_starts, shared, max_group or batch, max_shared, on),
+        _opts(scale, causal, 0, max_len, None, batch, cache.heads, on), at, n, _stream(stream, cache)))
+
+
+def new_summary(cache: Cache):
+    """Room for the extremes of every block's keys: uint8 (n_blocks, heads, 2, row(head_dim))."""
+    return torch.full((cache.n_blocks, cache.heads, 2, row(cache.head_dim)), 128, dtype=torch.uint8, device=cache.k.device)
+
+
+def _summary(t, cache) -> int:
+    if t.dtype is not torch.uint8 or t.shape != (cache.n_blocks, cache.heads, 2, row(cache.head_dim)) or not t.is_contiguous():
+        raise TypeError(f"summary: a contiguous uint8 tensor {(cache.n_blocks, cache.heads, 2, row(cache.head_dim))} is wanted")
+    if not _on(t, cache.device):
+        raise TypeError("summary: a tensor on the cache's GPU is wanted")
+    return t.data_ptr()
+
+
+def summarise(cache: Cache, blocks, lens, summary, starts=None, max_new: int = 1, stream=None) -> None:
+    """us_kv_summarise: the extremes of the keys of the blocks that the sequences' last tokens are in, after append."""
+    _check("us_kv_summarise", lib().us_kv_summarise(cache._there, _seqs(blocks, lens, starts, max_new, cache.device),
+                                                    _summary(summary, cache), _stream(stream, cache)))
+
+
+def _chosen(t, tokens, cache):
+    """Address of a (tokens, heads, top) table of blocks, and top."""
+    if t.dtype is not _I32 or t.dim() != 3 or t.shape[:2] != (tokens, cache.heads) or not t.is_contiguous():
+        raise TypeError(f"chosen: a contiguous int32 tensor ({tokens}, {cache.heads}, blocks) is wanted")
+    if not _on(t, cache.device):
+        raise TypeError("chosen: a tensor on the cache's GPU is wanted")
+    return t.data_ptr(), t.shape[2]
+
+
+def choose_workspace(cache: Cache, blocks, chosen, starts=None, max_q: int = 1):
+    """A zero-filled workspace for choose calls of these sizes."""
+    n = ctypes.c_size_t(0)
+    _check("us_kv_choose_workspace_size", lib().us_kv_choose_workspace_size(
+        cache._packed, _sizes(blocks, starts, max_q), chosen.shape[0], chosen.shape[2], ctypes.byref(n)))
+    return _zeros(n.value, cache.k.device)
+
+
+def choose(cache: Cache, summary, blocks, lens, q, scores, chosen, starts=None, max_q: int = 1, max_len=None, sinks: int = 1,
+           recent: int = 1, ws=None, stream=None) -> None:
+    """us_kv_choose: for every row of q and cache head, the first `sinks`, the last `recent` and else the blocks of
+    highest possible score, ascending, then -1: chosen (tokens, heads, top); the scores of all: (tokens, heads, blocks)."""
+    tokens, heads, on = q.shape[0], q.shape[1], cache.device
+    at, top = _chosen(chosen, tokens, cache)
+    at_scores, stride = _weights(scores, tokens, cache.heads, "scores", on)
+    at_ws, n = _workspace(ws, on)
+    _check("us_kv_choose", lib().us_kv_choose(
+        cache._there, _seqs(blocks, lens, starts, max_q, on), _summary(summary, cache), heads,
+        _rows(q, heads, cache.head_dim, "q", on), _pack_choice(at_scores, stride, at, top, sinks, recent, max_len or 0), at_ws, n,
+        _stream(stream, cache)))
+
+
+def attend_chosen_workspace(cache: Cache, q, blocks, chosen, starts=None, max_q: int = 1):
+    """A zero-filled workspace for attend_chosen calls of these sizes."""
+    n = ctypes.c_size_t(0)
+    _check("us_kv_attend_chosen_workspace_size", lib().us_kv_attend_chosen_workspace_size(
+        cache._packed, _sizes(blocks, starts, max_q), q.shape[1], q.shape[0], chosen.shape[2], ctypes.byref(n)))
+    return _zeros(n.value, cache.k.device)
+
+
+def attend_chosen(cache: Cache, blocks, lens, q, out, chosen, starts=None, max_q: int = 1, scale=None, ws=None,
+                  stream=None) -> None:
+    """us_kv_attend_chosen: attend over the blocks chosen[t, h] alone, for row t and cache head h."""
+    heads, d, on = q.shape[1], cache.head_dim, cache.device
+    at, top = _chosen(chosen, q.shape[0], cache)
+    at_ws, n = _workspace(ws, on)
+    _check("us_kv_attend_chosen", lib().us_kv_attend_chosen(
+        cache._there, _seqs(blocks, lens, starts, max_q, on), heads, _rows(q, heads, d, "q", on), _rows(out, heads, d, "out", on),
+        at, top, _opts(scale, True, 0, None, None, blocks.shape[0], cache.heads, on), at_ws, n, _stream(stream, cache)))

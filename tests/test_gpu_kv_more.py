@@ -1,0 +1,650 @@
+"""GPU parity of what surrounds the 8-bit key/value cache: rotations, forks, shared and sparse attention.
+
+Tables, references, copied blocks, extremes and chosen blocks are whole numbers and compared as
+such. Scores of blocks are defined as a float64 sum rounded once to float32: the sum's own
+rounding, 2 R 2^-53 of its terms, moves that by at most one more unit where it lies on a border.
+Attention is compared within the bounds of test_gpu_kv.py, whose kernels' bodies it shares; a join
+of two parts adds two products and a sum in float32, 3 2^-24 of the result's size. Rotations:
+
+* an angle is off by at most 3 |a| 2^-53 (products, their sum, the division by a turn); what is
+  left of it below pi / 4 is rounded to float32, 0.79 2^-24 at most; the series of sine and cosine
+  add at most 2 2^-24 in their last steps and 0.1 2^-24 left out: 3 2^-24 + 3 |a| 2^-53 together;
+* a norm's sum of D squares has at most 13 roundings in a row (8 of a lane, 5 of the join), halved
+  by the root; its division, the eps, the root, the inverse and two products add 6: 13 2^-24 of a value;
+* the turned value n1 c - n2 s adds 2 roundings of a product and a sum of |n1| + |n2|.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv as ref
+from paper_2608_09291_amd import kv
+from test_gpu_kv import DTYPES, OUT, Pool, _check, _starts, _torch_dtype
+from test_gpu_spmm import announce, torch_cuda  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+# --- rotations ---------------------------------------------------------------------
+
+ROTATE = [  # tokens, q heads, k heads, head_dim, pairs, axes, adjacent, norm
+    (1, 1, 0, 64, 32, 1, False, False), (1, 32, 32, 128, 64, 1, False, True), (5, 8, 2, 128, 64, 1, True, True),
+    (3, 3, 1, 80, 40, 2, False, True), (7, 4, 4, 96, 12, 3, True, False), (33, 2, 1, 256, 128, 1, False, True),
+    (300, 5, 1, 64, 16, 4, False, True), (17, 2, 2, 13, 6, 1, False, True), (9, 1, 1, 2, 1, 1, True, True),
+    (4, 3, 0, 1, 0, 0, False, True), (2100, 1, 1, 192, 5, 1, False, False), (2, 40, 40, 128, 0, 0, False, True),
+    (6, 71, 9, 100, 50, 1, True, False), (2050, 20, 4, 64, 32, 2, True, True), (11, 2, 1, 255, 127, 1, False, True),
+]
+
+
+def _rotate_bound(x, y, freq, positions, offset, adjacent, eps, dtype, weight=None):
+    """Bound of |got - y| by the module's derivation; x the rows before, y the oracle's after."""
+    n = np.abs(ref.rotate(x, weight=weight, eps=eps) if eps is not None else x.astype(np.float64))
+    e = (13 * U if eps is not None else 0) * n
+    if freq is not None:
+        pairs = freq.shape[1]
+        angle = (np.abs(positions.astype(np.float64) + offset)[:, :, None] * np.abs(freq)[:, None]).sum(0)   # tokens, pairs
+        one = slice(0, 2 * pairs, 2) if adjacent else slice(0, pairs)
+        two = slice(1, 2 * pairs, 2) if adjacent else slice(pairs, 2 * pairs)
+        both = n[..., one] + n[..., two]
+        more = both * ((5 + (13 if eps is not None else 0)) * U + 3 * angle[:, None] * 2.0 ** -53)
+        e[..., one], e[..., two] = more, more
+    return e + OUT[dtype] * np.abs(y) + (2.0 ** -25 if dtype == "f16" else 1e-44)
+
+
+def _rotate_case(torch, T, H, Hk, D, pairs, axes, adjacent, norm, dtype, far=5000, offset=0, spread=1.5, aligned=False, inplace=False,
+                 seed=0):
+    rng = np.random.default_rng(T + H + D + pairs + seed)
+    dt = _torch_dtype(torch, dtype)
+    pad = 0 if aligned else 3
+    wide = torch.from_numpy(rng.normal(0, spread, size=(T, H + Hk, D + pad)).astype(np.float32)).to(dt).cuda()
+    q, k = wide[:, :H, pad // 2:pad // 2 + D], wide[:, H:, pad // 2:pad // 2 + D] if Hk else None
+    freq = positions = None
+    if pairs:
+        freq = rng.uniform(0, 1, size=(axes, pairs)).astype(np.float32) ** 4
+        positions = rng.integers(-3, far, size=(axes, T)).astype(np.int32)
+    eps = 1e-5 if norm else None
+    qw = rng.uniform(0.5, 1.5, size=D).astype(np.float32) if norm else None
+    before = [x.double().cpu().numpy() for x in (q, k) if x is not None]
+    out = [torch.full((T, n, D), math.nan, dtype=dt, device="cuda") for n in (H, Hk) if n]
+    args = dict(adjacent=adjacent, norm=norm, offset=offset, q_weight=None if qw is None else torch.from_numpy(qw).cuda())
+    if norm:
+        args["eps"] = eps
+    if not inplace:
+        args.update(q_out=out[0], k_out=out[1] if Hk else None)
+    kv.rotate(q, k, None if freq is None else torch.from_numpy(freq).cuda(),
+              None if positions is None else torch.from_numpy(positions).cuda(), **args)
+    torch.cuda.synchronize()
+    got = [x.double().cpu().numpy() for x in ([q] + ([k] if Hk else []) if inplace else out)]
+    for x, y, w in zip(before, got, (qw, None)):
+        want = ref.rotate(x, freq, positions, offset, adjacent, w, eps)
+        bound = _rotate_bound(x, want, freq, positions, offset, adjacent, eps, dtype, w)
+        over = np.abs(y - want) - bound
+        assert (over <= 0).all(), (np.unravel_index(over.argmax(), over.shape), over.max())
+    return wide
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("aligned", [False, True])
+@pytest.mark.parametrize("T,H,Hk,D,pairs,axes,adjacent,norm", ROTATE)
+def test_rotate(torch_cuda, T, H, Hk, D, pairs, axes, adjacent, norm, aligned, dtype):
+    announce(f"kv rotate T={T} {H}+{Hk} D={D} pairs={pairs} axes={axes} adjacent={adjacent} norm={norm} aligned={aligned} {dtype}")
+    _rotate_case(torch_cuda, T, H, Hk, D, pairs, axes, adjacent, norm, dtype, aligned=aligned)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("aligned", [False, True])
+def test_rotate_in_place(torch_cuda, aligned, adjacent):
+    announce(f"kv rotate in place aligned={aligned} adjacent={adjacent}")
+    for D, pairs in ((128, 64), (80, 40), (64, 7)):
+        _rotate_case(torch_cuda, 50, 6, 3, D, pairs, 1, adjacent, True, "bf16", aligned=aligned, inplace=True)
+
+
+@pytest.mark.parametrize("offset", [-1, 7])
+def test_rotate_far_positions(torch_cuda, offset):
+    """Positions near 2^31, where float32 angles would be off by whole turns."""
+    announce(f"kv rotate far offset={offset}")
+    _rotate_case(torch_cuda, 40, 2, 2, 64, 32, 1, False, False, "f32", far=2 ** 31 - 1, offset=offset, aligned=True)
+
+
+@pytest.mark.parametrize("spread", [1e25, 1e-25])
+def test_norms_of_large_and_small_rows(torch_cuda, spread):
+    """Squares past float32's range: the norm is of the rows' values all the same."""
+    announce(f"kv rotate rows of {spread}")
+    _rotate_case(torch_cuda, 9, 3, 1, 128, 64, 1, False, True, "f32", spread=spread)
+
+
+def test_rotate_nan_and_infinity_stay_in_their_row(torch_cuda):
+    torch = torch_cuda
+    announce("kv rotate nan")
+    x = torch.randn((4, 3, 64), device="cuda")
+    x[1, 0, 5], x[2, 1, 40] = math.nan, math.inf
+    freq, pos = torch.rand(32, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(x)
+    kv.rotate(x, None, freq, pos, q_out=out, norm=True)
+    bad = ~torch.isfinite(out).all(-1)
+    assert bad.nonzero().tolist() == [[1, 0], [2, 1]]
+
+
+# --- forks ---------------------------------------------------------------------------
+
+FORK = [  # lens, parents (None: each its own), room, width of the new tables beyond the old, spare blocks
+    ([1], [0], None, 0, 2), ([64], [0], [1], 1, 3), ([130, 64, 5], [1, 1, 0, 0, 0, -1, 2], [1] * 7, 1, 20),
+    ([130, 64, 5], None, [64, 0, 200], 4, 12), ([0, 200], [0, 0, 1, 1], [3, 70, 0, 500], 3, 30),
+    ([300, 127, 128], [2, 2, 2], None, 0, 3), ([300, 20], [-1, -1, -7, 9], None, 0, 1), ([100], [0] * 70, [30] * 70, 1, 140),
+    ([65, 63, 64] * 30, [89 - i for i in range(90)], [1] * 90, 1, 100), ([500] * 3, [2, 2, 2, 2, 0], [-5, 0, 1, 100, 1000], 700, 30),
+    ([70, 70], [0, 0, 0], None, 0, 1),                     # too few free blocks: two copies, one block
+    ([70], [0], [10000], 300, 5), ([20000], [0, 0], [1, 1], 1, 3),
+]
+
+
+def _fork_case(torch, lens, parents, room, wider, spare, heads=2, D=80, refs_of=None, blocks_of=None):
+    rng = np.random.default_rng(sum(lens) + spare)
+    p = Pool(torch, rng, lens, heads, D, spare=spare)
+    for i in range(2):                                      # (scales that can be compared)
+        p.scales[i] = np.where(np.isnan(p.scales[i]), np.float32(0.5), p.scales[i])
+    blocks = [list(r) for r in p.blocks]
+    if blocks_of:
+        blocks_of(blocks, p)
+    refs = [0] * p.n
+    for row in blocks:
+        for x in row:
+            if 0 <= x < p.n:
+                refs[x] += 1
+    if refs_of:
+        refs_of(refs, blocks)
+    n = len(lens) if parents is None else len(parents)
+    width = p.width + wider
+    cache = p.cache()
+    pad = torch.full((n, width + 3), 99, dtype=torch.int32, device="cuda")     # rows further apart than they are wide
+    to, to_lens, missing = pad[:, :width], p.dev([7] * n), p.dev([7])
+    r = p.dev(refs)
+    ws = kv.fork_workspace(cache, p.dev(blocks), to)
+    args = (r, p.dev(blocks), p.dev(lens), None if parents is None else p.dev(parents), to, to_lens, missing)
+    kv.fork(cache, *args, room=None if room is None else p.dev(room), ws=ws)
+    torch.cuda.synchronize()
+    want = ref.fork(refs, blocks, lens, list(range(n)) if parents is None else parents, room, width)
+    assert missing.tolist() == [want[4]]
+    assert to.cpu().tolist() == want[0] and to_lens.tolist() == want[1] and r.tolist() == want[2]
+    assert (pad[:, width:] == 99).all()
+    for a, b in want[3]:
+        for x in p.codes + p.scales:
+            x[b] = x[a]
+    p.same(cache)
+    return p, cache, ws, want
+
+
+@pytest.mark.parametrize("lens,parents,room,wider,spare", FORK)
+def test_fork(torch_cuda, lens, parents, room, wider, spare):
+    announce(f"kv fork lens={lens[:6]} parents={parents and parents[:8]} room={room and room[:6]} wider={wider} spare={spare}")
+    _fork_case(torch_cuda, lens, parents, room, wider, spare)
+
+
+@pytest.mark.parametrize("heads,D", [(1, 64), (5, 128), (3, 192), (1, 256), (40, 96)])
+def test_fork_heads_and_widths(torch_cuda, heads, D):
+    announce(f"kv fork heads={heads} D={D}")
+    _fork_case(torch_cuda, [70, 130], [0, 1, 0, 1, 1], [1] * 5, 1, 20, heads, D)
+
+
+def test_fork_of_started_blocks_that_others_hold(torch_cuda):
+    """A started or spare block with more than one reference is not the first child's to write to."""
+    announce("kv fork held blocks")
+
+    def same_started(blocks, p):
+        blocks[1][1] = blocks[0][1]                         # (100 tokens each: their second block is one)
+
+    _fork_case(torch_cuda, [100, 100], [0, 1, 1], [1, 1, 1], 0, 9, blocks_of=same_started)
+
+    def held(refs, blocks):
+        refs[blocks[0][1]] += 1                             # by a table that the call does not see
+
+    _fork_case(torch_cuda, [100, 100], [0, 0, 1], [1, 1, 70], 1, 9, refs_of=held)
+
+
+def test_fork_over_holes_and_numbers_out_of_range(torch_cuda):
+    announce("kv fork holes")
+
+    def holes(blocks, p):
+        blocks[0][0], blocks[0][2], blocks[1][1], blocks[1][2] = -5, p.n, 2 ** 31 - 1, -2 ** 31
+
+    _fork_case(torch_cuda, [150, 192], [0, 0, 1, 1], [1, 100, 1, 0], 2, 12, blocks_of=holes)
+
+
+def test_fork_keeps_spare_blocks_and_drops_the_rest(torch_cuda):
+    """Blocks behind the tokens stay with the first child as far as it has room, and go back otherwise."""
+    announce("kv fork spare blocks")
+
+    def longer(blocks, p):
+        for row in blocks:
+            row[2:4] = [p.free.pop(), p.free.pop()]
+
+    _fork_case(torch_cuda, [100, 100, 250], [0, 0, 1], [40, 40, 0], 0, 12, blocks_of=longer)
+
+
+def test_fork_step_by_step_and_captured(torch_cuda):
+    """Beams that grow and fork at every token, eager and from a graph: tables, references and tokens as if copied."""
+    torch = torch_cuda
+    announce("kv fork captured")
+    rng = np.random.default_rng(3)
+    B, heads, D, steps = 4, 2, 64, 70
+    n_blocks, width = 40, 4
+    caches = [kv.new_cache(n_blocks, heads, D) for _ in range(2)]
+    ints = dict(dtype=torch.int32, device="cuda")
+    state = []
+    for c in caches:
+        s = dict(tables=[torch.full((B, width), -1, **ints) for _ in range(2)], lens=[torch.zeros(B, **ints) for _ in range(2)],
+                 refs=torch.zeros(n_blocks, **ints), missing=torch.zeros(1, **ints))
+        s["ws"] = kv.fork_workspace(c, s["tables"][0], s["tables"][1])
+        state.append(s)
+    parents, room = torch.zeros(B, **ints), torch.ones(B, **ints)
+    x = torch.zeros((B, heads, D), device="cuda")
+
+    def step(c, s, a):
+        kv.fork(c, s["refs"], s["tables"][a], s["lens"][a], parents, s["tables"][1 - a], s["lens"][1 - a], s["missing"], room=room,
+                ws=s["ws"])
+        s["lens"][1 - a].add_(1)
+        kv.append(c, s["tables"][1 - a], s["lens"][1 - a], x, x)
+
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for a in range(2):
+        with torch.cuda.graph(graphs[a]):
+            step(caches[0], state[0], a)
+    history = [[] for _ in range(B)]
+    for i in range(steps):
+        ps = [int(v) for v in rng.integers(0, B, size=B)]
+        parents.copy_(torch.tensor(ps, dtype=torch.int32))
+        x.copy_(torch.from_numpy(rng.normal(0, 1, size=(B, heads, D)).astype(np.float32)))
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(caches[1], state[1], i % 2)
+        torch.cuda.synchronize()
+        now = 1 - i % 2
+        history = [history[p] + [x[b].cpu()] for b, p in enumerate(ps)]
+        for c, s in zip(caches, state):
+            assert s["missing"].item() == 0 and s["lens"][now].tolist() == [i + 1] * B
+            table, count = s["tables"][now].cpu().numpy(), np.zeros(n_blocks, int)
+            np.add.at(count, table[table >= 0], 1)
+            assert (s["refs"].cpu().numpy() == count).all()
+        assert torch.equal(state[0]["tables"][now], state[1]["tables"][now])
+        assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v_scale, caches[1].v_scale)
+    n = steps
+    out = [torch.empty((B * n, heads, D), device="cuda") for _ in range(2)]
+    kv.read(caches[0], state[0]["tables"][n % 2], state[0]["lens"][n % 2], *out, starts=torch.arange(0, B * n + 1, n, **ints), max_new=n)
+    want = torch.stack([torch.stack(h) for h in history]).view(B * n, heads, D)
+    # a scale of at most 5 / 127 and half a step, once more for every growth of a block's scale: 64 of them at most
+    assert (out[0].cpu() - want).abs().max() <= 65 * 0.5 * want.abs().max() / 127
+    assert (out[0].cpu() - want).norm() <= 0.02 * want.norm()
+
+
+# --- shared prefixes -----------------------------------------------------------------
+
+SHARED = [  # group sizes, blocks in common, own tokens of each sequence, queries of each, q heads, cache heads, head_dim
+    ([1], [1], [1], [1], 1, 1, 64), ([3], [2], [1, 30, 64], [1] * 3, 4, 2, 128), ([2, 1, 3], [3, 0, 1], [5, 70, 200, 1, 64, 65], [1] * 6, 8, 2, 96),
+    ([5], [20], [10, 3, 90, 64, 1], [1] * 5, 8, 1, 128), ([20], [30], list(range(1, 21)), [1] * 20, 4, 4, 80),
+    ([40], [9], [7 + i for i in range(40)], [1] * 40, 16, 2, 128), ([3, 4], [4, 2], [9, 20, 4, 100, 70, 3, 8], [3, 1, 4, 0, 2, 3, 5], 6, 2, 64),
+    ([2], [3], [150, 90], [150, 90], 4, 2, 128), ([9], [5], [33] * 9, [30] * 9, 5, 1, 192), ([3], [6], [11, 12, 80], [2] * 3, 24, 1, 256),
+    ([70, 30], [11, 3], [3] * 100, [1] * 100, 4, 1, 64), ([2, 2], [200, 3], [30, 900, 2000, 1], [1] * 4, 8, 2, 128),
+]
+
+
+class Groups(Pool):
+    """A pool whose sequences have their groups' first blocks in common."""
+
+    def __init__(self, torch, rng, sizes, common, own, heads, D):
+        lens = [64 * c + 0 for n, c in zip(sizes, common) for _ in range(n)]
+        self.lens_ = [a + b for a, b in zip(lens, own)]
+        super().__init__(torch, rng, self.lens_, heads, D)
+        b = 0
+        for n, c in zip(sizes, common):
+            for j in range(1, n):
+                self.blocks[b + j][:c] = self.blocks[b][:c]
+            b += n
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("sizes,common,own,new,H,Hk,D", SHARED)
+def test_attend_shared(torch_cuda, sizes, common, own, new, H, Hk, D, causal, dtype):
+    torch = torch_cuda
+    announce(f"kv shared sizes={sizes} common={common} own={own[:6]} new={new[:6]} {H}/{Hk} D={D} causal={causal} {dtype}")
+    rng = np.random.default_rng(sum(own) + H + D)
+    p = Groups(torch, rng, sizes, common, own, Hk, D)
+    lens, T = p.lens_, sum(new)
+    cache = p.cache()
+    wide = torch.from_numpy(rng.normal(0, 1.5, size=(T, H, D + 3)).astype(np.float32)).to(_torch_dtype(torch, dtype)).cuda()
+    q = wide[:, :, 1:D + 1]
+    out = torch.full((T, H, D), math.nan, dtype=q.dtype, device="cuda")
+    one = new == [1] * len(new)
+    args = dict(starts=None if one else p.dev(_starts(new)), max_q=max(new), causal=causal)
+    groups = p.dev(_starts(sizes))
+    more = dict(max_group=max(sizes), max_shared=max(max(common), 1))
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, **args, **more)
+    first = None
+    for again in range(2):                                  # the workspace holds anything: the bytes of NaN the second time
+        out.fill_(math.nan)
+        kv.attend_shared(cache, p.dev(p.blocks), p.dev(lens), q, out, groups, p.dev(common), ws=ws, **args, **more)
+        torch.cuda.synchronize()
+        _check(torch, p, lens, new, q, out, dtype, causal=causal)
+        if first is None:
+            first = out.clone()
+            ws.fill_(-1)
+    assert torch.equal(first, out)
+    # without bounds of the groups, with the lengths' bound
+    out.fill_(math.nan)
+    args["max_len"] = max(lens)
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, **args)
+    kv.attend_shared(cache, p.dev(p.blocks), p.dev(lens), q, out, groups, p.dev(common), ws=ws, **args)
+    torch.cuda.synchronize()
+    _check(torch, p, lens, new, q, out, dtype, causal=causal)
+
+
+def test_attend_shared_sequences_of_no_group_and_short_ones(torch_cuda):
+    """Sequences ahead of the first group, behind the last, past max_group; sequences shorter than what they share, and empty ones."""
+    torch = torch_cuda
+    announce("kv shared outside of groups")
+    rng = np.random.default_rng(4)
+    lens, H, Hk, D = [100, 300, 257, 0, 40, 128, 300, 77], 4, 2, 64
+    p = Pool(torch, rng, lens, Hk, D)
+    for b in (2, 3, 4, 5):                                  # sequences 1 .. 5 are a group of 4 blocks, but 5 is past max_group
+        if b != 5:
+            p.blocks[b][:4] = p.blocks[1][:4]
+    cache = p.cache()
+    q = torch.randn((8, H, D), device="cuda")
+    out = torch.full_like(q, math.nan)
+    groups, common = p.dev([1, 6, 7]), p.dev([4, 2])
+    args = (cache, p.dev(p.blocks), p.dev(lens), q, out, groups, common)
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, max_group=4, max_shared=4)
+    kv.attend_shared(*args, max_group=4, max_shared=4, ws=ws)
+    torch.cuda.synchronize()
+    _check(torch, p, lens, [1] * 8, q, out, "f32")
+    assert (out[3] == 0).all()
+    # tables of anything: in range or not, nothing outside is read and other sequences' rows are theirs
+    for starts, shared in (([5, 2, -9], [4, 4]), ([0, 2 ** 31 - 1, 1], [2 ** 31 - 1, -2 ** 31]), ([-2 ** 31, 8, 8], [0, 3])):
+        kv.attend_shared(cache, p.dev(p.blocks), p.dev(lens), q, out, p.dev(starts), p.dev(shared), ws=ws, max_group=4, max_shared=4)
+        torch.cuda.synchronize()
+        assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_shared_keeps_a_nan_and_a_row_behind(torch_cuda, new):
+    """A NaN query spoils its own row alone; rows behind the last sequence's are left as they were."""
+    torch = torch_cuda
+    announce(f"kv shared nan new={new}")
+    rng = np.random.default_rng(5)
+    sizes, common, own, H, Hk, D = [6], [5], [50] * 6, 8, 2, 128
+    p = Groups(torch, rng, sizes, common, own, Hk, D)
+    cache, T = p.cache(), 6 * new
+    q = torch.randn((T + 3, H, D), device="cuda")
+    q[2, 3, 7] = math.nan
+    out = torch.full_like(q, 5.0)
+    groups = p.dev([0, 6])
+    args = dict(starts=p.dev([i * new for i in range(7)]), max_q=new, max_group=6, max_shared=5)
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, **args)
+    kv.attend_shared(cache, p.dev(p.blocks), p.dev(p.lens_), q, out, groups, p.dev(common), ws=ws, **args)
+    torch.cuda.synchronize()
+    assert (out[T:] == 5.0).all() and torch.isnan(out[2, 3]).all()
+    q[2, 3, 7] = 0.0
+    o2 = torch.full_like(q, 5.0)
+    kv.attend_shared(cache, p.dev(p.blocks), p.dev(p.lens_), q, o2, groups, p.dev(common), ws=ws, **args)
+    torch.cuda.synchronize()
+    same = torch.ones((T + 3, H), dtype=torch.bool, device="cuda")
+    same[2, 3] = False
+    assert torch.equal(out[same], o2[same])
+    _check(torch, p, p.lens_, [new] * 6, q[:T], o2[:T], "f32")
+
+
+@pytest.mark.parametrize("factor", [1e3, 1e6])
+def test_attend_shared_large_scores(torch_cuda, factor):
+    """Scores of millions, whose maxima lie in either part."""
+    torch = torch_cuda
+    announce(f"kv shared scores {factor}")
+    rng = np.random.default_rng(6)
+    sizes, common, own = [5, 2], [3, 9], [100, 3, 64, 1, 200, 30, 30]
+    p = Groups(torch, rng, sizes, common, own, 2, 128)
+    q = torch.from_numpy(rng.normal(0, factor, size=(7, 8, 128)).astype(np.float32)).cuda()
+    out = torch.empty_like(q)
+    groups = p.dev(_starts(sizes))
+    cache = p.cache()
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups)
+    kv.attend_shared(cache, p.dev(p.blocks), p.dev(p.lens_), q, out, groups, p.dev(common), ws=ws)
+    torch.cuda.synchronize()
+    got = out.double().cpu().numpy()
+    want, size, _, reach = ref.attend(p.codes[0], p.scales[0], p.codes[1], p.scales[1], 128, p.blocks, p.lens_, None, q.double().cpu().numpy())
+    # a score is off by (R + 8) 2^-24 of its reach, and 2^-22 for the query's halves: that much in the exponent
+    e = (136 * U + 2.0 ** -22) * reach[..., None]
+    assert (np.abs(got - want) <= (2 * np.expm1(2 * e) + 2.0 ** -20) * size.max() + 1e-30).all()
+
+
+# --- chosen blocks ---------------------------------------------------------------------
+
+CHOOSE = [  # lens, queries, q heads, cache heads, head_dim, top, sinks, recent
+    ([1], [1], 1, 1, 64, 1, 0, 0), ([64, 65, 200], [1] * 3, 4, 2, 128, 2, 1, 1), ([0, 700], [1, 1], 8, 2, 96, 4, 0, 1),
+    ([3000], [1], 8, 1, 128, 7, 1, 2), ([5000, 40, 900], [2, 3, 1], 5, 5, 80, 9, 2, 3), ([1500, 64], [1, 1], 20, 1, 64, 6, 0, 0),
+    ([300], [5], 2, 2, 256, 3, 1, 1), ([4100], [1], 6, 2, 192, 40, 1, 1), ([700], [1], 48, 1, 13, 100, 1, 1), ([640, 639], [1, 1], 2, 1, 1, 5, 5, 0),
+    ([30], [50], 2, 1, 64, 2, 0, 1), ([9000], [1], 3, 1, 128, 64, 0, 64),
+]
+
+
+def _summaries(torch, p, cache, lens):
+    """Summaries of the whole sequences, checked byte for byte; also as numpy (n_blocks, heads, 2, head_dim)."""
+    summary = kv.new_summary(cache)
+    summary.fill_(7)
+    most = max(max(lens), 1)
+    kv.summarise(cache, p.dev(p.blocks), p.dev(lens), summary, starts=p.dev([i * most for i in range(len(lens) + 1)]), max_new=most)
+    torch.cuda.synchronize()
+    got = summary.cpu().numpy()
+    want = np.full(got.shape, 7, np.uint8)[..., :p.D]
+    for b, n in enumerate(lens):
+        for i in range(-(-n // 64)):
+            for h in range(p.H):
+                if 0 <= p.blocks[b][i] < p.n:
+                    want[p.blocks[b][i], h] = ref.extremes(p.codes[0], p.D, p.blocks[b][i], h, min(64, n - 64 * i))
+    assert np.array_equal(got[..., :p.D], want)
+    return summary, want
+
+
+def _choose_case(torch, lens, new, H, Hk, D, top, sinks, recent, dtype, holes=(), spoil=None, max_len=None):
+    rng = np.random.default_rng(sum(lens) + H + D + top)
+    p = Pool(torch, rng, lens, Hk, D)
+    for b, i in holes:
+        p.blocks[b][i] = -1 if i % 2 else p.n
+    cache, T, G = p.cache(), sum(new), H // Hk
+    summary, ends = _summaries(torch, p, cache, lens)
+    wide = torch.from_numpy(rng.normal(0, 1.5, size=(T + 2, H, D + 3)).astype(np.float32)).to(_torch_dtype(torch, dtype)).cuda()
+    q = wide[:, :, 1:D + 1]
+    if spoil:
+        spoil(q)
+    one = new == [1] * len(new)
+    starts = None if one else p.dev(_starts(new))
+    scores = torch.full((T + 2, Hk, p.width + 1), 3.0, device="cuda")
+    chosen = torch.full((T + 2, Hk, top), 3, dtype=torch.int32, device="cuda")
+    args = dict(starts=starts, max_q=max(new), sinks=sinks, recent=recent, max_len=max_len)
+    ws = kv.choose_workspace(cache, p.dev(p.blocks), chosen, starts=starts, max_q=max(new))
+    qn, st, first = q.double().cpu().numpy(), _starts(new), None
+    for again in range(2):                                  # the workspace is left as it was found
+        scores.fill_(3.0)
+        chosen.fill_(3)
+        kv.choose(cache, summary, p.dev(p.blocks), p.dev(lens), q, scores, chosen, ws=ws, **args)
+        torch.cuda.synchronize()
+        assert not ws.any()
+        got, got_s = chosen.cpu().numpy(), scores.cpu().numpy()
+        assert (got[T:] == 3).all() and (got_s[T:] == 3.0).all()
+        for b, n in enumerate(lens):
+            for i in range(new[b]):
+                t, at = st[b] + i, n - new[b] + i
+                blocks = at // 64 + 1 if at >= 0 else 0
+                there = [0 <= p.blocks[b][j] < p.n for j in range(blocks)]
+                for h in range(Hk):
+                    want = [ref.score(ends[p.blocks[b][j], h], p.scales[0][p.blocks[b][j], h], qn[t, h * G:h * G + G])
+                            if there[j] else -math.inf for j in range(blocks)]
+                    # one unit in the last place where the float64 sums lie on a border
+                    same = got_s[t, h, :blocks].astype(np.float64)
+                    w = np.array(want, np.float64)
+                    fine = np.isfinite(w)
+                    assert np.array_equal(same[~fine], w[~fine])
+                    assert (np.abs(same[fine] - w[fine]) <= 2.0 ** -23 * np.abs(w[fine])).all()
+                    assert (got_s[t, h, blocks:] == 3.0).all()
+                    take = ref.choose(got_s[t, h, :blocks], there, top, sinks, recent)
+                    assert got[t, h].tolist() == take + [-1] * (top - len(take)), (t, h)
+        if first is None:
+            first = (chosen.clone(), scores.clone())
+    assert torch.equal(first[0], chosen) and torch.equal(first[1], scores)
+    return p, cache, q, chosen, starts
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new,H,Hk,D,top,sinks,recent", CHOOSE)
+def test_choose_and_attend(torch_cuda, lens, new, H, Hk, D, top, sinks, recent, dtype):
+    torch = torch_cuda
+    announce(f"kv choose lens={lens} new={new} {H}/{Hk} D={D} top={top} {sinks}+{recent} {dtype}")
+    p, cache, q, chosen, starts = _choose_case(torch, lens, new, H, Hk, D, top, sinks, recent, dtype)
+    _attend_chosen(torch, p, cache, q, chosen, lens, new, starts, dtype)
+
+
+def _attend_chosen(torch, p, cache, q, chosen, lens, new, starts, dtype, scale=None):
+    T, H, D = sum(new), q.shape[1], q.shape[2]
+    G = H // p.H
+    out = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda")
+    args = dict(starts=starts, max_q=max(new))
+    ws = kv.attend_chosen_workspace(cache, q, p.dev(p.blocks), chosen, **args)
+    first = None
+    for again in range(2):
+        out.fill_(5.0)
+        kv.attend_chosen(cache, p.dev(p.blocks), p.dev(lens), q, out, chosen, ws=ws, scale=scale, **args)
+        torch.cuda.synchronize()
+        if first is None:
+            first = out.clone()
+    assert torch.equal(first, out)                          # bit for bit, and the workspace is left as it was found
+    assert (out[T:] == 5.0).all()
+    got, qn, lists, st = out.double().cpu().numpy(), q.double().cpu().numpy(), chosen.cpu().tolist(), _starts(new)
+    R, most = ref.row_of(D), 64 * chosen.shape[2]
+    for b, n in enumerate(lens):
+        for i in range(new[b]):
+            t = st[b] + i
+            for h in range(H):
+                want, size, reach = ref.attend_chosen(p.codes[0], p.scales[0], p.codes[1], p.scales[1], D, p.blocks[b], n - new[b] + i,
+                                                      lists[t][h // G], qn[t, h], h // G, scale)
+                e_s = (R + 8) * U * reach + (2.0 ** -22 * reach if dtype == "f32" else 0)
+                e_p = 2 * e_s + 2.0 ** -21 + (0 if dtype == "f32" else 2.0 ** -11)
+                bound = (e_p + most * U) * size + OUT[dtype] * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 1e-30)
+                assert (np.abs(got[t, h] - want) <= bound).all(), (t, h)
+    return out
+
+
+@pytest.mark.parametrize("lens,new,holes", [([900, 64], [1, 1], [(0, 0), (0, 5), (0, 14), (1, 0)]), ([2000], [4], [(0, 31), (0, 30), (0, 1)])])
+def test_choose_over_blocks_that_are_not_there(torch_cuda, lens, new, holes):
+    announce(f"kv choose holes={holes}")
+    p, cache, q, chosen, starts = _choose_case(torch_cuda, lens, new, 4, 2, 64, 6, 1, 2, "bf16", holes=holes)
+    _attend_chosen(torch_cuda, p, cache, q, chosen, lens, new, starts, "bf16")
+
+
+def test_choose_with_nan_and_infinite_queries(torch_cuda):
+    """A query head with one does not count; where no head is left, the first blocks are as good as any."""
+    announce("kv choose nan")
+
+    def spoil(q):
+        q[0, 1, 3], q[0, 4, 0], q[0, 5, 63], q[1, 0, 2] = math.nan, math.inf, -math.inf, -math.inf
+        q[1, 3:6] = math.nan
+
+    _choose_case(torch_cuda, [1000, 900], [1, 1], 6, 2, 64, 5, 1, 1, "f32", spoil=spoil)
+
+
+def test_choose_between_equal_scores(torch_cuda):
+    """Blocks of the same keys and scale: the earlier ones are taken."""
+    torch = torch_cuda
+    announce("kv choose ties")
+    rng = np.random.default_rng(8)
+    p = Pool(torch, rng, [64 * 300], 2, 64)
+    for row in p.blocks[0][1:]:
+        p.codes[0][row], p.scales[0][row] = p.codes[0][p.blocks[0][0]], p.scales[0][p.blocks[0][0]]
+    cache = p.cache()
+    summary, _ = _summaries(torch, p, cache, [64 * 300])
+    q = torch.randn((1, 4, 64), device="cuda")
+    scores, chosen = torch.empty((1, 2, 300), device="cuda"), torch.empty((1, 2, 70), dtype=torch.int32, device="cuda")
+    ws = kv.choose_workspace(cache, p.dev(p.blocks), chosen)
+    kv.choose(cache, summary, p.dev(p.blocks), p.dev([64 * 300]), q, scores, chosen, sinks=0, recent=2, ws=ws)
+    assert chosen.cpu().tolist() == [[list(range(68)) + [298, 299]] * 2]
+    assert (scores == scores[..., :1]).all()
+
+
+@pytest.mark.parametrize("blocks,top", [(4096, 100), (4097, 4097), (20000, 64), (20000, 5000)])
+def test_choose_of_very_many_blocks(torch_cuda, blocks, top):
+    """Past what threads hold of the scores, over one block that the whole table names with scales of its own."""
+    torch = torch_cuda
+    announce(f"kv choose blocks={blocks} top={top}")
+    rng = np.random.default_rng(blocks + top)
+    n = 500
+    cache = kv.new_cache(n, 1, 64)
+    cache.k.copy_(torch.from_numpy(rng.integers(1, 256, size=tuple(cache.k.shape), dtype=np.uint8)))
+    cache.k_scale.copy_(torch.from_numpy(rng.uniform(0.01, 0.05, size=(n, 1)).astype(np.float32)))
+    table = torch.from_numpy(rng.integers(0, n, size=(1, blocks)).astype(np.int32)).cuda()
+    lens = torch.tensor([blocks * 64 - 3], dtype=torch.int32, device="cuda")
+    summary = kv.new_summary(cache)
+    kv.summarise(cache, torch.arange(n, dtype=torch.int32, device="cuda")[None], torch.tensor([64 * n], dtype=torch.int32, device="cuda"),
+                 summary, starts=torch.tensor([0, 64 * n], dtype=torch.int32, device="cuda"), max_new=64 * n)
+    q = torch.randn((1, 2, 64), device="cuda")
+    scores, chosen = torch.empty((1, 1, blocks), device="cuda"), torch.empty((1, 1, top), dtype=torch.int32, device="cuda")
+    ws = kv.choose_workspace(cache, table, chosen)
+    for again in range(2):
+        kv.choose(cache, summary, table, lens, q, scores, chosen, sinks=2, recent=3, ws=ws)
+        torch.cuda.synchronize()
+        s = scores[0, 0].cpu().numpy()
+        want = [ref.score(summary[i, 0].cpu().numpy(), cache.k_scale[i, 0].item(), q[0].double().cpu().numpy()) for i in range(n)]
+        w = np.array(want)[table[0].cpu().numpy()]
+        assert (np.abs(s.astype(np.float64) - w) <= 2.0 ** -23 * np.abs(w)).all()
+        assert chosen[0, 0].tolist() == ref.choose(s, [True] * blocks, top, 2, 3)
+
+
+def test_attend_chosen_lists_of_anything(torch_cuda):
+    """Any order, gaps, numbers out of range, blocks behind the position; a block twice counts twice; an empty list gives zeros."""
+    torch = torch_cuda
+    announce("kv chosen lists")
+    rng = np.random.default_rng(9)
+    lens, new, H, Hk, D = [1000, 130, 700], [1, 1, 1], 4, 2, 128
+    p = Pool(torch, rng, lens, Hk, D)
+    cache = p.cache()
+    q = torch.from_numpy(rng.normal(0, 1.5, size=(3, H, D)).astype(np.float32)).cuda()
+    lists = [[[3, -1, 9, 0, 15, 2 ** 31 - 1, 16, -7], [-1] * 8], [[2, 1, 0, 3, 100, -1, -1, -1], [-1, -1, -1, -1, -1, -1, -1, 2]],
+             [[5, 5, 1, 1, 1, 10, 11, -1], [-2 ** 31, 4, 4, 4, 4, 4, 4, 4]]]
+    out = _attend_chosen(torch, p, cache, q, p.dev(lists), lens, new, None, "f32")
+    assert (out[0, 2:] == 0).all()
+    for top in (1, 8):                                      # the same through one part and through several
+        wide = torch.full((3, Hk, 300), -1, dtype=torch.int32, device="cuda")
+        wide[:, :, 290:290 + top] = p.dev(lists)[:, :, :top]
+        _attend_chosen(torch, p, cache, q, wide, lens, new, None, "f32", scale=0.03)
+
+
+def test_choosing_all_blocks_is_attend(torch_cuda):
+    torch = torch_cuda
+    announce("kv chosen all")
+    rng = np.random.default_rng(10)
+    lens, new, H, Hk, D = [400, 65, 1, 0], [3, 1, 1, 1], 8, 2, 128
+    p, cache, q, chosen, starts = _choose_case(torch, lens, new, H, Hk, D, 9, 1, 1, "f32")
+    a, b = torch.empty_like(q[:6].contiguous()), torch.empty_like(q[:6].contiguous())
+    ws = kv.attend_workspace(cache, q[:6], p.dev(p.blocks), starts=starts, max_q=3)
+    kv.attend(cache, p.dev(p.blocks), p.dev(lens), q[:6], a, starts=starts, max_q=3, ws=ws)
+    out = _attend_chosen(torch, p, cache, q, chosen, lens, new, starts, "f32")
+    _check(torch, p, lens, new, q[:6], out[:6], "f32")
+    _check(torch, p, lens, new, q[:6], a, "f32")
+
+
+def test_scores_are_no_less_than_any_key_gives(torch_cuda):
+    torch = torch_cuda
+    announce("kv scores bound")
+    rng = np.random.default_rng(11)
+    lens = [1234]
+    p = Pool(torch, rng, lens, 2, 128)
+    cache = p.cache()
+    summary, _ = _summaries(torch, p, cache, lens)
+    q = torch.from_numpy(rng.normal(0, 1, size=(1, 6, 128)).astype(np.float32)).cuda()
+    scores, chosen = torch.empty((1, 2, 20), device="cuda"), torch.empty((1, 2, 4), dtype=torch.int32, device="cuda")
+    kv.choose(cache, summary, p.dev(p.blocks), p.dev(lens), q, scores, chosen, ws=kv.choose_workspace(cache, p.dev(p.blocks), chosen))
+    torch.cuda.synchronize()
+    for h in range(2):
+        c, s = ref.tokens(p.codes[0], p.scales[0], 128, True, p.blocks[0], 1234, h)
+        x = (c * s[:, None]) @ q[0, 3 * h:3 * h + 3].double().cpu().numpy().T
+        for i in range(20):
+            assert scores[0, h, i].item() >= x[64 * i:64 * i + 64].max() * (1 - 2.0 ** -20)
