@@ -11,6 +11,7 @@
 
 #include <type_traits>
 
+#include "us_device.h"
 #include "us_kv_common.h"
 
 namespace {
@@ -26,7 +27,7 @@ struct RotateArgs {
     const float *freq;
     const int32_t *positions;
     int64_t positions_stride;
-    int32_t pairs, axes, offset, adjacent, norm;
+    int32_t pairs, axes, offset, norm;
     int32_t group, part;                                   // tokens, and rows of each, that a workgroup takes together
     float eps;
     const float *qw, *kw;
@@ -44,97 +45,179 @@ __device__ inline float2 turn(double angle) {
     return make_float2(q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b);
 }
 
-// LANES lanes hold a row, an octet each; the rows of `group` tokens pass through
-// the workgroup together, which has their angles in LDS.
-template <int DT, int LANES, bool VEC>
+// A lane has 16 values of a row, in two octets: 8 pairs, first members in u and second ones in v, or 16 of
+// the values behind the pairs. Slot z's first value and its octets' places:
+struct Slot {
+    int a, b;                                              // first values of the octets
+    int na, nb;                                            // how many of them there are
+    __device__ Slot(int z, int D, int P, bool adjacent) {
+        const int turned = (P + 7) / 8, rest = 2 * P + 16 * (z - turned);
+        const bool pairs = z < turned;
+        a = !pairs ? rest : adjacent ? 16 * z : 8 * z;
+        b = pairs && !adjacent ? P + a : a + 8;
+        const int end = !pairs ? D : adjacent ? 2 * P : P; // of octet a; b's is one further where pairs lie apart
+        na = min(max(end - a, 0), 8);
+        nb = pairs && !adjacent ? na : min(max(end - b, 0), 8);
+    }
+};
+
+// An octet as it lies in memory, zeros past its n values.
+template <int DT, bool VEC>
+struct Octet {
+    typename Type<DT>::T raw[8] __attribute__((aligned(16)));
+    __device__ void load(const typename Type<DT>::T *p, int n) {
+        if constexpr (VEC) {                               // (n is 0 or 8)
+            constexpr int N = sizeof(raw) / 16;
+            u32x4 w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = n ? ((const u32x4 *)p)[i] : (u32x4){0, 0, 0, 0};
+            __builtin_memcpy(raw, w, sizeof(raw));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) raw[e] = e < n ? p[e] : (typename Type<DT>::T)0;
+        }
+    }
+    __device__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = Type<DT>::get(raw[e]);
+    }
+    __device__ void put(const float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[e] = Type<DT>::put(x[e]);
+    }
+    __device__ void store(typename Type<DT>::T *p, int n) const {
+        if constexpr (VEC) {
+            constexpr int N = sizeof(raw) / 16;
+            u32x4 w[N];
+            __builtin_memcpy(w, raw, sizeof(raw));
+            if (n)
+#pragma unroll
+                for (int i = 0; i < N; ++i) __builtin_nontemporal_store(w[i], (u32x4 *)p + i);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < n) p[e] = raw[e];
+        }
+    }
+};
+
+// n weights from w + at on, ones where there are none; n is 0 or 8 if VEC (they may lie at any float's place).
+template <bool VEC>
+__device__ inline void weights(const float *w, int at, int n, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 1.0f;
+    if (!w) return;
+    if constexpr (VEC) {
+        if (n) __builtin_memcpy(x, w + at, sizeof(x));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) x[e] = w[at + e];
+    }
+}
+
+// LANES lanes hold a row. A workgroup takes `part` rows of each of `group` tokens: it computes their angles
+// together, a thread each, then passes over the rows, as many at a time as it has lanes for; the next pass's
+// rows are asked for ahead of this one's arithmetic.
+template <int DT, int LANES, bool VEC, bool ADJ>
 __global__ __launch_bounds__(kThreads) void us_kv_rotate_kernel(RotateArgs a) {
     using T = typename Type<DT>::T;
     constexpr int kAtOnce = kThreads / LANES;
-    __shared__ float2 angle[kAngles];
-    const int tid = threadIdx.x, o = tid % LANES;
+    __shared__ __attribute__((aligned(16))) float2 angle[kAngles];
+    const int tid = threadIdx.x, z = tid % LANES, mine = tid / LANES;
     const int first = blockIdx.y * a.part, part = min(a.part, a.rows - first), P = a.pairs;
-    // This lane's weights, and those of the values that it rotates with.
-    int other[8], pair[8];
-    bool turns[8];
-    float wq[8], wk[8], vq[8], vk[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = 8 * o + e;
-        turns[e] = d < 2 * P;
-        other[e] = !turns[e] ? min(d, a.D - 1) : a.adjacent ? d ^ 1 : d < P ? d + P : d - P;
-        pair[e] = !turns[e] ? 0 : a.adjacent ? d >> 1 : d < P ? d : d - P;
-        const int at = min(d, a.D - 1);
-        wq[e] = a.qw ? a.qw[at] : 1.0f;
-        vq[e] = a.qw ? a.qw[other[e]] : 1.0f;
-        wk[e] = a.kw ? a.kw[at] : 1.0f;
-        vk[e] = a.kw ? a.kw[other[e]] : 1.0f;
+    const Slot slot(z, a.D, P, ADJ);
+    const bool turns = 8 * z < P;
+    // Tokens that a pass takes side by side, and passes over the rows of one.
+    const int side = max(kAtOnce / part, 1), passes = (part + kAtOnce - 1) / kAtOnce;
+    const int my_token = passes > 1 ? 0 : mine / part, my_row = passes > 1 ? mine : mine - my_token * part;
+    const int t0 = blockIdx.x * a.group, n = my_token < side ? min(a.group, a.tokens - t0) : 0;
+    const int times = (min(a.group, a.tokens - t0) + side - 1) / side;       // tokens of a pass, one after the other
+    Octet<DT, VEC> ra, rb;
+    const auto at = [&](const Rows &q, const Rows &k, int t, int row) {
+        const int r = first + row;
+        const bool key = r >= a.q_heads;
+        // (fields selected one by one: a selected struct would be looked up in memory)
+        T *data = (T *)(key ? k.data : q.data);
+        const int64_t tokens = key ? k.token_stride : q.token_stride, heads = key ? k.head_stride : q.head_stride;
+        return data + (int64_t)(t0 + t) * tokens + (int64_t)(key ? r - a.q_heads : r) * heads;
+    };
+    const auto fetch = [&](int t, int row) {
+        if (t >= n || row >= part) return;
+        const T *src = at(a.q, a.k, t, row);
+        ra.load(src + slot.a, slot.na);
+        rb.load(src + slot.b, slot.nb);
+    };
+    fetch(my_token, my_row);
+    float w[2][8];
+    const auto get_weights = [&](int row) {
+        const float *src = first + row >= a.q_heads ? a.kw : a.qw;
+        weights<VEC>(src, slot.a, slot.na, w[0]);
+        weights<VEC>(src, slot.b, slot.nb, w[1]);
+    };
+    if (a.norm) get_weights(my_row);
+    for (int i = tid; i < min(a.group, a.tokens - t0) * P; i += kThreads) {
+        const int t = i / P, p = i - t * P;
+        double sum = 0.0;
+        for (int x = 0; x < a.axes; ++x)
+            sum += ((double)a.positions[x * a.positions_stride + t0 + t] + a.offset) * (double)a.freq[x * P + p];
+        angle[i] = turn(sum);
     }
-    const bool whole = VEC && !a.adjacent && P % 8 == 0;   // an octet's others are one octet
-    const int step = gridDim.x;
-    const int groups = (a.tokens + a.group - 1) / a.group;
-    for (int g = blockIdx.x; g < groups; g += step) {
-        const int t0 = g * a.group, n = min(a.group, a.tokens - t0);
-        for (int i = tid; i < n * P; i += kThreads) {
-            const int t = i / P, p = i - t * P;
-            double sum = 0.0;
-            for (int x = 0; x < a.axes; ++x)
-                sum += ((double)a.positions[x * a.positions_stride + t0 + t] + a.offset) * (double)a.freq[x * P + p];
-            angle[i] = turn(sum);
+    __syncthreads();
+    for (int i = 0; i < passes * times; ++i) {
+        const int pass = i / times, t = (i - pass * times) * side + my_token, row = my_row + pass * kAtOnce;
+        float x[2][8];
+        ra.get(x[0]);
+        rb.get(x[1]);
+        const bool last = t + side - my_token >= times * side;               // of its pass
+        if (i + 1 < passes * times) fetch(last ? my_token : t + side, last ? row + kAtOnce : row);
+        // (the rows of a pass are of queries or keys for all tokens)
+        if (a.norm && i > 0 && t == my_token && (first + row >= a.q_heads) != (first + row - kAtOnce >= a.q_heads)) get_weights(row);
+        if (t >= n || row >= part) continue;               // (the lanes of a row go together)
+        float2 cs[8];
+        if (turns) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = angle[t * P + min(8 * z + e, P - 1)];
         }
-        __syncthreads();
-        for (int r = tid / LANES; r < n * part; r += kAtOnce) {
-            const int t = r / part, row = first + r - t * part;
-            const bool key = row >= a.q_heads;
-            const Rows &in = key ? a.k : a.q, &out = key ? a.k_out : a.q_out;
-            const int head = key ? row - a.q_heads : row;
-            const T *src = (const T *)in.data + (int64_t)(t0 + t) * in.token_stride + (int64_t)head * in.head_stride;
-            T *dst = (T *)out.data + (int64_t)(t0 + t) * out.token_stride + (int64_t)head * out.head_stride;
-            float x[8], y[8];
-            load_octet<DT, VEC>(src, o, a.D, x);
-            if (8 * o >= 2 * P) {
+        if (a.norm) {
+            float sum = 0.0f;
+            const auto add = [&](float unit) {
+                sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = 0.0f;
-            } else if (whole) {
-                load_octet<DT, true>(src, 8 * o < P ? o + P / 8 : o - P / 8, a.D, y);
-            } else if (a.adjacent) {
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
-            } else {
+                    for (int e = 0; e < 8; ++e) sum = fmaf(x[y][e] * unit, x[y][e] * unit, sum);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = turns[e] ? Type<DT>::get(src[other[e]]) : 0.0f;
+                for (int w = LANES / 2; w > 0; w >>= 1) sum += __shfl_xor(sum, w, 64);
+            };
+            add(1.0f);
+            float scale = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+            if (sum == INFINITY) {                         // of values past 2^63: the same of 2^-64 x
+                add(0x1p-64f);
+                scale = 0x1p-64f / sqrtf(sum / (float)a.D);
             }
-            float scale = 1.0f;
-            if (a.norm) {
-                float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int z = LANES / 2; z > 0; z >>= 1) sum += __shfl_xor(sum, z, 64);
-                scale = 1.0f / sqrtf(sum / (float)a.D + a.eps);
-                if (sum == INFINITY) {                     // of values past 2^63: the same of 2^-64 x
-                    sum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum = fmaf(x[e] * 0x1p-64f, x[e] * 0x1p-64f, sum);
-#pragma unroll
-                    for (int z = LANES / 2; z > 0; z >>= 1) sum += __shfl_xor(sum, z, 64);
-                    scale = 0x1p-64f / sqrtf(sum / (float)a.D);
-                }
-            }
+                for (int e = 0; e < 8; ++e) x[y][e] = x[y][e] * scale * w[y][e];
+        }
+        if (turns) {
+            // pair 8 z + e: values e of both octets, or 2 e and 2 e + 1 of the sixteen; values behind the last stay
+            // zero, and are not stored
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (a.norm) {
-                    x[e] = x[e] * scale * (key ? wk[e] : wq[e]);
-                    y[e] = y[e] * scale * (key ? vk[e] : vq[e]);
-                }
-                if (turns[e]) {
-                    const float2 cs = angle[t * P + pair[e]];
-                    const bool low = a.adjacent ? !(e & 1) : 8 * o + e < P;
-                    x[e] = fmaf(x[e], cs.x, low ? -y[e] * cs.y : y[e] * cs.y);
-                }
+                float &u = ADJ ? x[e >> 2][2 * (e & 3)] : x[0][e], &v = ADJ ? x[e >> 2][2 * (e & 3) + 1] : x[1][e];
+                const float n1 = u, n2 = v;
+                u = fmaf(n1, cs[e].x, -n2 * cs[e].y);
+                v = fmaf(n2, cs[e].x, n1 * cs[e].y);
             }
-            store_octet<DT, VEC>(dst, o, a.D, x);
         }
-        __syncthreads();
+        T *dst = at(a.q_out, a.k_out, t, row);
+        Octet<DT, VEC> out;
+        out.put(x[0]);
+        out.store(dst + slot.a, slot.na);
+        out.put(x[1]);
+        out.store(dst + slot.b, slot.nb);
     }
 }
 
@@ -169,19 +252,28 @@ extern "C" us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head
     a.q = rows_of(q), a.q_out = rows_of(q_out), a.k = rows_of(k), a.k_out = rows_of(k_out);
     a.q_heads = q_heads, a.rows = q_heads + k_heads, a.D = head_dim, a.tokens = q->tokens;
     a.freq = how->freq, a.positions = how->positions, a.positions_stride = how->positions_stride;
-    a.pairs = how->pairs, a.axes = how->axes, a.offset = how->offset, a.adjacent = how->adjacent, a.norm = how->norm;
+    a.pairs = how->pairs, a.axes = how->axes, a.offset = how->offset, a.norm = how->norm;
     a.eps = how->eps, a.qw = how->q_weight, a.kw = how->k_weight;
-    const int lanes = head_dim <= 64 ? 8 : head_dim <= 128 ? 16 : 32, at_once = kThreads / lanes;
-    // Few rows to a token: several tokens, as many as fill a pass. Few tokens: a workgroup takes a pass of
-    // their rows alone, so that the rest runs beside it.
-    int group = at_once / a.rows;
-    group = group < 1 ? 1 : group;
-    if (a.pairs && group * a.pairs > kAngles) group = kAngles / a.pairs;
+    const int P = a.pairs, slots = (P + 7) / 8 + (head_dim - 2 * P + 15) / 16;
+    const int lanes = slots <= 4 ? 4 : slots <= 8 ? 8 : slots <= 16 ? 16 : 32, at_once = kThreads / lanes;
+    // A workgroup's tokens: such that a thread has about six items, which one computing of angles and one
+    // loading of weights serve, but fewer where there would be less than four workgroups per CU, down to a
+    // pass of one token's rows. us for 8192 tokens of 64 + 8 heads of 128, bfloat16, one, two and four
+    // tokens: 61, 60 and 65; 5007 of 16 + 16 of 80, one, three and four: 20, 15.5 and 14.5.
+    const int64_t some = 4 * us_device::compute_units();
+    const int passes = (a.rows + at_once - 1) / at_once, side = at_once / a.rows;
+    int group = (passes < 6 ? 6 / passes : 1) * (side > 1 ? side : 1);
+    if (P && group > kAngles / P) group = kAngles / P;
+    if (group > a.tokens / some) group = (int)(a.tokens / some);
+    if (group < 1) group = 1;
     a.group = group;
     const int groups = (a.tokens + group - 1) / group;
-    a.part = groups >= 2048 || a.rows <= at_once ? a.rows : at_once;
-    const dim3 grid(groups < (1 << 22) ? groups : 1 << 22, (a.rows + a.part - 1) / a.part);
-    const bool vec = octets_aligned(*q, head_dim) && octets_aligned(*q_out, head_dim) &&
+    a.part = groups >= some || a.rows <= at_once ? a.rows : at_once;
+    const dim3 grid(groups, (a.rows + a.part - 1) / a.part);
+    // (a grid's dimension has fewer than 2^32 threads)
+    if (groups > (1 << 23)) return US_ERR_SHAPE;
+    // Octets move whole where every one begins at a multiple of 16 bytes and none is cut.
+    const bool vec = octets_aligned(*q, head_dim) && octets_aligned(*q_out, head_dim) && (how->adjacent ? 2 * P : P) % 8 == 0 &&
                      (!k || (octets_aligned(*k, head_dim) && octets_aligned(*k_out, head_dim)));
     const hipError_t e = with_type(q->dtype, [&](auto dt) {
         const auto go = [&](auto kern) {
@@ -189,11 +281,16 @@ extern "C" us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head
             return hipGetLastError();
         };
         const auto width = [&](auto n) {
-            return vec ? go(us_kv_rotate_kernel<decltype(dt)::value, decltype(n)::value, true>)
-                       : go(us_kv_rotate_kernel<decltype(dt)::value, decltype(n)::value, false>);
+            constexpr int DT = decltype(dt)::value, N = decltype(n)::value;
+            if (how->adjacent) return vec ? go(us_kv_rotate_kernel<DT, N, true, true>) : go(us_kv_rotate_kernel<DT, N, false, true>);
+            return vec ? go(us_kv_rotate_kernel<DT, N, true, false>) : go(us_kv_rotate_kernel<DT, N, false, false>);
         };
-        return lanes == 8 ? width(std::integral_constant<int, 8>())
-                          : lanes == 16 ? width(std::integral_constant<int, 16>()) : width(std::integral_constant<int, 32>());
+        switch (lanes) {
+            case 4: return width(std::integral_constant<int, 4>());
+            case 8: return width(std::integral_constant<int, 8>());
+            case 16: return width(std::integral_constant<int, 16>());
+        }
+        return width(std::integral_constant<int, 32>());
     });
     return e == hipSuccess ? US_OK : US_ERR_DEVICE;
 }
