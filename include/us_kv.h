@@ -330,8 +330,9 @@ typedef struct {
  * whose keys can have the largest score. With lo and hi the codes of a block's
  * summary and s its keys' scale, its score is
  *   s max over the query heads of sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d,
- * no less than any q . k_j of it, taken in 64 bits and rounded once to float32;
- * a query head with an infinity or a NaN does not count, -infinity if none does.
+ * no less than any q . k_j of it: exact for q held to 2^-30 of its largest
+ * value, rounded once to float32. A query head with an infinity or a NaN does
+ * not count; -infinity if none is left.
  * Row i of a sequence's n is at position p = lens - n + i and looks at the
  * blocks up to that of p. chosen gets, ascending, then -1, `top` of them: the
  * first `sinks` and the last `recent` ones, then those of largest score (equal

@@ -3,10 +3,14 @@
 //
 // With lo_d <= k_jd <= hi_d for all keys j of a block, q . k_j is at most
 //   sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d,
-// which is a product of 2 D values per block and query head: MFMA's 16 x 16 x 4
-// of float64, 16 blocks by 16 query heads. In 64 bits two blocks' scores change
-// places only where they agree to the last bits, and the choice is that of the
-// definition; the matrix cores take as long for it as the loads of the extremes.
+// a product of 2 D whole codes with 2 D values, of which half are 0. A query is
+// held as whole numbers below 2^30 times a power of two, each as four digits in
+// [-128, 127] of base 256; the matrix cores multiply digits and codes exactly, in
+// 32 bits, 16 blocks by the digits of four query heads at a time, and the digits'
+// sums are joined in 64 bits. What a score is off by is the rounding of the
+// query's small values (float32: below 2^-7 of its largest one, bfloat16: 2^-23,
+// float16: 2^-20), 2^-30 of the largest at most each; two blocks change places
+// only where their scores agree to about nine digits.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -19,7 +23,7 @@ namespace {
 
 using namespace us_kv;
 
-typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
@@ -176,13 +180,18 @@ __device__ inline void select(E each, int top, int *out, int *lds, int *hist) {
     for (int i = take + tid; i < top; i += kThreads) out[i] = -1;
 }
 
+// Lanes that hold a row's octets together: a power of two.
+constexpr int lanes_of(int row) { return row <= 64 ? 8 : row <= 128 ? 16 : 32; }
+
 template <int NT, int DT>
 __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     using T = typename Type<DT>::T;
-    constexpr int R = 32 * NT, kSteps = 2 * R / 64;        // of 64 values of a summary, 16 products each
-    // The queries as the products' right operand: step, product, lane.
-    __shared__ double qs[kSteps * 16 * 64];
-    __shared__ double total[kWaves][16];                   // of a query's values
+    constexpr int R = 32 * NT, kSteps = 2 * R / 64;        // of 64 values of a summary
+    constexpr int kLanes = lanes_of(R), kHeads = kThreads / kLanes;            // query heads that are laid out at a time
+    constexpr int kGroups = 4;                             // of four query heads, whose digits are columns together
+    // The digits as the products' right operand: group, step, lane (column, piece of 16 values).
+    __shared__ u32x4 digits[kGroups][kSteps][64];
+    __shared__ double unit_of[4 * kGroups];                // a head's power of two; NaN for one that does not count
     __shared__ int lds[kWaves + 2], hist[256], flag;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kk = lane >> 4, t = blockIdx.x, hk = blockIdx.y;
@@ -193,72 +202,104 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     if ((int)blockIdx.z >= parts) return;
     float *scores = a.scores + unit * a.stride;
     const T *q = (const T *)a.q.data + (int64_t)t * a.q.token_stride + (int64_t)hk * a.G * a.q.head_stride;
-    const auto load_queries = [&](int g0) {
-        double sum = 0.0;
-        __syncthreads();                                   // (of the heads before these)
-        for (int o = tid >> 4; o < R / 8; o += kThreads / 16) {
-            float x[8];
-            if (g0 + n < a.G) {
-                const T *p = q + (int64_t)(g0 + n) * a.q.head_stride;
+    // Heads g0 .. g0 + 15 (zeros past the last).
+    const auto lay_out = [&](int g0) {
+        for (int h0 = 0; h0 < min(4 * kGroups, (a.G - g0 + 3) / 4 * 4); h0 += kHeads) {
+            const int h = h0 + tid / kLanes, o = tid % kLanes, g = g0 + h;
+            const bool here = h < 4 * kGroups && o < R / 8;
+            float x[8], mx = 0.0f;
+            if (here && g < a.G) {
+                const T *p = q + (int64_t)g * a.q.head_stride;
                 if (a.vec) load_octet<DT, true>(p, o, a.D, x);
                 else load_octet<DT, false>(p, o, a.D, x);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.0f;
             }
+            mx = magnitude(x, mx);
+#pragma unroll
+            for (int z = kLanes / 2; z > 0; z >>= 1) mx = fmaxf(mx, __shfl_xor(mx, z, 64));
+            // 2^k that brings mx to [2^29, 2^30)
+            int e2;
+            frexpf(mx, &e2);                               // mx in [2^(e2 - 1), 2^e2)
+            const int k = mx > 0.0f && mx < INFINITY ? 30 - e2 : 0;
+            uint32_t lo[4][2] = {}, hi[4][2] = {};         // by digit, four values to a word
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int lo = 8 * o + e, hi = R + lo;
-                sum += x[e];
-                qs[((lo >> 6) * 16 + (lo & 15)) * 64 + ((lo >> 4) & 3) * 16 + n] = x[e] < 0.0f ? x[e] : 0.0f;
-                qs[((hi >> 6) * 16 + (hi & 15)) * 64 + ((hi >> 4) & 3) * 16 + n] = x[e] > 0.0f ? x[e] : 0.0f;
+                // (two steps, so that neither power leaves float32's range; past them nothing is rounded but the value)
+                const float y = ldexpf(ldexpf(x[e], k / 2), k - k / 2);
+                int v = mx < INFINITY ? (int)rintf(y) : 0;
+                const bool up = v > 0;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int digit = (int)(int8_t)v;
+                    v = (v - digit) >> 8;
+                    const uint32_t byte = (uint32_t)(digit & 255) << (8 * (e & 3));
+                    (up ? hi : lo)[d][e >> 2] |= byte;
+                }
+            }
+            if (here) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int col = 4 * (h & 3) + d, c = 8 * o;
+                    u32x2 *l = (u32x2 *)&digits[h >> 2][c >> 6][((c >> 4) & 3) * 16 + col] + (o & 1);
+                    const int c2 = R + c;
+                    u32x2 *u = (u32x2 *)&digits[h >> 2][c2 >> 6][((c2 >> 4) & 3) * 16 + col] + (o & 1);
+                    *l = (u32x2){lo[d][0], lo[d][1]};
+                    *u = (u32x2){hi[d][0], hi[d][1]};
+                }
+                if (o == 0) unit_of[h] = g < a.G && mx < INFINITY ? ldexp(1.0, -k) : NAN;
             }
         }
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        if (kk == 0) total[wave][n] = sum;
         __syncthreads();
     };
-    if (a.G <= 16) load_queries(0);
+    if (a.G <= 4 * kGroups) lay_out(0);
     for (int c = blockIdx.z; c < chunks; c += parts) {
         const int m0 = 64 * c + 16 * wave, mine = m0 + n;  // a wavefront's 16 blocks; lane n's
         const int id = mine < blocks ? a.s.block(b, mine) : -1;
         const int64_t where = (int64_t)max(id, 0) * a.heads + hk;
         const u32x4 *src = (const u32x4 *)(a.summary + where * (2 * R)) + kk;
-        u32x4 raw[kSteps];
+        u32x4 codes[kSteps];
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) raw[j] = src[4 * j];
+        for (int j = 0; j < kSteps; ++j) codes[j] = src[4 * j];
         const float ks = a.ks[where];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) codes[j] ^= 0x80808080u;              // bytes less 128
         double best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        for (int g0 = 0; g0 < a.G; g0 += 16) {
-            if (a.G > 16) load_queries(g0);
-            f64x4 x = {0.0, 0.0, 0.0, 0.0};
+        for (int g0 = 0; g0 < a.G; g0 += 4 * kGroups) {
+            if (a.G > 4 * kGroups) {
+                __syncthreads();                           // (the heads before these)
+                lay_out(g0);
+            }
+            for (int g = 0; g < min(kGroups, (a.G - g0 + 3) / 4); ++g) {
+                i32x4 x = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j)
+                for (int j = 0; j < kSteps; ++j)
+                    x = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, codes[j]),
+                                                              __builtin_bit_cast(i32x4, digits[g][j][lane]), x, 0, 0, 0);
+                // Lane (n, kk), element v: block 4 kk + v, digit n % 4 of query head n / 4. Their sums are whole
+                // numbers below 2^47, exact in 64 bits.
+                const double weight = ldexp(unit_of[4 * g + (n >> 2)], 8 * (n & 3));
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const double code = (double)((raw[j][e >> 2] >> (8 * (e & 3))) & 255u);
-                    x = __builtin_amdgcn_mfma_f64_16x16x4f64(code, qs[(j * 16 + e) * 64 + lane], x, 0, 0, 0);
+                for (int v = 0; v < 4; ++v) {
+                    double y = (double)x[v] * weight;
+                    y += __shfl_xor(y, 1, 64);
+                    y += __shfl_xor(y, 2, 64);
+                    best[v] = y > best[v] ? y : best[v];
                 }
-            // Lane (n, kk), element v: block 4 v + kk, query head n. The bytes are codes + 128.
-            const double bias = 128.0 * (total[0][n] + total[1][n] + total[2][n] + total[3][n]);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const double y = x[v] - bias;
-                best[v] = g0 + n < a.G && y > best[v] ? y : best[v];
             }
         }
 #pragma unroll
         for (int v = 0; v < 4; ++v)
 #pragma unroll
-            for (int z = 1; z < 16; z <<= 1) {
+            for (int z = 4; z < 16; z <<= 1) {
                 const double y = __shfl_xor(best[v], z, 64);
                 best[v] = y > best[v] ? y : best[v];
             }
         double y = best[0];
 #pragma unroll
         for (int v = 1; v < 4; ++v) y = n == v ? best[v] : y;
-        const int m = 4 * (n & 3) + kk;                    // of the 16, this lane's to store
+        const int m = 4 * kk + (n & 3);                    // of the 16, this lane's to store
         const float scale = __shfl(ks, m, 64);
         const bool there = __shfl(id, m, 64) >= 0;
         if (n < 4 && m0 + m < blocks) {
