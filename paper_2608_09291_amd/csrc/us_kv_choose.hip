@@ -101,7 +101,7 @@ struct ChooseArgs {
     int32_t *tickets;                                      // tokens x heads
 };
 
-constexpr int kHeld = 16;                                  // scores of a thread that stay in registers
+constexpr int kHeld = 4096;                                // keys that stay in LDS
 
 // Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
 __device__ inline uint32_t order_of(float x) {
@@ -109,74 +109,132 @@ __device__ inline uint32_t order_of(float x) {
     return x != x ? 1u : b >> 31 ? ~b : b | 0x80000000u;
 }
 
-__device__ inline int sum_before(int x, int *lds, int &all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int run = x;
-#pragma unroll
-    for (int z = 1; z < 64; z <<= 1) {
-        const int y = __shfl_up(run, z, 64);
-        if (lane >= z) run += y;
-    }
-    __syncthreads();                                       // (of an earlier call)
-    if (lane == 63) lds[wave] = run;
-    __syncthreads();
-    int sum = run - x;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) sum += lds[w];
-        all += lds[w];
-    }
-    return sum;
+// What of a row's scores the workgroup that chooses has in LDS.
+struct Pick {
+    uint32_t keys[kHeld];
+    __attribute__((aligned(16))) int hist[4][256];         // of the digits, the largest first
+    u32x4 of_wave[kWaves];
+    int counts[kWaves][2];
+};
+
+// The other lanes' x by data-parallel moves, a few cycles each where a permute through LDS takes a hundred.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t moved(uint32_t none, uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xF, false);
+}
+// Lane 63 gets f over all lanes, every lane that of the lanes up to its own; `none` is neutral to f.
+template <class F>
+__device__ inline uint32_t scan(uint32_t x, uint32_t none, F f) {
+    x = f(x, moved<0x111, 0xF>(none, x));                  // from 1, 2, 4 and 8 lanes before, in rows of 16
+    x = f(x, moved<0x112, 0xF>(none, x));
+    x = f(x, moved<0x114, 0xF>(none, x));
+    x = f(x, moved<0x118, 0xF>(none, x));
+    x = f(x, moved<0x142, 0xA>(none, x));                  // a row's last lane to the next row, of two
+    return f(x, moved<0x143, 0xC>(none, x));               // lane 31 to the upper half
 }
 
-// The places of the largest `top` of n keys to `out`, ascending, ties to the first; keys of 0 count for
-// nothing. each(f) calls f(place, key) for a thread's own run of places, in order.
-template <class E>
-__device__ inline void select(E each, int top, int *out, int *lds, int *hist) {
-    const int tid = threadIdx.x;
-    int there = 0, all;
-    each([&](int, uint32_t k) { there += k != 0; });
-    sum_before(there, lds, all);
-    const int take = min(top, all);
-    // The take-th largest key, 8 bits at a time.
+// What is known of some keys: how many are there and fixed, the smallest and the largest of the others.
+struct Seen {
+    uint32_t there = 0, fixed = 0, low = ~0u, high = 0;
+    __device__ void add(uint32_t k) {
+        there += k != 0;
+        fixed += k == ~0u;
+        if (k != 0 && k != ~0u) low = min(low, k), high = max(high, k);
+    }
+};
+
+// The places of the largest `top` of n keys to `out`, ascending, ties to the first. Keys of 0 count for
+// nothing, those of ~0 are fixed: taken in any case (they are no more than `top`). The others are sought by 8
+// bits of their distance from the smallest of them, shifted so that the largest distance fills 32 bits: the
+// scores of a row have most of their first bits in common. Every wavefront follows the whole search, so that a
+// step has one barrier. key(i) is asked for places up to the next multiple of kThreads past n, where it is 0.
+template <class F>
+__device__ inline void select(F key, Seen mine, int n, int top, int *out, Pick &p) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const auto plus = [](uint32_t a, uint32_t b) { return a + b; };
+    // A wavefront's places, 64 at a time.
+    const int run = (n + kThreads - 1) / kThreads * 64, i0 = wave * run + lane, i1 = i0 + run;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.hist[i][tid] = 0;
+    mine.there = scan(mine.there, 0, plus);
+    mine.fixed = scan(mine.fixed, 0, plus);
+    mine.low = scan(mine.low, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); });
+    mine.high = scan(mine.high, 0, [](uint32_t a, uint32_t b) { return max(a, b); });
+    if (lane == 63) p.of_wave[wave] = (u32x4){mine.there, mine.fixed, mine.low, mine.high};
+    __syncthreads();
+    uint32_t there = 0, fixed = 0, low = ~0u, high = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const u32x4 x = p.of_wave[w];
+        there += x[0];
+        fixed += x[1];
+        low = min(low, x[2]);
+        high = max(high, x[3]);
+    }
+    const int take = min(top, (int)there);
+    int rest = take - (int)fixed;                          // of those that agree with `limit` in its first bits
+    // A key is taken if it is fixed, above the limit, or among the first `rest` at it. Without a search: all that
+    // are there, or the fixed ones alone.
+    const bool none = take < (int)there && rest <= 0;
     uint32_t limit = 0;
-    int rest = take;                                       // of the keys that agree with limit so far
-    if (take < all) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            __syncthreads();
-            hist[tid] = 0;
-            __syncthreads();
-            each([&](int, uint32_t k) {
-                if (k && (shift == 24 || (k ^ limit) >> (shift + 8) == 0)) atomicAdd(hist + ((k >> shift) & 255), 1);
-            });
-            __syncthreads();
-            // thread z: keys of digit 255 - z, and of the larger ones
-            const int mine = hist[255 - tid];
-            int unused;
-            const int above = sum_before(mine, lds, unused);
-            __syncthreads();
-            if (above < rest && above + mine >= rest) {    // (one thread; rest >= 1)
-                lds[kWaves] = 255 - tid;
-                lds[kWaves + 1] = rest - above;
+    int shift = 32, up = 0;                                // bits of the limit that are not known yet
+    if (take < (int)there && rest > 0) {
+        up = high > low ? __builtin_clz(high - low) : 0;
+#pragma unroll 1
+        for (int step = 0; step < 4; ++step) {
+            shift -= 8;
+#pragma unroll 4
+            for (int i = i0; i < i1; i += 64) {
+                const uint32_t x = key(i), k = (x - low) << up;
+                if (x != 0 && x != ~0u && (step == 0 || (k ^ limit) >> (shift + 8) == 0)) atomicAdd(&p.hist[step][255 - ((k >> shift) & 255)], 1);
             }
             __syncthreads();
-            limit |= (uint32_t)lds[kWaves] << shift;
-            rest = lds[kWaves + 1];
+            // lane z: the digits 255 - 4 z .. 252 - 4 z, from the largest on
+            const u32x4 bin = *(const u32x4 *)&p.hist[step][4 * lane];
+            const int some = (int)(bin[0] + bin[1] + bin[2] + bin[3]);
+            int above = (int)scan((uint32_t)some, 0, plus) - some, digit = -1, left = 0, size = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (above < rest && above + (int)bin[i] >= rest) digit = 255 - 4 * lane - i, left = rest - above, size = (int)bin[i];
+                above += (int)bin[i];
+            }
+            const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));          // (there is one: rest is no more than all)
+            limit |= (uint32_t)__builtin_amdgcn_readlane(digit, who) << shift;
+            rest = __builtin_amdgcn_readlane(left, who);
+            if (rest == __builtin_amdgcn_readlane(size, who)) break;           // all that agree so far
         }
+        limit >>= shift;
     }
-    int more = 0, same = 0;
-    each([&](int, uint32_t k) {
-        more += k > limit;
-        same += k && k == limit;
-    });
-    int at = sum_before(more, lds, all), eq = sum_before(same, lds, all);
-    each([&](int i, uint32_t k) {
-        const bool tie = k && k == limit;
-        if (k > limit || (tie && eq < rest)) out[at + min(eq, rest)] = i;
-        at += k > limit;
-        eq += tie;
-    });
+    const auto masks = [&](int i, uint64_t &more, uint64_t &same) {
+        const uint32_t x = key(i), k = shift < 32 ? ((x - low) << up) >> shift : 1;
+        const bool other = x != 0 && x != ~0u && !none;
+        more = __builtin_amdgcn_ballot_w64(x == ~0u || (other && k > limit));
+        same = __builtin_amdgcn_ballot_w64(other && k == limit);
+    };
+    int m = 0, s = 0;
+#pragma unroll 4
+    for (int i = i0; i < i1; i += 64) {
+        uint64_t more, same;
+        masks(i, more, same);
+        m += __builtin_popcountll(more);
+        s += __builtin_popcountll(same);
+    }
+    if (lane == 0) p.counts[wave][0] = m, p.counts[wave][1] = s;
+    __syncthreads();
+    m = s = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) m += p.counts[w][0], s += p.counts[w][1];
+#pragma unroll 4
+    for (int i = i0; i < i1; i += 64) {
+        uint64_t more, same;
+        masks(i, more, same);
+        const int mm = m + __builtin_amdgcn_mbcnt_hi((uint32_t)(more >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)more, 0));
+        const int ss = s + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+        if ((more >> lane & 1) || ((same >> lane & 1) && ss < rest)) out[mm + min(ss, rest)] = i;
+        m += __builtin_popcountll(more);
+        s += __builtin_popcountll(same);
+    }
     for (int i = take + tid; i < top; i += kThreads) out[i] = -1;
 }
 
@@ -192,30 +250,31 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     // The digits as the products' right operand: group, step, lane (column, piece of 16 values).
     __shared__ u32x4 digits[kGroups][kSteps][64];
     __shared__ double unit_of[4 * kGroups];                // a head's power of two; NaN for one that does not count
-    __shared__ int lds[kWaves + 2], hist[256], flag;
+    __shared__ Pick pick;
+    __shared__ int flag;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kk = lane >> 4, t = blockIdx.x, hk = blockIdx.y;
+    const T *q = (const T *)a.q.data + (int64_t)t * a.q.token_stride + (int64_t)hk * a.G * a.q.head_stride;
+    // This thread's octet of the first heads, on its way while the row's place is looked up.
+    const int oct = tid % kLanes;
+    RowPart<DT, 1> raw;
+    raw.load(q + (int64_t)min(tid / kLanes, a.G - 1) * a.q.head_stride, min(oct, (a.D - 1) / 8), 0, a.D, a.vec);
     int b, at;
     if (!a.more.place(a.s, t, b, at)) return;
     const int64_t unit = (int64_t)t * a.heads + hk;
     const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + 63) / 64, parts = min(max(chunks, 1), (int)gridDim.z);
     if ((int)blockIdx.z >= parts) return;
     float *scores = a.scores + unit * a.stride;
-    const T *q = (const T *)a.q.data + (int64_t)t * a.q.token_stride + (int64_t)hk * a.G * a.q.head_stride;
     // Heads g0 .. g0 + 15 (zeros past the last).
     const auto lay_out = [&](int g0) {
         for (int h0 = 0; h0 < min(4 * kGroups, (a.G - g0 + 3) / 4 * 4); h0 += kHeads) {
-            const int h = h0 + tid / kLanes, o = tid % kLanes, g = g0 + h;
+            const int h = h0 + tid / kLanes, o = oct, g = g0 + h;
             const bool here = h < 4 * kGroups && o < R / 8;
+            if (g0 + h0 > 0) raw.load(q + (int64_t)min(g, a.G - 1) * a.q.head_stride, min(o, (a.D - 1) / 8), 0, a.D, a.vec);
             float x[8], mx = 0.0f;
-            if (here && g < a.G) {
-                const T *p = q + (int64_t)g * a.q.head_stride;
-                if (a.vec) load_octet<DT, true>(p, o, a.D, x);
-                else load_octet<DT, false>(p, o, a.D, x);
-            } else {
+            raw.octet(0, o, a.D, false, x);                // (zeros past D)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-            }
+            for (int e = 0; e < 8; ++e) x[e] = g < a.G ? x[e] : 0.0f;
             mx = magnitude(x, mx);
 #pragma unroll
             for (int z = kLanes / 2; z > 0; z >>= 1) mx = fmaxf(mx, __shfl_xor(mx, z, 64));
@@ -313,26 +372,42 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
         __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     }
-    const auto key_of = [&](int i) {
-        if (a.s.block(b, i) < 0) return 0u;
-        if (i < a.sinks || i >= blocks - a.recent) return 0xFFFFFFFFu;
-        return order_of(__hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    const auto key_of = [&](int i, int block, float score) {
+        return block < 0 ? 0u : i < a.sinks || i >= blocks - a.recent ? ~0u : min(order_of(score), ~0u - 1);
     };
-    const int per = (blocks + kThreads - 1) / kThreads, i0 = min(tid * per, blocks), i1 = min(i0 + per, blocks);
+    const auto score_of = [&](int i) { return __hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     int *out = a.chosen + unit * a.top;
-    if (per <= kHeld) {
-        uint32_t held[kHeld];
+    Seen seen;
+    const int per = (blocks + kThreads - 1) / kThreads;
+    if (blocks <= kHeld) {
+#pragma unroll 1
+        for (int e0 = 0; e0 < per; e0 += 4) {              // (four on their way together)
+            float score[4];
+            int block[4];
 #pragma unroll
-        for (int e = 0; e < kHeld; ++e) held[e] = i0 + e < i1 ? key_of(i0 + e) : 0u;
-        select([&](auto f) {
+            for (int e = 0; e < 4; ++e) {
+                const int i = min(tid + kThreads * (e0 + e), blocks - 1);
+                score[e] = score_of(i);
+                block[e] = a.s.block(b, i);
+            }
 #pragma unroll
-            for (int e = 0; e < kHeld; ++e)
-                if (e < per) f(i0 + e, held[e]);           // (past i1 a key of 0)
-        }, a.top, out, lds, hist);
+            for (int e = 0; e < 4; ++e) {
+                const int i = tid + kThreads * (e0 + e);
+                const uint32_t k = i < blocks ? key_of(i, block[e], score[e]) : 0u;
+                if (i < kHeld) pick.keys[i] = k;
+                seen.add(k);
+            }
+        }
+        __syncthreads();
+        select([&](int i) { return pick.keys[i]; }, seen, blocks, a.top, out, pick);
     } else {
-        select([&](auto f) {
-            for (int i = i0; i < i1; ++i) f(i, key_of(i));
-        }, a.top, out, lds, hist);
+        const auto key = [&](int i) {
+            const int j = min(i, blocks - 1);
+            const uint32_t k = key_of(j, a.s.block(b, j), score_of(j));
+            return i < blocks ? k : 0u;
+        };
+        for (int e = 0; e < per; ++e) seen.add(key(tid + kThreads * e));
+        select(key, seen, blocks, a.top, out, pick);
     }
 }
 
