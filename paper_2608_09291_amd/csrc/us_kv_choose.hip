@@ -26,7 +26,6 @@ using namespace us_kv;
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kThreads = 256, kWaves = 4;
 
 // --- summaries ----------------------------------------------------------------
 
@@ -36,7 +35,7 @@ __device__ inline uint32_t bits_of(u16x2 x) { return __builtin_bit_cast(uint32_t
 // A workgroup per (block, head, sequence), a wavefront per 32 values: lane
 // (t % 16, octet) has those of 16 byte pieces, tokens t and t + 16.
 template <int NT>
-__global__ __launch_bounds__(kThreads) void us_kv_summarise_kernel(const uint8_t *kp, uint8_t *summary, Seqs s) {
+__global__ __launch_bounds__(256) void us_kv_summarise_kernel(const uint8_t *kp, uint8_t *summary, Seqs s) {
     constexpr int R = 32 * NT;
     const int b = blockIdx.z, h = blockIdx.y, heads = gridDim.y, tid = threadIdx.x, lane = tid & 63;
     int r0, n;
@@ -48,7 +47,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_summarise_kernel(const uint8_t
     if (id < 0) return;
     const int64_t at = (int64_t)id * heads + h;
     const int t0 = lane >> 2;
-    for (int c = __builtin_amdgcn_readfirstlane(tid >> 6); c < NT; c += kWaves) {
+    for (int c = __builtin_amdgcn_readfirstlane(tid >> 6); c < NT; c += 4) {
         const u32x4 *src = (const u32x4 *)(kp + at * (kBlock * R) + 2048 * c) + lane;
         const u32x4 raw[2] = {src[0], src[64]};
         u16x2 lo[4], hi[4];
@@ -101,6 +100,7 @@ struct ChooseArgs {
     int32_t *tickets;                                      // tokens x heads
 };
 
+constexpr int kThreads = 512, kWaves = kThreads / 64, kChunk = 16 * kWaves;    // of a workgroup: blocks at a time
 constexpr int kHeld = 4096;                                // keys that stay in LDS
 
 // Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
@@ -154,8 +154,7 @@ __device__ inline void select(F key, Seen mine, int n, int top, int *out, Pick &
     const auto plus = [](uint32_t a, uint32_t b) { return a + b; };
     // A wavefront's places, 64 at a time.
     const int run = (n + kThreads - 1) / kThreads * 64, i0 = wave * run + lane, i1 = i0 + run;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p.hist[i][tid] = 0;
+    for (int i = tid; i < 1024; i += kThreads) (&p.hist[0][0])[i] = 0;
     mine.there = scan(mine.there, 0, plus);
     mine.fixed = scan(mine.fixed, 0, plus);
     mine.low = scan(mine.low, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); });
@@ -262,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     int b, at;
     if (!a.more.place(a.s, t, b, at)) return;
     const int64_t unit = (int64_t)t * a.heads + hk;
-    const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + 63) / 64, parts = min(max(chunks, 1), (int)gridDim.z);
+    const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + kChunk - 1) / kChunk, parts = min(max(chunks, 1), (int)gridDim.z);
     if ((int)blockIdx.z >= parts) return;
     float *scores = a.scores + unit * a.stride;
     // Heads g0 .. g0 + 15 (zeros past the last).
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     };
     if (a.G <= 4 * kGroups) lay_out(0);
     for (int c = blockIdx.z; c < chunks; c += parts) {
-        const int m0 = 64 * c + 16 * wave, mine = m0 + n;  // a wavefront's 16 blocks; lane n's
+        const int m0 = kChunk * c + 16 * wave, mine = m0 + n;  // a wavefront's 16 blocks; lane n's
         const int id = mine < blocks ? a.s.block(b, mine) : -1;
         const int64_t where = (int64_t)max(id, 0) * a.heads + hk;
         const u32x4 *src = (const u32x4 *)(a.summary + where * (2 * R)) + kk;
@@ -431,7 +430,7 @@ extern "C" us_status us_kv_summarise(const us_kv_cache *cache, const us_kv_seqs 
     const int most = seqs->max_new < seqs->width * kBlock ? seqs->max_new : seqs->width * kBlock;
     const dim3 grid((most + kBlock - 2) / kBlock + 1, cache->heads, seqs->batch);
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
-        hipLaunchKernelGGL(us_kv_summarise_kernel<decltype(nt)::value>, grid, dim3(kThreads), 0, (hipStream_t)stream, cache->k, summary, s);
+        hipLaunchKernelGGL(us_kv_summarise_kernel<decltype(nt)::value>, grid, dim3(256), 0, (hipStream_t)stream, cache->k, summary, s);
         return hipGetLastError();
     });
     return e == hipSuccess ? US_OK : US_ERR_DEVICE;
@@ -471,9 +470,9 @@ extern "C" us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *se
     a.more.batch = seqs->batch;
     a.scores = choice->scores, a.stride = choice->scores_stride, a.chosen = choice->chosen;
     a.top = choice->top, a.sinks = choice->sinks, a.recent = choice->recent, a.tickets = (int32_t *)ws;
-    // Workgroups of 64 blocks, but no more of them than fill the GPU a few times: each has its queries to lay out.
+    // Workgroups of kChunk blocks, but no more of them than fill the GPU a few times: each has its queries to lay out.
     const int64_t room = 8 * us_device::compute_units() / units;
-    int64_t parts = (most + 63) / 64;
+    int64_t parts = (most + kChunk - 1) / kChunk;
     if (parts > room) parts = room < 1 ? 1 : room;
     const dim3 grid(q->tokens, cache->heads, (unsigned)parts);
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
