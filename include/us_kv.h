@@ -294,10 +294,10 @@ typedef struct {
  * Queries see what us_kv_attend shows them, also if a sequence is shorter than
  * the common blocks, and results are off by as much. Sequences past max_group
  * in a group count as sequences of none. opts->window has to be 0 and
- * opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, 16-byte
- * aligned, which need not be zero; calls that may overlap need their own.
- * US_ERR_SHAPE as us_kv_attend, for groups as for sequences: for more than 2^25
- * query rows of a group and cache head.
+ * opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, as
+ * us_kv_attend's. US_ERR_SHAPE as us_kv_attend, for groups as for sequences (for
+ * more than 2^25 query rows of a group and cache head), and for more than 2^22
+ * workgroups of either part.
  */
 us_status us_kv_attend_shared_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                              int32_t tokens, const us_kv_groups *groups, const us_kv_attend_opts *opts,

@@ -3,9 +3,8 @@
 // a few tokens). What a workgroup's rows and keys are differs by KIND:
 //   kWhole   the rows of a sequence over all keys that they see;
 //   kChosen  a token's rows over the blocks that a list of it names;
-//   kShared  the rows of a group of sequences over the blocks that these have in common;
-//   kRest    the rows of a sequence over the keys behind those.
-// The last two leave partial rows, which us_kv_shared.hip joins.
+//   kPart    the rows of a group of sequences over the blocks that these have in common,
+//            or those of a sequence over the keys behind (us_kv_shared.hip).
 #ifndef UNIONSPARSE_US_KV_DECODE_H
 #define UNIONSPARSE_US_KV_DECODE_H
 
@@ -15,6 +14,126 @@
 namespace us_kv {
 
 constexpr int kDecodeThreads = 256, kDecodeWaves = 4, kDecodeRows = 16;
+
+// The end of a kPart workgroup. A unit is a tile of a sequence's rows; it has partial rows over its own keys
+// and, in one or two tiles of its group's rows, over the common ones. The last workgroup that leaves some of a
+// unit's joins them, in an order that does not depend on who that is. A workgroup over common keys has rows of up
+// to 16 units. (The tables may hold anything: both sorts of workgroups count a unit's parts from the same numbers.)
+template <int NT, int DT>
+__device__ inline void join_parts(const Args &a, const Others &more, bool rest, int u, int hk, int tile, const Group &group,
+                                  float *lds) {
+    constexpr int R = 32 * NT, kThreads = kDecodeThreads;
+    struct Unit {
+        int r0, base, rows;                                // of the sequence, and the tile's
+        int own, pre;                                      // splits over the sequence's own keys, and over the common ones
+        int at, unit;                                      // the first row's place among the group's; number of the unit
+    };
+    __shared__ Unit list[kDecodeRows];
+    __shared__ int found;
+    const int tid = threadIdx.x, end = group.n * a.G;
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (tid == 0) found = 0;
+    __syncthreads();
+    if (tid < 64) {
+        const int row0 = tile * kDecodeRows;
+        const int b1 = rest ? u + 1 : group.last;
+#pragma unroll 1
+        for (int b = (rest ? u : group.first) + tid; b < b1; b += 64) {
+            int r0, n, lo, hi;
+            a.s.rows(b, r0, n);
+            const int64_t far = (int64_t)(r0 - group.r0) * a.G;                // of its first row, among the group's
+            const int total = n * a.G, len = a.s.len(b);
+            const bool in = far >= 0 && far < end && group.cut > 0;
+            const int at0 = in ? (int)far : 0;
+            if (!rest && (!in || at0 + total <= row0 || at0 >= row0 + kDecodeRows)) continue;
+            const int t0 = rest ? tile : max(row0 - at0, 0) / kDecodeRows;
+            const int t1 = rest ? tile : (min(total, row0 + kDecodeRows - at0) - 1) / kDecodeRows;
+#pragma unroll 1
+            for (int t = t0; t <= t1; ++t) {
+                Unit x;
+                x.r0 = r0;
+                x.base = t * kDecodeRows;
+                x.rows = min(total - x.base, kDecodeRows);
+                a.mask.range((x.base + x.rows - 1) / a.G, n, len, lo, hi);
+                x.own = splits_of(group.cut, max(hi, group.cut), more.own.chunk);
+                x.at = at0 + x.base;
+                x.pre = in && x.at < end ? splits_of(0, group.cut, a.sp.chunk) : 0;
+                x.unit = (b * a.heads + hk) * more.own.tiles + t;
+                const int first = x.at >> more.pre_shift, last = (min(x.at + x.rows, end) - 1) >> more.pre_shift;
+                if (!rest && (!x.pre || tile < first || tile > last)) continue;
+                const int parts = x.own + (more.pre_groups && x.pre ? x.pre * (last - first + 1) : 0);
+                int32_t *ticket = more.own.tickets + x.unit;
+                if (__hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != parts - 1) continue;
+                __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const int i = atomicAdd(&found, 1);
+                if (i < kDecodeRows) list[i] = x;
+            }
+        }
+    }
+    __syncthreads();
+    __asm__ volatile("" ::: "memory");
+    const int count = __builtin_amdgcn_readfirstlane(min(found, kDecodeRows));
+    const int one = (more.own.rows * (R + 2) + 3) / 4 * 4, one_pre = (a.sp.rows * (R + 2) + 3) / 4 * 4;
+#pragma unroll 1
+    for (int f = 0; f < count; ++f) {
+        const Unit x = list[f];
+        const int unit = __builtin_amdgcn_readfirstlane(x.unit), first = __builtin_amdgcn_readfirstlane(x.at >> more.pre_shift);
+        const int ns_own = __builtin_amdgcn_readfirstlane(x.own), ns_pre = __builtin_amdgcn_readfirstlane(x.pre);
+        const Shared own(more.own.part + (int64_t)unit * more.own.splits * one);
+        const Shared pre(a.sp.part + (((int64_t)group.number * a.heads + hk) * a.sp.tiles + first) * a.sp.splits * one_pre);
+        // A thread per quad of a row's values, and of a few rows as many for each as there are threads, which
+        // take every runs-th partial row.
+        const int items = x.rows * (R / 4), runs = items < kThreads ? kThreads / items : 1;
+#pragma unroll 1
+        for (int base = 0; base < items; base += kThreads) {
+            const int run = runs > 1 ? tid / items : 0, it = runs > 1 ? tid - run * items : base + tid;
+            const int rr = it / (R / 4), quad = it % (R / 4);
+            float m = -INFINITY, l = 0.0f;
+            f32x4 y = {0, 0, 0, 0};
+            const auto add = [&](float mz, float lz, f32x4 part) {
+                const float m2 = fmaxf(m, mz), to = base_of(m2);
+                const float down = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(mz - to);
+                m = m2;
+                l = fmaf(l, down, lz * w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = fmaf(y[e], down, part[e] * w);
+            };
+            const auto all = [&](const Shared &mem, int ns, int step, int row, int ml) {
+#pragma unroll 4
+                for (int z = run; z < ns; z += runs) {
+                    float mz, lz;
+                    mem.get2(z * step + ml, mz, lz);
+                    add(mz, lz, mem.get(z * step + row));
+                }
+            };
+            if (run < runs && it < items) {
+                all(own, ns_own, one, rr * R + 4 * quad, more.own.rows * R + 2 * rr);
+                const int at = x.at + rr, t = (at >> more.pre_shift) - first, pr = at - ((t + first) << more.pre_shift);
+                const int start = t * a.sp.splits * one_pre;
+                if (at < end) all(pre, ns_pre, one_pre, start + pr * R + 4 * quad, start + a.sp.rows * R + 2 * pr);
+            }
+            if (runs > 1) {
+                // thread's quad, then its (m, l)
+                f32x4 *quads = (f32x4 *)lds;
+                float2 *mls = (float2 *)(lds + 4 * kThreads);
+                __syncthreads();
+                quads[tid] = y;
+                mls[tid] = make_float2(m, l);
+                __syncthreads();
+                if (run == 0)
+#pragma unroll 1
+                    for (int z = 1; z < runs; ++z) {
+                        const float2 ml = mls[z * items + it];
+                        add(ml.x, ml.y, quads[z * items + it]);
+                    }
+            }
+            if (run == 0 && it < items) {
+                const int gr = x.base + rr, ti = gr / a.G;
+                put_quad<DT>(a, x.r0 + ti, hk * a.G + gr - ti * a.G, quad, y, l);
+            }
+        }
+    }
+}
 
 template <int KIND, int NT, int DT>
 __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
@@ -32,63 +151,88 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
     // Workgroups go round the XCDs in order of blockIdx, x first: heads and
     // sequences spread over them, where splits, of which short sequences leave
     // the later ones empty, would load a few (64 ragged sequences to 8k: 100 us).
-    const int tile = blockIdx.z % a.sp.tiles, split = blockIdx.z / a.sp.tiles, hk = blockIdx.x, u = blockIdx.y;
+    int tile, split, hk, u;
+    bool rest = false;                                     // of kPart: the second sort
+    if constexpr (KIND == kPart) {
+        int x = blockIdx.x;
+        rest = x >= more.pre_groups;
+        const int units = rest ? more.batch : more.groups, tiles = rest ? more.own.tiles : a.sp.tiles;
+        x -= rest ? more.pre_groups : 0;
+        hk = x % a.heads;
+        x /= a.heads;
+        u = x % units;
+        x /= units;
+        tile = x % tiles;
+        split = x / tiles;
+    } else {
+        tile = blockIdx.z % a.sp.tiles, split = blockIdx.z / a.sp.tiles, hk = blockIdx.x, u = blockIdx.y;
+    }
+    const int chunk = KIND == kPart && rest ? more.own.chunk : a.sp.chunk;
+    const int tile_rows = KIND == kPart && rest ? more.own.rows : a.sp.rows;
     // Without a window the first block to look up is known before the length is.
     int guess = -1;
     if constexpr (KIND == kWhole)
         guess = a.s.blocks[u * a.s.stride + min(split * a.sp.chunk + wave + kWaves * lane, (a.s.max_len - 1) / kBlock)];
     // The rows, and the row of the table, b; with a list, the row's own keys end at list_end.
-    int r0, n, b = u, len = 0, cut = 0, list_end = 0;
+    int r0, n, b = u, len = 0, cut = 0, list_end = 0, unused;
     Group group;
-    if constexpr (KIND == kWhole || KIND == kRest) {
+    if constexpr (KIND == kWhole) {
         a.s.rows(b, r0, n);
         len = a.s.len(b);
-        if constexpr (KIND == kRest) {
-            int g;
-            cut = more.group_of(a.s, b, g).cut;
-        }
     } else if constexpr (KIND == kChosen) {
         int at;
         if (!more.place(a.s, u, b, at)) return;
         list_end = at + 1;
         r0 = u;
         n = 1;
+    } else if (rest) {
+        a.s.rows(b, r0, n);
+        len = a.s.len(b);
+        group = more.group_of(a.s, b);
+        cut = group.cut;
     } else {
         group = more.group(a.s, u);
         b = group.first;
         r0 = group.r0;
         n = group.n;
         cut = group.cut;
+        if (cut == 0) return;
     }
     const int total = n * a.G, base = tile * kRows;
     if (base >= total) return;
     const int last_row = min(base + kRows, total) - 1;
     int lo0, hi0, lo1, hi1;                                // of the tile's first and last row
-    if constexpr (KIND == kWhole || KIND == kRest) {
+    if constexpr (KIND == kWhole) {
         a.mask.range(base / a.G, n, len, lo0, hi0);
         a.mask.range(last_row / a.G, n, len, lo1, hi1);
-    } else {
+    } else if constexpr (KIND == kChosen) {
         lo0 = lo1 = 0;
-        hi0 = hi1 = KIND == kChosen ? list_end : cut;
-    }
-    if constexpr (KIND == kRest) {
+        hi0 = hi1 = list_end;
+    } else if (rest) {
+        a.mask.range(base / a.G, n, len, unused, hi0);
+        a.mask.range(last_row / a.G, n, len, unused, hi1);
         lo0 = lo1 = cut;
         hi1 = max(hi1, cut);
+    } else {
+        lo0 = lo1 = 0;
+        hi1 = cut;
     }
     // (of a list, places in it)
     const int first = lo0 / kBlock, end = KIND == kChosen ? (list_end > 0 ? more.top : 0) : (hi1 + kBlock - 1) / kBlock;
-    const int ns = KIND == kChosen ? (list_end > 0 ? a.sp.splits : 1) : splits_of(lo0, hi1, a.sp.chunk);
+    const int ns = KIND == kChosen ? (list_end > 0 ? a.sp.splits : 1) : splits_of(lo0, hi1, chunk);
     if (split >= ns) return;
     const int row = min(base + r, last_row), i = row / a.G, head = hk * a.G + row - i * a.G;
     int lo, hi;
-    if constexpr (KIND == kWhole || KIND == kRest) {
+    if constexpr (KIND == kWhole) {
         a.mask.range(i, n, len, lo, hi);
-        if constexpr (KIND == kRest) lo = cut;
-    } else {
+    } else if constexpr (KIND == kChosen) {
         lo = 0;
         hi = list_end;
-    }
-    if constexpr (KIND == kShared) {                       // every row has an end of its own
+    } else if (rest) {
+        a.mask.range(i, n, len, unused, hi);
+        lo = cut;
+    } else {                                               // every row has an end of its own
+        lo = 0;
         hi = hi0 = group.sees(a.s, a.mask, r0 + i);
 #pragma unroll
         for (int z = 1; z < 16; z <<= 1) hi0 = min(hi0, __shfl_xor(hi0, z, 64));
@@ -100,7 +244,7 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
     raw.load((const T *)a.q.data + (int64_t)(r0 + i) * a.q.token_stride + (int64_t)head * a.q.head_stride, g, 4, a.D, a.vec);
 
     // This wavefront's blocks: start, start + 4, ... A lane looks one of them up.
-    const int start = first + split * a.sp.chunk + wave, stop = min(first + (split + 1) * a.sp.chunk, end);
+    const int start = first + split * chunk + wave, stop = min(first + (split + 1) * chunk, end);
     int count = start < stop ? (stop - start + kWaves - 1) / kWaves : 0;
     int my_id, my_at = 0;                                  // (my_at: with a list, the block's place in the sequence)
     float my_ks, my_vs;
@@ -274,10 +418,13 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) all = fmaxf(all, wm[w][r]);
     const float mine = __builtin_amdgcn_exp2f(m - base_of(all));
-    const int64_t unit = ((int64_t)u * a.heads + hk) * a.sp.tiles + tile;
+    // (fields selected one by one: a selected struct would be looked up in memory)
+    const int tiles = KIND == kPart && rest ? more.own.tiles : a.sp.tiles, splits = KIND == kPart && rest ? more.own.splits : a.sp.splits;
+    float *parts = KIND == kPart && rest ? more.own.part : a.sp.part;
+    const int64_t unit = ((int64_t)u * a.heads + hk) * tiles + tile;
     const int rows_here = last_row - base + 1;
-    const int one = (a.sp.rows * (R + 2) + 3) / 4 * 4;     // floats of a split
-    const Shared mem(a.sp.part + unit * a.sp.splits * one);
+    const int one = (tile_rows * (R + 2) + 3) / 4 * 4;     // floats of a split
+    const Shared mem(parts + unit * splits * one);
 #pragma unroll
     for (int c0 = 0; c0 < R; c0 += kCols) {
         if (c0) __syncthreads();
@@ -304,18 +451,24 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] += sum[w][rr][8 * oc + e];
             const int gr = base + rr, ti = gr / a.G, hd = hk * a.G + gr - ti * a.G;
-            if (ns == 1 && (KIND == kWhole || KIND == kChosen)) {
+            if (ns == 1 && KIND != kPart) {
                 put_octet<DT>(a, r0 + ti, hd, c0 / 8 + oc, x, ll);
                 if (KIND == kWhole && a.sp.ml && c0 == 0 && oc == 0) a.sp.ml[32 * row_block(a, hk, b, r0, gr) + gr % 32] = ml_of(am, ll);
             } else {
                 const uint32_t dst = split * one + rr * R + c0 + 8 * oc;
                 mem.put(dst, (f32x4){x[0], x[1], x[2], x[3]});
                 mem.put(dst + 4, (f32x4){x[4], x[5], x[6], x[7]});
-                if (c0 == 0 && oc == 0) mem.put2(split * one + a.sp.rows * R + 2 * rr, am, ll);
+                if (c0 == 0 && oc == 0) mem.put2(split * one + tile_rows * R + 2 * rr, am, ll);
             }
         }
     }
-    if constexpr (KIND == kShared || KIND == kRest) return;     // left to the join of both
+    if constexpr (KIND == kPart) {
+        if (more.inside) {
+            __syncthreads();                               // (of the sums' place in LDS)
+            join_parts<NT, DT>(a, more, rest, u, hk, tile, group, (float *)sum);
+        }
+        return;
+    }
     if (ns == 1 || !last_of(a.sp.tickets + unit, ns, &flag)) return;
     // The last workgroup joins the splits, in an order that does not depend on
     // their arrival: first the rows' maxima and sums, 16 splits at a time, then

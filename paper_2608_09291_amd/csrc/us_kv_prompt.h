@@ -83,10 +83,7 @@ __device__ __forceinline__ void prompt_rows(const Args a, const Others &more) {
     } else {
         a.s.rows(b, r0, n);
         len = a.s.len(b);
-        if constexpr (KIND == kRest) {
-            int g;
-            cut = more.group_of(a.s, b, g).cut;
-        }
+        if constexpr (KIND == kRest) cut = more.group_of(a.s, b).cut;
     }
     const int total = n * a.G, base = tile * kRows;
     if (base >= total) return;

@@ -5,9 +5,11 @@
 //   m = max(m1, m2),  out = (o1 2^(m1 - m) + o2 2^(m2 - m)) / (l1 2^(m1 - m) + l2 2^(m2 - m)).
 // The first part's rows are those of all sequences of a group, taken together,
 // so that their common keys are read once for all of them; the second's are a
-// sequence's over the keys behind. Both take the kernels of us_kv_attend (their
-// bodies: us_kv_decode.h, us_kv_prompt.h), leave partial rows, and a third
-// kernel joins them.
+// sequence's over the keys behind. Both take the bodies of us_kv_attend's kernels
+// (us_kv_decode.h, us_kv_prompt.h) and leave partial rows. Where both have few
+// rows, one launch does it all: the last workgroup that leaves some of a unit's
+// joins them. Common keys of many rows have a launch of their own ahead of it. Where
+// the sequences themselves have many rows, a third one joins.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -17,9 +19,9 @@
 namespace us_kv {
 namespace {
 
-template <int KIND, int NT, int DT>
+template <int NT, int DT>
 __global__ __launch_bounds__(kDecodeThreads, NT > 4 ? 1 : 2) void us_kv_shared_few_kernel(Args a, Others more) {
-    decode_rows<KIND, NT, DT>(a, more);
+    decode_rows<kPart, NT, DT>(a, more);
 }
 
 template <int KIND, int NT, int DT, int W>
@@ -39,9 +41,9 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
     constexpr int R = 32 * NT, kEach = 256 / (R / 4);
     const int b = blockIdx.y, H = a.heads * a.G, quad = threadIdx.x % (R / 4);
     const int64_t place = (int64_t)blockIdx.x * kEach + threadIdx.x / (R / 4);
-    int r0, n, g;
+    int r0, n;
     a.s.rows(b, r0, n);
-    const Group group = more.group_of(a.s, b, g);
+    const Group group = more.group_of(a.s, b);
     if ((int)threadIdx.x >= kEach * (R / 4) || place >= (int64_t)n * H) return;
     const int i = (int)(place / H), head = (int)(place - (int64_t)i * H), hk = head / a.G, hh = head - hk * a.G;
     float m = -INFINITY, l = 0.0f;
@@ -69,7 +71,7 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
     };
     if (group.cut > 0) {
         const int at = (r0 - group.r0 + i) * a.G + hh;     // among the group's rows
-        if (at < group.n * a.G) add(pre, g, at, splits_of(0, group.cut, pre.chunk));
+        if (at < group.n * a.G) add(pre, group.number, at, splits_of(0, group.cut, pre.chunk));
     }
     const int row = i * a.G + hh, base = row / own.rows * own.rows;
     int lo, hi;
@@ -80,8 +82,11 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
 
 struct SharedPlan {
     Plan pre, own;
-    size_t own_part, total;                                // bytes; the first part's rows lie at 0
+    int64_t pre_groups, own_groups;                        // workgroups of either part
+    size_t pre_part, own_part, total;                      // bytes; the tickets lie at 0
 };
+
+constexpr int64_t kMost = 1 << 22;
 
 size_t part_bytes(const Plan &p, int64_t pairs, int R) {
     return (size_t)(pairs * p.tiles * p.splits) * (size_t)up((int64_t)p.rows * (R + 2), 4) * 4;
@@ -117,18 +122,25 @@ us_status shared_plan(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, in
     us_status st = plan_of(c, all, q_heads, tokens, f32, first, p.pre);
     if (st == US_OK) st = plan_of(c, s, q_heads, tokens, f32, o, p.own);
     if (st != US_OK) return st;
-    p.own_part = part_bytes(p.pre, (int64_t)g.groups * c.heads, R);
-    p.total = p.own_part + part_bytes(p.own, (int64_t)s.batch * c.heads, R);
+    const int64_t pre = (int64_t)g.groups * c.heads, own = (int64_t)s.batch * c.heads;
+    p.pre_groups = pre * p.pre.tiles * p.pre.splits;
+    p.own_groups = own * p.own.tiles * p.own.splits;
+    // (in one dimension, of fewer than 2^32 threads)
+    if (p.pre_groups > kMost || p.own_groups > kMost) return US_ERR_SHAPE;
+    p.pre_part = p.own.decode ? (size_t)up(own * p.own.tiles * 4, 16) : 0;
+    p.own_part = p.pre_part + part_bytes(p.pre, pre, R);
+    p.total = p.own_part + part_bytes(p.own, own, R);
     return US_OK;
 }
 
+template <int NT, int DT>
+hipError_t launch_few(const Args &a, const Others &more, int64_t groups, hipStream_t stream) {
+    hipLaunchKernelGGL((us_kv_shared_few_kernel<NT, DT>), dim3((unsigned)groups), dim3(kDecodeThreads), 0, stream, a, more);
+    return hipGetLastError();
+}
+
 template <int KIND, int NT, int DT>
-hipError_t launch_part(const Args &a, const Others &more, const Plan &p, int units, hipStream_t stream) {
-    if (p.decode) {
-        hipLaunchKernelGGL((us_kv_shared_few_kernel<KIND, NT, DT>), dim3(a.heads, units, p.splits * p.tiles), dim3(kDecodeThreads), 0,
-                           stream, a, more);
-        return hipGetLastError();
-    }
+hipError_t launch_many(const Args &a, const Others &more, int64_t groups, hipStream_t stream) {
     constexpr int R = 32 * NT, W = prompt_waves(R), kLds = prompt_lds<R, DT == US_F32>();
     auto kern = us_kv_shared_many_kernel<KIND, NT, DT, W>;
     if constexpr (kLds > 65536 - 1024) {
@@ -136,7 +148,7 @@ hipError_t launch_part(const Args &a, const Others &more, const Plan &p, int uni
         const hipError_t e = allow_lds(kern, set);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)units * a.heads * p.tiles * p.splits), dim3(64 * W), kLds, stream, a, more);
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(64 * W), kLds, stream, a, more);
     return hipGetLastError();
 }
 
@@ -179,7 +191,8 @@ extern "C" us_status us_kv_attend_shared(const us_kv_cache *cache, const us_kv_s
     st = shared_plan(*cache, *seqs, q_heads, q->tokens, q->dtype == US_F32, *groups, o, p);
     if (st != US_OK) return st;
     if (!ws || (uintptr_t)ws % 16 || ws_bytes < p.total) return US_ERR_ARG;
-    float *first = (float *)ws, *second = (float *)((uint8_t *)ws + p.own_part);
+    uint8_t *w = (uint8_t *)ws;
+    float *first = (float *)(w + p.pre_part), *second = (float *)(w + p.own_part);
     Args a = {};
     a.k = cache->k, a.v = cache->v, a.ks = cache->k_scale, a.vs = cache->v_scale;
     a.heads = cache->heads, a.D = cache->head_dim, a.G = q_heads / cache->heads;
@@ -196,11 +209,24 @@ extern "C" us_status us_kv_attend_shared(const us_kv_cache *cache, const us_kv_s
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
         return with_type(q->dtype, [&](auto dt) {
             constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value, kEach = 256 / (8 * NT);
+            more.own = split_of(p.own, second);
+            more.own.tickets = (int32_t *)w;
             a.sp = split_of(p.pre, first);
-            hipError_t e = launch_part<kShared, NT, DT>(a, more, p.pre, groups->groups, hs);
+            // (a tile of fewer than 16 rows is the only one)
+            more.pre_shift = p.pre.rows < kDecodeRows ? 30 : __builtin_ctz(p.pre.rows);
+            hipError_t e = hipSuccess;
+            if (!p.pre.decode) e = launch_many<kShared, NT, DT>(a, more, p.pre_groups, hs);
             if (e != hipSuccess) return e;
-            a.sp = split_of(p.own, second);
-            e = launch_part<kRest, NT, DT>(a, more, p.own, seqs->batch, hs);
+            if (p.own.decode) {
+                more.inside = 1;
+                more.pre_groups = p.pre.decode ? (int)p.pre_groups : 0;
+                return launch_few<NT, DT>(a, more, more.pre_groups + p.own_groups, hs);
+            }
+            more.pre_groups = (int)p.pre_groups;
+            if (p.pre.decode) e = launch_few<NT, DT>(a, more, p.pre_groups, hs);
+            if (e != hipSuccess) return e;
+            a.sp = more.own;
+            e = launch_many<kRest, NT, DT>(a, more, p.own_groups, hs);
             if (e != hipSuccess) return e;
             const Parts pre{first, p.pre.chunk, p.pre.splits, p.pre.tiles, p.pre.rows};
             const Parts own{second, p.own.chunk, p.own.splits, p.own.tiles, p.own.rows};
