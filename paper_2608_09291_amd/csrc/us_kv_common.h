@@ -57,8 +57,11 @@ struct Seqs {
             r0 = starts[b];
             n = starts[b + 1] - r0;
         }
+        n = bounded(r0, n);
+    }
+    __device__ int bounded(int r0, int n) const {
         // (64 bits: the table may hold anything)
-        n = r0 < 0 || r0 >= tokens ? 0 : (int)min((int64_t)max(min(n, max_new), 0), (int64_t)tokens - r0);
+        return r0 < 0 || r0 >= tokens ? 0 : (int)min((int64_t)max(min(n, max_new), 0), (int64_t)tokens - r0);
     }
     // The block that holds block `i` of sequence b, or -1. i < max_len / 64, rounded up.
     __device__ int valid(int id) const { return id >= 0 && id < n_blocks ? id : -1; }

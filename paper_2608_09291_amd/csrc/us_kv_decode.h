@@ -15,13 +15,28 @@ namespace us_kv {
 
 constexpr int kDecodeThreads = 256, kDecodeWaves = 4, kDecodeRows = 16;
 
+// Partial rows of other workgroups, as Shared reads them, at addresses that differ between lanes.
+__device__ inline void get_pair(const float *p, float &x, float &y) {
+    const uint64_t w = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    x = __uint_as_float((uint32_t)w);
+    y = __uint_as_float((uint32_t)(w >> 32));
+}
+__device__ inline f32x4 get_part(const float *p) {
+    float a, b, c, d;
+    get_pair(p, a, b);
+    get_pair(p + 2, c, d);
+    return (f32x4){a, b, c, d};
+}
+
 // The end of a kPart workgroup. A unit is a tile of a sequence's rows; it has partial rows over its own keys
 // and, in one or two tiles of its group's rows, over the common ones. The last workgroup that leaves some of a
 // unit's joins them, in an order that does not depend on who that is. A workgroup over common keys has rows of up
-// to 16 units. (The tables may hold anything: both sorts of workgroups count a unit's parts from the same numbers.)
+// to 16 units, and joins all that it is the last of together. (The tables may hold anything: both sorts of
+// workgroups count a unit's parts from the same numbers.) r0, n, len: of a lane's sequence, the first of which is
+// `seq`, up to `seqs`.
 template <int NT, int DT>
-__device__ inline void join_parts(const Args &a, const Others &more, bool rest, int u, int hk, int tile, const Group &group,
-                                  float *lds) {
+__device__ inline void join_parts(const Args &a, const Others &more, bool rest, int seq, int seqs, int hk, int tile, const Group &group,
+                                  int r0, int n, int len, float *lds) {
     constexpr int R = 32 * NT, kThreads = kDecodeThreads;
     struct Unit {
         int r0, base, rows;                                // of the sequence, and the tile's
@@ -36,13 +51,15 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     __syncthreads();
     if (tid < 64) {
         const int row0 = tile * kDecodeRows;
-        const int b1 = rest ? u + 1 : group.last;
 #pragma unroll 1
-        for (int b = (rest ? u : group.first) + tid; b < b1; b += 64) {
-            int r0, n, lo, hi;
-            a.s.rows(b, r0, n);
+        for (int b = seq + tid; b < seqs; b += 64) {
+            int lo, hi;
+            if (b != seq + tid) {
+                a.s.rows(b, r0, n);
+                len = a.s.len(b);
+            }
             const int64_t far = (int64_t)(r0 - group.r0) * a.G;                // of its first row, among the group's
-            const int total = n * a.G, len = a.s.len(b);
+            const int total = n * a.G;
             const bool in = far >= 0 && far < end && group.cut > 0;
             const int at0 = in ? (int)far : 0;
             if (!rest && (!in || at0 + total <= row0 || at0 >= row0 + kDecodeRows)) continue;
@@ -63,8 +80,10 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
                 if (!rest && (!x.pre || tile < first || tile > last)) continue;
                 const int parts = x.own + (more.pre_groups && x.pre ? x.pre * (last - first + 1) : 0);
                 int32_t *ticket = more.own.tickets + x.unit;
-                if (__hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != parts - 1) continue;
-                __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (parts > 1) {
+                    if (__hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != parts - 1) continue;
+                    __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
                 const int i = atomicAdd(&found, 1);
                 if (i < kDecodeRows) list[i] = x;
             }
@@ -73,64 +92,75 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     __syncthreads();
     __asm__ volatile("" ::: "memory");
     const int count = __builtin_amdgcn_readfirstlane(min(found, kDecodeRows));
+    if (count == 0) return;
+    int rows = 0;
+    for (int f = 0; f < count; ++f) rows += list[f].rows;
+    rows = __builtin_amdgcn_readfirstlane(rows);
     const int one = (more.own.rows * (R + 2) + 3) / 4 * 4, one_pre = (a.sp.rows * (R + 2) + 3) / 4 * 4;
+    // A thread per quad of a row's values, and of a few rows as many for each as there are threads, which take
+    // every runs-th partial row.
+    const int items = rows * (R / 4), runs = items < kThreads ? kThreads / items : 1;
+    const int64_t splits = (int64_t)a.sp.splits * one_pre;
 #pragma unroll 1
-    for (int f = 0; f < count; ++f) {
+    for (int base = 0; base < items; base += kThreads) {
+        const int run = runs > 1 ? tid / items : 0, it = runs > 1 ? tid - run * items : base + tid;
+        const bool here = run < runs && it < items;
+        int rr = here ? it / (R / 4) : 0, f = 0;
+        const int quad = it % (R / 4);
+        for (; rr >= list[f].rows; ++f) rr -= list[f].rows;
         const Unit x = list[f];
-        const int unit = __builtin_amdgcn_readfirstlane(x.unit), first = __builtin_amdgcn_readfirstlane(x.at >> more.pre_shift);
-        const int ns_own = __builtin_amdgcn_readfirstlane(x.own), ns_pre = __builtin_amdgcn_readfirstlane(x.pre);
-        const Shared own(more.own.part + (int64_t)unit * more.own.splits * one);
-        const Shared pre(a.sp.part + (((int64_t)group.number * a.heads + hk) * a.sp.tiles + first) * a.sp.splits * one_pre);
-        // A thread per quad of a row's values, and of a few rows as many for each as there are threads, which
-        // take every runs-th partial row.
-        const int items = x.rows * (R / 4), runs = items < kThreads ? kThreads / items : 1;
-#pragma unroll 1
-        for (int base = 0; base < items; base += kThreads) {
-            const int run = runs > 1 ? tid / items : 0, it = runs > 1 ? tid - run * items : base + tid;
-            const int rr = it / (R / 4), quad = it % (R / 4);
-            float m = -INFINITY, l = 0.0f;
-            f32x4 y = {0, 0, 0, 0};
-            const auto add = [&](float mz, float lz, f32x4 part) {
-                const float m2 = fmaxf(m, mz), to = base_of(m2);
-                const float down = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(mz - to);
-                m = m2;
-                l = fmaf(l, down, lz * w);
+        float m = -INFINITY, l = 0.0f;
+        f32x4 y = {0, 0, 0, 0};
+        const auto add = [&](float mz, float lz, f32x4 part) {
+            const float m2 = fmaxf(m, mz), to = base_of(m2);
+            const float down = __builtin_amdgcn_exp2f(m - to), w = __builtin_amdgcn_exp2f(mz - to);
+            m = m2;
+            l = fmaf(l, down, lz * w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = fmaf(y[e], down, part[e] * w);
-            };
-            const auto all = [&](const Shared &mem, int ns, int step, int row, int ml) {
-#pragma unroll 4
-                for (int z = run; z < ns; z += runs) {
-                    float mz, lz;
-                    mem.get2(z * step + ml, mz, lz);
-                    add(mz, lz, mem.get(z * step + row));
-                }
-            };
-            if (run < runs && it < items) {
-                all(own, ns_own, one, rr * R + 4 * quad, more.own.rows * R + 2 * rr);
-                const int at = x.at + rr, t = (at >> more.pre_shift) - first, pr = at - ((t + first) << more.pre_shift);
-                const int start = t * a.sp.splits * one_pre;
-                if (at < end) all(pre, ns_pre, one_pre, start + pr * R + 4 * quad, start + a.sp.rows * R + 2 * pr);
-            }
-            if (runs > 1) {
-                // thread's quad, then its (m, l)
-                f32x4 *quads = (f32x4 *)lds;
-                float2 *mls = (float2 *)(lds + 4 * kThreads);
-                __syncthreads();
-                quads[tid] = y;
-                mls[tid] = make_float2(m, l);
-                __syncthreads();
-                if (run == 0)
+            for (int e = 0; e < 4; ++e) y[e] = fmaf(y[e], down, part[e] * w);
+        };
+        if (here) {
+            // Own parts, then the common ones: addresses of the quad and of (m, l), z-th of ns.
+            const int at = x.at + rr, t = at >> more.pre_shift, pr = at - (t << more.pre_shift);
+            const float *own = more.own.part + (int64_t)x.unit * more.own.splits * one;
+            const float *pre = a.sp.part + (((int64_t)group.number * a.heads + hk) * a.sp.tiles + t) * splits;
+            const int ns = x.own + (at < end ? x.pre : 0);
 #pragma unroll 1
-                    for (int z = 1; z < runs; ++z) {
-                        const float2 ml = mls[z * items + it];
-                        add(ml.x, ml.y, quads[z * items + it]);
-                    }
+            for (int z0 = run; z0 < ns; z0 += 4 * runs) {
+                f32x4 part[4];
+                float mz[4], lz[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {              // (past the last: it once more, for nothing)
+                    const int z = min(z0 + i * runs, ns - 1);
+                    const bool mine = z < x.own;
+                    const float *src = mine ? own + (int64_t)z * one : pre + (int64_t)(z - x.own) * one_pre;
+                    const int row = mine ? rr : pr, rows = mine ? more.own.rows : a.sp.rows;
+                    part[i] = get_part(src + row * R + 4 * quad);
+                    get_pair(src + rows * R + 2 * row, mz[i], lz[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (z0 + i * runs < ns) add(mz[i], lz[i], part[i]);
             }
-            if (run == 0 && it < items) {
-                const int gr = x.base + rr, ti = gr / a.G;
-                put_quad<DT>(a, x.r0 + ti, hk * a.G + gr - ti * a.G, quad, y, l);
-            }
+        }
+        if (runs > 1) {
+            // thread's quad, then its (m, l)
+            f32x4 *quads = (f32x4 *)lds;
+            float2 *mls = (float2 *)(lds + 4 * kThreads);
+            __syncthreads();
+            quads[tid] = y;
+            mls[tid] = make_float2(m, l);
+            __syncthreads();
+            if (run == 0)
+#pragma unroll 1
+                for (int z = 1; z < runs; ++z) {
+                    const float2 ml = mls[z * items + it];
+                    add(ml.x, ml.y, quads[z * items + it]);
+                }
+        }
+        if (run == 0 && here) {
+            const int gr = x.base + rr, ti = gr / a.G;
+            put_quad<DT>(a, x.r0 + ti, hk * a.G + gr - ti * a.G, quad, y, l);
         }
     }
 }
@@ -190,6 +220,7 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
         len = a.s.len(b);
         group = more.group_of(a.s, b);
         cut = group.cut;
+        if (more.inside && cut > 0) more.rows_of(a.s, group);                  // (for the join)
     } else {
         group = more.group(a.s, u);
         b = group.first;
@@ -465,7 +496,8 @@ __device__ __forceinline__ void decode_rows(const Args a, const Others &more) {
     if constexpr (KIND == kPart) {
         if (more.inside) {
             __syncthreads();                               // (of the sums' place in LDS)
-            join_parts<NT, DT>(a, more, rest, u, hk, tile, group, (float *)sum);
+            join_parts<NT, DT>(a, more, rest, rest ? u : group.first, rest ? u + 1 : group.last, hk, tile, group,
+                               rest ? r0 : group.my_r0, rest ? n : group.my_n, rest ? len : group.my_len, (float *)sum);
         }
         return;
     }

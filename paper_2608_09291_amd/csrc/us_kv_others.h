@@ -26,26 +26,41 @@ __device__ inline int last_at_most(const int32_t *p, int n, int x) {
     }
 }
 
-// A group's sequences [first, last), their token rows, and the keys that they have in common.
+// A group's sequences [first, last), their token rows, and the keys that they have in common. A lane has the
+// first row, the number of rows and the length of a sequence of the first 64.
 struct Group {
     int first, last, r0, n, cut, number;
+    int my_r0, my_n, my_len;
 
-    // Keys of the group's that row t sees: none if it is no row of its sequences.
+    // Keys of the group's that row t sees: none if it is no row of its sequences. By whole wavefronts.
     __device__ int sees(const Seqs &s, const Mask &mask, int t) const {
-        int b = t;
-        if (s.starts) {
-            b = first;
-            for (int e = last; e - b > 1;) {
-                const int mid = (b + e) >> 1;
-                if (s.starts[mid] <= t) b = mid;
-                else e = mid;
+        int r, rows, len, lo, hi;
+        if (last - first <= 64) {
+            int at = 0;                                    // the last that begins at t or before
+#pragma unroll
+            for (int step = 32; step > 0; step >>= 1) {
+                const int r1 = __shfl(my_r0, at + step, 64);
+                at = at + step < last - first && r1 <= t ? at + step : at;
             }
+            r = __shfl(my_r0, at, 64);
+            rows = __shfl(my_n, at, 64);
+            len = __shfl(my_len, at, 64);
+        } else {
+            int b = t;
+            if (s.starts) {
+                b = first;
+                for (int e = last; e - b > 1;) {
+                    const int mid = (b + e) >> 1;
+                    if (s.starts[mid] <= t) b = mid;
+                    else e = mid;
+                }
+            }
+            if (b < first || b >= last) return 0;
+            s.rows(b, r, rows);
+            len = s.len(b);
         }
-        if (b < first || b >= last) return 0;
-        int r, rows, lo, hi;
-        s.rows(b, r, rows);
         if (t < r || t - r >= rows) return 0;
-        mask.range(t - r, rows, s.len(b), lo, hi);
+        mask.range(t - r, rows, len, lo, hi);
         return min(hi, cut);
     }
 };
@@ -72,41 +87,81 @@ struct Others {
         at = s.len(b) - n + (t - r);
         return true;
     }
-    // Whether the groups are in order: each sequence is then in one of them at most, and a launch's workgroups
-    // agree on which. (Where they are not, nothing is in common.) By whole wavefronts, as the next two.
-    __device__ bool ordered() const {
+    // What all of a launch's workgroups read of the groups; by whole wavefronts. Up to 64 groups come in one
+    // load, a lane each. Whether they are in order: each sequence is then in one of them at most, and the
+    // workgroups agree on which. (Where they are not, nothing is in common.)
+    struct Table {
+        int start, end, shared;                            // this lane's
+        bool ordered;
+    };
+    __device__ Table table() const {
         const int lane = threadIdx.x & 63;
-        uint64_t down = 0;
-        for (int i = lane; i - lane < groups; i += 64)
+        Table t;
+        t.start = group_starts[min(lane, groups)];
+        t.end = group_starts[min(lane + 1, groups)];
+        t.shared = shared[min(lane, groups - 1)];
+        uint64_t down = __builtin_amdgcn_ballot_w64(t.start > t.end);
+        for (int i = lane + 64; i - lane < groups; i += 64)
             down |= __builtin_amdgcn_ballot_w64(i < groups && group_starts[min(i, groups - 1)] > group_starts[min(i, groups - 1) + 1]);
-        return down == 0;
+        t.ordered = down == 0;
+        return t;
     }
-    __device__ Group group(const Seqs &s, int g) const {
-        Group x = group_at(s, g);
-        if (!ordered()) x.cut = x.n = 0;
-        return x;
-    }
-    __device__ Group group_at(const Seqs &s, int g) const {
+    // Group g's sequences and keys in common.
+    __device__ Group sequences(const Seqs &s, const Table &t, int g) const {
+        int a, z, c;
+        if (groups <= 64) {
+            a = __builtin_amdgcn_readlane(t.start, g);
+            z = __builtin_amdgcn_readlane(t.end, g);
+            c = __builtin_amdgcn_readlane(t.shared, g);
+        } else {
+            a = group_starts[g];
+            z = group_starts[g + 1];
+            c = shared[g];
+        }
         Group x;
         x.number = g;
-        x.first = min(max(group_starts[g], 0), batch);
-        x.last = min(max(group_starts[g + 1], x.first), (int)min((int64_t)batch, (int64_t)x.first + max_group));
-        x.cut = (int)min((int64_t)min(max(shared[g], 0), max_shared) * kBlock, (int64_t)s.max_len);
-        x.r0 = s.starts ? s.starts[x.first] : x.first;
-        const int64_t n = (int64_t)(s.starts ? s.starts[x.last] : x.last) - x.r0;
+        x.first = min(max(a, 0), batch);
+        x.last = min(max(z, x.first), (int)min((int64_t)batch, (int64_t)x.first + max_group));
+        x.cut = t.ordered ? (int)min((int64_t)min(max(c, 0), max_shared) * kBlock, (int64_t)s.max_len) : 0;
+        return x;
+    }
+    // And their rows.
+    __device__ void rows_of(const Seqs &s, Group &x) const {
+        const int b = x.first + (threadIdx.x & 63);
+        int next = b + 1;
+        x.my_r0 = b;
+        x.my_n = x.my_len = 0;
+        if (b < x.last) {
+            if (s.starts) {
+                x.my_r0 = s.starts[b];
+                next = s.starts[b + 1];
+            }
+            x.my_len = s.len(b);
+        }
+        x.r0 = __builtin_amdgcn_readlane(x.my_r0, 0);
+        int end = x.last;
+        if (s.starts) end = x.last - x.first <= 64 ? __builtin_amdgcn_readlane(next, max(x.last - x.first - 1, 0)) : s.starts[x.last];
+        if (b < x.last) x.my_n = s.bounded(x.my_r0, next - x.my_r0);
+        const int64_t n = x.first < x.last ? (int64_t)end - x.r0 : 0;
         x.n = x.r0 < 0 || x.r0 >= s.tokens
                   ? 0
                   : (int)min(min(max(n, (int64_t)0), (int64_t)max_group * s.max_new), (int64_t)s.tokens - x.r0);
+    }
+    __device__ Group group(const Seqs &s, int g) const {
+        Group x = sequences(s, table(), g);
+        rows_of(s, x);
         return x;
     }
-    // The group of sequence b; one that has nothing in common for a sequence of none.
+    // The group of sequence b, without its rows; one that has nothing in common for a sequence of none.
     __device__ Group group_of(const Seqs &s, int b) const {
-        const int g = last_at_most(group_starts, groups, b);
-        if (g >= 0 && ordered()) {
-            const Group x = group_at(s, g);
+        const Table t = table();
+        const int g = groups <= 64 ? __builtin_popcountll(__builtin_amdgcn_ballot_w64((int)(threadIdx.x & 63) < groups && t.start <= b)) - 1
+                                   : last_at_most(group_starts, groups, b);
+        if (g >= 0) {
+            const Group x = sequences(s, t, g);
             if (b >= x.first && b < x.last) return x;
         }
-        return Group{b, b + 1, 0, 0, 0, 0};
+        return Group{b, b + 1, 0, 0, 0, 0, 0, 0, 0};
     }
 };
 

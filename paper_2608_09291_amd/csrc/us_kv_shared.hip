@@ -43,7 +43,8 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
     const int64_t place = (int64_t)blockIdx.x * kEach + threadIdx.x / (R / 4);
     int r0, n;
     a.s.rows(b, r0, n);
-    const Group group = more.group_of(a.s, b);
+    Group group = more.group_of(a.s, b);
+    if (group.cut > 0) more.rows_of(a.s, group);
     if ((int)threadIdx.x >= kEach * (R / 4) || place >= (int64_t)n * H) return;
     const int i = (int)(place / H), head = (int)(place - (int64_t)i * H), hk = head / a.G, hh = head - hk * a.G;
     float m = -INFINITY, l = 0.0f;
