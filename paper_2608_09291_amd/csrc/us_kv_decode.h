@@ -97,14 +97,17 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     for (int f = 0; f < count; ++f) rows += list[f].rows;
     rows = __builtin_amdgcn_readfirstlane(rows);
     const int one = (more.own.rows * (R + 2) + 3) / 4 * 4, one_pre = (a.sp.rows * (R + 2) + 3) / 4 * 4;
-    // A thread per quad of a row's values, and of a few rows as many for each as there are threads, which take
-    // every runs-th partial row.
-    const int items = rows * (R / 4), runs = items < kThreads ? kThreads / items : 1;
+    // A quad of a row's values per thread, or, where units are small and parts many, per `runs` of them, which
+    // take every runs-th partial row: how many is the same for all workgroups of the call, and with it the order
+    // of the sums. (6 sequences of 4 rows with up to 10 parts: 13.1 us with one, 20.5 with four.)
+    const int items = rows * (R / 4), unit_items = more.own.rows * (R / 4);
+    const int runs = more.own.splits + a.sp.splits < 32 || unit_items > 128 ? 1 : unit_items > 64 ? 2 : unit_items > 32 ? 4 : 8;
+    const int pass = kThreads / runs, run = tid / pass;
     const int64_t splits = (int64_t)a.sp.splits * one_pre;
 #pragma unroll 1
-    for (int base = 0; base < items; base += kThreads) {
-        const int run = runs > 1 ? tid / items : 0, it = runs > 1 ? tid - run * items : base + tid;
-        const bool here = run < runs && it < items;
+    for (int base = 0; base < items; base += pass) {
+        const int it = base + tid - run * pass;
+        const bool here = it < items;
         int rr = here ? it / (R / 4) : 0, f = 0;
         const int quad = it % (R / 4);
         for (; rr >= list[f].rows; ++f) rr -= list[f].rows;
@@ -151,11 +154,11 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
             quads[tid] = y;
             mls[tid] = make_float2(m, l);
             __syncthreads();
-            if (run == 0)
+            if (run == 0 && here)
 #pragma unroll 1
                 for (int z = 1; z < runs; ++z) {
-                    const float2 ml = mls[z * items + it];
-                    add(ml.x, ml.y, quads[z * items + it]);
+                    const float2 ml = mls[z * pass + tid];
+                    add(ml.x, ml.y, quads[z * pass + tid]);
                 }
         }
         if (run == 0 && here) {

@@ -324,14 +324,14 @@ def test_attend_shared(torch_cuda, sizes, common, own, new, H, Hk, D, causal, dt
     more = dict(max_group=max(sizes), max_shared=max(max(common), 1))
     ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, **args, **more)
     first = None
-    for again in range(2):
+    for again in range(12):                                 # bit for bit, whichever workgroup joins what
         out.fill_(math.nan)
         kv.attend_shared(cache, p.dev(p.blocks), p.dev(lens), q, out, groups, p.dev(common), ws=ws, **args, **more)
         torch.cuda.synchronize()
-        _check(torch, p, lens, new, q, out, dtype, causal=causal)
         if first is None:
+            _check(torch, p, lens, new, q, out, dtype, causal=causal)
             first = out.clone()
-    assert torch.equal(first, out)                          # bit for bit, and the workspace is left as it was found
+        assert torch.equal(first, out), again
     # without bounds of the groups, with the lengths' bound
     out.fill_(math.nan)
     args["max_len"] = max(lens)
