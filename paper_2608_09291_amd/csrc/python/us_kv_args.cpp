@@ -98,6 +98,25 @@ PyObject *rows_of(PyObject *const *args, Py_ssize_t n) {
     return Py_BuildValue("KLLLi", address(*t), (long long)t->stride(0), (long long)t->stride(1), (long long)t->size(0), dtype);
 }
 
+// (freq or None, positions, tokens, device) -> address of freq, pairs, axes, address of positions, their stride
+PyObject *turns_of(PyObject *const *args, Py_ssize_t n) {
+    if (!count(n, 4)) return nullptr;
+    if (args[0] == Py_None) return Py_BuildValue("KiiKL", 0ull, 0, 0, 0ull, 0ll);
+    const at::Tensor *f = tensor(args, 0, "freq"), *p = f ? tensor(args, 1, "positions") : nullptr;
+    if (!p) return nullptr;
+    const long long tokens = PyLong_AsLongLong(args[2]), device = PyLong_AsLongLong(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    if (f->scalar_type() != at::kFloat || f->dim() < 1 || f->dim() > 2 || !f->is_contiguous() || !on(*f, device))
+        return refuse("freq", "a contiguous float32 tensor (axes, pairs) on the rows' GPU is wanted");
+    const int64_t axes = f->dim() == 1 ? 1 : f->size(0), pairs = f->size(f->dim() - 1), last = p->dim() - 1;
+    if (p->scalar_type() != at::kInt || last < 0 || last > 1 || p->size(last) != tokens || (tokens > 1 && p->stride(last) != 1) ||
+        axes != (last ? p->size(0) : 1) || axes > 1000 || pairs > 1000 || !on(*p, device))
+        return PyErr_Format(PyExc_TypeError, "positions: int32 numbers (%lld, %lld) in contiguous rows on the rows' GPU are wanted",
+                            (long long)axes, tokens);
+    return Py_BuildValue("KiiKL", address(*f), (int)pairs, (int)axes, address(*p), (long long)(axes > 1 ? p->stride(0) : tokens));
+}
+
+PyObject *py_turns(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(turns_of, args, n); }
 PyObject *py_cache(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(cache_of, args, n); }
 PyObject *py_seqs(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(seqs_of, args, n); }
 PyObject *py_rows(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(rows_of, args, n); }
@@ -105,6 +124,7 @@ PyObject *py_rows(PyObject *, PyObject *const *args, Py_ssize_t n) { return guar
 PyMethodDef methods[] = {{"cache", (PyCFunction)(void (*)(void))py_cache, METH_FASTCALL, nullptr},
                          {"seqs", (PyCFunction)(void (*)(void))py_seqs, METH_FASTCALL, nullptr},
                          {"rows", (PyCFunction)(void (*)(void))py_rows, METH_FASTCALL, nullptr},
+                         {"turns", (PyCFunction)(void (*)(void))py_turns, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_args", "Checks and addresses of the key/value cache's tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

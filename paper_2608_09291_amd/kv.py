@@ -363,17 +363,7 @@ def rotate(q, k, freq, positions, q_out=None, k_out=None, adjacent: bool = False
         k_rows_out = k_rows if k_out is None else _rows(k_out, k_heads, d, "k_out", on)
     elif k_out is not None:
         raise TypeError("k_out: there is no k")
-    axes, pairs, at, at_pos, stride = 0, 0, 0, 0, 0
-    if freq is not None:
-        axes, pairs = (1, freq.shape[0]) if freq.dim() == 1 else freq.shape
-        if freq.dtype is not _F32 or freq.dim() > 2 or not freq.is_contiguous() or not _on(freq, on):
-            raise TypeError("freq: a contiguous float32 tensor (axes, pairs) on the rows' GPU is wanted")
-        shape = (tokens,) if positions.dim() == 1 else (axes, tokens)
-        if positions.dtype is not _I32 or positions.shape != shape or (positions.stride(-1) != 1 and tokens > 1) or \
-                (positions.dim() == 1 and axes != 1) or not _on(positions, on):
-            raise TypeError(f"positions: int32 numbers ({axes}, {tokens}) in contiguous rows on the rows' GPU are wanted")
-        at, at_pos = freq.data_ptr(), positions.data_ptr()
-        stride = positions.stride(0) if positions.dim() == 2 and axes > 1 else tokens
+    at, pairs, axes, at_pos, stride = _args.turns(freq, positions, tokens, on)
     how = _pack_rotation(at, pairs, axes, at_pos, stride, offset, 1 if adjacent else 0, 1 if norm else 0, eps,
                          _vector(q_weight, d, _F32, "q_weight", on), _vector(k_weight, d, _F32, "k_weight", on))
     _check("us_kv_rotate", L.us_kv_rotate(heads, k_heads, d, rows, rows_out, k_rows, k_rows_out, how,
