@@ -116,6 +116,41 @@ PyObject *turns_of(PyObject *const *args, Py_ssize_t n) {
     return Py_BuildValue("KiiKL", address(*f), (int)pairs, (int)axes, address(*p), (long long)(axes > 1 ? p->stride(0) : tokens));
 }
 
+// (tensor, rows, heads, name, device) -> address and length of the last dimension of a contiguous (rows, heads, n) tensor
+PyObject *table_of(PyObject *const *args, Py_ssize_t n, at::ScalarType type, const char *what) {
+    if (!count(n, 5)) return nullptr;
+    const char *name = PyUnicode_AsUTF8(args[3]);
+    const at::Tensor *t = name ? tensor(args, 0, name) : nullptr;
+    if (!t) return nullptr;
+    const long long rows = PyLong_AsLongLong(args[1]), heads = PyLong_AsLongLong(args[2]), device = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    if (t->dim() != 3 || t->scalar_type() != type || t->size(0) != rows || t->size(1) != heads || !t->is_contiguous())
+        return PyErr_Format(PyExc_TypeError, "%s: a contiguous %s tensor (%lld, %lld, blocks) is wanted", name, what, rows, heads);
+    if (!on(*t, device)) return refuse(name, "a tensor on the cache's GPU is wanted");
+    return Py_BuildValue("KL", address(*t), (long long)t->size(2));
+}
+PyObject *ints_of(PyObject *const *args, Py_ssize_t n) { return table_of(args, n, at::kInt, "int32"); }
+PyObject *floats_of(PyObject *const *args, Py_ssize_t n) { return table_of(args, n, at::kFloat, "float32"); }
+
+// (summary, blocks, heads, row, device) -> address of a contiguous uint8 (blocks, heads, 2, row) tensor
+PyObject *summary_of(PyObject *const *args, Py_ssize_t n) {
+    if (!count(n, 5)) return nullptr;
+    const at::Tensor *t = tensor(args, 0, "summary");
+    if (!t) return nullptr;
+    long long size[4] = {PyLong_AsLongLong(args[1]), PyLong_AsLongLong(args[2]), 2, PyLong_AsLongLong(args[3])};
+    const long long device = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    bool same = t->dim() == 4 && t->scalar_type() == at::kByte && t->is_contiguous();
+    for (int i = 0; i < 4 && same; ++i) same = t->size(i) == size[i];
+    if (!same)
+        return PyErr_Format(PyExc_TypeError, "summary: a contiguous uint8 tensor (%lld, %lld, 2, %lld) is wanted", size[0], size[1], size[3]);
+    if (!on(*t, device)) return refuse("summary", "a tensor on the cache's GPU is wanted");
+    return Py_BuildValue("K", address(*t));
+}
+
+PyObject *py_ints(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(ints_of, args, n); }
+PyObject *py_floats(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(floats_of, args, n); }
+PyObject *py_summary(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(summary_of, args, n); }
 PyObject *py_turns(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(turns_of, args, n); }
 PyObject *py_cache(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(cache_of, args, n); }
 PyObject *py_seqs(PyObject *, PyObject *const *args, Py_ssize_t n) { return guarded(seqs_of, args, n); }
@@ -124,6 +159,9 @@ PyObject *py_rows(PyObject *, PyObject *const *args, Py_ssize_t n) { return guar
 PyMethodDef methods[] = {{"cache", (PyCFunction)(void (*)(void))py_cache, METH_FASTCALL, nullptr},
                          {"seqs", (PyCFunction)(void (*)(void))py_seqs, METH_FASTCALL, nullptr},
                          {"rows", (PyCFunction)(void (*)(void))py_rows, METH_FASTCALL, nullptr},
+                         {"ints", (PyCFunction)(void (*)(void))py_ints, METH_FASTCALL, nullptr},
+                         {"floats", (PyCFunction)(void (*)(void))py_floats, METH_FASTCALL, nullptr},
+                         {"summary", (PyCFunction)(void (*)(void))py_summary, METH_FASTCALL, nullptr},
                          {"turns", (PyCFunction)(void (*)(void))py_turns, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_args", "Checks and addresses of the key/value cache's tensors.", -1, methods,

@@ -111,7 +111,7 @@ __device__ inline uint32_t order_of(float x) {
 
 // What of a row's scores the workgroup that chooses has in LDS.
 struct Pick {
-    uint32_t keys[kHeld];
+    __attribute__((aligned(16))) uint32_t keys[kHeld];
     __attribute__((aligned(16))) int hist[4][256];         // of the digits, the largest first
     u32x4 of_wave[kWaves];
     int counts[kWaves][2];
@@ -239,6 +239,34 @@ __device__ inline void select(F key, Seen mine, int n, int top, int *out, Pick &
 
 // Lanes that hold a row's octets together: a power of two.
 constexpr int lanes_of(int row) { return row <= 64 ? 8 : row <= 128 ? 16 : 32; }
+
+// The same of up to kFew keys in LDS, by counting for each how many come before it: up to a hundred or so,
+// that takes less than the steps above.
+constexpr int kFew = 128;
+__device__ inline void select_few(int n, int top, int *out, Pick &p) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int before = 0;
+    const uint32_t mine = tid < kFew ? p.keys[tid] : 0;
+    if (tid < kFew) {
+#pragma unroll 2
+        for (int j = 0; j < n; j += 4) {
+            const u32x4 k = *(const u32x4 *)&p.keys[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) before += j + i < tid ? k[i] >= mine : k[i] > mine;
+        }
+    }
+    const uint64_t taken = __builtin_amdgcn_ballot_w64(mine != 0 && before < top);
+    if (lane == 0) p.counts[wave][0] = __builtin_popcountll(taken);
+    __syncthreads();
+    int first = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kFew / 64; ++w) {
+        first += w < wave ? p.counts[w][0] : 0;
+        all += p.counts[w][0];
+    }
+    if (taken >> lane & 1) out[first + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0))] = tid;
+    for (int i = all + tid; i < top; i += kThreads) out[i] = -1;
+}
 
 template <int NT, int DT>
 __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
@@ -378,7 +406,16 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     int *out = a.chosen + unit * a.top;
     Seen seen;
     const int per = (blocks + kThreads - 1) / kThreads;
-    if (blocks <= kHeld) {
+    if (blocks <= kFew) {
+        if (tid < kFew) {
+            const int i = min(tid, max(blocks - 1, 0));
+            const float score = blocks ? score_of(i) : 0.0f;
+            const int block = blocks ? a.s.block(b, i) : -1;
+            pick.keys[tid] = tid < blocks ? key_of(i, block, score) : 0u;
+        }
+        __syncthreads();
+        select_few(blocks, a.top, out, pick);
+    } else if (blocks <= kHeld) {
 #pragma unroll 1
         for (int e0 = 0; e0 < per; e0 += 4) {              // (four on their way together)
             float score[4];

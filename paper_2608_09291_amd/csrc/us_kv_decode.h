@@ -104,6 +104,7 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     const int runs = more.own.splits + a.sp.splits < 32 || unit_items > 128 ? 1 : unit_items > 64 ? 2 : unit_items > 32 ? 4 : 8;
     const int pass = kThreads / runs, run = tid / pass;
     const int64_t splits = (int64_t)a.sp.splits * one_pre;
+    constexpr int kAhead = 8;                              // partial rows on their way
 #pragma unroll 1
     for (int base = 0; base < items; base += pass) {
         const int it = base + tid - run * pass;
@@ -129,11 +130,11 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
             const float *pre = a.sp.part + (((int64_t)group.number * a.heads + hk) * a.sp.tiles + t) * splits;
             const int ns = x.own + (at < end ? x.pre : 0);
 #pragma unroll 1
-            for (int z0 = run; z0 < ns; z0 += 4 * runs) {
-                f32x4 part[4];
-                float mz[4], lz[4];
+            for (int z0 = run; z0 < ns; z0 += kAhead * runs) {
+                f32x4 part[kAhead];
+                float mz[kAhead], lz[kAhead];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {              // (past the last: it once more, for nothing)
+                for (int i = 0; i < kAhead; ++i) {              // (past the last: it once more, for nothing)
                     const int z = min(z0 + i * runs, ns - 1);
                     const bool mine = z < x.own;
                     const float *src = mine ? own + (int64_t)z * one : pre + (int64_t)(z - x.own) * one_pre;
@@ -142,7 +143,7 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
                     get_pair(src + rows * R + 2 * row, mz[i], lz[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < kAhead; ++i)
                     if (z0 + i * runs < ns) add(mz[i], lz[i], part[i]);
             }
         }

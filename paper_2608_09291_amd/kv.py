@@ -429,26 +429,14 @@ def new_summary(cache: Cache):
 
 
 def _summary(t, cache) -> int:
-    if t.dtype is not torch.uint8 or t.shape != (cache.n_blocks, cache.heads, 2, row(cache.head_dim)) or not t.is_contiguous():
-        raise TypeError(f"summary: a contiguous uint8 tensor {(cache.n_blocks, cache.heads, 2, row(cache.head_dim))} is wanted")
-    if not _on(t, cache.device):
-        raise TypeError("summary: a tensor on the cache's GPU is wanted")
-    return t.data_ptr()
+    return _args.summary(t, cache.n_blocks, cache.heads, row(cache.head_dim), cache.device)
 
 
 def summarise(cache: Cache, blocks, lens, summary, starts=None, max_new: int = 1, stream=None) -> None:
     """us_kv_summarise: the extremes of the keys of the blocks that the sequences' last tokens are in, after append."""
-    _check("us_kv_summarise", lib().us_kv_summarise(cache._there, _seqs(blocks, lens, starts, max_new, cache.device),
+    L = lib()
+    _check("us_kv_summarise", L.us_kv_summarise(cache._there, _seqs(blocks, lens, starts, max_new, cache.device),
                                                     _summary(summary, cache), _stream(stream, cache)))
-
-
-def _chosen(t, tokens, cache):
-    """Address of a (tokens, heads, top) table of blocks, and top."""
-    if t.dtype is not _I32 or t.dim() != 3 or t.shape[:2] != (tokens, cache.heads) or not t.is_contiguous():
-        raise TypeError(f"chosen: a contiguous int32 tensor ({tokens}, {cache.heads}, blocks) is wanted")
-    if not _on(t, cache.device):
-        raise TypeError("chosen: a tensor on the cache's GPU is wanted")
-    return t.data_ptr(), t.shape[2]
 
 
 def choose_workspace(cache: Cache, blocks, chosen, starts=None, max_q: int = 1):
@@ -463,11 +451,12 @@ def choose(cache: Cache, summary, blocks, lens, q, scores, chosen, starts=None, 
            recent: int = 1, ws=None, stream=None) -> None:
     """us_kv_choose: for every row of q and cache head, the first `sinks`, the last `recent` and else the blocks of
     highest possible score, ascending, then -1: chosen (tokens, heads, top); the scores of all: (tokens, heads, blocks)."""
-    tokens, heads, on = q.shape[0], q.shape[1], cache.device
-    at, top = _chosen(chosen, tokens, cache)
-    at_scores, stride = _weights(scores, tokens, cache.heads, "scores", on)
+    L, on = lib(), cache.device
+    tokens, heads, _ = q.shape
+    at, top = _args.ints(chosen, tokens, cache.heads, "chosen", on)
+    at_scores, stride = _args.floats(scores, tokens, cache.heads, "scores", on)
     at_ws, n = _workspace(ws, on)
-    _check("us_kv_choose", lib().us_kv_choose(
+    _check("us_kv_choose", L.us_kv_choose(
         cache._there, _seqs(blocks, lens, starts, max_q, on), _summary(summary, cache), heads,
         _rows(q, heads, cache.head_dim, "q", on), _pack_choice(at_scores, stride, at, top, sinks, recent, max_len or 0), at_ws, n,
         _stream(stream, cache)))
@@ -484,9 +473,10 @@ def attend_chosen_workspace(cache: Cache, q, blocks, chosen, starts=None, max_q:
 def attend_chosen(cache: Cache, blocks, lens, q, out, chosen, starts=None, max_q: int = 1, scale=None, ws=None,
                   stream=None) -> None:
     """us_kv_attend_chosen: attend over the blocks chosen[t, h] alone, for row t and cache head h."""
-    heads, d, on = q.shape[1], cache.head_dim, cache.device
-    at, top = _chosen(chosen, q.shape[0], cache)
+    L, d, on = lib(), cache.head_dim, cache.device
+    tokens, heads, _ = q.shape
+    at, top = _args.ints(chosen, tokens, cache.heads, "chosen", on)
     at_ws, n = _workspace(ws, on)
-    _check("us_kv_attend_chosen", lib().us_kv_attend_chosen(
+    _check("us_kv_attend_chosen", L.us_kv_attend_chosen(
         cache._there, _seqs(blocks, lens, starts, max_q, on), heads, _rows(q, heads, d, "q", on), _rows(out, heads, d, "out", on),
-        at, top, _opts(scale, True, 0, None, None, blocks.shape[0], cache.heads, on), at_ws, n, _stream(stream, cache)))
+        at, top, None if scale is None else _pack_opts(scale, 1, 0, 0, 0, 0), at_ws, n, _stream(stream, cache)))
