@@ -93,15 +93,22 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     __asm__ volatile("" ::: "memory");
     const int count = __builtin_amdgcn_readfirstlane(min(found, kDecodeRows));
     if (count == 0) return;
-    int rows = 0;
-    for (int f = 0; f < count; ++f) rows += list[f].rows;
-    rows = __builtin_amdgcn_readfirstlane(rows);
+    // The units' rows after each other.
+    __shared__ int all_rows, where[kDecodeRows * kDecodeRows];
+    if (tid < count) {
+        int at = 0;
+        for (int f = 0; f < tid; ++f) at += list[f].rows;
+        for (int i = 0; i < list[tid].rows; ++i) where[at + i] = tid << 8 | i;
+        if (tid == count - 1) all_rows = at + list[tid].rows;
+    }
+    __syncthreads();
     const int one = (more.own.rows * (R + 2) + 3) / 4 * 4, one_pre = (a.sp.rows * (R + 2) + 3) / 4 * 4;
-    // A quad of a row's values per thread, or, where units are small and parts many, per `runs` of them, which
-    // take every runs-th partial row: how many is the same for all workgroups of the call, and with it the order
-    // of the sums. (6 sequences of 4 rows with up to 10 parts: 13.1 us with one, 20.5 with four.)
-    const int items = rows * (R / 4), unit_items = more.own.rows * (R / 4);
-    const int runs = more.own.splits + a.sp.splits < 32 || unit_items > 128 ? 1 : unit_items > 64 ? 2 : unit_items > 32 ? 4 : 8;
+    // A quad of a row's values per thread, or, where groups have few rows and parts are many, per `runs` of them,
+    // which take every runs-th partial row: how many is the same for all workgroups of the call, and with it the
+    // order of the sums. (A pass over the rows costs 2 us, eight partial rows more 1 us: 16 sequences of a row each
+    // with 54 parts took 41 us with eight.)
+    const int items = all_rows * (R / 4), tile_items = a.sp.rows * (R / 4);
+    const int runs = a.sp.splits < 16 || tile_items > 64 ? 1 : tile_items > 32 ? 4 : 8;
     const int pass = kThreads / runs, run = tid / pass;
     const int64_t splits = (int64_t)a.sp.splits * one_pre;
     constexpr int kAhead = 8;                              // partial rows on their way
@@ -109,10 +116,8 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
     for (int base = 0; base < items; base += pass) {
         const int it = base + tid - run * pass;
         const bool here = it < items;
-        int rr = here ? it / (R / 4) : 0, f = 0;
-        const int quad = it % (R / 4);
-        for (; rr >= list[f].rows; ++f) rr -= list[f].rows;
-        const Unit x = list[f];
+        const int place = where[here ? it / (R / 4) : 0], rr = place & 255, quad = it % (R / 4);
+        const Unit x = list[place >> 8];
         float m = -INFINITY, l = 0.0f;
         f32x4 y = {0, 0, 0, 0};
         const auto add = [&](float mz, float lz, f32x4 part) {

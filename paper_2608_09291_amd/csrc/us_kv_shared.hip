@@ -123,6 +123,13 @@ us_status shared_plan(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, in
     us_status st = plan_of(c, all, q_heads, tokens, f32, first, p.pre);
     if (st == US_OK) st = plan_of(c, s, q_heads, tokens, f32, o, p.own);
     if (st != US_OK) return st;
+    // Of few rows at most 16 parts, as long as these stay below 64 blocks: a join passes over all of them. (One
+    // group of 6 sequences, 4 heads over 1, 11456 common tokens, with 45 parts and 12: 27 and 22 us.)
+    const int most = (first.max_len + kBlock - 1) / kBlock, chunk = (most + 15) / 16;
+    if (p.pre.decode && p.own.decode && p.pre.chunk < chunk) {
+        p.pre.chunk = chunk < 64 ? chunk : 64;
+        p.pre.splits = (most + p.pre.chunk - 1) / p.pre.chunk;
+    }
     const int64_t pre = (int64_t)g.groups * c.heads, own = (int64_t)s.batch * c.heads;
     p.pre_groups = pre * p.pre.tiles * p.pre.splits;
     p.own_groups = own * p.own.tiles * p.own.splits;
