@@ -288,6 +288,7 @@ SHARED = [  # group sizes, blocks in common, own tokens of each sequence, querie
     ([40], [9], [7 + i for i in range(40)], [1] * 40, 16, 2, 128), ([3, 4], [4, 2], [9, 20, 4, 100, 70, 3, 8], [3, 1, 4, 0, 2, 3, 5], 6, 2, 64),
     ([2], [3], [150, 90], [150, 90], 4, 2, 128), ([9], [5], [33] * 9, [30] * 9, 5, 1, 192), ([3], [6], [11, 12, 80], [2] * 3, 24, 1, 256),
     ([70, 30], [11, 3], [3] * 100, [1] * 100, 4, 1, 64), ([2, 2], [200, 3], [30, 900, 2000, 1], [1] * 4, 8, 2, 128),
+    ([2], [1100], [30, 1], [1, 1], 1, 1, 64), ([3], [1050], [2, 70, 9], [1] * 3, 1, 1, 64), ([5], [4], [9] * 5, [1, 0, 0, 1, 1], 2, 1, 13),
 ]
 
 
@@ -651,3 +652,242 @@ def test_scores_are_no_less_than_any_key_gives(torch_cuda):
         x = (c * s[:, None]) @ q[0, 3 * h:3 * h + 3].double().cpu().numpy().T
         for i in range(20):
             assert scores[0, h, i].item() >= x[64 * i:64 * i + 64].max() * (1 - 2.0 ** -20)
+
+
+# --- the calls together, elsewhere, and far away -----------------------------------------
+
+def _step_state(torch, B, n_blocks, width, H, Hk, D, top):
+    ints = dict(dtype=torch.int32, device="cuda")
+    c = kv.new_cache(n_blocks, Hk, D)
+    s = dict(cache=c, summary=kv.new_summary(c), tables=[torch.full((B, width), -1, **ints) for _ in range(2)],
+             lens=[torch.zeros(B, **ints) for _ in range(2)], refs=torch.zeros(n_blocks, **ints), missing=torch.zeros(1, **ints),
+             scores=torch.zeros((B, Hk, width), device="cuda"), chosen=torch.zeros((B, Hk, top), **ints))
+    s["out"], s["part"] = (torch.zeros((B, H, D), device="cuda") for _ in range(2))
+    s["fork"] = kv.fork_workspace(c, *s["tables"])
+    return s
+
+
+def test_a_step_of_all_calls_captured(torch_cuda):
+    """Fork, rotate, append, summarise, shared and sparse attention in one graph on another stream, replayed over growing
+    sequences: bit for bit what the same calls give eagerly, with workspaces that are left as they were found."""
+    torch = torch_cuda
+    announce("kv step of all calls captured")
+    rng = np.random.default_rng(12)
+    B, H, Hk, D, width, top = 5, 8, 2, 64, 8, 3
+    ints = dict(dtype=torch.int32, device="cuda")
+    both = [_step_state(torch, B, 80, width, H, Hk, D, top) for _ in range(2)]
+    y = torch.zeros((B, H + 2 * Hk, D), device="cuda")
+    parents, room = torch.arange(B, **ints), torch.ones(B, **ints)
+    groups, shared = torch.tensor([0, 3, 5], **ints), torch.zeros(2, **ints)
+    freq = torch.rand(32, device="cuda")
+    for s in both:
+        q = y[:, :H]
+        s["ws"] = [kv.attend_shared_workspace(s["cache"], q, s["tables"][0], groups, max_group=3),
+                   kv.choose_workspace(s["cache"], s["tables"][0], s["chosen"]),
+                   kv.attend_chosen_workspace(s["cache"], q, s["tables"][0], s["chosen"])]
+
+    def step(s, a):
+        c, t, n = s["cache"], s["tables"][1 - a], s["lens"][1 - a]
+        kv.fork(c, s["refs"], s["tables"][a], s["lens"][a], parents, t, n, s["missing"], room=room, ws=s["fork"])
+        n.add_(1)
+        z = y.clone()
+        q, k, v = z[:, :H], z[:, H:H + Hk], z[:, H + Hk:]
+        kv.rotate(q, k, freq, n, offset=-1, norm=True)
+        kv.append(c, t, n, k, v)
+        kv.summarise(c, t, n, s["summary"])
+        kv.attend_shared(c, t, n, q, s["out"], groups, shared, max_group=3, ws=s["ws"][0])
+        kv.choose(c, s["summary"], t, n, q, s["scores"], s["chosen"], ws=s["ws"][1])
+        kv.attend_chosen(c, t, n, q, s["part"], s["chosen"], ws=s["ws"][2])
+
+    torch.cuda.synchronize()
+    graphs, stream = [torch.cuda.CUDAGraph() for _ in range(2)], torch.cuda.Stream()
+    for a in range(2):
+        with torch.cuda.graph(graphs[a], stream=stream):
+            step(both[0], a)
+    for i in range(140):
+        if i == 100:                                        # the first three go on from one, and have its full block in common
+            parents.copy_(torch.tensor([1, 1, 1, 3, 4], dtype=torch.int32))
+            shared.copy_(torch.tensor([1, 0], dtype=torch.int32))
+        elif i == 101:
+            parents.copy_(torch.arange(B, dtype=torch.int32))
+        y.copy_(torch.from_numpy(rng.normal(0, 1, size=y.shape).astype(np.float32)))
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(both[1], i % 2)
+        torch.cuda.synchronize()
+        for name in ("out", "part", "chosen", "scores", "refs", "missing", "summary"):
+            assert torch.equal(both[0][name], both[1][name]), (i, name)
+    assert both[0]["missing"].item() == 0 and both[0]["lens"][i % 2 ^ 1].tolist() == [140] * B
+    assert (both[0]["tables"][i % 2 ^ 1][:3, 0] == both[0]["tables"][i % 2 ^ 1][0, 0]).all()
+    # blocks chosen: all three of 140 tokens, so both attentions are the same but for rounding
+    assert (both[0]["out"] - both[0]["part"]).abs().max() < 1e-5 * both[0]["out"].abs().max()
+
+
+def test_calls_refuse_another_gpu(torch_cuda, monkeypatch):
+    """All of a call is on the cache's GPU, and that is the current one. (The cache's number is changed: one GPU will do.)"""
+    torch = torch_cuda
+    announce("kv calls on another GPU")
+    c = kv.new_cache(4, 2, 80)
+    here = torch.cuda.current_device()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    blocks, lens, chosen = torch.zeros((3, 2), **i32), torch.zeros(3, **i32), torch.zeros((3, 2, 2), **i32)
+    x, scores, one, summary = torch.zeros((3, 2, 80), device="cuda"), torch.zeros((3, 2, 2), device="cuda"), torch.zeros(1, **i32), kv.new_summary(c)
+    ws, groups = torch.zeros(1 << 16, **i32), torch.zeros(2, **i32)
+    freq = torch.rand(40, device="cuda")
+    calls = (lambda **a: kv.fork(c, torch.zeros(4, **i32), blocks, lens, None, blocks.clone(), lens.clone(), one, ws=ws, **a),
+             lambda **a: kv.attend_shared(c, blocks, lens, x, x.clone(), groups, one, ws=ws, **a),
+             lambda **a: kv.summarise(c, blocks, lens, summary, **a),
+             lambda **a: kv.choose(c, summary, blocks, lens, x, scores, chosen, ws=ws, **a),
+             lambda **a: kv.attend_chosen(c, blocks, lens, x, x.clone(), chosen, ws=ws, **a),
+             lambda **a: kv.rotate(x, x.clone(), freq, lens, **a))
+
+    class Elsewhere:
+        cuda_stream, device = 0, torch.device("cuda", here + 1)
+
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(stream=Elsewhere)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: here + 1)
+        for call in calls:
+            with pytest.raises(ValueError):
+                call()
+    c.device = here + 1
+    for call in calls[:-1]:
+        with pytest.raises(TypeError):
+            call()
+    c.device = here
+    for call in calls:                                      # (lengths of 0: nothing is stored)
+        call()
+        call(stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+
+
+def test_binding_refuses_tensors(torch_cuda):
+    torch = torch_cuda
+    announce("kv binding refusals")
+    c = kv.new_cache(4, 2, 80)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    blocks, lens, one, ws = torch.zeros((3, 2), **i32), torch.zeros(3, **i32), torch.zeros(1, **i32), torch.zeros(1 << 16, **i32)
+    x, summary = torch.zeros((3, 2, 80), device="cuda"), kv.new_summary(c)
+    scores, chosen, groups = torch.zeros((3, 2, 2), device="cuda"), torch.zeros((3, 2, 2), **i32), torch.zeros(2, **i32)
+    freq, pos = torch.zeros((2, 40), device="cuda"), torch.zeros((2, 3), **i32)
+
+    def refused(call, good, bad):
+        call(**good)
+        for name, value in bad:
+            with pytest.raises((TypeError, ValueError, RuntimeError)):
+                call(**{**good, name: value})
+
+    refused(kv.rotate, dict(q=x, k=x.clone(), freq=freq, positions=pos),
+            [("freq", freq.double()), ("freq", freq[:, ::2]), ("freq", freq[0]), ("freq", torch.zeros((2, 41), device="cuda")), ("freq", None),
+             ("positions", pos.long()), ("positions", pos[:, :2]), ("positions", pos[0]), ("positions", pos.t().contiguous().t()),
+             ("positions", pos.cpu()), ("q", x.cpu()), ("q", x.double()), ("k", x[:2].clone()), ("k", x.half()), ("q_weight", x[0, 0]),
+             ("k_out", x[..., :79]), ("q_out", x.half())])
+    refused(kv.rotate, dict(q=x, k=None, freq=None, positions=None, norm=True, q_weight=x[0, 0]),
+            [("q_weight", x[0, 0, :79]), ("q_weight", x[0, 0].half()), ("q_weight", x[0, 0].cpu()), ("k_out", x), ("eps", 0.0), ("norm", False)])
+    refused(kv.fork, dict(cache=c, refs=torch.zeros(4, **i32), blocks=blocks, lens=lens, parents=lens, to_blocks=blocks.clone(),
+                          to_lens=lens.clone(), missing=one, room=lens, ws=ws),
+            [("refs", torch.zeros(3, **i32)), ("refs", torch.zeros(4, device="cuda")), ("parents", lens[:2]), ("parents", lens.long()),
+             ("to_blocks", blocks), ("to_lens", lens), ("to_lens", lens[:2]), ("to_blocks", blocks[:, :1].clone()), ("room", lens.cpu()),
+             ("missing", lens), ("ws", None), ("ws", ws[:8]), ("ws", ws.cpu()), ("to_blocks", blocks.long())])
+    refused(kv.attend_shared, dict(cache=c, blocks=blocks, lens=lens, q=x, out=x.clone(), group_starts=groups, shared=one, ws=ws),
+            [("shared", lens), ("shared", one.long()), ("group_starts", one), ("group_starts", groups.cpu()), ("ws", None), ("max_group", 70000),
+             ("max_shared", 3), ("scale", math.nan), ("out", x.half()), ("q", x[:, :1])])
+    refused(kv.summarise, dict(cache=c, blocks=blocks, lens=lens, summary=summary), [("summary", summary[:3]), ("summary", summary.cpu())])
+    refused(kv.choose, dict(cache=c, summary=summary, blocks=blocks, lens=lens, q=x, scores=scores, chosen=chosen, ws=ws),
+            [("summary", summary[..., :80]), ("scores", scores[..., :1].clone()), ("scores", scores.half()), ("chosen", chosen[:2]),
+             ("chosen", chosen.long()), ("sinks", 3), ("recent", -1), ("ws", None), ("q", x[:2]), ("scores", scores.cpu())])
+    refused(kv.attend_chosen, dict(cache=c, blocks=blocks, lens=lens, q=x, out=x.clone(), chosen=chosen),
+            [("chosen", chosen[:, :1]), ("chosen", chosen.float()), ("chosen", chosen.cpu()), ("out", x[:2]), ("scale", -1.0)])
+    torch.cuda.synchronize()
+
+
+def test_blocks_and_rows_past_32_bits(torch_cuda):
+    """Blocks and rows that lie more than 2^32 bytes into their arrays."""
+    torch = torch_cuda
+    announce("kv calls past 32 bits")
+    n_blocks, Hk, D = 70000, 8, 128                         # 4.6 GB of keys
+    cache = kv.Cache(*[torch.empty((n_blocks, Hk, 64 * D), dtype=torch.uint8, device="cuda") for _ in range(2)],
+                     *[torch.zeros((n_blocks, Hk), device="cuda") for _ in range(2)], D)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    stride = (1 << 31) // 64                                # rows 32 M elements apart: the last ones past 2^31
+    far = torch.empty(201 * stride, dtype=torch.float16, device="cuda")
+    rows = far.as_strided((200, Hk, D), (stride, D, 1))
+    rows.copy_(torch.randn((200, Hk, D), generator=g, device="cuda"))
+    near = rows.clone()
+    freq, pos = torch.rand(64, device="cuda"), torch.arange(200, **i32)
+    kv.rotate(rows, None, freq, pos, norm=True)
+    kv.rotate(near, None, freq, pos, norm=True)
+    assert torch.equal(rows, near)
+    a, b = n_blocks - 1, n_blocks - 3
+    blocks, lens, st = torch.tensor([[a, b, 7, n_blocks - 9]], **i32), torch.tensor([200], **i32), torch.tensor([0, 200], **i32)
+    kv.append(cache, blocks, lens, near, near, starts=st, max_new=200)
+    # two that go on: the second one's started block is a copy, past 2^32 bytes as well
+    refs = torch.ones(n_blocks, **i32)
+    refs[n_blocks - 20] = 0
+    to, to_lens, missing = torch.empty((2, 4), **i32), torch.empty(2, **i32), torch.empty(1, **i32)
+    kv.fork(cache, refs, blocks, lens, torch.zeros(2, **i32), to, to_lens, missing, ws=kv.fork_workspace(cache, blocks, to))
+    assert to.tolist() == [[a, b, 7, n_blocks - 9], [a, b, 7, n_blocks - 20]] and missing.item() == 0
+    summary = kv.new_summary(cache)
+    kv.summarise(cache, to, to_lens, summary, starts=torch.tensor([0, 200, 400], **i32), max_new=200)
+    q = near[:2].contiguous()
+    scores, chosen = torch.empty((2, Hk, 4), device="cuda"), torch.empty((2, Hk, 4), **i32)
+    kv.choose(cache, summary, to, to_lens, q, scores, chosen, ws=kv.choose_workspace(cache, to, chosen))
+    assert (chosen == torch.arange(4, device="cuda")).all()
+    outs = [torch.empty_like(q) for _ in range(3)]
+    groups, shared = torch.tensor([0, 2], **i32), torch.tensor([3], **i32)
+    kv.attend(cache, to, to_lens, q, outs[0], ws=kv.attend_workspace(cache, q, to))
+    kv.attend_chosen(cache, to, to_lens, q, outs[1], chosen, ws=kv.attend_chosen_workspace(cache, q, to, chosen))
+    kv.attend_shared(cache, to, to_lens, q, outs[2], groups, shared, ws=kv.attend_shared_workspace(cache, q, to, groups))
+    x = near.double().permute(1, 2, 0).contiguous()
+    s = torch.bmm(q.double().permute(1, 0, 2).contiguous(), x)
+    # a block's score is no less than any of its keys gives, whose values are stored to half a step, 5 / 254 at most
+    most = torch.stack([part.amax(-1) for part in s.split(64, -1)], -1).permute(1, 0, 2)
+    assert (scores.double() >= most - q.double().abs().sum(-1, keepdim=True) * 5 / 254).all() and (scores < 8 * most.max()).all()
+    s /= math.sqrt(D)
+    want = torch.bmm(torch.softmax(s, -1), x.transpose(1, 2).contiguous()).permute(1, 0, 2)
+    for out in outs:
+        # keys and values off by half a step (at most 5 / 254) each, and rounding: a wrong row would be off by about 1
+        assert (out.double() - want).abs().max() < 0.25 and (out.double() - want).square().mean().sqrt() < 0.02
+        assert (out.double() - outs[0].double()).abs().max() < 2.0 ** -9 * want.abs().max()
+
+
+def test_workspace_of_sparse_attention_serves_attend(torch_cuda):
+    """One zero-filled workspace for both in turn."""
+    torch = torch_cuda
+    announce("kv workspace of both")
+    rng = np.random.default_rng(13)
+    lens = [3000, 2500]
+    p = Pool(torch, rng, lens, 2, 64)
+    cache, q = p.cache(), torch.randn((2, 8, 64), device="cuda")
+    chosen = torch.arange(40, dtype=torch.int32, device="cuda").expand(2, 2, 40).contiguous()
+    sizes = [w.numel() for w in (kv.attend_workspace(cache, q, p.dev(p.blocks)), kv.attend_chosen_workspace(cache, q, p.dev(p.blocks), chosen))]
+    assert min(sizes) > 0
+    ws, got = torch.zeros(max(sizes), dtype=torch.int32, device="cuda"), []
+    for _ in range(3):
+        for call in (lambda o: kv.attend(cache, p.dev(p.blocks), p.dev(lens), q, o, ws=ws),
+                     lambda o: kv.attend_chosen(cache, p.dev(p.blocks), p.dev(lens), q, o, chosen, ws=ws)):
+            got.append(torch.empty_like(q))
+            call(got[-1])
+    torch.cuda.synchronize()
+    _check(torch, p, lens, [1, 1], q, got[0], "f32")
+    assert all(torch.equal(got[i], got[i % 2]) for i in range(6))
+    _check(torch, p, [40 * 64, 2500], [1, 1], q, got[1], "f32", causal=False)
+
+
+def test_example_of_samples(torch_cuda):
+    """The operators together: samples of one prompt over a cache that they share."""
+    import importlib.util
+    import os
+    announce("kv samples example")
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "kv_samples.py")
+    spec = importlib.util.spec_from_file_location("kv_samples", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    off, less, used = m.main(["--samples", "5", "--prompt", "300", "--tokens", "70", "--blocks", "6"])
+    # both off by their scores, 72 * 2^-24 of about 10 each, and probabilities by twice that
+    assert off < 2.0 ** -12 and less < 1
+    assert used < 5 * 6                                     # (5 x 370 tokens would take 30 blocks)
