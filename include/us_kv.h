@@ -238,6 +238,8 @@ typedef struct {
  * Angles are taken in 64 bits, the rest in float32, rounded once. q_out may be q
  * and k_out may be k, with the same strides; otherwise they overlap nothing. All
  * rows have one type and number. k = k_out = NULL with k_heads = 0: queries alone.
+ * US_ERR_SHAPE for more than 2^23 times as many rows as a workgroup takes together
+ * (one, at least).
  */
 us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head_dim, const us_rows *q, const us_rows *q_out,
                        const us_rows *k, const us_rows *k_out, const us_kv_rotation *how, void *stream);
@@ -269,8 +271,9 @@ typedef struct {
  * stay as they are and count on; else missing is 0.
  * A started block that is not there stays so. Only the blocks of seqs count:
  * its starts and max_new are not looked at.
- * ws: us_kv_fork_workspace_size bytes, as us_kv_attend's. US_ERR_SHAPE for more
- * than 32767 heads.
+ * ws: us_kv_fork_workspace_size bytes, 16-byte aligned, zero-filled before its
+ * first use; not one that other calls use, nor calls that may overlap.
+ * US_ERR_SHAPE for more than 32767 heads.
  */
 us_status us_kv_fork_workspace_size(const us_kv_cache *cache, int32_t batch, int32_t to_batch, size_t *bytes);
 us_status us_kv_fork(const us_kv_cache *cache, int32_t *refs, const us_kv_seqs *seqs, const int32_t *parents,
@@ -295,9 +298,10 @@ typedef struct {
  * the common blocks, and results are off by as much. Sequences past max_group
  * in a group count as sequences of none. opts->window has to be 0 and
  * opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, as
- * us_kv_attend's. US_ERR_SHAPE as us_kv_attend, for groups as for sequences (for
- * more than 2^25 query rows of a group and cache head), and for more than 2^22
- * workgroups of either part.
+ * us_kv_attend's, and one workspace serves both in turn. US_ERR_SHAPE as
+ * us_kv_attend, for groups as for sequences (for more than 2^25 query rows of a
+ * group and cache head), for more than 2^25 rows of a sequence and all heads, and
+ * for more than 2^22 workgroups over the common keys or the others.
  */
 us_status us_kv_attend_shared_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                              int32_t tokens, const us_kv_groups *groups, const us_kv_attend_opts *opts,
@@ -339,7 +343,8 @@ typedef struct {
  * scores: the earlier one; a NaN counts as the smallest). Blocks that are not
  * there are not chosen. scores gets the scores of the blocks that a row looks
  * at (-infinity for one that is not there). Rows that are none of the sequences'
- * are left as they were. ws: us_kv_choose_workspace_size bytes, as us_kv_attend's.
+ * are left as they were. ws: us_kv_choose_workspace_size bytes, zero-filled
+ * before its first use and left so; not one that other calls use.
  * US_ERR_SHAPE for more than 65535 rows.
  */
 us_status us_kv_choose_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t tokens, int32_t top,
@@ -354,8 +359,8 @@ us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *seqs, const u
  * up to that position count for nothing, a number that is there twice counts
  * twice. Rows without any key get zeros. For single tokens and a few drafted
  * ones: a row's blocks are read for it alone. opts: causal, without window and
- * weights. ws: us_kv_attend_chosen_workspace_size bytes, as us_kv_attend's; one
- * zero-filled workspace serves both in turn. US_ERR_SHAPE for more than 65535 rows.
+ * weights. ws: us_kv_attend_chosen_workspace_size bytes, as us_kv_attend's, and
+ * one workspace serves both in turn. US_ERR_SHAPE for more than 65535 rows.
  */
 us_status us_kv_attend_chosen_workspace_size(const us_kv_cache *cache, const us_kv_seqs *seqs, int32_t q_heads,
                                              int32_t tokens, int32_t top, size_t *bytes);

@@ -238,6 +238,10 @@ __device__ inline int64_t row_block(const Args &a, int hk, int b, int r0, int ro
     return hk * a.sp.row_blocks + (int64_t)r0 * a.G / 32 + b + row / 32;
 }
 
+// The tickets, which have to be zero between calls, have a place of their own at
+// a workspace's start, that no other part of any attention call takes.
+constexpr int64_t kTickets = 16384;
+
 // What an attention call launches, and where its parts of the workspace lie (bytes).
 struct Plan {
     bool decode;

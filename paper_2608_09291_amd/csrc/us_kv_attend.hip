@@ -12,9 +12,7 @@ using namespace us_kv;
 constexpr us_kv_attend_opts kDefault = {0.0f, 1, 0, 0, nullptr, 0};
 
 // What a call launches, and where its parts of the workspace lie (bytes).
-// The tickets, which have to be zero between calls, have a place of their own
-// that no other part of any call takes; calls of more units do not split.
-constexpr int64_t kTickets = 16384;
+// (Calls of more units than there are tickets do not split.)
 // Workgroups of the prompt kernel, whose grid has one dimension of 512 threads each.
 constexpr int64_t kMostPrompt = INT32_MAX / 512;
 

@@ -16,7 +16,6 @@ __global__ __launch_bounds__(kDecodeThreads, NT > 4 ? 1 : 2) void us_kv_chosen_k
 }
 
 constexpr us_kv_attend_opts kDefault = {0.0f, 1, 0, 0, nullptr, 0};
-constexpr int64_t kTickets = 16384;                        // as us_kv_attend's, so that one workspace serves both
 
 struct ChosenPlan {
     int chunk, splits, tiles, rows;

@@ -9,7 +9,8 @@
 // (us_kv_decode.h, us_kv_prompt.h) and leave partial rows. Where both have few
 // rows, one launch does it all: the last workgroup that leaves some of a unit's
 // joins them. Common keys of many rows have a launch of their own ahead of it. Where
-// the sequences themselves have many rows, a third one joins.
+// the sequences themselves have many rows, or there are more units than tickets, a
+// third one joins.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -84,6 +85,7 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
 struct SharedPlan {
     Plan pre, own;
     int64_t pre_groups, own_groups;                        // workgroups of either part
+    bool inside;                                           // these join
     size_t pre_part, own_part, total;                      // bytes; the tickets lie at 0
 };
 
@@ -104,7 +106,8 @@ us_status check_shared(const us_kv_cache *c, const us_kv_seqs *s, int q_heads, i
     if (tokens < 1 || g->groups < 1 || g->groups > 65535 || g->max_group < 1 || g->max_group > 65535 || g->max_shared < 0 ||
         g->max_shared > s->width)
         return US_ERR_SHAPE;
-    return (int64_t)g->max_group * s->max_new > US_KV_NEW_MAX ? US_ERR_SHAPE : US_OK;
+    // (rows of a group; of a sequence with all heads, which the join has in one dimension of its grid)
+    return (int64_t)g->max_group * s->max_new > US_KV_NEW_MAX || (int64_t)s->max_new * q_heads > US_KV_NEW_MAX ? US_ERR_SHAPE : US_OK;
 }
 
 // max_shared == 0: as wide as the table.
@@ -135,7 +138,8 @@ us_status shared_plan(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, in
     p.own_groups = own * p.own.tiles * p.own.splits;
     // (in one dimension, of fewer than 2^32 threads)
     if (p.pre_groups > kMost || p.own_groups > kMost) return US_ERR_SHAPE;
-    p.pre_part = p.own.decode ? (size_t)up(own * p.own.tiles * 4, 16) : 0;
+    p.inside = p.own.decode && own * p.own.tiles <= kTickets;
+    p.pre_part = 4 * kTickets;                             // (also where this call draws none)
     p.own_part = p.pre_part + part_bytes(p.pre, pre, R);
     p.total = p.own_part + part_bytes(p.own, own, R);
     return US_OK;
@@ -225,17 +229,16 @@ extern "C" us_status us_kv_attend_shared(const us_kv_cache *cache, const us_kv_s
             hipError_t e = hipSuccess;
             if (!p.pre.decode) e = launch_many<kShared, NT, DT>(a, more, p.pre_groups, hs);
             if (e != hipSuccess) return e;
-            if (p.own.decode) {
-                more.inside = 1;
-                more.pre_groups = p.pre.decode ? (int)p.pre_groups : 0;
-                return launch_few<NT, DT>(a, more, more.pre_groups + p.own_groups, hs);
+            more.inside = p.inside;
+            more.pre_groups = p.pre.decode ? (int)p.pre_groups : 0;
+            const int64_t few = more.pre_groups + (p.own.decode ? p.own_groups : 0);
+            if (few) e = launch_few<NT, DT>(a, more, few, hs);
+            if (e != hipSuccess || p.inside) return e;
+            if (!p.own.decode) {
+                a.sp = more.own;
+                e = launch_many<kRest, NT, DT>(a, more, p.own_groups, hs);
+                if (e != hipSuccess) return e;
             }
-            more.pre_groups = (int)p.pre_groups;
-            if (p.pre.decode) e = launch_few<NT, DT>(a, more, p.pre_groups, hs);
-            if (e != hipSuccess) return e;
-            a.sp = more.own;
-            e = launch_many<kRest, NT, DT>(a, more, p.own_groups, hs);
-            if (e != hipSuccess) return e;
             const Parts pre{first, p.pre.chunk, p.pre.splits, p.pre.tiles, p.pre.rows};
             const Parts own{second, p.own.chunk, p.own.splits, p.own.tiles, p.own.rows};
             const unsigned x = (unsigned)(((int64_t)seqs->max_new * q_heads + kEach - 1) / kEach);

@@ -878,6 +878,70 @@ def test_workspace_of_sparse_attention_serves_attend(torch_cuda):
     _check(torch, p, [40 * 64, 2500], [1, 1], q, got[1], "f32", causal=False)
 
 
+def test_workspace_of_shared_attention_serves_other_sizes(torch_cuda):
+    """One zero-filled workspace, as large as the largest call asks for, for calls of few and many units and for attend."""
+    torch = torch_cuda
+    announce("kv shared workspace of other sizes")
+    rng = np.random.default_rng(14)
+    calls = []
+    for sizes, common, own, new, H, Hk in (([3], [2], [9, 30, 64], 1, 4, 2), ([90, 20], [3, 1], [5] * 110, 1, 8, 2), ([2], [5], [70, 90], 60, 4, 2),
+                                           ([40], [30], [7] * 40, 1, 16, 1)):
+        p = Groups(torch, rng, sizes, common, own, Hk, 64)
+        T, B = len(own) * new, len(own)
+        q = torch.from_numpy(rng.normal(0, 1.5, size=(T, H, 64)).astype(np.float32)).cuda()
+        args = dict(starts=p.dev([i * new for i in range(B + 1)]), max_q=new, max_group=max(sizes), max_shared=max(common))
+        calls.append((p, p.cache(), q, p.dev(_starts(sizes)), p.dev(common), new, args))
+    need = [kv.attend_shared_workspace(c, q, p.dev(p.blocks), g, **args).numel() for p, c, q, g, _, _, args in calls]
+    ws = torch.zeros(max(need), dtype=torch.int32, device="cuda")
+    for turn in range(3):
+        for p, c, q, g, s, new, args in calls[::-1] if turn == 1 else calls:
+            out = torch.full_like(q, math.nan)
+            kv.attend_shared(c, p.dev(p.blocks), p.dev(p.lens_), q, out, g, s, ws=ws, **args)
+            torch.cuda.synchronize()
+            _check(torch, p, p.lens_, [new] * len(p.lens_), q, out, "f32")
+            kv.attend(c, p.dev(p.blocks), p.dev(p.lens_), q, out, starts=args["starts"], max_q=new, ws=ws)
+            torch.cuda.synchronize()
+            _check(torch, p, p.lens_, [new] * len(p.lens_), q, out, "f32")
+
+
+def test_attend_shared_of_more_units_than_tickets(torch_cuda):
+    """2100 sequences of 8 heads: a kernel of its own joins."""
+    torch = torch_cuda
+    announce("kv shared many units")
+    rng = np.random.default_rng(15)
+    B, H, Hk, D = 2100, 8, 8, 64
+    cache = kv.new_cache(10, Hk, D)
+    for x in (cache.k, cache.v):
+        x.copy_(torch.from_numpy(rng.integers(1, 256, size=tuple(x.shape), dtype=np.uint8)))
+    for x in (cache.k_scale, cache.v_scale):
+        x.copy_(torch.from_numpy(rng.uniform(0.005, 0.02, size=tuple(x.shape)).astype(np.float32)))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    own = torch.from_numpy(rng.integers(5, 10, size=(B, 1)).astype(np.int32)).cuda()
+    blocks = torch.cat((torch.arange(5, **i32).expand(B, 5), own), 1).contiguous()
+    lens = torch.from_numpy(rng.integers(321, 385, size=B).astype(np.int32)).cuda()
+    q = torch.randn((B, H, D), device="cuda")
+    outs = [torch.empty_like(q) for _ in range(2)]
+    groups, shared = torch.tensor([0, 2000, B], **i32), torch.tensor([5, 3], **i32)
+    ws = kv.attend_shared_workspace(cache, q, blocks, groups)
+    kv.attend_shared(cache, blocks, lens, q, outs[0], groups, shared, ws=ws)
+    kv.attend(cache, blocks, lens, q, outs[1], ws=kv.attend_workspace(cache, q, blocks))
+    torch.cuda.synchronize()
+    at = [torch.from_numpy(ref.places(D, keys)).cuda() for keys in (True, False)]
+    k, v = ((x[..., p].double() - 128) * s.double()[..., None, None] for x, s, p in ((cache.k, cache.k_scale, at[0]), (cache.v, cache.v_scale, at[1])))
+    for b in (0, 1, 1999, 2000, B - 1):
+        n = int(lens[b])
+        key, val = (x[blocks[b].long()].permute(1, 0, 2, 3).reshape(Hk, -1, D)[:, :n] for x in (k, v))
+        x = (key * q[b].double()[:, None]).sum(-1) / math.sqrt(D)
+        reach = ((key * q[b].double()[:, None]).abs().sum(-1) / math.sqrt(D)).amax(-1)
+        p = torch.softmax(x, -1)[..., None]
+        want, size = (p * val).sum(1), (p * val.abs()).sum(1)
+        e = (2 * (72 * U + 2.0 ** -22) * reach[:, None] + 2.0 ** -21 + 384 * U) * size + U * want.abs()
+        for out in outs:
+            assert ((out[b].double() - want).abs() <= e).all(), b
+    # (of all others: both within their bounds)
+    assert (outs[0] - outs[1]).abs().max() < 1e-3 * outs[1].abs().max()
+
+
 def test_example_of_samples(torch_cuda):
     """The operators together: samples of one prompt over a cache that they share."""
     import importlib.util
