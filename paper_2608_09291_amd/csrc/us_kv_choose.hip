@@ -100,8 +100,15 @@ struct ChooseArgs {
     int32_t *tickets;                                      // tokens x heads
 };
 
-constexpr int kThreads = 512, kWaves = kThreads / 64, kChunk = 16 * kWaves;    // of a workgroup: blocks at a time
-constexpr int kHeld = 4096;                                // keys that stay in LDS
+// A workgroup's wavefronts, and the keys that it holds in LDS. Where no sequence has more than kFew blocks, four:
+// more workgroups fit a CU, and units are many rather than long (3 rows of 20 sequences of 58 blocks, 128 heads
+// over 32: 37.7 us a call with eight, with the summaries).
+constexpr int kFew = 128;
+template <bool FEW>
+struct Shape {
+    static constexpr int kWaves = FEW ? 4 : 8, kThreads = 64 * kWaves, kHeld = FEW ? kFew : 4096;
+    static constexpr int kChunk = 16 * kWaves;             // blocks scored at a time
+};
 
 // Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
 __device__ inline uint32_t order_of(float x) {
@@ -110,9 +117,11 @@ __device__ inline uint32_t order_of(float x) {
 }
 
 // What of a row's scores the workgroup that chooses has in LDS.
-struct Pick {
+template <bool FEW>
+struct Pick : Shape<FEW> {
+    using Shape<FEW>::kWaves, Shape<FEW>::kHeld;
     __attribute__((aligned(16))) uint32_t keys[kHeld];
-    __attribute__((aligned(16))) int hist[4][256];         // of the digits, the largest first
+    __attribute__((aligned(16))) int hist[FEW ? 1 : 4][256];                   // of the digits, the largest first
     u32x4 of_wave[kWaves];
     int counts[kWaves][2];
 };
@@ -149,7 +158,8 @@ struct Seen {
 // scores of a row have most of their first bits in common. Every wavefront follows the whole search, so that a
 // step has one barrier. key(i) is asked for places up to the next multiple of kThreads past n, where it is 0.
 template <class F>
-__device__ inline void select(F key, Seen mine, int n, int top, int *out, Pick &p) {
+__device__ inline void select(F key, Seen mine, int n, int top, int *out, Pick<false> &p) {
+    constexpr int kWaves = Shape<false>::kWaves, kThreads = Shape<false>::kThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const auto plus = [](uint32_t a, uint32_t b) { return a + b; };
     // A wavefront's places, 64 at a time.
@@ -242,8 +252,9 @@ constexpr int lanes_of(int row) { return row <= 64 ? 8 : row <= 128 ? 16 : 32; }
 
 // The same of up to kFew keys in LDS, by counting for each how many come before it: up to a hundred or so,
 // that takes less than the steps above.
-constexpr int kFew = 128;
-__device__ inline void select_few(int n, int top, int *out, Pick &p) {
+template <bool FEW>
+__device__ inline void select_few(int n, int top, int *out, Pick<FEW> &p) {
+    constexpr int kThreads = Shape<FEW>::kThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int before = 0;
     const uint32_t mine = tid < kFew ? p.keys[tid] : 0;
@@ -268,8 +279,9 @@ __device__ inline void select_few(int n, int top, int *out, Pick &p) {
     for (int i = all + tid; i < top; i += kThreads) out[i] = -1;
 }
 
-template <int NT, int DT>
-__global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
+template <int NT, int DT, bool FEW>
+__global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(ChooseArgs a) {
+    constexpr int kThreads = Shape<FEW>::kThreads, kChunk = Shape<FEW>::kChunk, kHeld = Shape<FEW>::kHeld;
     using T = typename Type<DT>::T;
     constexpr int R = 32 * NT, kSteps = 2 * R / 64;        // of 64 values of a summary
     constexpr int kLanes = lanes_of(R), kHeads = kThreads / kLanes;            // query heads that are laid out at a time
@@ -277,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     // The digits as the products' right operand: group, step, lane (column, piece of 16 values).
     __shared__ u32x4 digits[kGroups][kSteps][64];
     __shared__ double unit_of[4 * kGroups];                // a head's power of two; NaN for one that does not count
-    __shared__ Pick pick;
+    __shared__ Pick<FEW> pick;
     __shared__ int flag;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kk = lane >> 4, t = blockIdx.x, hk = blockIdx.y;
@@ -404,9 +416,7 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
     };
     const auto score_of = [&](int i) { return __hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     int *out = a.chosen + unit * a.top;
-    Seen seen;
-    const int per = (blocks + kThreads - 1) / kThreads;
-    if (blocks <= kFew) {
+    if (FEW || blocks <= kFew) {
         if (tid < kFew) {
             const int i = min(tid, max(blocks - 1, 0));
             const float score = blocks ? score_of(i) : 0.0f;
@@ -415,35 +425,41 @@ __global__ __launch_bounds__(kThreads) void us_kv_choose_kernel(ChooseArgs a) {
         }
         __syncthreads();
         select_few(blocks, a.top, out, pick);
-    } else if (blocks <= kHeld) {
+        return;
+    }
+    if constexpr (!FEW) {
+        Seen seen;
+        const int per = (blocks + kThreads - 1) / kThreads;
+        if (blocks <= kHeld) {
 #pragma unroll 1
-        for (int e0 = 0; e0 < per; e0 += 4) {              // (four on their way together)
-            float score[4];
-            int block[4];
+            for (int e0 = 0; e0 < per; e0 += 4) {          // (four on their way together)
+                float score[4];
+                int block[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = min(tid + kThreads * (e0 + e), blocks - 1);
-                score[e] = score_of(i);
-                block[e] = a.s.block(b, i);
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const int i = min(tid + kThreads * (e0 + e), blocks - 1);
+                    score[e] = score_of(i);
+                    block[e] = a.s.block(b, i);
+                }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = tid + kThreads * (e0 + e);
-                const uint32_t k = i < blocks ? key_of(i, block[e], score[e]) : 0u;
-                if (i < kHeld) pick.keys[i] = k;
-                seen.add(k);
+                for (int e = 0; e < 4; ++e) {
+                    const int i = tid + kThreads * (e0 + e);
+                    const uint32_t k = i < blocks ? key_of(i, block[e], score[e]) : 0u;
+                    if (i < kHeld) pick.keys[i] = k;
+                    seen.add(k);
+                }
             }
+            __syncthreads();
+            select([&](int i) { return pick.keys[i]; }, seen, blocks, a.top, out, pick);
+        } else {
+            const auto key = [&](int i) {
+                const int j = min(i, blocks - 1);
+                const uint32_t k = key_of(j, a.s.block(b, j), score_of(j));
+                return i < blocks ? k : 0u;
+            };
+            for (int e = 0; e < per; ++e) seen.add(key(tid + kThreads * e));
+            select(key, seen, blocks, a.top, out, pick);
         }
-        __syncthreads();
-        select([&](int i) { return pick.keys[i]; }, seen, blocks, a.top, out, pick);
-    } else {
-        const auto key = [&](int i) {
-            const int j = min(i, blocks - 1);
-            const uint32_t k = key_of(j, a.s.block(b, j), score_of(j));
-            return i < blocks ? k : 0u;
-        };
-        for (int e = 0; e < per; ++e) seen.add(key(tid + kThreads * e));
-        select(key, seen, blocks, a.top, out, pick);
     }
 }
 
@@ -507,15 +523,19 @@ extern "C" us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *se
     a.more.batch = seqs->batch;
     a.scores = choice->scores, a.stride = choice->scores_stride, a.chosen = choice->chosen;
     a.top = choice->top, a.sinks = choice->sinks, a.recent = choice->recent, a.tickets = (int32_t *)ws;
-    // Workgroups of kChunk blocks, but no more of them than fill the GPU a few times: each has its queries to lay out.
+    // Workgroups of a chunk of blocks, but no more of them than fill the GPU a few times: each has its queries to lay out.
+    const bool few = most <= kFew;
+    const int chunk = few ? Shape<true>::kChunk : Shape<false>::kChunk;
     const int64_t room = 8 * us_device::compute_units() / units;
-    int64_t parts = (most + kChunk - 1) / kChunk;
+    int64_t parts = (most + chunk - 1) / chunk;
     if (parts > room) parts = room < 1 ? 1 : room;
     const dim3 grid(q->tokens, cache->heads, (unsigned)parts);
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
         return with_type(q->dtype, [&](auto dt) {
-            hipLaunchKernelGGL((us_kv_choose_kernel<decltype(nt)::value, decltype(dt)::value>), grid, dim3(kThreads), 0,
-                               (hipStream_t)stream, a);
+            constexpr int NT = decltype(nt)::value, DT = decltype(dt)::value;
+            const hipStream_t hs = (hipStream_t)stream;
+            if (few) hipLaunchKernelGGL((us_kv_choose_kernel<NT, DT, true>), grid, dim3(Shape<true>::kThreads), 0, hs, a);
+            else hipLaunchKernelGGL((us_kv_choose_kernel<NT, DT, false>), grid, dim3(Shape<false>::kThreads), 0, hs, a);
             return hipGetLastError();
         });
     });

@@ -538,6 +538,14 @@ def _attend_chosen(torch, p, cache, q, chosen, lens, new, starts, dtype, scale=N
     return out
 
 
+@pytest.mark.parametrize("length,more", [(8191, 0), (8192, 0), (8192, 1), (8193, 0)])
+@pytest.mark.parametrize("top", [1, 127, 128, 131])
+def test_choose_of_about_128_blocks(torch_cuda, length, more, top):
+    # Where the counting of keys, and the fewer wavefronts of calls of few blocks, end; `more`: of the call's bound alone.
+    announce(f"kv choose len={length} bound={length + more} top={top}")
+    _choose_case(torch_cuda, [length, 5], [2, 1], 18, 2, 64, top, 1, 0, "f16", holes=[(0, 3), (0, 126)], max_len=length + more)
+
+
 @pytest.mark.parametrize("lens,new,holes", [([900, 64], [1, 1], [(0, 0), (0, 5), (0, 14), (1, 0)]), ([2000], [4], [(0, 31), (0, 30), (0, 1)])])
 def test_choose_over_blocks_that_are_not_there(torch_cuda, lens, new, holes):
     announce(f"kv choose holes={holes}")

@@ -47,8 +47,9 @@ def _of(kernels, name):
 def test_every_row_width_and_type_is_built(kernels):
     widths, types = (2, 3, 4, 6, 8), (0, 1, 2)
     both = {(w, t) for w in widths for t in types}
-    for name in ("us_kv_choose_kernel", "us_kv_chosen_kernel", "us_kv_shared_few_kernel", "us_kv_shared_join_kernel"):
+    for name in ("us_kv_chosen_kernel", "us_kv_shared_few_kernel", "us_kv_shared_join_kernel"):
         assert set(_of(kernels, name)) == both, name
+    assert set(_of(kernels, "us_kv_choose_kernel")) == {(w, t, few) for w, t in both for few in (0, 1)}
     many = _of(kernels, "us_kv_shared_many_kernel")
     assert {k[1:3] for k in many} == both and len(many) == 2 * len(both)
     assert set(_of(kernels, "us_kv_summarise_kernel")) == {(w,) for w in widths}
