@@ -244,7 +244,9 @@ typedef struct {
 us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head_dim, const us_rows *q, const us_rows *q_out,
                        const us_rows *k, const us_rows *k_out, const us_kv_rotation *how, void *stream);
 
-/* The sequences that a fork makes; none of it overlaps what the call reads. */
+/* The sequences that a fork makes; none of it overlaps what the call reads (old
+ * and new tables that do, US_ERR_ARG; in one tensor, rows of one stride beside
+ * each other). */
 typedef struct {
     int32_t *blocks;        /* device, batch x stride                           */
     int64_t stride;
@@ -259,9 +261,9 @@ typedef struct {
  * the old ones: none) and blocks for room[b] more (NULL or below 0: none), as far
  * as the table is wide. refs[i] is how often the tables name block i; 0 is a free
  * block. Full blocks are shared by all children of a sequence. The block that a
- * sequence's next token goes to, and those behind it, stay with its first child
- * (the lowest b) if refs is 1; any other child is given a block for each of
- * them, a copy of the started one. Blocks that are given are the free ones of
+ * sequence's next token goes to, and those behind it that its room reaches, stay
+ * with its first child (the lowest b) if refs is 1; any other child is given a
+ * block for each of them, a copy of the started one. Blocks that are given are the free ones of
  * lowest number, in the order of sequences and of their tables. Then the old
  * tables count for nothing any more, over their whole width: entries without a
  * block have to be outside [0, n_blocks). So a call frees what no child
@@ -316,7 +318,9 @@ us_status us_kv_attend_shared(const us_kv_cache *cache, const us_kv_seqs *seqs, 
  * summary (n_blocks x heads x 2 x us_kv_row(head_dim) bytes, 16-byte aligned)
  * gets the smallest byte of each value over the sequence's tokens in the block,
  * then the largest. Called after the append of these tokens, also because that
- * may change a block's scale and with it older codes.
+ * may change a block's scale and with it older codes; after us_kv_evict for all
+ * tokens that are left. us_kv_fork copies no summary: a started block that it
+ * copies has one after the next append to it, or a call for its tokens.
  */
 us_status us_kv_summarise(const us_kv_cache *cache, const us_kv_seqs *seqs, uint8_t *summary, void *stream);
 

@@ -1,6 +1,10 @@
 // us_kv_attend_chosen: the attention of single tokens over the blocks that a
 // list of each names. The body is that of the attention with few query rows
 // (us_kv_decode.h); a token and cache head is a unit, as its list is its own.
+// Chosen blocks are 8 KB of keys and 8 KB of values each for heads of 128, read at
+// the rate of whole sequences or more, as tokens of a sequence choose alike: 32
+// tokens, 8 cache heads, 48 blocks each take 29.5 us, 6.8 TB/s. One token with 64
+// takes 10.4 us for 8.4 MB: the start, the first loads, the join of its parts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -3,7 +3,7 @@
 // A row (a token's head) of D values x becomes n = x w / sqrt(mean x^2 + eps),
 // then its pairs (n1, n2) become (n1 cos - n2 sin, n2 cos + n1 sin) of the angle
 // sum over the axes of position times frequency. The angle is taken in 64 bits:
-// in 32, a position of a million would be off by a sixteenth of a radian. What is
+// in 32, a position of a million would be off by up to a 32nd of a radian. What is
 // left of it after whole quarters of a turn is at most pi / 4, and in float32
 // there off by 2^-26 at most.
 #include <hip/hip_runtime.h>

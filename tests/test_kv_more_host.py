@@ -131,6 +131,21 @@ def test_fork_refuses(change, status):
     assert r == status
 
 
+@pytest.mark.parametrize("at_first,stride,width,batch,meets", [
+    (24, 6, 4, 3, False), (23, 6, 4, 3, False), (15, 6, 4, 3, True), (16, 9, 6, 2, False), (-4, 9, 5, 1, True), (-5, 9, 5, 1, False),
+    (4, 10, 6, 3, False), (4, 10, 7, 3, True), (3, 10, 6, 3, True), (-6, 10, 6, 3, False), (-6, 10, 7, 2, True), (4, 11, 6, 2, True)])
+def test_fork_refuses_tables_that_share_memory(at_first, stride, width, batch, meets):
+    # The old table: 3 rows of 4 entries, as far apart as the new ones' are, or 6. (What is refused after it: SHAPE.)
+    seqs, c = _seqs(), _cache()
+    seqs.stride = stride if stride > 9 and stride != 11 else 6
+    c.heads = 32768
+    seqs.blocks = 2 * P
+    own = {seqs.stride * i + j for i in range(3) for j in range(4)}
+    assert meets == bool(own & {at_first + stride * i + j for i in range(batch) for j in range(width)})
+    to = kv.ForkedStruct(2 * P + 4 * at_first, stride, width, batch, 4 * P)
+    assert kv.lib().us_kv_fork(at(c), P, at(seqs), P, P, at(to), P, P, BIG, None) == (ARG if meets else SHAPE)
+
+
 def test_fork_workspace_refuses():
     L, n = kv.lib(), ctypes.c_size_t(7)
     for batch, to_batch in ((0, 3), (3, 0), (65536, 3), (3, 65536), (-1, 3)):
