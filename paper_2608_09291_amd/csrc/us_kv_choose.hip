@@ -17,8 +17,8 @@
 // read 64 times as much, so it is short, and bound by its chain of steps: the row's
 // place, queries, digits, block numbers, summaries, products, a ticket, the scores
 // again, three to five passes of the choice. us on the GPU (and its bytes' time):
-// 131071 keys, 8 cache heads of 128, one query, 13.0 (0.9); 16 sequences of 9000 to
-// 16384 and two queries of each, 11.7 (1.4); 8 of 3000 to 9000, 32 heads, 10.4 (1.3);
+// 131071 keys, 8 cache heads of 128, one query, 12.9 (0.9); 16 sequences of 9000 to
+// 16384 and two queries of each, 9.8 (1.4); 8 of 3000 to 9000, 32 heads, 9.4 (1.3);
 // with scores alone 6.2 to 8.6. Summaries are HBM's: 32700 keys of 8 heads, 9.0 us,
 // 3.7 TB/s.
 #include <hip/hip_runtime.h>
@@ -119,6 +119,12 @@ struct Shape {
     static constexpr int kWaves = FEW ? 4 : 8, kThreads = 64 * kWaves, kHeld = FEW ? kFew : 4096;
     static constexpr int kChunk = 16 * kWaves;             // blocks scored at a time
 };
+// Chunks that one workgroup takes alone: its scores are keys in LDS at once, without a ticket and a second look at
+// them. us of 8 float32 rows, 32 heads over 32, 47 to 141 blocks, alone and with two workgroups where there are two
+// chunks: 9.4, 10.5; of 32 rows, 32 over 8, up to 256 blocks: 9.8, 11.7. For four and sixteen chunks, half as many
+// workgroups take 1.4 and 1.5 us longer.
+constexpr int kAlone = 2;
+static_assert(kAlone * Shape<true>::kChunk >= kFew, "calls of few blocks draw no tickets");
 
 // Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
 __device__ inline uint32_t order_of(float x) {
@@ -311,7 +317,8 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
     int b, at;
     if (!a.more.place(a.s, t, b, at)) return;
     const int64_t unit = (int64_t)t * a.heads + hk;
-    const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + kChunk - 1) / kChunk, parts = min(max(chunks, 1), (int)gridDim.z);
+    const int blocks = at < 0 ? 0 : at / kBlock + 1, chunks = (blocks + kChunk - 1) / kChunk;
+    const int parts = chunks <= kAlone ? 1 : min(chunks, (int)gridDim.z);
     if ((int)blockIdx.z >= parts) return;
     float *scores = a.scores + unit * a.stride;
     // Heads g0 .. g0 + 15 (zeros past the last).
@@ -361,16 +368,29 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
         }
         __syncthreads();
     };
-    if (a.G <= 4 * kGroups) lay_out(0);
-    for (int c = blockIdx.z; c < chunks; c += parts) {
-        const int m0 = kChunk * c + 16 * wave, mine = m0 + n;  // a wavefront's 16 blocks; lane n's
-        const int id = mine < blocks ? a.s.block(b, mine) : -1;
+    const auto key_of = [&](int i, bool there, float score) {
+        return !there ? 0u : i < a.sinks || i >= blocks - a.recent ? ~0u : min(order_of(score), ~0u - 1);
+    };
+    // A wavefront's 16 blocks, of which a lane has the n-th; the first ones are on their way ahead of the queries' digits.
+    u32x4 codes[kSteps];
+    float ks;
+    const auto look_up = [&](int c) {
+        const int mine = kChunk * c + 16 * wave + n;
+        return mine < blocks ? a.s.block(b, mine) : -1;
+    };
+    const auto fetch = [&](int id) {
         const int64_t where = (int64_t)max(id, 0) * a.heads + hk;
         const u32x4 *src = (const u32x4 *)(a.summary + where * (2 * R)) + kk;
-        u32x4 codes[kSteps];
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) codes[j] = src[4 * j];
-        const float ks = a.ks[where];
+        ks = a.ks[where];
+    };
+    int id = look_up(blockIdx.z);
+    fetch(id);
+    if (a.G <= 4 * kGroups) lay_out(0);
+    const bool alone = FEW || (parts == 1 && blocks <= kHeld);
+    for (int c = blockIdx.z; c < chunks; c += parts) {
+        const int m0 = kChunk * c + 16 * wave, next = look_up(c + parts);
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) codes[j] ^= 0x80808080u;              // bytes less 128
         double best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -413,34 +433,41 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
         if (n < 4 && m0 + m < blocks) {
             const float score = there ? (float)(y * (double)scale) : -INFINITY;
             __hip_atomic_store(scores + m0 + m, score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (alone) pick.keys[m0 + m] = key_of(m0 + m, there, score);
         }
+        id = next;
+        if (c + parts < chunks) fetch(id);
     }
-    if (parts > 1) {
+    // Keys past the last block, up to where the choice looks.
+    if (alone)
+        for (int i = blocks + tid; i < (blocks <= kFew ? kFew : (int)up(blocks, kThreads)); i += kThreads) pick.keys[i] = 0;
+    if (!FEW && parts > 1) {
         if (!last_of(a.tickets + unit, parts, &flag)) return;
     } else {
         __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     }
-    const auto key_of = [&](int i, int block, float score) {
-        return block < 0 ? 0u : i < a.sinks || i >= blocks - a.recent ? ~0u : min(order_of(score), ~0u - 1);
-    };
     const auto score_of = [&](int i) { return __hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     int *out = a.chosen + unit * a.top;
     if (FEW || blocks <= kFew) {
-        if (tid < kFew) {
-            const int i = min(tid, max(blocks - 1, 0));
-            const float score = blocks ? score_of(i) : 0.0f;
-            const int block = blocks ? a.s.block(b, i) : -1;
-            pick.keys[tid] = tid < blocks ? key_of(i, block, score) : 0u;
+        if (!alone) {
+            if (tid < kFew) {
+                const int i = min(tid, blocks - 1);
+                const float score = score_of(i);
+                const int block = a.s.block(b, i);
+                pick.keys[tid] = tid < blocks ? key_of(i, block >= 0, score) : 0u;
+            }
+            __syncthreads();
         }
-        __syncthreads();
         select_few(blocks, a.top, out, pick);
         return;
     }
     if constexpr (!FEW) {
         Seen seen;
         const int per = (blocks + kThreads - 1) / kThreads;
-        if (blocks <= kHeld) {
+        if (alone) {
+            for (int e = 0; e < per; ++e) seen.add(pick.keys[tid + kThreads * e]);
+        } else if (blocks <= kHeld) {
 #pragma unroll 1
             for (int e0 = 0; e0 < per; e0 += 4) {          // (four on their way together)
                 float score[4];
@@ -454,17 +481,19 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = tid + kThreads * (e0 + e);
-                    const uint32_t k = i < blocks ? key_of(i, block[e], score[e]) : 0u;
+                    const uint32_t k = i < blocks ? key_of(i, block[e] >= 0, score[e]) : 0u;
                     if (i < kHeld) pick.keys[i] = k;
                     seen.add(k);
                 }
             }
             __syncthreads();
+        }
+        if (blocks <= kHeld) {
             select([&](int i) { return pick.keys[i]; }, seen, blocks, a.top, out, pick);
         } else {
             const auto key = [&](int i) {
                 const int j = min(i, blocks - 1);
-                const uint32_t k = key_of(j, a.s.block(b, j), score_of(j));
+                const uint32_t k = key_of(j, a.s.block(b, j) >= 0, score_of(j));
                 return i < blocks ? k : 0u;
             };
             for (int e = 0; e < per; ++e) seen.add(key(tid + kThreads * e));
@@ -538,6 +567,7 @@ extern "C" us_status us_kv_choose(const us_kv_cache *cache, const us_kv_seqs *se
     const int chunk = few ? Shape<true>::kChunk : Shape<false>::kChunk;
     const int64_t room = 8 * us_device::compute_units() / units;
     int64_t parts = (most + chunk - 1) / chunk;
+    if (parts <= kAlone) parts = 1;
     if (parts > room) parts = room < 1 ? 1 : room;
     const dim3 grid(q->tokens, cache->heads, (unsigned)parts);
     const hipError_t e = with_row(cache->head_dim, [&](auto nt) {
