@@ -60,6 +60,7 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
             }
             const int64_t far = (int64_t)(r0 - group.r0) * a.G;                // of its first row, among the group's
             const int total = n * a.G;
+            if (total == 0) continue;                      // (no unit: no workgroup of its own would draw its ticket)
             const bool in = far >= 0 && far < end && group.cut > 0;
             const int at0 = in ? (int)far : 0;
             if (!rest && (!in || at0 + total <= row0 || at0 >= row0 + kDecodeRows)) continue;

@@ -342,6 +342,25 @@ def test_attend_shared(torch_cuda, sizes, common, own, new, H, Hk, D, causal, dt
     _check(torch, p, lens, new, q, out, dtype, causal=causal)
 
 
+@pytest.mark.parametrize("H,Hk", [(2, 1), (4, 4), (24, 2)])
+def test_attend_shared_with_sequences_that_have_no_rows(torch_cuda, H, Hk):
+    """A sequence without rows among a group's leaves no ticket behind, for the call in which it has some."""
+    torch = torch_cuda
+    announce(f"kv shared without rows {H}/{Hk}")
+    rng = np.random.default_rng(6)
+    p = Groups(torch, rng, [5, 3], [40, 3], [9, 70, 200, 1, 64, 3, 90, 5], Hk, 64)
+    cache, groups, common = p.cache(), p.dev([0, 5, 8]), p.dev([40, 3])
+    most = dict(max_q=4, max_group=5, max_shared=40)
+    ws = kv.attend_shared_workspace(cache, torch.empty((32, H, 64), device="cuda"), p.dev(p.blocks), groups, starts=groups, **most)
+    for new in ([1, 0, 0, 1, 1, 0, 1, 0], [1] * 8, [0, 0, 3, 0, 0, 0, 0, 0], [0] * 7 + [4], [2, 1, 1, 0, 1, 1, 3, 1]):
+        q = torch.from_numpy(rng.normal(0, 1.5, size=(sum(new), H, 64)).astype(np.float32)).cuda()
+        out = torch.full_like(q, math.nan)
+        kv.attend_shared(cache, p.dev(p.blocks), p.dev(p.lens_), q, out, groups, common, starts=p.dev(_starts(new)), ws=ws, **most)
+        torch.cuda.synchronize()
+        assert not ws[:16384].any(), new                    # the tickets
+        _check(torch, p, p.lens_, new, q, out, "f32")
+
+
 def test_attend_shared_sequences_of_no_group_and_short_ones(torch_cuda):
     """Sequences ahead of the first group, behind the last, past max_group; sequences shorter than what they share, and empty ones."""
     torch = torch_cuda
