@@ -361,6 +361,27 @@ def test_attend_shared_with_sequences_that_have_no_rows(torch_cuda, H, Hk):
         _check(torch, p, p.lens_, new, q, out, "f32")
 
 
+@pytest.mark.parametrize("queries,causal", [(1, True), (3, True), (34, False)])
+@pytest.mark.parametrize("count", [64, 65, 131])
+def test_attend_shared_many_groups(torch_cuda, count, queries, causal):
+    """As many groups as come in one look at their table, and more."""
+    torch = torch_cuda
+    announce(f"kv shared {count} groups of {queries} queries causal={causal}")
+    rng = np.random.default_rng(count + queries)
+    sizes, common = [1 + g % 3 % 2 for g in range(count)], [g % 4 for g in range(count)]
+    n, H, Hk, D = sum(sizes), 2, 1, 64
+    p = Groups(torch, rng, sizes, common, [queries + 5 * (b % 7) for b in range(n)], Hk, D)
+    cache, new = p.cache(), [queries] * n
+    q = torch.from_numpy(rng.normal(0, 1.5, size=(sum(new), H, D)).astype(np.float32)).cuda()
+    out = torch.full_like(q, math.nan)
+    groups, args = p.dev(_starts(sizes)), dict(starts=p.dev(_starts(new)), max_q=queries, causal=causal, max_group=2, max_shared=3)
+    ws = kv.attend_shared_workspace(cache, q, p.dev(p.blocks), groups, **args)
+    kv.attend_shared(cache, p.dev(p.blocks), p.dev(p.lens_), q, out, groups, p.dev(common), ws=ws, **args)
+    torch.cuda.synchronize()
+    assert not ws[:16384].any()
+    _check(torch, p, p.lens_, new, q, out, "f32", causal=causal)
+
+
 def test_attend_shared_sequences_of_no_group_and_short_ones(torch_cuda):
     """Sequences ahead of the first group, behind the last, past max_group; sequences shorter than what they share, and empty ones."""
     torch = torch_cuda
