@@ -11,7 +11,8 @@
 // query's small values (float32: below 2^-7 of its largest one, bfloat16: 2^-23,
 // float16: 2^-20), 2^-30 of the largest at most each; two blocks change places
 // only where their scores agree to about nine digits. (The same products in 64
-// bit floating point, without the choice: 2 to 3 times as long.)
+// bit floating point: 23.5 us a call with summaries, in place of 16 at that time, for
+// 8 sequences of 3000 to 9000, 32 heads.)
 //
 // A launch reads 2 D bytes of a block and cache head where the attention would
 // read 64 times as much, so it is short, and bound by its chain of steps: the row's

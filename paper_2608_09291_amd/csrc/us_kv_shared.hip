@@ -14,10 +14,10 @@
 //
 // Common keys with few rows are bound by memory, with many by the matrix and vector
 // units as a prompt is; with the keys of its own, no sequence takes more than in
-// us_kv_attend. us on the GPU: 6 sequences of 1 K common tokens 13.2 in one launch
+// us_kv_attend. us on the GPU: 6 sequences of 1 K common tokens 12.7 in one launch
 // (about 6 of which every workgroup of this body takes, short as its keys are); 24 of
-// 5 documents of 3000 to 12000, 3 tokens each, 98 to 105 (4 or 5 TB/s); 64 of 16 K
-// common tokens 53.4 + 28.3, in which the first launch's products take 35 and its
+// 5 documents of 3000 to 12000, 3 tokens each, 98 to 102 (4 or 5 TB/s); 64 of 16 K
+// common tokens 53.5 + 27.2, in which the first launch's products take 35 and its
 // start, queries and partial rows (34 MB) the rest.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
