@@ -6,6 +6,11 @@
 // in 32, a position of a million would be off by up to a 32nd of a radian. What is
 // left of it after whole quarters of a turn is at most pi / 4, and in float32
 // there off by 2^-26 at most.
+//
+// Bound by memory: every value is read and written once, some ten operations
+// each. us on the GPU: 8192 tokens, 64 + 8 heads of 128, normed, bfloat16, 48.8;
+// 5007 tokens, 16 + 16 heads of 80, three axes, 14.6; one token of 64 heads 2.9,
+// below what a launch takes the host.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -90,6 +95,7 @@ struct Octet {
             constexpr int N = sizeof(raw) / 16;
             u32x4 w[N];
             __builtin_memcpy(w, raw, sizeof(raw));
+            // (past the caches: 8192 tokens of 72 heads of 128 take 48.8 us on the GPU, 62 without)
             if (n)
 #pragma unroll
                 for (int i = 0; i < N; ++i) __builtin_nontemporal_store(w[i], (u32x4 *)p + i);
