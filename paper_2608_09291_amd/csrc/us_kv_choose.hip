@@ -322,12 +322,13 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
     const int parts = chunks <= kAlone ? 1 : min(chunks, (int)gridDim.z);
     if ((int)blockIdx.z >= parts) return;
     float *scores = a.scores + unit * a.stride;
-    // Heads g0 .. g0 + 15 (zeros past the last).
-    const auto lay_out = [&](int g0) {
+    // Heads g0 .. g0 + 15 (zeros past the last). The first heads are in `raw` for the first chunk of blocks alone: with
+    // more than 16, every chunk lays all of them out again, each over the ones before.
+    const auto lay_out = [&](int g0, bool fetched) {
         for (int h0 = 0; h0 < min(4 * kGroups, (a.G - g0 + 3) / 4 * 4); h0 += kHeads) {
             const int h = h0 + tid / kLanes, o = oct, g = g0 + h;
             const bool here = h < 4 * kGroups && o < R / 8;
-            if (g0 + h0 > 0) raw.load(q + (int64_t)min(g, a.G - 1) * a.q.head_stride, min(o, (a.D - 1) / 8), 0, a.D, a.vec);
+            if (!fetched || g0 + h0 > 0) raw.load(q + (int64_t)min(g, a.G - 1) * a.q.head_stride, min(o, (a.D - 1) / 8), 0, a.D, a.vec);
             float x[8], mx = 0.0f;
             raw.octet(0, o, a.D, false, x);                // (zeros past D)
 #pragma unroll
@@ -388,7 +389,7 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
     };
     int id = look_up(blockIdx.z);
     fetch(id);
-    if (a.G <= 4 * kGroups) lay_out(0);
+    if (a.G <= 4 * kGroups) lay_out(0, true);
     const bool alone = FEW || (parts == 1 && blocks <= kHeld);
     for (int c = blockIdx.z; c < chunks; c += parts) {
         const int m0 = kChunk * c + 16 * wave, next = look_up(c + parts);
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
         for (int g0 = 0; g0 < a.G; g0 += 4 * kGroups) {
             if (a.G > 4 * kGroups) {
                 __syncthreads();                           // (the heads before these)
-                lay_out(g0);
+                lay_out(g0, c == (int)blockIdx.z);
             }
             for (int g = 0; g < min(kGroups, (a.G - g0 + 3) / 4); ++g) {
                 i32x4 x = {0, 0, 0, 0};
