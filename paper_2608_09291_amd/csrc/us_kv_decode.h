@@ -58,11 +58,11 @@ __device__ inline void join_parts(const Args &a, const Others &more, bool rest, 
                 a.s.rows(b, r0, n);
                 len = a.s.len(b);
             }
-            const int64_t far = (int64_t)(r0 - group.r0) * a.G;                // of its first row, among the group's
+            const int far = place_of(r0, group.r0, a.G, 0, end);               // of its first row
             const int total = n * a.G;
             if (total == 0) continue;                      // (no unit: no workgroup of its own would draw its ticket)
-            const bool in = far >= 0 && far < end && group.cut > 0;
-            const int at0 = in ? (int)far : 0;
+            const bool in = far >= 0 && group.cut > 0;
+            const int at0 = in ? far : 0;
             if (!rest && (!in || at0 + total <= row0 || at0 >= row0 + kDecodeRows)) continue;
             const int t0 = rest ? tile : max(row0 - at0, 0) / kDecodeRows;
             const int t1 = rest ? tile : (min(total, row0 + kDecodeRows - at0) - 1) / kDecodeRows;

@@ -22,6 +22,13 @@ struct Mask {
     }
 };
 
+// The place among a group's `end` query rows, G to a token from token row `first` on, of row `row` of a sequence whose
+// tokens begin at row r0; -1 where it is none of them. (64 bits: the tables of both may hold anything, in any order.)
+__host__ __device__ inline int place_of(int32_t r0, int32_t first, int32_t G, int32_t row, int32_t end) {
+    const int64_t at = ((int64_t)r0 - first) * G + row;
+    return at >= 0 && at < end ? (int)at : -1;
+}
+
 // How a prompt workgroup passes the blocks of a row tile through its LDS stages:
 // block i lies in stage i % stages, keys and values apart. Ahead of step 0 the
 // first blocks are staged, then a barrier, then block 0's scores are taken. Step

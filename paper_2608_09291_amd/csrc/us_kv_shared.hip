@@ -79,11 +79,11 @@ __global__ __launch_bounds__(256) void us_kv_shared_join_kernel(Args a, Others m
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], w, x[e]);
         }
     };
-    if (group.cut > 0) {
-        const int at = (r0 - group.r0 + i) * a.G + hh;     // among the group's rows
-        if (at < group.n * a.G) add(pre, group.number, at, splits_of(0, group.cut, pre.chunk));
-    }
     const int row = i * a.G + hh, base = row / own.rows * own.rows;
+    if (group.cut > 0) {
+        const int at = place_of(r0, group.r0, a.G, row, group.n * a.G);
+        if (at >= 0) add(pre, group.number, at, splits_of(0, group.cut, pre.chunk));
+    }
     int lo, hi;
     a.mask.range((min(base + own.rows, n * a.G) - 1) / a.G, n, a.s.len(b), lo, hi);
     add(own, b, row, splits_of(group.cut, max(hi, group.cut), own.chunk));
