@@ -433,7 +433,8 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
         const float scale = __shfl(ks, m, 64);
         const bool there = __shfl(id, m, 64) >= 0;
         if (n < 4 && m0 + m < blocks) {
-            const float score = there ? (float)(y * (double)scale) : -INFINITY;
+            // (without a finite query head y is -infinity, also times a scale of 0)
+            const float score = there && y > -INFINITY ? (float)(y * (double)scale) : -INFINITY;
             __hip_atomic_store(scores + m0 + m, score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (alone) pick.keys[m0 + m] = key_of(m0 + m, there, score);
         }

@@ -1,7 +1,10 @@
 """The choice of blocks where a cache head has more query heads than are laid out together (16), over one and several
-chunks of blocks to a workgroup. Bounds are those of test_gpu_kv_more.py, whose cases and oracle these share."""
+chunks of blocks to a workgroup, and where no query head is finite. Bounds are those of test_gpu_kv_more.py, whose cases and oracle these share."""
+import math
+
 import pytest
 
+from paper_2608_09291_amd import kv
 from test_gpu_kv import DTYPES
 from test_gpu_kv_more import _attend_chosen, _choose_case
 from test_gpu_spmm import announce, torch_cuda  # noqa: F401
@@ -35,3 +38,22 @@ def test_choose_with_many_query_heads_and_rows(torch_cuda):
 def test_choose_with_many_query_heads_and_blocks_that_are_not_there(torch_cuda):
     announce("kv choose of many heads over holes")
     _choose_case(torch_cuda, [7000], [2], 24, 1, 64, 6, 1, 1, "f32", holes=[(0, 0), (0, 64), (0, 90), (0, 109)])
+
+
+@pytest.mark.parametrize("blocks,top", [(1, 1), (20, 4), (140, 9), (5000, 70)])
+def test_choose_without_a_finite_query(torch_cuda, blocks, top):
+    """Scores are -infinity, of blocks of scale 0 as well, and the first blocks are taken."""
+    torch = torch_cuda
+    announce(f"kv choose without a finite query blocks={blocks}")
+    cache = kv.new_cache(blocks, 2, 64)
+    cache.k_scale[::3, 0] = 0.5                             # (zeros are what a block of zeros has)
+    cache.k_scale[1:, 1] = 0.25
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, lens = torch.arange(blocks, **i32)[None], torch.tensor([64 * blocks], **i32)
+    for bad in (math.nan, math.inf, -math.inf):
+        q = torch.randn((1, 6, 64), device="cuda")
+        q[0, :, 5] = bad
+        scores, chosen = torch.zeros((1, 2, blocks), device="cuda"), torch.zeros((1, 2, top), **i32)
+        kv.choose(cache, kv.new_summary(cache), table, lens, q, scores, chosen, sinks=0, recent=0, ws=kv.choose_workspace(cache, table, chosen))
+        assert (scores == -math.inf).all()
+        assert chosen.tolist() == [[list(range(top))] * 2]
