@@ -236,7 +236,9 @@ typedef struct {
  *   a_i = sum over the axes of (positions[axis, row] + offset) freq[axis, i],
  * and the rest stays. (An axis that does not turn a pair has frequency 0 there.)
  * Angles are taken in 64 bits, the rest in float32, rounded once. q_out may be q
- * and k_out may be k, with the same strides; otherwise they overlap nothing. All
+ * and k_out may be k, with the same strides (others, US_ERR_ARG); otherwise they
+ * overlap nothing, and no rows of an output share memory (US_ERR_ARG): a head that
+ * is there once for several is turned into an output of its own. All
  * rows have one type and number. k = k_out = NULL with k_heads = 0: queries alone.
  * US_ERR_SHAPE for more than 2^23 times as many rows as a workgroup takes together
  * (one, at least).

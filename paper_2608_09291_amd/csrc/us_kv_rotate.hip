@@ -235,6 +235,26 @@ us_status check_pair(const us_rows *in, const us_rows *out, int tokens, int dtyp
     return in->tokens == tokens && out->tokens == tokens ? US_OK : US_ERR_SHAPE;
 }
 
+// Whether some of an output's rows share memory.
+bool rows_meet(const us_rows &r, int heads, int D) {
+    const int64_t t = r.token_stride, h = r.head_stride;
+    if ((r.tokens > 1 && t < D) || (heads > 1 && h < D)) return true;
+    if (r.tokens == 1 || heads == 1) return false;
+    const __int128 most = (__int128)t * (r.tokens - 1);    // first value of the last token
+    if (t - D >= (__int128)h * (heads - 1) || h - D >= most) return false;
+    for (int j = 1; j < heads; ++j) {                      // (head j of a token and the first of the tokens next to it)
+        const __int128 at = (__int128)h * j, below = at - at % t, above = below + t;
+        if (at - D >= most) return false;
+        if ((below > 0 && below <= most && at - below < D) || (above <= most && above - at < D)) return true;
+    }
+    return false;
+}
+
+// Whether an output is its input, and other rows of it.
+bool other_rows(const us_rows &in, const us_rows &out, int heads) {
+    return in.data == out.data && ((in.tokens > 1 && in.token_stride != out.token_stride) || (heads > 1 && in.head_stride != out.head_stride));
+}
+
 }  // namespace
 
 extern "C" us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head_dim, const us_rows *q, const us_rows *q_out,
@@ -245,6 +265,9 @@ extern "C" us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head
     if (st != US_OK) return st;
     if (!row_of(head_dim) || q_heads < 1 || q_heads > 65535 || k_heads < 0 || k_heads > 65535 || (k_heads > 0) != (k != nullptr))
         return US_ERR_SHAPE;
+    // (such rows would be turned more than once, or while others read them)
+    if (rows_meet(*q_out, q_heads, head_dim) || other_rows(*q, *q_out, q_heads)) return US_ERR_ARG;
+    if (k && (rows_meet(*k_out, k_heads, head_dim) || other_rows(*k, *k_out, k_heads))) return US_ERR_ARG;
     if (how->pairs < 0 || how->pairs > head_dim / 2 || (how->pairs && (how->axes < 1 || how->axes > US_KV_AXES_MAX)))
         return US_ERR_SHAPE;
     if (how->pairs && how->positions_stride < q->tokens && how->axes > 1) return US_ERR_SHAPE;

@@ -47,3 +47,18 @@ def test_rotate_weights(torch_cuda, T, H, Hk, D, pairs, adjacent, which, aligned
         want = ref.rotate(x, freq, pos, 0, adjacent, w, 1e-5)
         over = np.abs(y - want) - _rotate_bound(x, want, freq, pos, 0, adjacent, 1e-5, dtype, w)
         assert (over <= 0).all(), (np.unravel_index(over.argmax(), over.shape), over.max())
+
+
+def test_rotate_a_head_that_is_there_once(torch_cuda):
+    """One key head for all: turned into an output of its own, not in place."""
+    torch = torch_cuda
+    announce("kv rotate a broadcast head")
+    one, freq, pos = torch.randn((20, 1, 64), device="cuda"), torch.rand(32, device="cuda"), torch.arange(20, dtype=torch.int32, device="cuda")
+    q, k, before = torch.randn((20, 8, 64), device="cuda"), one.expand(20, 4, 64), one.clone()
+    with pytest.raises((RuntimeError, ValueError)):
+        kv.rotate(q.clone(), k, freq, pos)
+    out, alone = torch.empty((20, 4, 64), device="cuda"), torch.empty_like(one)
+    kv.rotate(q, k, freq, pos, k_out=out)
+    kv.rotate(one, None, freq, pos, q_out=alone)
+    torch.cuda.synchronize()
+    assert torch.equal(one, before) and torch.equal(out, alone.expand(20, 4, 64))
