@@ -37,7 +37,6 @@ using namespace us_kv;
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-
 // --- summaries ----------------------------------------------------------------
 
 __device__ inline u16x2 pair_of(uint32_t x) { return __builtin_bit_cast(u16x2, x); }
@@ -125,7 +124,7 @@ struct Shape {
 // chunks: 9.4, 10.5; of 32 rows, 32 over 8, up to 256 blocks: 9.8, 11.7. For four and sixteen chunks, half as many
 // workgroups take 1.4 and 1.5 us longer.
 constexpr int kAlone = 2;
-static_assert(kAlone * Shape<true>::kChunk >= kFew, "calls of few blocks draw no tickets");
+static_assert(kAlone * Shape<true>::kChunk >= kFew && kAlone * Shape<false>::kChunk >= kFew, "few blocks are one workgroup's");
 
 // Scores in the order of whole numbers; a NaN below all of them, 0 for a block that is not there.
 __device__ inline uint32_t order_of(float x) {
@@ -452,16 +451,7 @@ __global__ __launch_bounds__(Shape<FEW>::kThreads) void us_kv_choose_kernel(Choo
     }
     const auto score_of = [&](int i) { return __hip_atomic_load(scores + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     int *out = a.chosen + unit * a.top;
-    if (FEW || blocks <= kFew) {
-        if (!alone) {
-            if (tid < kFew) {
-                const int i = min(tid, blocks - 1);
-                const float score = score_of(i);
-                const int block = a.s.block(b, i);
-                pick.keys[tid] = tid < blocks ? key_of(i, block >= 0, score) : 0u;
-            }
-            __syncthreads();
-        }
+    if (FEW || blocks <= kFew) {                           // (alone: the keys are there)
         select_few(blocks, a.top, out, pick);
         return;
     }
