@@ -11,8 +11,6 @@ using namespace us_kv;
 
 constexpr us_kv_attend_opts kDefault = {0.0f, 1, 0, 0, nullptr, 0};
 
-// What a call launches, and where its parts of the workspace lie (bytes).
-// (Calls of more units than there are tickets do not split.)
 // Workgroups of the prompt kernel, whose grid has one dimension of 512 threads each.
 constexpr int64_t kMostPrompt = INT32_MAX / 512;
 
@@ -96,7 +94,7 @@ us_status plan_of(const us_kv_cache &c, const us_kv_seqs &s, int q_heads, int to
     mix = mix < 1 ? 1 : mix > share ? share : mix;
     while (share % mix) --mix;
     p.mix = (int)mix;
-    // (a unit's partial rows lie within 2^31 bytes)
+    // (a unit's partial rows lie within 2^31 bytes; decode calls of more units than there are tickets do not split)
     if (p.chunk < (most + 4095) / 4096) p.chunk = (int)((most + 4095) / 4096);
     if ((p.decode && units > kTickets) || most <= p.chunk) p.chunk = (int)most;
     if (p.decode && ((most + p.chunk - 1) / p.chunk) * p.tiles > 65535) p.chunk = (int)((most * p.tiles + 65534) / 65535) + 1;
