@@ -91,9 +91,8 @@ def main(argv=None):
         _, k, v = layer.project(x, torch.arange(at, at + n, **ints))
         layer.lens[0][0] += n
         starts = torch.tensor([0] + [n] * S, **ints)
-        for put in (lambda: kv.append(layer.cache, layer.tables[0], layer.lens[0], k, v, starts=starts, max_new=n),
-                    lambda: kv.summarise(layer.cache, layer.tables[0], layer.lens[0], layer.summary, starts=starts, max_new=n)):
-            put()
+        kv.append(layer.cache, layer.tables[0], layer.lens[0], k, v, starts=starts, max_new=n)
+        kv.summarise(layer.cache, layer.tables[0], layer.lens[0], layer.summary, starts=starts, max_new=n)
     # One group of all samples, which have the prompt's full blocks in common.
     groups, shared = torch.tensor([0, S], **ints), torch.tensor([P // kv.BLOCK], **ints)
     parents, room = torch.zeros(S, **ints), torch.ones(S, **ints)
