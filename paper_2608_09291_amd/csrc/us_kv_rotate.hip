@@ -296,11 +296,11 @@ extern "C" us_status us_kv_rotate(int32_t q_heads, int32_t k_heads, int32_t head
     if (group > a.tokens / some) group = (int)(a.tokens / some);
     if (group < 1) group = 1;
     a.group = group;
-    const int groups = (a.tokens + group - 1) / group;
+    const int64_t groups = ((int64_t)a.tokens + group - 1) / group;
     a.part = groups >= some || a.rows <= at_once ? a.rows : at_once;
-    const dim3 grid(groups, (a.rows + a.part - 1) / a.part);
     // (a grid's dimension has fewer than 2^32 threads)
     if (groups > (1 << 23)) return US_ERR_SHAPE;
+    const dim3 grid((unsigned)groups, (a.rows + a.part - 1) / a.part);
     // Octets move whole where every one begins at a multiple of 16 bytes and none is cut.
     const bool vec = octets_aligned(*q, head_dim) && octets_aligned(*q_out, head_dim) && (how->adjacent ? 2 * P : P) % 8 == 0 &&
                      (!k || (octets_aligned(*k, head_dim) && octets_aligned(*k_out, head_dim)));

@@ -62,3 +62,15 @@ def test_rotate_a_head_that_is_there_once(torch_cuda):
     kv.rotate(one, None, freq, pos, q_out=alone)
     torch.cuda.synchronize()
     assert torch.equal(one, before) and torch.equal(out, alone.expand(20, 4, 64))
+
+
+def test_rotate_as_many_rows_as_there_can_be(torch_cuda):
+    """2^31 - 1 rows of one value, whose number and that of a workgroup's rows add up to more than 32 bits hold."""
+    torch = torch_cuda
+    announce("kv rotate 2^31 - 1 rows")
+    x = torch.full((2 ** 31 - 1, 1, 1), 2.0, dtype=torch.float16, device="cuda")
+    x[-1], x[12345] = -3.0, 0.5
+    kv.rotate(x, None, None, None, norm=True, q_weight=torch.tensor([4.0], device="cuda"))
+    torch.cuda.synchronize()
+    assert x[-1].item() == -4.0                             # (1 - eps / (2 x^2) times 4, to half a step of 2^-9)
+    assert (x[:-1] == 4.0).all()
