@@ -20,7 +20,8 @@
 // again, three to five passes of the choice. us on the GPU (and its bytes' time):
 // 131071 keys, 8 cache heads of 128, one query, 12.9 (0.9); 16 sequences of 9000 to
 // 16384 and two queries of each, 9.8 (1.4); 8 of 3000 to 9000, 32 heads, 9.4 (1.3);
-// with scores alone 6.2 to 8.6. Summaries are HBM's: 32700 keys of 8 heads, 9.0 us,
+// with scores alone 6.2 to 8.6. Past 16 query heads to a cache head, lots of 16 after each other: one query on
+// 16384 keys, 16 heads over 1 11.1, 32 over 1 19.6. Summaries are HBM's: 32700 keys of 8 heads, 9.0 us,
 // 3.7 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -348,7 +348,8 @@ def _vector(t, n, dtype, name, device) -> int:
 def rotate(q, k, freq, positions, q_out=None, k_out=None, adjacent: bool = False, norm: bool = False, q_weight=None,
            k_weight=None, eps: float = 1e-6, offset: int = 0, stream=None) -> None:
     """us_kv_rotate: norms (norm=True) of query and key heads, and their rotation by freq (axes, pairs) times
-    positions (axes, tokens); in place where no q_out and k_out are given. k may be None, and freq (no rotation)."""
+    positions (axes, tokens); in place where no q_out and k_out are given (not for a head that is expanded over several).
+    k may be None, and freq (no rotation)."""
     L = lib()
     tokens, heads, d = q.shape
     on = q.get_device() if q.is_cuda else -1
@@ -401,7 +402,8 @@ def _groups(group_starts, shared, max_group, max_shared, device) -> bytes:
 
 def attend_shared_workspace(cache: Cache, q, blocks, group_starts, starts=None, max_q: int = 1, max_group=None,
                             max_shared=None, max_len=None, causal: bool = True):
-    """A workspace for attend_shared calls of these sizes (groups of up to max_group sequences, or of all)."""
+    """A workspace for attend_shared calls of these sizes. Without max_group every group is taken to be as large as the
+    batch, without max_shared as long as the table: the workspace and the launch grow with both."""
     batch, n = blocks.shape[0], ctypes.c_size_t(0)
     at, count = group_starts.data_ptr(), group_starts.shape[0] - 1
     _check("us_kv_attend_shared_workspace_size", lib().us_kv_attend_shared_workspace_size(
@@ -414,7 +416,8 @@ def attend_shared_workspace(cache: Cache, q, blocks, group_starts, starts=None, 
 def attend_shared(cache: Cache, blocks, lens, q, out, group_starts, shared, starts=None, max_q: int = 1, max_group=None,
                   max_shared=None, max_len=None, scale=None, causal: bool = True, ws=None, stream=None) -> None:
     """us_kv_attend_shared: attend, with the first shared[g] blocks of group g's sequences (group_starts[g] ..
-    group_starts[g + 1] - 1) read once for all of them."""
+    group_starts[g + 1] - 1) read once for all of them. max_group and max_shared as for the workspace: they also choose
+    the kernel."""
     heads, d, on, batch = q.shape[1], cache.head_dim, cache.device, blocks.shape[0]
     at, n = _workspace(ws, on)
     _check("us_kv_attend_shared", lib().us_kv_attend_shared(
