@@ -304,11 +304,13 @@ typedef struct {
  * the common blocks, and results are off by as much. Sequences past max_group
  * in a group count as sequences of none. Where the sequences' token rows are not in
  * order, or one of them has more than max_new, rows of its group may miss common
- * keys. What pays depends on the sizes: with 32 heads over 8 of 128 a call takes less
- * than us_kv_attend from 8 sequences on 4096 common tokens, or 2 on 16384, on, and
- * more on 1024, for one or two cache heads, and for sequences with whole prompts of
- * their own. max_group and max_shared bound the workspace and choose the kernel: as
- * low as they are known. opts->window has to be 0 and opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, as
+ * keys. What pays depends on the sizes. With 32 heads over 8 of 128 a call takes less
+ * than us_kv_attend on 16384 common tokens from 2 sequences on (1.2 times as fast; 2.7
+ * with 64); on 4096 it does with 8 (1.2) and from 32 on, not with 4 or 16; on 1024 it
+ * is 0.8 to 1.1 times as fast. It takes longer with one cache head, and for
+ * sequences with whole prompts of their own. max_group and max_shared bound the
+ * workspace and choose the kernel: as low as they are known. opts->window has to be 0
+ * and opts->weights NULL. ws: us_kv_attend_shared_workspace_size bytes, as
  * us_kv_attend's, and one workspace serves both in turn. US_ERR_SHAPE as
  * us_kv_attend, for groups as for sequences (for more than 2^25 query rows of a
  * group and cache head), for more than 2^25 rows of a sequence and all heads, and
